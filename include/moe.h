@@ -325,6 +325,79 @@ double moe_estimate_streamed_ms(const moe_shape* shape, const int32_t* rows_per_
 moe_status moe_layer_views(const moe_shape* shape, void* workspace, int32_t** topk_idx, float** topk_w,
                            int32_t** expert_offsets, int32_t** inv_perm);
 
+/* ---- Training a router --------------------------------------------------------------------
+ * What a program needs beside the calls above to tune the gate matrix (and bias) of a layer whose experts stay as they are, and, with
+ * the gradients that leave here, the tensors around it.  In the order of a step: moe_route (with logits), moe_permute,
+ * moe_grouped_ffn, moe_combine; then moe_combine_backward, moe_balance_loss, moe_route_backward, and moe_clip_gradients over all
+ * tensors.  Conventions as above; the calls record no profiling intervals.  Every gradient is that of the call's outputs as written
+ * here, sums are fp32 or wider, and the same inputs give the same bits.
+ *  - keep_or_null [T] uint8 device: 0 marks a padding token.  It counts nowhere, its rows of dlogits and dx are zero, and what its rows
+ *    of logits and x hold (infinities and NaN, too) does not matter.  NULL: every token counts.
+ *  - Limits beyond those above: logits [T,E] and dwg [H,E] in fp32 are below 4 GiB, too.
+ *  - Pointers to rows of H elements are 16-byte aligned (MOE_E_ARG), others aligned to their elements.
+ *  - shape->F and shape->num_shared do not matter to these calls, but have to be valid. */
+
+/* Bytes of device workspace for moe_balance_loss and moe_route_backward with this shape; 0 for an invalid shape. */
+size_t moe_backward_workspace_bytes(const moe_shape* shape);
+
+/* Load-balancing loss of a routing, its gradient, and the picks per expert.  With n kept tokens, c_e picks of expert e among them
+ * and p the softmax of a token's logits over all E experts:
+ *   loss[0] = E * sum_e (c_e / (top_k * n)) * mean_t p[t,e]         (1 for even picks)
+ *   loss[1] = mean_t (log sum_e exp logits[t,e])^2
+ *   dlogits = d (balance_coef * loss[0] + z_coef * loss[1]) / d logits, the counts taken as constants
+ * all of them 0 when no token is kept.
+ *   logits [T,E] fp32 device in (moe_route's logits), topk_idx [T,k] int32 device in (ids outside [0,E) are not counted)
+ *   counts [E] int32, loss [2] fp32, dlogits_or_null [T,E] fp32: device out; dlogits must not be logits
+ * T = 0: counts and loss are set to 0. */
+moe_status moe_balance_loss(moe_ctx* ctx, const moe_shape* shape, const float* logits, const int32_t* topk_idx, const uint8_t* keep_or_null,
+                            double balance_coef, double z_coef, int32_t* counts, float* loss, float* dlogits_or_null,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradient of moe_route.  With g the gradient of the weights (dtopk_w at a token's picks, 0 elsewhere) and p the softmax that they
+ * are taken from (over all experts; with renormalize over the token's picks):
+ *   dl = routed_scale * p * (g - sum_e p g) + dlogits,   dx = dl Wg^T,   dwg = x^T dl,   dbias = sum_t dl[t]
+ * dl and the sums of dwg and dbias as fp32 has them; dx is rounded to bf16 once.  A gradient that is not finite comes out as not finite.
+ *   x_bf16 [T,H], wg_bf16 [H,E] (logical layout whatever "gate_packed" says), logits [T,E] fp32 (with the bias, as moe_route gives them),
+ *   topk_idx [T,k] int32 (distinct ids in a row), dtopk_w [T,k] fp32, dlogits_or_null [T,E] fp32: device in
+ *   dx_or_null [T,H] bf16, dwg [H,E] fp32, dbias_or_null [E] fp32: device out; with accumulate = 1 dwg and dbias are added to (each
+ *   element once, after the sum over the tokens), with 0 they are written.
+ * T = 0: dwg and dbias are set to 0 unless accumulate. */
+moe_status moe_route_backward(moe_ctx* ctx, const moe_shape* shape, const void* x_bf16, const void* wg_bf16, const float* logits,
+                              const int32_t* topk_idx, const float* dtopk_w, const float* dlogits_or_null, const uint8_t* keep_or_null,
+                              void* dx_or_null, float* dwg, float* dbias_or_null, int32_t accumulate, void* workspace,
+                              size_t workspace_bytes, void* hip_stream);
+
+/* Gradient of moe_combine: dtopk_w[t,j] = sum_h y_perm[inv_perm[t*k+j],h] * dout[t,h] (in fp32),
+ * dy_perm[inv_perm[t*k+j],:] = topk_w[t,j] * dout[t,:].  The gradient of y_shared is dout itself.
+ *   dout [T,H] bf16 (fp32 under "out_fp32" = 1), y_perm [T*k,H] fp32 (bf16 under "y_fp32" = 0), inv_perm [T*k] int32 (a permutation),
+ *   topk_w [T,k] fp32 (read for dy_perm only): device in
+ *   dtopk_w [T,k] fp32, dy_perm_or_null [T*k,H] of y_perm's type: device out; dy_perm must not be y_perm. */
+moe_status moe_combine_backward(moe_ctx* ctx, const moe_shape* shape, const void* dout, const void* y_perm, const int32_t* inv_perm,
+                                const float* topk_w, float* dtopk_w, void* dy_perm_or_null, void* hip_stream);
+
+/* A list of gradients, made once for buffers that stay where they are.  The struct and the device buffer are the caller's; the fields
+ * are the library's. */
+typedef struct {
+    void* buffer;
+    int32_t chunks;
+    int32_t in_place;
+} moe_gradient_list;
+
+/* Device bytes of a list of `tensors` tensors with elements[i] elements of 4 (is_fp32[i] = 1) or 2 bytes; 0 for invalid arguments. */
+size_t moe_gradient_list_bytes(int32_t tensors, const int64_t* elements, const int32_t* is_fp32);
+
+/* Fills `list` and its buffer.  grads, outs: HOST arrays of DEVICE pointers, aligned to their elements; is_fp32[i]: 1 fp32, 0 bf16.
+ * outs[i] may be grads[i] (scaled in place); otherwise no two of the tensors overlap (MOE_E_ARG).  Tensors of no elements are
+ * left out.  buffer: device, 256-byte aligned, moe_gradient_list_bytes bytes (MOE_E_WORKSPACE), the list's until its last use; it holds
+ * the scratch of moe_clip_gradients, so calls with one list follow each other on one stream.  SYNCHRONISES hip_stream. */
+moe_status moe_gradient_list_make(moe_ctx* ctx, int32_t tensors, const void* const* grads, void* const* outs, const int64_t* elements,
+                                  const int32_t* is_fp32, void* buffer, size_t buffer_bytes, moe_gradient_list* list, void* hip_stream);
+
+/* norm[0] = sqrt of the sum of all squares of the list's gradients (fp32 device out, formed in 64 bits);
+ * out = grad * (norm > max_norm ? max_norm / norm : 1), rounded to the tensor's type.  max_norm >= 0 (infinity: the norm alone, and copies).
+ * A norm that is NaN scales nothing, one that is infinite gives factor 0. */
+moe_status moe_clip_gradients(moe_ctx* ctx, const moe_gradient_list* list, double max_norm, float* norm, void* hip_stream);
+
 /* Profiling.  While enabled, every kernel group a call enqueues is bracketed by HIP events on
  * the call's stream.  moe_profile_read waits for the recorded events, adds the elapsed
  * milliseconds per stage into ms_sum[MOE_STAGE_COUNT] and the number of intervals into

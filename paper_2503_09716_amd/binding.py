@@ -24,6 +24,8 @@ EXPORTS = [
     "moe_gate_packed_bytes", "moe_pack_gate",
     "moe_route", "moe_permute", "moe_grouped_ffn", "moe_combine", "moe_layer", "moe_layer_static", "moe_layer_views",
     "moe_layer_streamed", "moe_stream_stats", "moe_estimate_streamed_ms", "moe_accumulate", "moe_layer_chunked",
+    "moe_backward_workspace_bytes", "moe_balance_loss", "moe_route_backward", "moe_combine_backward",
+    "moe_gradient_list_bytes", "moe_gradient_list_make", "moe_clip_gradients",
     "moe_profile_enable", "moe_profile_read", "moe_profile_read_intervals", "moe_profile_mfma_ceiling",
 ]
 
@@ -31,6 +33,10 @@ EXPORTS = [
 class MoeShape(C.Structure):
     _fields_ = [("T", C.c_int32), ("H", C.c_int32), ("F", C.c_int32), ("E", C.c_int32), ("top_k", C.c_int32),
                 ("num_shared", C.c_int32), ("renormalize", C.c_int32), ("routed_scale", C.c_float)]
+
+
+class GradientListStruct(C.Structure):
+    _fields_ = [("buffer", C.c_void_p), ("chunks", C.c_int32), ("in_place", C.c_int32)]
 
 
 class MoeError(RuntimeError):
@@ -89,8 +95,19 @@ def load_library():
                                              C.POINTER(C.c_double), C.POINTER(C.c_double), vp]
     lib.moe_estimate_streamed_ms.argtypes = [sp, C.POINTER(C.c_int32), C.c_int32, C.c_int32, C.c_double, C.c_double]
     lib.moe_estimate_streamed_ms.restype = C.c_double
+    lib.moe_backward_workspace_bytes.argtypes = [sp]
+    lib.moe_backward_workspace_bytes.restype = C.c_size_t
+    lib.moe_balance_loss.argtypes = [C.c_void_p, sp, f32p, i32p, vp, C.c_double, C.c_double, i32p, f32p, f32p, vp, C.c_size_t, vp]
+    lib.moe_route_backward.argtypes = [C.c_void_p, sp, vp, vp, f32p, i32p, f32p, f32p, vp, vp, f32p, f32p, C.c_int32, vp, C.c_size_t, vp]
+    lib.moe_combine_backward.argtypes = [C.c_void_p, sp, vp, vp, i32p, f32p, f32p, vp, vp]
+    i64s, i32s = C.POINTER(C.c_int64), C.POINTER(C.c_int32)
+    lib.moe_gradient_list_bytes.argtypes = [C.c_int32, i64s, i32s]
+    lib.moe_gradient_list_bytes.restype = C.c_size_t
+    lib.moe_gradient_list_make.argtypes = [C.c_void_p, C.c_int32, tab, tab, i64s, i32s, vp, C.c_size_t, C.POINTER(GradientListStruct), vp]
+    lib.moe_clip_gradients.argtypes = [C.c_void_p, C.POINTER(GradientListStruct), C.c_double, f32p, vp]
     for name in EXPORTS:
-        if name not in ("moe_destroy", "moe_last_error", "moe_workspace_bytes", "moe_h_scratch_bytes", "moe_gate_packed_bytes",
+        if name not in ("moe_backward_workspace_bytes", "moe_gradient_list_bytes",
+                        "moe_destroy", "moe_last_error", "moe_workspace_bytes", "moe_h_scratch_bytes", "moe_gate_packed_bytes",
                         "moe_estimate_streamed_ms"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
@@ -112,6 +129,10 @@ def workspace_bytes(shape: MoeShape) -> int:
 
 def h_scratch_bytes(shape: MoeShape) -> int:
     return int(load_library().moe_h_scratch_bytes(C.byref(shape)))
+
+
+def backward_workspace_bytes(shape: MoeShape) -> int:
+    return int(load_library().moe_backward_workspace_bytes(C.byref(shape)))
 
 
 def estimate_streamed_ms(shape: MoeShape, rows_per_expert, experts_per_group: int, num_slots: int, link_gbs: float,
@@ -139,6 +160,22 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _typed(t: Optional[torch.Tensor], dtype, numel: int):
+    """_ptr of a tensor that the call reads or writes as `numel` elements of `dtype`."""
+    if t is None:
+        return None
+    assert t.dtype == dtype and t.numel() == numel, "tensor of %d elements of %s required" % (numel, dtype)
+    assert t.is_cuda and t.is_contiguous(), "device-resident contiguous tensor required"
+    return t.data_ptr()
+
+
+class GradientList:
+    """Tensors whose gradients are clipped together (Moe.gradient_list): keeps them and the device table alive."""
+
+    def __init__(self, struct: GradientListStruct, buffer: torch.Tensor, grads, outs):
+        self.struct, self.buffer, self.grads, self.outs = struct, buffer, grads, outs
+
+
 class Moe:
     """One library context on one GPU.  Methods mirror the C entry points one to one."""
 
@@ -150,6 +187,7 @@ class Moe:
         if st != 0 or not h:
             raise MoeError(st, "moe_create failed on device %d" % device)
         self.h = h
+        self.options = {}   # what set_option was given
 
     def close(self):
         if getattr(self, "h", None):
@@ -168,6 +206,7 @@ class Moe:
 
     def set_option(self, key: str, value: int):
         self._check(self.lib.moe_set_option(self.h, key.encode(), int(value)))
+        self.options[key] = int(value)
 
     def new_workspace(self, shape: MoeShape) -> torch.Tensor:
         n = workspace_bytes(shape)
@@ -219,6 +258,60 @@ class Moe:
     def combine(self, shape, y_perm, inv_perm, topk_w, y_shared, out):
         self._check(self.lib.moe_combine(self.h, C.byref(shape), _ptr(y_perm), _ptr(inv_perm), _ptr(topk_w),
                                          _ptr(y_shared), _ptr(out), _stream()))
+
+    # ---- training a router ---------------------------------------------------------------
+    def new_backward_workspace(self, shape: MoeShape) -> torch.Tensor:
+        """Workspace of balance_loss and route_backward."""
+        n = backward_workspace_bytes(shape)
+        if n == 0:
+            raise MoeError(2, "unsupported or invalid shape")
+        return torch.empty(n, dtype=torch.uint8, device="cuda:%d" % self.device)
+
+    def balance_loss(self, shape, logits, topk_idx, keep, balance_coef, z_coef, counts, loss, dlogits, workspace):
+        """keep: bool [T] or None; dlogits: fp32 [T, E] or None."""
+        T, E = shape.T, shape.E
+        self._check(self.lib.moe_balance_loss(self.h, C.byref(shape), _typed(logits, torch.float32, T * E),
+                                              _typed(topk_idx, torch.int32, T * shape.top_k), _typed(keep, torch.bool, T),
+                                              balance_coef, z_coef, _typed(counts, torch.int32, E), _typed(loss, torch.float32, 2),
+                                              _typed(dlogits, torch.float32, T * E), _ptr(workspace), workspace.numel(), _stream()))
+
+    def route_backward(self, shape, x, wg, logits, topk_idx, dtopk_w, dlogits, keep, dx, dwg, dbias, accumulate, workspace):
+        """dlogits, keep (bool [T]), dx and dbias may be None."""
+        T, H, E, R = shape.T, shape.H, shape.E, shape.T * shape.top_k
+        f32, b16 = torch.float32, torch.bfloat16
+        self._check(self.lib.moe_route_backward(self.h, C.byref(shape), _typed(x, b16, T * H), _typed(wg, b16, H * E),
+                                                _typed(logits, f32, T * E), _typed(topk_idx, torch.int32, R), _typed(dtopk_w, f32, R),
+                                                _typed(dlogits, f32, T * E), _typed(keep, torch.bool, T), _typed(dx, b16, T * H),
+                                                _typed(dwg, f32, H * E), _typed(dbias, f32, E), 1 if accumulate else 0,
+                                                _ptr(workspace), workspace.numel(), _stream()))
+
+    def combine_backward(self, shape, dout, y_perm, inv_perm, topk_w, dtopk_w, dy_perm):
+        """dout as option "out_fp32" has it, y_perm and dy_perm (or None) as "y_fp32" has them."""
+        T, H, R = shape.T, shape.H, shape.T * shape.top_k
+        f32, b16 = torch.float32, torch.bfloat16
+        y, o = (f32 if self.options.get(n, d) else b16 for n, d in (("y_fp32", 1), ("out_fp32", 0)))
+        self._check(self.lib.moe_combine_backward(self.h, C.byref(shape), _typed(dout, o, T * H), _typed(y_perm, y, R * H),
+                                                  _typed(inv_perm, torch.int32, R), _typed(topk_w, f32, R), _typed(dtopk_w, f32, R),
+                                                  _typed(dy_perm, y, R * H), _stream()))
+
+    def gradient_list(self, grads: Sequence[torch.Tensor], outs: Sequence[torch.Tensor]) -> GradientList:
+        """The tensors (fp32 or bf16) that clip_gradients takes together; outs[i] receives grads[i] scaled and may be it."""
+        grads, outs = list(grads), list(outs)
+        assert len(grads) == len(outs)
+        for g, o in zip(grads, outs):
+            assert g.dtype in (torch.float32, torch.bfloat16) and o.dtype == g.dtype and o.numel() == g.numel()
+            assert g.is_cuda and o.is_cuda and g.is_contiguous() and o.is_contiguous()
+        n = len(grads)
+        sizes = (C.c_int64 * n)(*[g.numel() for g in grads])
+        types = (C.c_int32 * n)(*[int(g.dtype == torch.float32) for g in grads])
+        buffer = torch.empty(int(self.lib.moe_gradient_list_bytes(n, sizes, types)), dtype=torch.uint8, device="cuda:%d" % self.device)
+        struct = GradientListStruct()
+        self._check(self.lib.moe_gradient_list_make(self.h, n, _table(grads), _table(outs), sizes, types, _ptr(buffer),
+                                                    buffer.numel(), C.byref(struct), _stream()))
+        return GradientList(struct, buffer, grads, outs)
+
+    def clip_gradients(self, gradients: GradientList, max_norm: float, norm):
+        self._check(self.lib.moe_clip_gradients(self.h, C.byref(gradients.struct), max_norm, _typed(norm, torch.float32, 1), _stream()))
 
     # ---- fused call --------------------------------------------------------------------
     def layer(self, shape, x, wg, bias, w1p, w3p, w2p, out, workspace, tables=None):

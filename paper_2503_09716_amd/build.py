@@ -10,7 +10,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoe_mi355.so")
-SOURCES = ["api.hip", "route.hip", "permute.hip", "ffn_gemm.hip", "ffn_small.hip", "combine.hip", "stream.hip", "profile.hip"]
+SOURCES = ["api.hip", "route.hip", "permute.hip", "ffn_gemm.hip", "ffn_small.hip", "combine.hip", "stream.hip", "profile.hip",
+           "balance.hip", "route_backward.hip", "combine_backward.hip", "clip.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument",
          "-Wno-unknown-attributes"]
@@ -25,7 +26,8 @@ def _stale(target: str, deps) -> bool:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
-    headers = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "plan.h"), os.path.join(CSRC, "topk.h"), os.path.join(ROOT, "include", "moe.h")]
+    headers = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "plan.h"), os.path.join(CSRC, "topk.h"), os.path.join(CSRC, "train.h"),
+               os.path.join(CSRC, "router_rows.h"), os.path.join(ROOT, "include", "moe.h")]
     jobs = []
     for src in SOURCES:
         s = os.path.join(CSRC, src)

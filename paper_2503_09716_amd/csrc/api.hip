@@ -3,11 +3,13 @@
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <vector>
 
 #include "common.h"
+#include "train.h"
 
 using namespace moe;
 
@@ -810,6 +812,125 @@ moe_status layer_with_workspace(moe_ctx* c, const moe_shape* s, const void* x, c
     return MOE_OK;
 }
 
+// ---- training a router --------------------------------------------------------------------
+// Workspace of moe_balance_loss and moe_route_backward: each has it to itself from the start on.
+struct BalanceLayout {
+    int count_blocks, count_tokens, loss_blocks;
+    size_t partial_counts, partial_loss, done, total;
+};
+BalanceLayout balance_layout(const moe_shape& s) {
+    BalanceLayout L;
+    // a workgroup of the counts takes at least 2048 picks, one of the loss 16 tokens at a time
+    int64_t n = ((int64_t)s.T * s.top_k + 2047) / 2048;
+    if (n > BALANCE_COUNT_BLOCKS) n = BALANCE_COUNT_BLOCKS;
+    if (n < 1) n = 1;
+    L.count_tokens = (int)((s.T + n - 1) / n);
+    if (L.count_tokens < 1) L.count_tokens = 1;
+    L.count_blocks = s.T ? (s.T + L.count_tokens - 1) / L.count_tokens : 1;
+    const int64_t quads = ((int64_t)s.T + 15) / 16;
+    L.loss_blocks = (int)(quads < 1 ? 1 : quads < BALANCE_LOSS_BLOCKS ? quads : BALANCE_LOSS_BLOCKS);
+    size_t o = 0;
+    auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
+    L.partial_counts = take((size_t)L.count_blocks * (s.E + 1) * 4);
+    L.partial_loss = take((size_t)L.loss_blocks * 2 * 8);
+    L.done = take(4);
+    L.total = o;
+    return L;
+}
+
+struct RouteBackwardLayout {
+    int nb, kb, steps, splits, split_steps;
+    size_t zeros, masks, dl_dx, dl_dw, wg_blocks, partial, total;
+};
+RouteBackwardLayout route_backward_layout(const moe_shape& s) {
+    RouteBackwardLayout L;
+    L.nb = route_backward_blocks(s.E);
+    L.kb = (s.E + 31) / 32;
+    L.steps = (s.T + 31) / 32;
+    if (L.steps < 1) L.steps = 1;
+    // as many parts of the tokens as fill the CUs with workgroups (two to a CU up to 32 experts, whose ring is small)
+    const int tiles = (s.H + ROUTE_BACKWARD_TILE - 1) / ROUTE_BACKWARD_TILE, want = (L.nb <= 2 ? 512 : 256) / tiles;
+    const int parts = want < 1 ? 1 : want < L.steps ? want : L.steps;
+    L.split_steps = (L.steps + parts - 1) / parts;
+    L.splits = (L.steps + L.split_steps - 1) / L.split_steps;
+    size_t o = 0;
+    auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
+    L.zeros = take(1024);
+    L.masks = take((size_t)L.steps * 4);
+    L.dl_dx = take((size_t)L.steps * 4 * L.kb * 1024);
+    L.dl_dw = take((size_t)L.steps * 3 * L.nb * 1024);
+    L.wg_blocks = take((size_t)s.H / 16 * L.kb * 1024);
+    L.partial = take((size_t)L.splits * (s.H + 1) * 16 * L.nb * 4);
+    L.total = o;
+    return L;
+}
+
+size_t backward_bytes(const moe_shape& s) {
+    const size_t a = balance_layout(s).total, b = route_backward_layout(s).total;
+    return a > b ? a : b;
+}
+
+const char* training_shape_problem(const moe_shape* s, moe_status* st) {
+    if (const char* why = shape_problem(s, st)) return why;
+    const int64_t lim = (int64_t)1 << 32;
+    if ((int64_t)s->T * s->E * 4 >= lim || (int64_t)s->H * s->E * 4 >= lim) {
+        *st = MOE_E_UNSUPPORTED;
+        return "logits or dwg reaches 4 GiB";
+    }
+    return nullptr;
+}
+
+moe_status check_training(moe_ctx* c, const moe_shape* s) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    moe_status st;
+    if (const char* why = training_shape_problem(s, &st)) return fail(c, st, "%s", why);
+    HIP_TRY(c, hipSetDevice(c->device));
+    return MOE_OK;
+}
+
+moe_status check_backward_ws(moe_ctx* c, const moe_shape* s, const void* ws, size_t bytes) {
+    if (!ws) return fail(c, MOE_E_ARG, "workspace is NULL");
+    if ((uintptr_t)ws & 255) return fail(c, MOE_E_ARG, "workspace must be 256-byte aligned");
+    const size_t need = backward_bytes(*s);
+    if (bytes < need) return fail(c, MOE_E_WORKSPACE, "workspace %zu bytes < required %zu", bytes, need);
+    return MOE_OK;
+}
+
+bool misaligned(std::initializer_list<const void*> ps, uintptr_t to) {
+    for (const void* p : ps)
+        if ((uintptr_t)p & (to - 1)) return true;
+    return false;
+}
+
+struct Extent {
+    uintptr_t from, to;
+    int32_t tensor;
+};
+int by_start(const void* a, const void* b) {
+    const uintptr_t x = ((const Extent*)a)->from, y = ((const Extent*)b)->from;
+    return x < y ? -1 : x > y;
+}
+
+// Whether tensors of the list overlap other than an output its own gradient.  e: 2 n extents, sorted here.
+bool overlapping(Extent* e, int64_t n) {
+    qsort(e, n, sizeof(Extent), by_start);
+    // an output in place is the same extent twice: those are next to each other unless a third starts there, which overlaps them
+    for (int64_t i = 0; i < n; ++i) {
+        int64_t j = i + 1;
+        if (j < n && e[j].from == e[i].from && e[j].to == e[i].to && e[j].tensor == e[i].tensor) ++j;
+        if (j < n && e[j].from < e[i].to) return true;
+        i = j - 1;
+    }
+    return false;
+}
+
+// Chunks of a tensor: those after the first start on a 128-byte line of the gradient.
+int64_t tensor_chunks(uintptr_t src, int64_t bytes) {
+    if (bytes == 0) return 0;
+    return ((int64_t)(src & 127) + bytes + CLIP_CHUNK - 1) / CLIP_CHUNK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -821,7 +942,7 @@ moe_status moe_create(moe_ctx** out, int device) {
     moe_ctx* c = new moe_ctx();
     c->device = device;
     c->tab_shadow.assign(3 * MAX_GROUPS, nullptr);
-    bool ok = ffn_gemm_init() == hipSuccess;
+    bool ok = ffn_gemm_init() == hipSuccess && route_backward_init() == hipSuccess;
     ok = ok && hipGetSymbolAddress((void**)&c->static_ws, HIP_SYMBOL(scratch)) == hipSuccess && c->static_ws != nullptr &&
          ((uintptr_t)c->static_ws & 255) == 0;
     ok = ok && hipStreamCreateWithFlags(&c->copy_stream, hipStreamNonBlocking) == hipSuccess &&
@@ -1190,6 +1311,140 @@ moe_status moe_layer_views(const moe_shape* s, void* ws, int32_t** idx, float** 
     if (w) *w = (float*)(w8 + L.topk_w);
     if (offsets) *offsets = (int32_t*)(w8 + L.offsets);
     if (inv_perm) *inv_perm = (int32_t*)(w8 + L.inv_perm);
+    return MOE_OK;
+}
+
+size_t moe_backward_workspace_bytes(const moe_shape* s) {
+    moe_status st;
+    if (training_shape_problem(s, &st)) return 0;
+    return backward_bytes(*s);
+}
+
+moe_status moe_balance_loss(moe_ctx* c, const moe_shape* s, const float* logits, const int32_t* idx, const uint8_t* keep, double balance_coef,
+                            double z_coef, int32_t* counts, float* loss, float* dlogits, void* ws, size_t ws_bytes, void* stream) {
+    if (moe_status st = check_training(c, s)) return st;
+    if (!counts || !loss || (s->T > 0 && (!logits || !idx))) return fail(c, MOE_E_ARG, "balance_loss: NULL pointer");
+    if (dlogits && dlogits == logits) return fail(c, MOE_E_ARG, "balance_loss: dlogits must not be logits");
+    if (!isfinite(balance_coef) || !isfinite(z_coef)) return fail(c, MOE_E_ARG, "balance_loss: coefficients must be finite");
+    if (misaligned({logits, idx, counts, loss, dlogits}, 4)) return fail(c, MOE_E_ARG, "balance_loss: misaligned pointer");
+    if (s->T > 0)
+        if (moe_status st = check_backward_ws(c, s, ws, ws_bytes)) return st;
+    const BalanceLayout L = balance_layout(*s);
+    char* const w8 = (char*)ws;
+    const BalanceArgs a{logits, idx, keep, balance_coef, z_coef, counts, loss, dlogits, s->T, s->E, s->top_k, L.count_blocks, L.count_tokens, L.loss_blocks,
+                        (int32_t*)(w8 + L.partial_counts), (double*)(w8 + L.partial_loss), (int32_t*)(w8 + L.done)};
+    HIP_TRY(c, launch_balance_loss(a, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+moe_status moe_route_backward(moe_ctx* c, const moe_shape* s, const void* x, const void* wg, const float* logits, const int32_t* idx, const float* dw,
+                              const float* dlogits, const uint8_t* keep, void* dx, float* dwg, float* dbias, int32_t accumulate, void* ws,
+                              size_t ws_bytes, void* stream) {
+    if (moe_status st = check_training(c, s)) return st;
+    if (!dwg || (s->T > 0 && (!x || !wg || !logits || !idx || !dw))) return fail(c, MOE_E_ARG, "route_backward: NULL pointer");
+    if (accumulate != 0 && accumulate != 1) return fail(c, MOE_E_ARG, "route_backward: accumulate must be 0 or 1");
+    if (dx && (dx == x || dx == wg)) return fail(c, MOE_E_ARG, "route_backward: dx must not be x or wg");
+    if (misaligned({x, dx}, 16) || misaligned({wg}, 2) || misaligned({logits, idx, dw, dlogits, dwg, dbias}, 4))
+        return fail(c, MOE_E_ARG, "route_backward: misaligned pointer");
+    hipStream_t hs = (hipStream_t)stream;
+    if (s->T == 0) {
+        if (!accumulate) HIP_TRY(c, launch_route_backward_empty(*s, dwg, dbias, hs));
+        return MOE_OK;
+    }
+    if (moe_status st = check_backward_ws(c, s, ws, ws_bytes)) return st;
+    const RouteBackwardLayout L = route_backward_layout(*s);
+    char* const w8 = (char*)ws;
+    const RouteBackwardArgs a{(const char*)x, (const char*)wg, logits, idx, dw, dlogits, keep, (char*)dx, dwg, dbias, s->T, s->H, s->E, s->top_k,
+                              s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.splits, L.split_steps, w8 + L.zeros, (uint32_t*)(w8 + L.masks), w8 + L.dl_dx,
+                              w8 + L.dl_dw, w8 + L.wg_blocks, (float*)(w8 + L.partial)};
+    HIP_TRY(c, launch_route_backward(a, hs));
+    return MOE_OK;
+}
+
+moe_status moe_combine_backward(moe_ctx* c, const moe_shape* s, const void* dout, const void* y_perm, const int32_t* inv_perm, const float* w, float* dw,
+                                void* dy_perm, void* stream) {
+    if (moe_status st = check_common(c, s)) return st;
+    if (s->T == 0) return MOE_OK;   // an empty batch: nothing to do
+    if (!dout || !y_perm || !inv_perm || !dw || (dy_perm && !w)) return fail(c, MOE_E_ARG, "combine_backward: NULL pointer");
+    if (dy_perm && (dy_perm == y_perm || dy_perm == dout)) return fail(c, MOE_E_ARG, "combine_backward: dy_perm must not be y_perm or dout");
+    if (dw == w) return fail(c, MOE_E_ARG, "combine_backward: dtopk_w must not be topk_w");
+    if (misaligned({dout, y_perm, dy_perm}, 16) || misaligned({inv_perm, w, dw}, 4)) return fail(c, MOE_E_ARG, "combine_backward: misaligned pointer");
+    HIP_TRY(c, launch_combine_backward(*s, dout, y_perm, inv_perm, w, dw, dy_perm, c->y_fp32, c->out_fp32, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+size_t moe_gradient_list_bytes(int32_t tensors, const int64_t* elements, const int32_t* is_fp32) {
+    if (tensors < 0 || (tensors > 0 && (!elements || !is_fp32))) return 0;
+    int64_t chunks = 0;
+    for (int32_t i = 0; i < tensors; ++i) {
+        if (elements[i] < 0 || elements[i] > ((int64_t)1 << 40) || (is_fp32[i] != 0 && is_fp32[i] != 1)) return 0;
+        chunks += tensor_chunks(127, elements[i] * (is_fp32[i] ? 4 : 2));   // the worst alignment
+        if (chunks > 0x7fffffff - CLIP_BLOCKS) return 0;
+    }
+    return align_up(CLIP_BLOCKS * sizeof(double)) + align_up((size_t)chunks * sizeof(ClipChunk));
+}
+
+moe_status moe_gradient_list_make(moe_ctx* c, int32_t tensors, const void* const* grads, void* const* outs, const int64_t* elements, const int32_t* is_fp32,
+                                  void* buffer, size_t buffer_bytes, moe_gradient_list* list, void* stream) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    const size_t need = moe_gradient_list_bytes(tensors, elements, is_fp32);
+    if (need == 0) return fail(c, MOE_E_ARG, "gradient_list: invalid sizes or types");
+    if (!list || !buffer || (tensors > 0 && (!grads || !outs))) return fail(c, MOE_E_ARG, "gradient_list: NULL pointer");
+    if ((uintptr_t)buffer & 255) return fail(c, MOE_E_ARG, "gradient_list: buffer must be 256-byte aligned");
+    if (buffer_bytes < need) return fail(c, MOE_E_WORKSPACE, "gradient_list: buffer %zu bytes < required %zu", buffer_bytes, need);
+    int64_t chunks = 0, extents = 0;
+    for (int32_t i = 0; i < tensors; ++i) {
+        if (elements[i] == 0) continue;
+        const int size = is_fp32[i] ? 4 : 2;
+        if (!grads[i] || !outs[i]) return fail(c, MOE_E_ARG, "gradient_list: pointer %d is NULL", (int)i);
+        if (misaligned({grads[i], outs[i]}, size)) return fail(c, MOE_E_ARG, "gradient_list: pointer %d is misaligned", (int)i);
+        chunks += tensor_chunks((uintptr_t)grads[i], elements[i] * size);
+        extents += 2;
+    }
+    Extent* const e = (Extent*)malloc((extents + 1) * sizeof(Extent));
+    ClipChunk* const table = (ClipChunk*)malloc((chunks + 1) * sizeof(ClipChunk));
+    moe_status st = MOE_OK;
+    if (!e || !table) st = fail(c, MOE_E_ARG, "gradient_list: no host memory for %lld chunks", (long long)chunks);
+    if (st == MOE_OK) {
+        int64_t n = 0, m = 0;
+        bool in_place = false;
+        for (int32_t i = 0; i < tensors; ++i) {
+            if (elements[i] == 0) continue;
+            const int64_t bytes = elements[i] * (is_fp32[i] ? 4 : 2);
+            e[m++] = {(uintptr_t)grads[i], (uintptr_t)grads[i] + bytes, i};
+            e[m++] = {(uintptr_t)outs[i], (uintptr_t)outs[i] + bytes, i};
+            in_place = in_place || grads[i] == outs[i];
+            for (int64_t at = 0, end; at < bytes; at = end) {
+                end = at + CLIP_CHUNK - (at == 0 ? (int64_t)((uintptr_t)grads[i] & 127) : 0);
+                if (end > bytes) end = bytes;
+                table[n++] = {(const char*)grads[i] + at, (char*)outs[i] + at, (uint32_t)((end - at) / (is_fp32[i] ? 4 : 2)), (uint32_t)is_fp32[i]};
+            }
+        }
+        if (overlapping(e, m)) st = fail(c, MOE_E_ARG, "gradient_list: tensors overlap");
+        hipError_t r = hipSuccess;
+        if (st == MOE_OK) r = hipSetDevice(c->device);
+        if (st == MOE_OK && r == hipSuccess && n > 0)
+            r = hipMemcpyAsync((char*)buffer + align_up(CLIP_BLOCKS * sizeof(double)), table, n * sizeof(ClipChunk), hipMemcpyHostToDevice, (hipStream_t)stream);
+        if (st == MOE_OK && r == hipSuccess) r = hipStreamSynchronize((hipStream_t)stream);
+        if (r != hipSuccess) st = fail(c, MOE_E_HIP, "gradient_list: %s", hipGetErrorString(r));
+        if (st == MOE_OK) *list = moe_gradient_list{buffer, (int32_t)n, in_place ? 1 : 0};
+    }
+    free(e);
+    free(table);
+    return st;
+}
+
+moe_status moe_clip_gradients(moe_ctx* c, const moe_gradient_list* list, double max_norm, float* norm, void* stream) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    if (!list || !list->buffer || list->chunks < 0 || !norm) return fail(c, MOE_E_ARG, "clip_gradients: NULL pointer or a list that was not made");
+    if (!(max_norm >= 0)) return fail(c, MOE_E_ARG, "clip_gradients: max_norm must be >= 0");
+    if (misaligned({norm}, 4)) return fail(c, MOE_E_ARG, "clip_gradients: misaligned pointer");
+    HIP_TRY(c, hipSetDevice(c->device));
+    const ClipArgs a{(const ClipChunk*)((char*)list->buffer + align_up(CLIP_BLOCKS * sizeof(double))), (double*)list->buffer, norm, max_norm, list->chunks,
+                     list->in_place};
+    HIP_TRY(c, launch_clip(a, (hipStream_t)stream));
     return MOE_OK;
 }
 

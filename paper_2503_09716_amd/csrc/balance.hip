@@ -1,0 +1,173 @@
+// Balance loss of the router with its per-expert counts and its gradient.
+//
+// n kept tokens, c_e picks of expert e among them, p_te the softmax of a token's logits, lse_t the logarithm of their sum of
+// exponentials:   loss_0 = E sum_e c_e / (k n) mean_t p_te,   loss_1 = mean_t lse_t^2.
+// With off_e = E c_e / (k n) - 1 and sum_e p_te = 1:   loss_0 = 1 + mean_t s_t,   s_t = sum_e p_te off_e,
+// so a token adds one number to the loss, no sums of p over tokens are kept for each expert, and the gradient hangs on the same s_t:
+//   dlogits_te = p_te ((off_e - s_t) balance_coef / n + 2 z_coef / n lse_t)     (the counts have no gradient).
+// off is what the gradient of nearly even counts consists of: its numerator E c_e - k n is formed in whole numbers.
+//
+// Two launches: the counts (integer sums in LDS, one partial histogram to a workgroup: no atomics on global memory but the one
+// that finds the last workgroup), then one pass over the logits with a token in a row of 16 lanes.  The last workgroup of the second
+// launch adds the workgroups' partial losses in order, in 64 bits.
+#include "common.h"
+#include "router_rows.h"
+#include "train.h"
+
+namespace moe {
+namespace {
+
+constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int MAX_E = 256;
+
+// Picks of the kept tokens in [t0, t1) into hist (LDS, zeroed here); the kept tokens among them.  Ids outside [0, E) are not counted.
+__device__ __forceinline__ int count_picks(int* hist, int* kept, const int32_t* __restrict__ idx, const uint8_t* __restrict__ keep, const int t0, const int t1,
+                                           const int E, const int k) {
+    for (int e = threadIdx.x; e < MAX_E; e += blockDim.x) hist[e] = 0;
+    if (threadIdx.x == 0) *kept = 0;
+    __syncthreads();
+    int mine = 0;
+    if (!keep) {
+        const size_t p0 = (size_t)t0 * k;
+        const int n = (t1 - t0) * k;
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            const uint32_t e = (uint32_t)idx[p0 + i];
+            if (e < (uint32_t)E) atomicAdd(&hist[e], 1);
+        }
+        if (threadIdx.x == 0) mine = t1 - t0;
+    } else {
+        for (int t = t0 + threadIdx.x; t < t1; t += blockDim.x) {
+            if (!keep[t]) continue;
+            ++mine;
+            for (int j = 0; j < k; ++j) {
+                const uint32_t e = (uint32_t)idx[(size_t)t * k + j];
+                if (e < (uint32_t)E) atomicAdd(&hist[e], 1);
+            }
+        }
+    }
+    if (mine) atomicAdd(kept, mine);
+    __syncthreads();
+    return *kept;
+}
+
+__global__ __launch_bounds__(THREADS) void balance_count_kernel(const BalanceArgs a) {
+    __shared__ int hist[MAX_E], kept;
+    const int t0 = blockIdx.x * a.count_tokens, t1 = min(t0 + a.count_tokens, a.T);
+    const int n = count_picks(hist, &kept, a.idx, a.keep, t0, t1, a.E, a.k);
+    int32_t* const out = a.partial_counts + (size_t)blockIdx.x * (a.E + 1);
+    for (int e = threadIdx.x; e < a.E; e += THREADS) out[e] = hist[e];
+    if (threadIdx.x == 0) {
+        out[a.E] = n;
+        if (blockIdx.x == 0) *a.done = 0;
+    }
+}
+
+// ALONE: one workgroup, which counts for itself.
+template <int NV, bool WIDE, bool ALONE>
+__global__ __launch_bounds__(ALONE ? 1024 : THREADS) void balance_loss_kernel(const BalanceArgs a) {
+    constexpr int NW = ALONE ? 16 : WAVES;
+    __shared__ int hist[MAX_E + 1], kept;
+    __shared__ float off[MAX_E];
+    __shared__ double sums[2][NW];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15;
+    const int E = a.E;
+    if (ALONE) {
+        count_picks(hist, &kept, a.idx, a.keep, 0, a.T, E, a.k);
+        if (threadIdx.x == 0) hist[E] = kept;
+    } else {
+        for (int e = threadIdx.x; e <= E; e += THREADS) {
+            int c = 0;
+#pragma unroll 8
+            for (int b = 0; b < a.count_blocks; ++b) c += a.partial_counts[(size_t)b * (E + 1) + e];
+            hist[e] = c;
+        }
+    }
+    __syncthreads();
+    const int n = hist[E];
+    const double kn = (double)a.k * n;
+    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+        off[e] = n ? (float)(((double)hist[e] * E - kn) / kn) : 0.f;
+        if (blockIdx.x == 0) a.counts[e] = hist[e];
+    }
+    __syncthreads();
+    float o[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = row16_expert<WIDE>(row, i);
+        o[i] = e < E ? off[e] : 0.f;
+    }
+    const float bal = n ? (float)(a.balance_coef / n) : 0.f, zc = n ? (float)(2.0 * a.z_coef / n) : 0.f;
+    double sum_s = 0, sum_z = 0;
+    for (int q = blockIdx.x * NW + wave; q * 4 < a.T; q += gridDim.x * NW) {
+        const int tok = q * 4 + (lane >> 4), t = min(tok, a.T - 1);
+        const bool on = tok < a.T && (!a.keep || a.keep[t]);
+        float v[NV];
+        load_row16<NV, WIDE>(v, a.logits, t, E, row, -INFINITY);
+        const float lse = softmax_row16<NV>(v);
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) s = fmaf(v[i], o[i], s);
+        s = row16_sum(s);
+        if (on && row == 0) {
+            sum_s += s;
+            sum_z += (double)lse * lse;
+        }
+        if (a.dlogits && tok < a.T) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] = on ? v[i] * ((o[i] - s) * bal + lse * zc) : 0.f;
+            store_row16<NV, WIDE>(v, a.dlogits, t, E, row);
+        }
+    }
+#pragma unroll
+    for (int m = 16; m < 64; m *= 2) {   // the sums sit in lanes 0, 16, 32, 48
+        sum_s += __shfl_xor(sum_s, m, 64);
+        sum_z += __shfl_xor(sum_z, m, 64);
+    }
+    if (lane == 0) { sums[0][wave] = sum_s; sums[1][wave] = sum_z; }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        double v = 0;
+        for (int w = 0; w < NW; ++w) v += sums[threadIdx.x][w];
+        if (ALONE) {
+            a.loss[threadIdx.x] = n ? (float)(threadIdx.x ? v / n : 1.0 + v / n) : 0.f;
+        } else {
+            __hip_atomic_store(&a.partial_loss[2 * blockIdx.x + threadIdx.x], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __threadfence();
+        }
+    }
+    if (ALONE || wave != 0) return;
+    // The last workgroup to get here adds up what all have written.
+    int before = 0;
+    if (lane == 0) before = __hip_atomic_fetch_add(a.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    if (__builtin_amdgcn_readfirstlane(before) != (int)gridDim.x - 1) return;
+    __threadfence();
+    double v = 0;
+    for (int b = lane; b < 2 * (int)gridDim.x; b += 64) v += __hip_atomic_load(&a.partial_loss[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int m = 2; m < 64; m *= 2) v += __shfl_xor(v, m, 64);   // even lanes the balance terms, odd lanes the z terms
+    if (lane < 2) a.loss[lane] = n ? (float)(lane ? v / n : 1.0 + v / n) : 0.f;
+}
+
+__global__ void balance_empty_kernel(int E, int32_t* counts, float* loss) {
+    for (int e = threadIdx.x; e < E; e += blockDim.x) counts[e] = 0;
+    if (threadIdx.x < 2) loss[threadIdx.x] = 0.f;
+}
+
+}  // namespace
+
+hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t st) {
+    if (a.T == 0) {
+        hipLaunchKernelGGL(balance_empty_kernel, dim3(1), dim3(256), 0, st, a.E, a.counts, a.loss);
+        return hipGetLastError();
+    }
+    const bool wide = wide_rows(a.E, {a.logits, a.dlogits ? a.dlogits : a.logits});
+    const bool alone = (int64_t)a.T * a.E <= BALANCE_ALONE;
+    if (!alone) hipLaunchKernelGGL(balance_count_kernel, dim3(a.count_blocks), dim3(THREADS), 0, st, a);
+    return for_row16(a.E, wide, [&]<int NV, bool WIDE>() {
+        if (alone) hipLaunchKernelGGL((balance_loss_kernel<NV, WIDE, true>), dim3(1), dim3(1024), 0, st, a);
+        else hipLaunchKernelGGL((balance_loss_kernel<NV, WIDE, false>), dim3(a.loss_blocks), dim3(THREADS), 0, st, a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace moe

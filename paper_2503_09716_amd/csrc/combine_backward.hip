@@ -1,0 +1,114 @@
+// Backward pass of the weighted combine: out_t = sum_j w_tj y_row(t,j) (+ y_shared_t) gives
+//   dw_tj = <y_row(t,j), dout_t>,   dy_row(t,j) = w_tj dout_t   (and dout_t itself for the shared experts).
+// HBM-bound: every row of y is read and, with dy_perm, written once.  W wavefronts take a pair's row; those of a token's pairs are one
+// workgroup, so that dout's row comes from memory once.  A row's product is added up in fp32 along each lane and then across
+// the lanes.
+#include "common.h"
+#include "topk.h"
+#include "train.h"
+
+namespace moe {
+namespace {
+
+// N consecutive elements of a row.
+template <bool F32, int N>
+struct Row {
+    typedef uint32_t words __attribute__((ext_vector_type(N * (F32 ? 4 : 2) / 4)));
+    words v;
+    __device__ __forceinline__ void load(const char* row, const int c) { v = reinterpret_cast<const words*>(row)[c]; }
+    __device__ __forceinline__ float operator[](const int i) const {
+        return __uint_as_float(F32 ? v[i] : ((i & 1) ? v[i / 2] & 0xffff0000u : v[i / 2] << 16));
+    }
+};
+
+constexpr int AHEAD = 4;   // pieces of a row that a lane has in flight
+
+template <bool YF32, bool DF32, bool DY, int W>
+__global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __restrict__ dout, const char* __restrict__ y_perm,
+                                                                const int32_t* __restrict__ inv_perm, const float* __restrict__ w, const int k, const int H,
+                                                                float* __restrict__ dw, char* __restrict__ dy_perm) {
+    constexpr int N = YF32 || DF32 ? 4 : 8;
+    __shared__ float part[16];
+    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int rows = (blockDim.x >> 6) / W, r = wave / W, sub = wave % W;
+    const int n = H / N;
+    const char* const d = dout + (size_t)t * H * (DF32 ? 4 : 2);
+    for (int j0 = 0; j0 < k; j0 += rows) {
+        const int j = j0 + r;
+        float sum = 0.f;
+        if (j < k) {
+            const size_t p = (size_t)t * k + j, at = (size_t)inv_perm[p] * H * (YF32 ? 4 : 2);
+            const float wj = DY ? w[p] : 0.f;
+            for (int c0 = sub * 64 + lane; c0 < n; c0 += AHEAD * W * 64) {
+                Row<YF32, N> y[AHEAD];
+                Row<DF32, N> g[AHEAD];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int c = min(c0 + u * W * 64, n - 1);
+                    y[u].load(y_perm + at, c);
+                    g[u].load(d, c);
+                }
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int c = c0 + u * W * 64;
+                    if (c >= n) break;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) sum = fmaf(y[u][i], g[u][i], sum);
+                    if (DY) {
+                        if (YF32) {
+                            f32x4 o;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[i] = wj * g[u][i];
+                            reinterpret_cast<f32x4*>(dy_perm + at)[c] = o;
+                        } else {
+                            typedef __bf16 bf16_n __attribute__((ext_vector_type(N)));
+                            bf16_n o;
+#pragma unroll
+                            for (int i = 0; i < N; ++i) o[i] = (__bf16)(wj * g[u][i]);
+                            reinterpret_cast<bf16_n*>(dy_perm + at)[c] = o;
+                        }
+                    }
+                }
+            }
+            sum = row16_sum(sum);
+            sum += pair_f<16>(sum);
+            sum += pair_f<32>(sum);
+            if (W == 1 && lane == 0) dw[p] = sum;
+        }
+        if (W > 1) {
+            if (lane == 0) part[wave] = sum;
+            __syncthreads();
+            if (threadIdx.x < (unsigned)rows && j0 + (int)threadIdx.x < k) {
+                float v = 0.f;
+#pragma unroll
+                for (int q = 0; q < W; ++q) v += part[threadIdx.x * W + q];
+                dw[(size_t)t * k + j0 + threadIdx.x] = v;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_combine_backward(const moe_shape& s, const void* dout, const void* y_perm, const int32_t* inv_perm, const float* w, float* dw,
+                                   void* dy_perm, bool y_fp32, bool dout_fp32, hipStream_t st) {
+    const int64_t pairs = (int64_t)s.T * s.top_k;
+    const bool split = pairs <= 2048 && s.H >= 1024;
+    auto run = [&]<bool Y, bool D, bool DY, int W>() {
+        const int rows = s.top_k < 16 / W ? s.top_k : 16 / W;
+        hipLaunchKernelGGL((combine_backward_kernel<Y, D, DY, W>), dim3(s.T), dim3(rows * W * 64), 0, st, (const char*)dout, (const char*)y_perm, inv_perm,
+                           w, s.top_k, s.H, dw, (char*)dy_perm);
+        return hipGetLastError();
+    };
+    auto with_split = [&]<bool Y, bool D, bool DY>() {
+        return split ? run.template operator()<Y, D, DY, 4>() : run.template operator()<Y, D, DY, 1>();
+    };
+    auto with_dy = [&]<bool Y, bool D>() {
+        return dy_perm ? with_split.template operator()<Y, D, true>() : with_split.template operator()<Y, D, false>();
+    };
+    if (y_fp32) return dout_fp32 ? with_dy.operator()<true, true>() : with_dy.operator()<true, false>();
+    return dout_fp32 ? with_dy.operator()<false, true>() : with_dy.operator()<false, false>();
+}
+
+}  // namespace moe

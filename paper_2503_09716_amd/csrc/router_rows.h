@@ -1,0 +1,86 @@
+// A token's row of logits in 16 lanes, for the kernels that train the router (balance.hip, route_backward.hip).
+#pragma once
+#include "topk.h"
+
+namespace moe {
+namespace {
+
+// Lane c of a row of 16 holds NV values.  WIDE: experts 4c..4c+3 of every 64, 16 bytes to a load (E % 4 == 0 and 16-byte aligned
+// matrices); else experts c, c + 16, ..., so that matrices of any alignment and odd E are read 64 bytes to a row.
+template <int NV, bool WIDE>
+__device__ __forceinline__ void load_row16(float (&v)[NV], const float* __restrict__ m, const size_t t, const int E, const int row, const float pad) {
+    const float* const p = m + t * E;
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int b = 0; b < NV / 4; ++b) {
+            const int e = row * 4 + 64 * b;
+            f32x4 q = {pad, pad, pad, pad};
+            if (e < E) q = *reinterpret_cast<const f32x4*>(p + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[4 * b + i] = q[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = row + 16 * i < E ? p[row + 16 * i] : pad;
+    }
+}
+
+template <int NV, bool WIDE>
+__device__ __forceinline__ void store_row16(const float (&v)[NV], float* __restrict__ m, const size_t t, const int E, const int row) {
+    float* const p = m + t * E;
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int b = 0; b < NV / 4; ++b) {
+            const int e = row * 4 + 64 * b;
+            if (e < E) *reinterpret_cast<f32x4*>(p + e) = f32x4{v[4 * b], v[4 * b + 1], v[4 * b + 2], v[4 * b + 3]};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (row + 16 * i < E) p[row + 16 * i] = v[i];
+    }
+}
+
+// Logits to their softmax over the row; the logarithm of the sum of their exponentials.  Values of -inf get probability 0.
+template <int NV>
+__device__ __forceinline__ float softmax_row16(float (&v)[NV]) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) m = fmaxf(m, v[i]);
+    m = row16_max(m);
+    float z = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) { v[i] = expf(v[i] - m); z += v[i]; }
+    z = row16_sum(z);
+    const float rz = 1.0f / z;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] *= rz;
+    return m + logf(z);
+}
+
+}  // namespace
+
+// Runs f.template operator()<NV, WIDE>() for the narrowest row that holds E experts.
+template <class F>
+hipError_t for_row16(const int E, const bool wide, F&& f) {
+    if (wide) {
+        if (E <= 64) return f.template operator()<4, true>();
+        if (E <= 128) return f.template operator()<8, true>();
+        if (E <= 192) return f.template operator()<12, true>();
+        return f.template operator()<16, true>();
+    }
+    if (E <= 16) return f.template operator()<1, false>();
+    if (E <= 32) return f.template operator()<2, false>();
+    if (E <= 64) return f.template operator()<4, false>();
+    if (E <= 128) return f.template operator()<8, false>();
+    if (E <= 192) return f.template operator()<12, false>();
+    return f.template operator()<16, false>();
+}
+
+inline bool wide_rows(const int E, std::initializer_list<const void*> matrices) {
+    bool ok = E % 4 == 0 && E > 16;   // up to 16 experts a lane has one of them
+    for (const void* m : matrices) ok = ok && ((uintptr_t)m & 15) == 0;
+    return ok;
+}
+
+}  // namespace moe

@@ -1,0 +1,75 @@
+// Arguments and launchers of the kernels that train a router: balance loss, gradients of the router and of the combine, clipping.
+#pragma once
+#include <initializer_list>
+
+#include "common.h"
+
+namespace moe {
+
+struct BalanceArgs {
+    const float* logits;
+    const int32_t* idx;
+    const uint8_t* keep;       // or nullptr: every token counts
+    double balance_coef, z_coef;
+    int32_t* counts;
+    float *loss, *dlogits;     // dlogits: or nullptr
+    int32_t T, E, k;
+    int32_t count_blocks, count_tokens, loss_blocks;   // workgroups of the two launches; tokens to one of the first
+    int32_t* partial_counts;   // [count_blocks][E + 1]: histograms, kept tokens
+    double* partial_loss;      // [loss_blocks][2]
+    int32_t* done;
+};
+constexpr int BALANCE_COUNT_BLOCKS = 64, BALANCE_LOSS_BLOCKS = 512;
+constexpr int64_t BALANCE_ALONE = 4096;   // logits up to which one workgroup does all
+hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t st);
+
+// The gradient of the logits travels in pieces of bf16 (hi + mid + lo = its 24 bits) in the order in which the matrix instructions
+// take operands: 1 KiB blocks of 16 rows x 32 contraction steps, lane l's 16 bytes at 16 l (row l % 16, steps 8 (l / 16) .. + 7).
+struct RouteBackwardArgs {
+    const char *x, *wg;
+    const float* logits;
+    const int32_t* idx;
+    const float* dw;           // gradient of the weights
+    const float* dlogits;      // or nullptr
+    const uint8_t* keep;       // or nullptr
+    char* dx;                  // or nullptr
+    float *dwg, *dbias;        // dbias: or nullptr
+    int32_t T, H, E, k, renorm, accumulate;
+    float scale;
+    int32_t nb, kb;            // blocks of 16 experts (as many as the kernel's variant takes), of 32 experts
+    int32_t steps;             // blocks of 32 tokens
+    int32_t splits, split_steps;   // parts of the tokens that dWg is summed over apart, blocks of 32 tokens to one
+    char* zeros;               // 1 KiB that the first launch clears
+    uint32_t* masks;           // [T / 32]: the tokens that count
+    char* dl_dx;               // [T / 16][hi, mid][kb] blocks: rows are tokens, steps experts
+    char* dl_dw;               // [T / 32][hi, mid, lo][nb] blocks: rows are experts, steps tokens
+    char* wg_blocks;           // [H / 32][2][kb] blocks: row i of block b is h = 8 (i / 4) + 4 b + i % 4 of 32, steps are experts
+    float* partial;            // [splits][H + 1][16 nb]: row H the sum of dl
+};
+int route_backward_blocks(int E);   // nb
+constexpr int ROUTE_BACKWARD_TILE = 256;   // columns of x to a workgroup of the dWg product
+hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st);
+hipError_t launch_route_backward_empty(const moe_shape& s, float* dwg, float* dbias, hipStream_t st);
+hipError_t route_backward_init();
+
+hipError_t launch_combine_backward(const moe_shape& s, const void* dout, const void* y_perm, const int32_t* inv_perm, const float* w, float* dw,
+                                   void* dy_perm, bool y_fp32, bool dout_fp32, hipStream_t st);
+
+// A piece of a tensor: at most CLIP_CHUNK bytes.
+struct ClipChunk {
+    const char* src;
+    char* dst;
+    uint32_t elements, fp32;
+};
+constexpr int CLIP_CHUNK = 32768;
+struct ClipArgs {
+    const ClipChunk* chunks;
+    double* partial;           // [CLIP_BLOCKS]
+    float* norm;
+    double max_norm;
+    int32_t n_chunks, in_place;   // in_place: an output is its own gradient
+};
+constexpr int CLIP_BLOCKS = 1024;
+hipError_t launch_clip(const ClipArgs& a, hipStream_t st);
+
+}  // namespace moe
