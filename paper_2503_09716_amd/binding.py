@@ -169,6 +169,11 @@ def _typed(t: Optional[torch.Tensor], dtype, numel: int):
     return t.data_ptr()
 
 
+def _raw_stream(device: int):
+    """The device's current stream; torch.cuda.current_stream() makes an object for it, which takes longer than a small kernel's launch."""
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 class GradientList:
     """Tensors whose gradients are clipped together (Moe.gradient_list): keeps them and the device table alive."""
 
@@ -273,7 +278,7 @@ class Moe:
         self._check(self.lib.moe_balance_loss(self.h, C.byref(shape), _typed(logits, torch.float32, T * E),
                                               _typed(topk_idx, torch.int32, T * shape.top_k), _typed(keep, torch.bool, T),
                                               balance_coef, z_coef, _typed(counts, torch.int32, E), _typed(loss, torch.float32, 2),
-                                              _typed(dlogits, torch.float32, T * E), _ptr(workspace), workspace.numel(), _stream()))
+                                              _typed(dlogits, torch.float32, T * E), _ptr(workspace), workspace.numel(), _raw_stream(self.device)))
 
     def route_backward(self, shape, x, wg, logits, topk_idx, dtopk_w, dlogits, keep, dx, dwg, dbias, accumulate, workspace):
         """dlogits, keep (bool [T]), dx and dbias may be None."""
@@ -283,7 +288,7 @@ class Moe:
                                                 _typed(logits, f32, T * E), _typed(topk_idx, torch.int32, R), _typed(dtopk_w, f32, R),
                                                 _typed(dlogits, f32, T * E), _typed(keep, torch.bool, T), _typed(dx, b16, T * H),
                                                 _typed(dwg, f32, H * E), _typed(dbias, f32, E), 1 if accumulate else 0,
-                                                _ptr(workspace), workspace.numel(), _stream()))
+                                                _ptr(workspace), workspace.numel(), _raw_stream(self.device)))
 
     def combine_backward(self, shape, dout, y_perm, inv_perm, topk_w, dtopk_w, dy_perm):
         """dout as option "out_fp32" has it, y_perm and dy_perm (or None) as "y_fp32" has them."""
@@ -292,7 +297,7 @@ class Moe:
         y, o = (f32 if self.options.get(n, d) else b16 for n, d in (("y_fp32", 1), ("out_fp32", 0)))
         self._check(self.lib.moe_combine_backward(self.h, C.byref(shape), _typed(dout, o, T * H), _typed(y_perm, y, R * H),
                                                   _typed(inv_perm, torch.int32, R), _typed(topk_w, f32, R), _typed(dtopk_w, f32, R),
-                                                  _typed(dy_perm, y, R * H), _stream()))
+                                                  _typed(dy_perm, y, R * H), _raw_stream(self.device)))
 
     def gradient_list(self, grads: Sequence[torch.Tensor], outs: Sequence[torch.Tensor]) -> GradientList:
         """The tensors (fp32 or bf16) that clip_gradients takes together; outs[i] receives grads[i] scaled and may be it."""
@@ -307,11 +312,11 @@ class Moe:
         buffer = torch.empty(int(self.lib.moe_gradient_list_bytes(n, sizes, types)), dtype=torch.uint8, device="cuda:%d" % self.device)
         struct = GradientListStruct()
         self._check(self.lib.moe_gradient_list_make(self.h, n, _table(grads), _table(outs), sizes, types, _ptr(buffer),
-                                                    buffer.numel(), C.byref(struct), _stream()))
+                                                    buffer.numel(), C.byref(struct), _raw_stream(self.device)))
         return GradientList(struct, buffer, grads, outs)
 
     def clip_gradients(self, gradients: GradientList, max_norm: float, norm):
-        self._check(self.lib.moe_clip_gradients(self.h, C.byref(gradients.struct), max_norm, _typed(norm, torch.float32, 1), _stream()))
+        self._check(self.lib.moe_clip_gradients(self.h, C.byref(gradients.struct), max_norm, _typed(norm, torch.float32, 1), _raw_stream(self.device)))
 
     # ---- fused call --------------------------------------------------------------------
     def layer(self, shape, x, wg, bias, w1p, w3p, w2p, out, workspace, tables=None):

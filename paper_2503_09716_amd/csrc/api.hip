@@ -820,15 +820,15 @@ struct BalanceLayout {
 };
 BalanceLayout balance_layout(const moe_shape& s) {
     BalanceLayout L;
-    // a workgroup of the counts takes at least 2048 picks, one of the loss 16 tokens at a time
+    // a workgroup of the counts takes at least 2048 picks, one of the loss 64 tokens at a time
     int64_t n = ((int64_t)s.T * s.top_k + 2047) / 2048;
     if (n > BALANCE_COUNT_BLOCKS) n = BALANCE_COUNT_BLOCKS;
     if (n < 1) n = 1;
     L.count_tokens = (int)((s.T + n - 1) / n);
     if (L.count_tokens < 1) L.count_tokens = 1;
     L.count_blocks = s.T ? (s.T + L.count_tokens - 1) / L.count_tokens : 1;
-    const int64_t quads = ((int64_t)s.T + 15) / 16;
-    L.loss_blocks = (int)(quads < 1 ? 1 : quads < BALANCE_LOSS_BLOCKS ? quads : BALANCE_LOSS_BLOCKS);
+    const int64_t most = ((int64_t)s.T + 63) / 64;
+    L.loss_blocks = (int)(most < 1 ? 1 : most < BALANCE_LOSS_BLOCKS ? most : BALANCE_LOSS_BLOCKS);
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
     L.partial_counts = take((size_t)L.count_blocks * (s.E + 1) * 4);

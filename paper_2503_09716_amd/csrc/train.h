@@ -19,7 +19,7 @@ struct BalanceArgs {
     double* partial_loss;      // [loss_blocks][2]
     int32_t* done;
 };
-constexpr int BALANCE_COUNT_BLOCKS = 64, BALANCE_LOSS_BLOCKS = 512;
+constexpr int BALANCE_COUNT_BLOCKS = 32, BALANCE_LOSS_BLOCKS = 256;
 constexpr int64_t BALANCE_ALONE = 4096;   // logits up to which one workgroup does all
 hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t st);
 
