@@ -187,16 +187,58 @@ __global__ __launch_bounds__(256) void route_backward_prep_kernel(const RouteBac
     }
 }
 
+// Hand-over point of an LDS ring: at most N of this wave's loads and stores are in flight and its LDS reads have returned; then it
+// meets the others.
+template <int N>
+__device__ __forceinline__ void ring_wait() {
+    static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | 0x0070);  // vmcnt(N) lgkmcnt(0), gfx9 encoding
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void ring_meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Consecutive places of an XCD's run of workgroups (ids are dealt over the 8 XCDs in turn) in [0, n): neighbours share an L2.
+__device__ __forceinline__ int xcd_place(const int id, const int n) {
+    const int x = id & 7;
+    return x * (n >> 3) + min(x, n & 7) + (id >> 3);
+}
+
 // ---- dx = dl Wg^T ---------------------------------------------------------------------------
-// A wavefront keeps the dl of 32 tokens in registers and walks over H, 32 columns at a time: the gate matrix is the row operand, so
-// that a lane ends up with 8 consecutive columns of a token (two blocks whose rows are interleaved by fours) and stores 16 bytes.
-constexpr int DX_TOKENS = 128;
+// A workgroup of 8 wavefronts takes 256 tokens and a part of H.  A wavefront keeps the dl of 32 tokens in registers; the gate matrix
+// comes 128 columns at a time through a ring of LDS stages.  The gate matrix is the row operand, so that a lane ends up with 8
+// consecutive columns of a token (two blocks whose rows are interleaved by fours) and stores 16 bytes.
 template <int KB>
-__global__ __launch_bounds__(256) void route_backward_dx_kernel(const RouteBackwardArgs a, const int token_tiles, const int parts, const int part_groups) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int tile = blockIdx.x % token_tiles, part = blockIdx.x / token_tiles;
-    const int t32 = tile * 4 + wave;
-    if (t32 >= a.steps) return;   // no barrier follows
+struct DxTile {
+    static constexpr int GROUPS = 4;                  // groups of 32 columns to a stage
+    static constexpr int STAGE = GROUPS * 2 * KB * 1024;   // KB wave-loads of 1 KiB to a wavefront
+    static constexpr int NS = KB <= 4 ? 4 : KB <= 6 ? 3 : 2;
+    static constexpr int LDS = NS * STAGE;
+    static constexpr int STORES = GROUPS * 2;         // of a wavefront, to a stage
+};
+
+template <int KB>
+__device__ __forceinline__ void dx_tile(const RouteBackwardArgs& a, const int id, const lds_t lds) {
+    typedef DxTile<KB> L;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = id % a.dx_tiles, part = id / a.dx_tiles;
+    const int t32 = tile * 8 + wave, here = min(t32, a.steps - 1);
+    const bool full = t32 * 32 + 32 <= a.T;
+    const int g0 = part * a.dx_groups, g1 = min(g0 + a.dx_groups, a.H / 32);
+    const int n = (g1 - g0 + L::GROUPS - 1) / L::GROUPS;
+    const int last_block = g1 * 2 * KB - 1;
+    auto issue = [&](const int i, const int stage) {
+#pragma unroll
+        for (int u = 0; u < KB; ++u) {
+            const int q = wave * KB + u;
+            const int blk = min((g0 + min(i, n - 1) * L::GROUPS) * 2 * KB + q, last_block);
+            load16_to_lds(a.wg_blocks + (size_t)blk * 1024 + lane * 16, lds + stage * L::STAGE + q * 1024);
+        }
+    };
     bf16x8 d[2][2][KB];   // [half][piece]
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -204,30 +246,48 @@ __global__ __launch_bounds__(256) void route_backward_dx_kernel(const RouteBackw
         for (int q = 0; q < 2; ++q)
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
-                d[half][q][kb] = reinterpret_cast<const bf16x8*>(a.dl_dx)[((size_t)(t32 * 2 + half) * 2 * KB + q * KB + kb) * 64 + lane];
-    const int g0 = part * part_groups, g1 = min(g0 + part_groups, a.H / 32);
-    const bf16x8* w = reinterpret_cast<const bf16x8*>(a.wg_blocks) + (size_t)g0 * 2 * KB * 64 + lane;
-    for (int g = g0; g < g1; ++g, w += 2 * KB * 64) {
-        f32x4 acc[2][2] = {};
+                d[half][q][kb] = reinterpret_cast<const bf16x8*>(a.dl_dx)[((size_t)(here * 2 + half) * 2 * KB + q * KB + kb) * 64 + lane];
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+    for (int i = 0; i < L::NS - 1; ++i) issue(i, i);
+    const int t = t32 * 32 + (lane & 15);
+    int stage = 0;
+    for (int i = 0; i < n; ++i) {
+        // Loads and stores retire in the order they were issued.  A wavefront whose tokens all exist stores the same number of times in
+        // every stage but the last, so it can leave those behind the stage's loads in flight; others wait for all but loads.
+        if (full) ring_wait<(L::NS - 2) * KB + (L::NS - 1) * L::STORES>();
+        else ring_wait<(L::NS - 2) * KB>();
+        ring_meet();
+        int next = stage + L::NS - 1;
+        if (next >= L::NS) next -= L::NS;
+        issue(i + L::NS - 1, next);
+        const lds_t w = lds + stage * L::STAGE + lane * 16;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const bf16x8 m = w[(b * KB + kb) * 64];
+        for (int u = 0; u < L::GROUPS; ++u) {
+            const int g = g0 + i * L::GROUPS + u;
+            if (g >= g1) break;
+            f32x4 acc[2][2] = {};
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                    for (int q = 1; q >= 0; --q) acc[half][b] = mfma(m, d[half][q][kb], acc[half][b]);
+                for (int q = 1; q >= 0; --q)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const bf16x8 m = *(frag_ptr_t)(w + ((u * 2 + b) * KB + kb) * 1024);
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) acc[half][b] = mfma(m, d[half][q][kb], acc[half][b]);
+                    }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                bf16x8 o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { o[j] = (__bf16)acc[half][0][j]; o[4 + j] = (__bf16)acc[half][1][j]; }
+                if (full || t + 16 * half < a.T)
+                    *reinterpret_cast<bf16x8*>(a.dx + ((size_t)(t + 16 * half) * a.H + g * 32 + 8 * (lane >> 4)) * 2) = o;
             }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int t = t32 * 32 + half * 16 + (lane & 15);
-            bf16x8 o;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { o[i] = (__bf16)acc[half][0][i]; o[4 + i] = (__bf16)acc[half][1][i]; }
-            if (t < a.T) *reinterpret_cast<bf16x8*>(a.dx + ((size_t)t * a.H + g * 32 + 8 * (lane >> 4)) * 2) = o;
         }
+        if (++stage == L::NS) stage = 0;
     }
+    ring_wait<0>();   // no load may land in LDS that belongs to another workgroup
 }
 
 // ---- dWg = x^T dl ---------------------------------------------------------------------------
@@ -244,29 +304,20 @@ struct DwTile {
     static constexpr int EB = NB / WE;                // blocks of 16 experts to a wavefront
     static constexpr int XBYTES = 32 * ROUTE_BACKWARD_TILE * 2;
     static constexpr int NL = (16 + 3 * NB + 7) / 8;  // wave-loads of 1 KiB to a wavefront and stage
-    static constexpr int STAGE = NL * 8 * 1024;
-    static constexpr int NS = 3 * STAGE <= 160 * 1024 ? 3 : 2;
+    static constexpr int MORE = (16 + 3 * NB) % 8;    // wavefronts with NL wave-loads, where not all have as many
+    static constexpr int STAGE = (16 + 3 * NB) * 1024;
+    static constexpr int NS = 4 * STAGE <= 80 * 1024 ? 4 : 3 * STAGE <= 160 * 1024 ? 3 : 2;
+    static constexpr int LDS = NS * STAGE;
 };
-
-// Waits until at most N of this wave's direct loads are in flight and its LDS reads have returned, then meets the others.
-template <int N>
-__device__ __forceinline__ void ring_sync() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | 0x0070);  // vmcnt(N) lgkmcnt(0), gfx9 encoding
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
 
 // Rows 0..3 and 8..11 (16..19 and 24..27, ...), which a transposing read takes at a time, in different 32-byte chunks of 256 bytes.
 __device__ __forceinline__ int swizzle(const int r) { return (r & 3) | ((r >> 1) & 4); }
 
 template <int NB>
-__global__ __launch_bounds__(512) void route_backward_dw_kernel(const RouteBackwardArgs a, const int h_tiles) {
+__device__ __forceinline__ void dw_tile(const RouteBackwardArgs& a, const int id, const lds_t lds) {
     typedef DwTile<NB> L;
-    extern __shared__ char lds_raw[];
-    const lds_t lds = (lds_t)lds_raw;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int ht = blockIdx.x % h_tiles, split = blockIdx.x / h_tiles;
+    const int ht = id % a.dw_tiles, split = id / a.dw_tiles;
     const int h0 = ht * ROUTE_BACKWARD_TILE;
     const int s0 = split * a.split_steps, s1 = min(s0 + a.split_steps, a.steps);
     const int we = wave % L::WE, wh = wave / L::WE;
@@ -280,13 +331,14 @@ __global__ __launch_bounds__(512) void route_backward_dw_kernel(const RouteBackw
 #pragma unroll
         for (int i = 0; i < L::NL; ++i) {
             const int q = wave + 8 * i;
+            if (q >= 16 + 3 * NB) break;   // the last of some wavefronts
             const char* p = a.zeros + lane * 16;
             if (i < 2) {
                 const int r = 2 * q + (lane >> 5);
                 const int c = (lane & 31) ^ (swizzle(r) << 1);      // source chunk of 16 bytes
                 const int h = h0 + c * 8;
                 if ((mask >> r & 1) && h < a.H) p = a.x + ((size_t)(step * 32 + r) * a.H + h) * 2;
-            } else if (q < 16 + 3 * NB) {
+            } else {
                 p = a.dl_dw + ((size_t)step * 3 * NB + (q - 16)) * 1024 + lane * 16;
             }
             load16_to_lds(p, base + q * 1024);
@@ -308,7 +360,9 @@ __global__ __launch_bounds__(512) void route_backward_dw_kernel(const RouteBackw
         int stage = 0;
         uint32_t mask = masks[min(s0 + L::NS - 1, s1 - 1)];
         for (int s = s0; s < s1; ++s) {
-            ring_sync<(L::NS - 2) * L::NL>();
+            if (L::MORE == 0 || wave < L::MORE) ring_wait<(L::NS - 2) * L::NL>();
+            else ring_wait<(L::NS - 2) * (L::NL - 1)>();
+            ring_meet();
             int next = stage + L::NS - 1;
             if (next >= L::NS) next -= L::NS;
             issue(min(s + L::NS - 1, s1 - 1), mask, next);
@@ -337,8 +391,7 @@ __global__ __launch_bounds__(512) void route_backward_dw_kernel(const RouteBackw
     };
     if (sums) steps.template operator()<true>();
     else steps.template operator()<false>();
-    // The ring's last loads must not land in LDS that belongs to another workgroup.
-    ring_sync<0>();
+    ring_wait<0>();   // no load may land in LDS that belongs to another workgroup
     float* const out = a.partial + (size_t)split * (a.H + 1) * (16 * NB);
 #pragma unroll
     for (int hb = 0; hb < L::HB; ++hb) {
@@ -352,6 +405,20 @@ __global__ __launch_bounds__(512) void route_backward_dw_kernel(const RouteBackw
 #pragma unroll
         for (int eb = 0; eb < L::EB; ++eb)
             *reinterpret_cast<f32x4*>(out + (size_t)a.H * (16 * NB) + (we * L::EB + eb) * 16 + 4 * (lane >> 4)) = bias[eb];
+}
+
+// Both products in one launch: the workgroups of dWg, then those of dx.
+template <int NB>
+__global__ __launch_bounds__(512) void route_backward_products_kernel(const RouteBackwardArgs a) {
+    extern __shared__ char lds_raw[];
+    const lds_t lds = (lds_t)lds_raw;
+    const int n = a.dw_tiles * a.splits;
+    if ((int)blockIdx.x < n) dw_tile<NB>(a, xcd_place(blockIdx.x, n), lds);
+    else dx_tile<(NB + 1) / 2>(a, blockIdx.x - n, lds);
+}
+template <int NB>
+constexpr int products_lds() {
+    return DwTile<NB>::LDS > DxTile<(NB + 1) / 2>::LDS ? DwTile<NB>::LDS : DxTile<(NB + 1) / 2>::LDS;
 }
 
 // dWg and dbias: the parts of the tokens added in order.
@@ -401,8 +468,7 @@ hipError_t route_backward_init() {
     hipError_t e = hipSuccess;
     for (int nb : {1, 2, 4, 6, 8, 10, 12, 16}) {
         const hipError_t r = for_blocks(nb, []<int NB>() {
-            return hipFuncSetAttribute((const void*)route_backward_dw_kernel<NB>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                       DwTile<NB>::NS * DwTile<NB>::STAGE);
+            return hipFuncSetAttribute((const void*)route_backward_products_kernel<NB>, hipFuncAttributeMaxDynamicSharedMemorySize, products_lds<NB>());
         });
         if (e == hipSuccess) e = r;
     }
@@ -418,23 +484,11 @@ hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st) {
     });
     if (e != hipSuccess) return e;
     e = for_blocks(a.nb, [&]<int NB>() {
-        const int h_tiles = (a.H + ROUTE_BACKWARD_TILE - 1) / ROUTE_BACKWARD_TILE;
-        hipLaunchKernelGGL(route_backward_dw_kernel<NB>, dim3(h_tiles * a.splits), dim3(512), DwTile<NB>::NS * DwTile<NB>::STAGE, st, a, h_tiles);
+        const unsigned grid = (unsigned)(a.dw_tiles * a.splits + (a.dx ? a.dx_tiles * a.dx_parts : 0));
+        hipLaunchKernelGGL(route_backward_products_kernel<NB>, dim3(grid), dim3(512), products_lds<NB>(), st, a);
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    if (a.dx) {
-        const int tiles = (a.steps + 3) / 4, groups = a.H / 32;
-        int parts = (1024 + tiles - 1) / tiles;
-        if (parts > groups) parts = groups;
-        const int per = (groups + parts - 1) / parts;
-        parts = (groups + per - 1) / per;
-#define DX(KB_)                                                                                                                          \
-    case KB_: hipLaunchKernelGGL(route_backward_dx_kernel<KB_>, dim3(tiles * parts), dim3(256), 0, st, a, tiles, parts, per); break
-        switch (a.kb) { DX(1); DX(2); DX(3); DX(4); DX(5); DX(6); DX(7); DX(8); }
-#undef DX
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
     hipLaunchKernelGGL(route_backward_sum_kernel, dim3((unsigned)(((size_t)(a.H + 1) * a.E + 255) / 256)), dim3(256), 0, st, a);
     return hipGetLastError();
 }

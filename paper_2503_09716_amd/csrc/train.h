@@ -38,7 +38,8 @@ struct RouteBackwardArgs {
     float scale;
     int32_t nb, kb;            // blocks of 16 experts (as many as the kernel's variant takes), of 32 experts
     int32_t steps;             // blocks of 32 tokens
-    int32_t splits, split_steps;   // parts of the tokens that dWg is summed over apart, blocks of 32 tokens to one
+    int32_t dw_tiles, splits, split_steps;    // dWg: tiles of H, parts of the tokens that are summed apart, blocks of 32 tokens to one
+    int32_t dx_tiles, dx_parts, dx_groups;    // dx: tiles of 256 tokens, parts of H, groups of 32 columns to one
     char* zeros;               // 1 KiB that the first launch clears
     uint32_t* masks;           // [T / 32]: the tokens that count
     char* dl_dx;               // [T / 16][hi, mid][kb] blocks: rows are tokens, steps experts
