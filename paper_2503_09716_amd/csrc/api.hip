@@ -839,8 +839,8 @@ BalanceLayout balance_layout(const moe_shape& s) {
 }
 
 struct RouteBackwardLayout {
-    int nb, kb, steps, dw_tiles, splits, split_steps, dx_tiles, dx_parts, dx_groups;
-    size_t zeros, masks, dl_dx, dl_dw, wg_blocks, partial, total;
+    int nb, kb, steps, tiles, splits, split_steps;
+    size_t zeros, masks, dl_blocks, wg_blocks, partial, total;
 };
 RouteBackwardLayout route_backward_layout(const moe_shape& s) {
     RouteBackwardLayout L;
@@ -849,25 +849,17 @@ RouteBackwardLayout route_backward_layout(const moe_shape& s) {
     L.steps = (s.T + 31) / 32;
     if (L.steps < 1) L.steps = 1;
     // as many parts of the tokens as fill the CUs with workgroups (two to a CU up to 32 experts, whose ring is small)
-    const int cus = L.nb <= 2 ? 512 : 256;
-    L.dw_tiles = (s.H + ROUTE_BACKWARD_TILE - 1) / ROUTE_BACKWARD_TILE;
-    const int want = cus / L.dw_tiles;
+    const int columns = route_backward_columns(L.nb);
+    L.tiles = (s.H + columns - 1) / columns;
+    const int want = (L.nb <= 2 ? 512 : 256) / L.tiles;
     const int parts = want < 1 ? 1 : want < L.steps ? want : L.steps;
     L.split_steps = (L.steps + parts - 1) / parts;
     L.splits = (L.steps + L.split_steps - 1) / L.split_steps;
-    // dx the same, its parts of H a whole number of stages of 4 groups
-    const int stages = (s.H / 32 + 3) / 4;
-    L.dx_tiles = (L.steps + 7) / 8;
-    int hp = (cus + L.dx_tiles - 1) / L.dx_tiles;
-    hp = hp < stages ? hp : stages;
-    L.dx_groups = (stages + hp - 1) / hp * 4;
-    L.dx_parts = (s.H / 32 + L.dx_groups - 1) / L.dx_groups;
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
     L.zeros = take(1024);
     L.masks = take((size_t)L.steps * 4);
-    L.dl_dx = take((size_t)L.steps * 4 * L.kb * 1024);
-    L.dl_dw = take((size_t)L.steps * 3 * L.nb * 1024);
+    L.dl_blocks = take((size_t)L.steps * 3 * L.nb * 1024);
     L.wg_blocks = take((size_t)s.H / 16 * L.kb * 1024);
     L.partial = take((size_t)L.splits * (s.H + 1) * 16 * L.nb * 4);
     L.total = o;
@@ -1364,8 +1356,8 @@ moe_status moe_route_backward(moe_ctx* c, const moe_shape* s, const void* x, con
     const RouteBackwardLayout L = route_backward_layout(*s);
     char* const w8 = (char*)ws;
     const RouteBackwardArgs a{(const char*)x, (const char*)wg, logits, idx, dw, dlogits, keep, (char*)dx, dwg, dbias, s->T, s->H, s->E, s->top_k,
-                              s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.dw_tiles, L.splits, L.split_steps, L.dx_tiles, L.dx_parts, L.dx_groups, w8 + L.zeros, (uint32_t*)(w8 + L.masks), w8 + L.dl_dx,
-                              w8 + L.dl_dw, w8 + L.wg_blocks, (float*)(w8 + L.partial)};
+                              s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.tiles, L.splits, L.split_steps, w8 + L.zeros,
+                              (uint32_t*)(w8 + L.masks), w8 + L.dl_blocks, w8 + L.wg_blocks, (float*)(w8 + L.partial)};
     HIP_TRY(c, launch_route_backward(a, hs));
     return MOE_OK;
 }

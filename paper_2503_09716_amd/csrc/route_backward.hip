@@ -34,36 +34,64 @@ __device__ __forceinline__ void load16_to_lds(const char* p, lds_t l) {
 #endif
 }
 
-// Column blocks of x as matrix operands, from rows of 512 bytes in LDS.  ds_read_b64_tr_b16 takes four rows of 16 bf16 to a group of 16
-// lanes: lane i gives the address of elements 4 (i % 4) .. + 3 of row i / 4 and gets column i.  Two of them, four rows apart, make a
-// lane's 8 steps.  Assembly with its own wait: before the builtin the compiler waits for every direct load in flight.
-__device__ __forceinline__ void read_transposed(bf16x8 (&f)[2], const lds_t p0, const lds_t p1) {
+// Columns of rows of bf16 in LDS as matrix operands.  ds_read_b64_tr_b16 takes four rows of 16 to a group of 16 lanes: lane i gives the
+// address of elements 4 (i % 4) .. + 3 of row i / 4 and gets column i.  Two of them make a lane's 8 steps.  Assembly with its own wait:
+// before the builtin the compiler waits for every direct load in flight.
+// Two operands: from p0 + A and q0 + A2, from p1 + B and q1 + B2.
+template <int A, int A2, int B, int B2>
+__device__ __forceinline__ void read_transposed(bf16x8& f0, bf16x8& f1, const lds_t p0, const lds_t q0, const lds_t p1, const lds_t q1) {
 #if defined(__gfx950__)
     u32x2 a, b, c, d;
-    asm volatile("ds_read_b64_tr_b16 %0, %4\n\t"
-                 "ds_read_b64_tr_b16 %1, %4 offset:2048\n\t"
-                 "ds_read_b64_tr_b16 %2, %5\n\t"
-                 "ds_read_b64_tr_b16 %3, %5 offset:2048\n\t"
+    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%8\n\t"
+                 "ds_read_b64_tr_b16 %1, %5 offset:%9\n\t"
+                 "ds_read_b64_tr_b16 %2, %6 offset:%10\n\t"
+                 "ds_read_b64_tr_b16 %3, %7 offset:%11\n\t"
                  "s_waitcnt lgkmcnt(0)"
-                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d) : "v"((uint32_t)(uintptr_t)p0), "v"((uint32_t)(uintptr_t)p1) : "memory");
-    f[0] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
-    f[1] = __builtin_bit_cast(bf16x8, u32x4{c[0], c[1], d[0], d[1]});
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
+                 : "v"((uint32_t)(uintptr_t)p0), "v"((uint32_t)(uintptr_t)q0), "v"((uint32_t)(uintptr_t)p1), "v"((uint32_t)(uintptr_t)q1), "n"(A), "n"(A2),
+                   "n"(B), "n"(B2) : "memory");
+    f0 = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+    f1 = __builtin_bit_cast(bf16x8, u32x4{c[0], c[1], d[0], d[1]});
 #endif
 }
+// Four operands, the second half of each NEXT bytes behind its first.
+template <int NEXT>
 __device__ __forceinline__ void read_transposed(bf16x8 (&f)[4], const lds_t p0, const lds_t p1, const lds_t p2, const lds_t p3) {
 #if defined(__gfx950__)
     u32x2 a, b, c, d, e, g, h, i;
     asm volatile("ds_read_b64_tr_b16 %0, %8\n\t"
-                 "ds_read_b64_tr_b16 %1, %8 offset:2048\n\t"
+                 "ds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
                  "ds_read_b64_tr_b16 %2, %9\n\t"
-                 "ds_read_b64_tr_b16 %3, %9 offset:2048\n\t"
+                 "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
                  "ds_read_b64_tr_b16 %4, %10\n\t"
-                 "ds_read_b64_tr_b16 %5, %10 offset:2048\n\t"
+                 "ds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
                  "ds_read_b64_tr_b16 %6, %11\n\t"
-                 "ds_read_b64_tr_b16 %7, %11 offset:2048\n\t"
+                 "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d), "=&v"(e), "=&v"(g), "=&v"(h), "=&v"(i)
-                 : "v"((uint32_t)(uintptr_t)p0), "v"((uint32_t)(uintptr_t)p1), "v"((uint32_t)(uintptr_t)p2), "v"((uint32_t)(uintptr_t)p3) : "memory");
+                 : "v"((uint32_t)(uintptr_t)p0), "v"((uint32_t)(uintptr_t)p1), "v"((uint32_t)(uintptr_t)p2), "v"((uint32_t)(uintptr_t)p3), "n"(NEXT) : "memory");
+    f[0] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+    f[1] = __builtin_bit_cast(bf16x8, u32x4{c[0], c[1], d[0], d[1]});
+    f[2] = __builtin_bit_cast(bf16x8, u32x4{e[0], e[1], g[0], g[1]});
+    f[3] = __builtin_bit_cast(bf16x8, u32x4{h[0], h[1], i[0], i[1]});
+#endif
+}
+// Four operands, from p + A and q + A to p + D and q + D.
+template <int A, int B, int C, int D>
+__device__ __forceinline__ void read_transposed(bf16x8 (&f)[4], const lds_t p, const lds_t q) {
+#if defined(__gfx950__)
+    u32x2 a, b, c, d, e, g, h, i;
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%10\n\t"
+                 "ds_read_b64_tr_b16 %1, %9 offset:%10\n\t"
+                 "ds_read_b64_tr_b16 %2, %8 offset:%11\n\t"
+                 "ds_read_b64_tr_b16 %3, %9 offset:%11\n\t"
+                 "ds_read_b64_tr_b16 %4, %8 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %5, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %6, %8 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %7, %9 offset:%13\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d), "=&v"(e), "=&v"(g), "=&v"(h), "=&v"(i)
+                 : "v"((uint32_t)(uintptr_t)p), "v"((uint32_t)(uintptr_t)q), "n"(A), "n"(B), "n"(C), "n"(D) : "memory");
     f[0] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
     f[1] = __builtin_bit_cast(bf16x8, u32x4{c[0], c[1], d[0], d[1]});
     f[2] = __builtin_bit_cast(bf16x8, u32x4{e[0], e[1], g[0], g[1]});
@@ -75,6 +103,10 @@ __device__ __forceinline__ void read_transposed(bf16x8 (&f)[4], const lds_t p0, 
 // A workgroup takes 32 tokens, a token in a row of 16 lanes; they meet in LDS and leave as operand blocks.  Workgroups past those of
 // the tokens lay the gate matrix out.
 constexpr int PREP_TOKENS = 32;
+
+// The expert (of 16) that lies e-th among those of tokens 8 g .. + 7 in a block of dl, and the other way round: what the transposing read
+// takes at a time of two neighbouring g lies in different banks.
+__device__ __forceinline__ int dl_row(const int e, const int g) { return e ^ ((g & 1) << 2); }
 
 // v as bf16 pieces.
 __device__ __forceinline__ void split3(const float v, __bf16& hi, __bf16& mid, __bf16& lo) {
@@ -153,37 +185,21 @@ __global__ __launch_bounds__(256) void route_backward_prep_kernel(const RouteBac
     }
     __syncthreads();
     if (threadIdx.x == 0) a.masks[blockIdx.x] = mask;
-    // For dWg: blocks of 16 experts, steps are the 32 tokens.
-    char* const out = a.dl_dw + (size_t)blockIdx.x * 3 * a.nb * 1024;
+    // Blocks of 16 experts, steps are the 32 tokens.
+    char* const out = a.dl_blocks + (size_t)blockIdx.x * 3 * a.nb * 1024;
     for (int p = threadIdx.x; p < a.nb * 64; p += 256) {
-        const int l = p & 63, e = (p >> 6) * 16 + (l & 15), t0 = 8 * (l >> 4);
+        const int at = p & 63, g = at >> 4, e = (p >> 6) * 16 + dl_row(at & 15, g);
         bf16x8 hi, mid, lo;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             __bf16 h, m, w;
-            split3(e < 16 * NV ? dl[t0 + i][e] : 0.f, h, m, w);
+            split3(e < 16 * NV ? dl[8 * g + i][e] : 0.f, h, m, w);
             hi[i] = h; mid[i] = m; lo[i] = w;
         }
         bf16x8* const o = reinterpret_cast<bf16x8*>(out) + p;
         o[0] = hi;
         o[a.nb * 64] = mid;
         o[2 * a.nb * 64] = lo;
-    }
-    if (!a.dx) return;
-    // For dx: blocks of 16 tokens, steps are experts.
-    char* const out2 = a.dl_dx + (size_t)blockIdx.x * 4 * a.kb * 1024;
-    for (int p = threadIdx.x; p < 2 * a.kb * 64; p += 256) {
-        const int l = p & 63, half = (p >> 6) / a.kb, kb = (p >> 6) % a.kb, t = 16 * half + (l & 15), e0 = kb * 32 + 8 * (l >> 4);
-        bf16x8 hi, mid;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            __bf16 h, m, w;
-            split3(e0 + i < 16 * NV ? dl[t][e0 + i] : 0.f, h, m, w);
-            hi[i] = h; mid[i] = m;
-        }
-        bf16x8* const o = reinterpret_cast<bf16x8*>(out2) + (size_t)half * 2 * a.kb * 64 + kb * 64 + l;
-        o[0] = hi;
-        o[a.kb * 64] = mid;
     }
 }
 
@@ -208,151 +224,113 @@ __device__ __forceinline__ int xcd_place(const int id, const int n) {
     return x * (n >> 3) + min(x, n & 7) + (id >> 3);
 }
 
-// ---- dx = dl Wg^T ---------------------------------------------------------------------------
-// A workgroup of 8 wavefronts takes 256 tokens and a part of H.  A wavefront keeps the dl of 32 tokens in registers; the gate matrix
-// comes 128 columns at a time through a ring of LDS stages.  The gate matrix is the row operand, so that a lane ends up with 8
-// consecutive columns of a token (two blocks whose rows are interleaved by fours) and stores 16 bytes.
-template <int KB>
-struct DxTile {
-    static constexpr int GROUPS = 4;                  // groups of 32 columns to a stage
-    static constexpr int STAGE = GROUPS * 2 * KB * 1024;   // KB wave-loads of 1 KiB to a wavefront
-    static constexpr int NS = KB <= 4 ? 4 : KB <= 6 ? 3 : 2;
-    static constexpr int LDS = NS * STAGE;
-    static constexpr int STORES = GROUPS * 2;         // of a wavefront, to a stage
-};
-
-template <int KB>
-__device__ __forceinline__ void dx_tile(const RouteBackwardArgs& a, const int id, const lds_t lds) {
-    typedef DxTile<KB> L;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile = id % a.dx_tiles, part = id / a.dx_tiles;
-    const int t32 = tile * 8 + wave, here = min(t32, a.steps - 1);
-    const bool full = t32 * 32 + 32 <= a.T;
-    const int g0 = part * a.dx_groups, g1 = min(g0 + a.dx_groups, a.H / 32);
-    const int n = (g1 - g0 + L::GROUPS - 1) / L::GROUPS;
-    const int last_block = g1 * 2 * KB - 1;
-    auto issue = [&](const int i, const int stage) {
-#pragma unroll
-        for (int u = 0; u < KB; ++u) {
-            const int q = wave * KB + u;
-            const int blk = min((g0 + min(i, n - 1) * L::GROUPS) * 2 * KB + q, last_block);
-            load16_to_lds(a.wg_blocks + (size_t)blk * 1024 + lane * 16, lds + stage * L::STAGE + q * 1024);
-        }
-    };
-    bf16x8 d[2][2][KB];   // [half][piece]
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-                d[half][q][kb] = reinterpret_cast<const bf16x8*>(a.dl_dx)[((size_t)(here * 2 + half) * 2 * KB + q * KB + kb) * 64 + lane];
-#pragma unroll
-    for (int i = 0; i < L::NS - 1; ++i) issue(i, i);
-    const int t = t32 * 32 + (lane & 15);
-    int stage = 0;
-    for (int i = 0; i < n; ++i) {
-        // Loads and stores retire in the order they were issued.  A wavefront whose tokens all exist stores the same number of times in
-        // every stage but the last, so it can leave those behind the stage's loads in flight; others wait for all but loads.
-        if (full) ring_wait<(L::NS - 2) * KB + (L::NS - 1) * L::STORES>();
-        else ring_wait<(L::NS - 2) * KB>();
-        ring_meet();
-        int next = stage + L::NS - 1;
-        if (next >= L::NS) next -= L::NS;
-        issue(i + L::NS - 1, next);
-        const lds_t w = lds + stage * L::STAGE + lane * 16;
-#pragma unroll
-        for (int u = 0; u < L::GROUPS; ++u) {
-            const int g = g0 + i * L::GROUPS + u;
-            if (g >= g1) break;
-            f32x4 acc[2][2] = {};
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int q = 1; q >= 0; --q)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const bf16x8 m = *(frag_ptr_t)(w + ((u * 2 + b) * KB + kb) * 1024);
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) acc[half][b] = mfma(m, d[half][q][kb], acc[half][b]);
-                    }
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                bf16x8 o;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { o[j] = (__bf16)acc[half][0][j]; o[4 + j] = (__bf16)acc[half][1][j]; }
-                if (full || t + 16 * half < a.T)
-                    *reinterpret_cast<bf16x8*>(a.dx + ((size_t)(t + 16 * half) * a.H + g * 32 + 8 * (lane >> 4)) * 2) = o;
-            }
-        }
-        if (++stage == L::NS) stage = 0;
-    }
-    ring_wait<0>();   // no load may land in LDS that belongs to another workgroup
-}
-
-// ---- dWg = x^T dl ---------------------------------------------------------------------------
-// A workgroup of 8 wavefronts takes 256 columns of x, all experts and a part of the tokens, 32 tokens at a time through a ring of LDS
-// stages filled by direct loads: x as it lies (rows of 512 bytes, 32-byte chunks swizzled by row), dl in operand blocks.  The tokens
-// are the contraction, so x is read from LDS by the transposing read.  Rows of x past the end and of tokens that do not count come
-// from a page of zeros: their dl is zero, but what x holds there may be no number.
-// Experts are the row operand: a lane ends up with four consecutive experts of a column.
+// ---- dWg = x^T dl and dx = dl Wg^T ------------------------------------------------------------
+// A workgroup of 8 wavefronts takes HT columns of x, all experts and a part of the tokens, 32 tokens at a time through a ring of LDS
+// stages filled by direct loads: x as it lies (32-byte chunks swizzled by row) and dl in operand blocks.  Both products use the stage:
+//   dWg: the tokens are the contraction, so x comes out of LDS by the transposing read.  Experts are the row operand: a lane ends up
+//        with four consecutive experts of a column.  The accumulators stay for all tokens.
+//   dx:  the experts are the contraction, so dl comes out by the transposing read.  A wavefront takes a quarter of the columns, whose
+//        part of the gate matrix stays in its registers as the row operand, and 16 of the tokens: a lane ends up with 8 consecutive
+//        columns of a token, two blocks whose rows are interleaved by fours.
+// So x is read and dx written side by side, dl is read once for both.  Rows of x past the end and of tokens that do not count come from
+// a page of zeros: their dl is zero, but what x holds there may be no number.
+// More than 160 experts take half the columns, or the accumulators and the gate matrix would not fit the registers.
 template <int NB>
-struct DwTile {
-    static constexpr int WE = NB >= 4 ? 2 : 1;        // wavefronts along the experts
-    static constexpr int WH = 8 / WE;                 // and along the columns
-    static constexpr int HB = 16 / WH;                // blocks of 16 columns to a wavefront
-    static constexpr int EB = NB / WE;                // blocks of 16 experts to a wavefront
-    static constexpr int XBYTES = 32 * ROUTE_BACKWARD_TILE * 2;
-    static constexpr int NL = (16 + 3 * NB + 7) / 8;  // wave-loads of 1 KiB to a wavefront and stage
-    static constexpr int MORE = (16 + 3 * NB) % 8;    // wavefronts with NL wave-loads, where not all have as many
-    static constexpr int STAGE = (16 + 3 * NB) * 1024;
-    static constexpr int NS = 4 * STAGE <= 80 * 1024 ? 4 : 3 * STAGE <= 160 * 1024 ? 3 : 2;
+struct Tile {
+    static constexpr int HT = NB <= 10 ? 256 : 128;
+    static constexpr int KB = (NB + 1) / 2;            // blocks of 32 experts
+    static constexpr int WE = NB <= 2 ? 1 : NB <= 10 ? 2 : 4;   // wavefronts along the experts
+    static constexpr int WH = 8 / WE;                  // and along the columns
+    static constexpr int HB = HT / 16 / WH;            // blocks of 16 columns to a wavefront
+    static constexpr int EB = NB / WE;                 // blocks of 16 experts to a wavefront
+    static constexpr int DB = HT / 64;                 // dx: blocks of 16 columns to a wavefront
+    static constexpr int ROW = HT * 2;                 // bytes of a row of x
+    static constexpr int XL = HT / 128;                // wave-loads of 1 KiB of x to a wavefront
+    static constexpr int LOADS = 8 * XL + 3 * NB;      // to a stage
+    static constexpr int NL = (LOADS + 7) / 8;         // to a wavefront
+    static constexpr int MORE = LOADS % 8;             // wavefronts with NL of them, where not all have as many
+    static constexpr int STAGE = LOADS * 1024;
+    static constexpr int NS = (NB <= 2 ? 80 : 160) * 1024 / STAGE;
     static constexpr int LDS = NS * STAGE;
+    static constexpr int STORES = DB / 2;              // of dx, of a wavefront in a stage
+    static_assert(HB * WH * 16 == HT && EB * WE == NB && NS >= 2);
 };
 
 // Rows 0..3 and 8..11 (16..19 and 24..27, ...), which a transposing read takes at a time, in different 32-byte chunks of 256 bytes.
 __device__ __forceinline__ int swizzle(const int r) { return (r & 3) | ((r >> 1) & 4); }
 
-template <int NB>
-__device__ __forceinline__ void dw_tile(const RouteBackwardArgs& a, const int id, const lds_t lds) {
-    typedef DwTile<NB> L;
+template <int NB, bool DX>
+__global__ __launch_bounds__(512) void route_backward_products_kernel(const RouteBackwardArgs a) {
+    typedef Tile<NB> L;
+    extern __shared__ char lds_raw[];
+    const lds_t lds = (lds_t)lds_raw;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int ht = id % a.dw_tiles, split = id / a.dw_tiles;
-    const int h0 = ht * ROUTE_BACKWARD_TILE;
+    const int id = xcd_place(blockIdx.x, a.tiles * a.splits);
+    const int ht = id % a.tiles, split = id / a.tiles;
+    const int h0 = ht * L::HT;
     const int s0 = split * a.split_steps, s1 = min(s0 + a.split_steps, a.steps);
     const int we = wave % L::WE, wh = wave / L::WE;
 
     // Which of a step's tokens count, read one step ahead.
     typedef const __attribute__((address_space(4))) uint32_t* masks_t;
     const masks_t masks = (masks_t)a.masks;
-    // wave-load i of this wave is load q = wave + 8 i of the stage: 16 of x (two rows each), then dl's blocks
-    auto issue = [&](const int step, const uint32_t mask, const int stage) {
-        const lds_t base = lds + stage * L::STAGE;
+    // wave-load i of this wave is load q = wave + 8 i of the stage: those of x, then dl's blocks
+    uint32_t x_at[L::XL];    // of this lane's piece from the step's first row on
+    int x_row[L::XL];
+    bool x_in[L::XL];
 #pragma unroll
-        for (int i = 0; i < L::NL; ++i) {
-            const int q = wave + 8 * i;
-            if (q >= 16 + 3 * NB) break;   // the last of some wavefronts
-            const char* p = a.zeros + lane * 16;
-            if (i < 2) {
-                const int r = 2 * q + (lane >> 5);
-                const int c = (lane & 31) ^ (swizzle(r) << 1);      // source chunk of 16 bytes
-                const int h = h0 + c * 8;
-                if ((mask >> r & 1) && h < a.H) p = a.x + ((size_t)(step * 32 + r) * a.H + h) * 2;
-            } else {
-                p = a.dl_dw + ((size_t)step * 3 * NB + (q - 16)) * 1024 + lane * 16;
+    for (int i = 0; i < L::XL; ++i) {
+        constexpr int PER = L::ROW / 16;   // lanes to a row
+        x_row[i] = (wave + 8 * i) * (64 / PER) + lane / PER;
+        const int c = (lane % PER) ^ (swizzle(x_row[i]) << 1);   // source chunk of 16 bytes
+        x_in[i] = h0 + c * 8 < a.H;
+        x_at[i] = (uint32_t)x_row[i] * (uint32_t)a.H * 2 + (uint32_t)(h0 + c * 8) * 2;
+    }
+    const bool inside = h0 + L::HT <= a.H;
+    auto issue = [&](const int step, const uint32_t mask, const int stage) {
+        const lds_t base = lds + stage * L::STAGE + wave * 1024;
+        const char* const xs = a.x + (size_t)step * 64 * a.H;
+        if (inside && mask == ~0u) {   // addresses without a vector operation
+#pragma unroll
+            for (int i = 0; i < L::XL; ++i) load16_to_lds(xs + x_at[i], base + i * 8192);
+        } else {
+#pragma unroll
+            for (int i = 0; i < L::XL; ++i) {
+                const char* const p = x_in[i] && (mask >> x_row[i] & 1) ? xs + x_at[i] : a.zeros + lane * 16;
+                load16_to_lds(p, base + i * 8192);
             }
-            load16_to_lds(p, base + q * 1024);
+        }
+        const char* const ds = a.dl_blocks + ((size_t)step * 3 * NB + wave) * 1024;
+#pragma unroll
+        for (int i = L::XL; i < L::NL; ++i) {
+            if (wave + 8 * i >= L::LOADS) break;   // the last of some wavefronts
+            load16_to_lds(ds + (i - L::XL) * 8192 + (uint32_t)lane * 16, base + i * 8192);
         }
     };
 
+    // dx: this wavefront's columns and tokens
+    const int dh = h0 + (wave & 3) * (L::DB * 16), th = wave >> 2;
+    // dl as the column operand: tokens 8 g .. + 7 of two g, four experts from e on and four more
+    const int g = 2 * th + ((lane & 3) >> 1), e = 8 * ((lane >> 4) & 1) + ((lane & 15) >> 2);
+    const int dl_lane = g * 256 + (lane & 1) * 8 + (NB > 1 ? (lane >> 5) * 1024 : 0);   // one block: its rows again, times zeros of the gate matrix
+    const int dl_first = dl_lane + dl_row(e, g) * 16, dl_next = dl_lane + dl_row(e + 4, g) * 16;
+    bf16x8 wg[L::DB][L::KB];
+    if (DX)
+#pragma unroll
+        for (int b = 0; b < L::DB; ++b)
+#pragma unroll
+            for (int kb = 0; kb < L::KB; ++kb) {
+                const size_t group = min(dh / 32 + b / 2, a.H / 32 - 1);
+                wg[b][kb] = reinterpret_cast<const bf16x8*>(a.wg_blocks)[((group * 2 + b % 2) * L::KB + kb) * 64 + lane];
+            }
+
     f32x4 acc[L::EB][L::HB] = {};
     f32x4 bias[L::EB] = {};
-    const bool sums = ht == 0 && wh == 0;   // whose dl blocks are added up for dbias, too
-
     for (int i = 0; i < L::NS - 1; ++i) {
         const int s = min(s0 + i, s1 - 1);
         issue(s, masks[s], i);
     }
+    // SUMS: dl's blocks are added up for dbias, too.
     auto steps = [&]<bool SUMS>() {
         bf16x8 ones;
 #pragma unroll
@@ -360,35 +338,108 @@ __device__ __forceinline__ void dw_tile(const RouteBackwardArgs& a, const int id
         int stage = 0;
         uint32_t mask = masks[min(s0 + L::NS - 1, s1 - 1)];
         for (int s = s0; s < s1; ++s) {
-            if (L::MORE == 0 || wave < L::MORE) ring_wait<(L::NS - 2) * L::NL>();
-            else ring_wait<(L::NS - 2) * (L::NL - 1)>();
+            // Loads and stores retire in the order they were issued.  Behind this stage's loads there are those of NS - 2 stages and, from
+            // the ring's second round on, NS - 1 steps' stores (all tokens exist in every step but the last, and all columns or none).
+            if (DX && s - s0 >= L::NS - 1 && dh + L::DB * 16 <= a.H) {
+                if (L::MORE == 0 || wave < L::MORE) ring_wait<(L::NS - 2) * L::NL + (L::NS - 1) * L::STORES>();
+                else ring_wait<(L::NS - 2) * (L::NL - 1) + (L::NS - 1) * L::STORES>();
+            } else {
+                if (L::MORE == 0 || wave < L::MORE) ring_wait<(L::NS - 2) * L::NL>();
+                else ring_wait<(L::NS - 2) * (L::NL - 1)>();
+            }
             ring_meet();
             int next = stage + L::NS - 1;
             if (next >= L::NS) next -= L::NS;
             issue(min(s + L::NS - 1, s1 - 1), mask, next);
             mask = masks[min(s + L::NS, s1 - 1)];
-            const lds_t xs = lds + stage * L::STAGE, ds = xs + L::XBYTES;
-            bf16x8 xf[L::HB];
+            const lds_t xs = lds + stage * L::STAGE, ds = xs + 32 * L::ROW;
             {
-                const int r = 8 * (lane >> 4) + ((lane & 15) >> 2);
-                const lds_t p = xs + r * 512 + (lane & 3) * 8;
-                const int f = swizzle(r);   // that of row r + 4, too
-                const int c = wh * L::HB;
-                if constexpr (L::HB == 2) read_transposed(xf, p + ((c ^ f) << 5), p + (((c + 1) ^ f) << 5));
-                else read_transposed(xf, p + ((c ^ f) << 5), p + (((c + 1) ^ f) << 5), p + (((c + 2) ^ f) << 5), p + (((c + 3) ^ f) << 5));
-            }
+                // dl's blocks are read some ahead of the products that need them, the first of them before x's
+                constexpr int N = 3 * L::EB, AHEAD = N < 6 ? N : 6;
+                const lds_t dp = ds + we * L::EB * 1024 + ((lane & 48) + dl_row(lane & 15, lane >> 4)) * 16;
+                auto read = [&](const int i) { return *(frag_ptr_t)(dp + ((2 - i % 3) * NB + i / 3) * 1024); };
+                bf16x8 df[AHEAD];
 #pragma unroll
-            for (int eb = 0; eb < L::EB; ++eb)
+                for (int i = 0; i < AHEAD; ++i) df[i] = read(i);
+                bf16x8 xf[L::HB];
+                {
+                    const int r = 8 * (lane >> 4) + ((lane & 15) >> 2);
+                    const lds_t p = xs + r * L::ROW + (lane & 3) * 8;
+                    const int f = swizzle(r);   // that of row r + 4, too
+                    const int c = wh * L::HB;
+                    auto at = [&](const int hb) { return p + (((c + hb) ^ f) << 5); };
+                    if constexpr (L::HB == 2) read_transposed<0, 4 * L::ROW, 0, 4 * L::ROW>(xf[0], xf[1], at(0), at(0), at(1), at(1));
+                    else read_transposed<4 * L::ROW>(xf, at(0), at(1), at(2), at(3));
+                }
 #pragma unroll
-                for (int q = 2; q >= 0; --q) {
-                    const bf16x8 d = *(frag_ptr_t)(ds + (q * NB + we * L::EB + eb) * 1024 + lane * 16);
+                for (int i = 0; i < N; ++i) {
+                    const int eb = i / 3;
+                    const bf16x8 d = df[i % AHEAD];
+                    if (i + AHEAD < N) df[i % AHEAD] = read(i + AHEAD);
 #pragma unroll
                     for (int hb = 0; hb < L::HB; ++hb) acc[eb][hb] = mfma(d, xf[hb], acc[eb][hb]);
                     if (SUMS) bias[eb] = mfma(d, ones, bias[eb]);
+                    __builtin_amdgcn_sched_barrier(0);   // a read and the products of an earlier one in turn
                 }
+            }
+            if (DX) {
+                f32x4 out[L::DB] = {};
+                const lds_t p = ds + dl_first, q4 = ds + dl_next;
+                auto two = [&]<int K>() {   // blocks K and K + 1 of 32 experts, mid and hi
+                    bf16x8 d[4];
+                    read_transposed<NB * 1024 + K * 2048, K * 2048, NB * 1024 + (K + 1) * 2048, (K + 1) * 2048>(d, p, q4);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int b = 0; b < L::DB; ++b) out[b] = mfma(wg[b][K + q / 2], d[q], out[b]);
+                };
+                auto one = [&]<int K>() {
+                    bf16x8 d[2];
+                    read_transposed<NB * 1024 + K * 2048, NB * 1024 + K * 2048, K * 2048, K * 2048>(d[0], d[1], p, q4, p, q4);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int b = 0; b < L::DB; ++b) out[b] = mfma(wg[b][K], d[q], out[b]);
+                };
+                if constexpr (L::KB >= 2) two.template operator()<0>();
+                if constexpr (L::KB >= 4) two.template operator()<2>();
+                if constexpr (L::KB >= 6) two.template operator()<4>();
+                if constexpr (L::KB >= 8) two.template operator()<6>();
+                if constexpr (L::KB % 2) one.template operator()<L::KB - 1>();
+                u32x4 o[L::DB / 2];   // 8 columns of token lane % 16 in each group of 32
+#pragma unroll
+                for (int g = 0; g < L::DB / 2; ++g) {
+                    bf16x8 v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) { v[r] = (__bf16)out[2 * g][r]; v[4 + r] = (__bf16)out[2 * g + 1][r]; }
+                    o[g] = __builtin_bit_cast(u32x4, v);
+                }
+                const int t0 = s * 32 + th * 16;
+                if constexpr (L::DB == 4) {
+                    // Lanes of tokens i and i + 8 exchange a group, so that a store writes whole lines: 128 bytes of 8 tokens.
+                    const bool upper = lane & 8;
+                    u32x4 first, second;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t got = dpp_move<0x128>(upper ? o[0][r] : o[1][r]);   // row_ror:8
+                        first[r] = upper ? got : o[0][r];
+                        second[r] = upper ? o[1][r] : got;
+                    }
+                    const int t = t0 + (lane & 7);
+                    char* const at = a.dx + ((size_t)t * a.H + dh) * 2 + (lane & 8) * 8 + (lane >> 4) * 16;
+                    if (dh + 64 <= a.H) {
+                        if (t < a.T) *reinterpret_cast<u32x4*>(at) = first;
+                        if (t + 8 < a.T) *reinterpret_cast<u32x4*>(at + (size_t)a.H * 16) = second;
+                    }
+                } else {
+                    const int t = t0 + (lane & 15);
+                    if (dh + 32 <= a.H && t < a.T) *reinterpret_cast<u32x4*>(a.dx + ((size_t)t * a.H + dh) * 2 + (lane >> 4) * 16) = o[0];
+                }
+            }
             if (++stage == L::NS) stage = 0;
         }
     };
+    const bool sums = ht == 0 && wh == 0;
     if (sums) steps.template operator()<true>();
     else steps.template operator()<false>();
     ring_wait<0>();   // no load may land in LDS that belongs to another workgroup
@@ -405,20 +456,6 @@ __device__ __forceinline__ void dw_tile(const RouteBackwardArgs& a, const int id
 #pragma unroll
         for (int eb = 0; eb < L::EB; ++eb)
             *reinterpret_cast<f32x4*>(out + (size_t)a.H * (16 * NB) + (we * L::EB + eb) * 16 + 4 * (lane >> 4)) = bias[eb];
-}
-
-// Both products in one launch: the workgroups of dWg, then those of dx.
-template <int NB>
-__global__ __launch_bounds__(512) void route_backward_products_kernel(const RouteBackwardArgs a) {
-    extern __shared__ char lds_raw[];
-    const lds_t lds = (lds_t)lds_raw;
-    const int n = a.dw_tiles * a.splits;
-    if ((int)blockIdx.x < n) dw_tile<NB>(a, xcd_place(blockIdx.x, n), lds);
-    else dx_tile<(NB + 1) / 2>(a, blockIdx.x - n, lds);
-}
-template <int NB>
-constexpr int products_lds() {
-    return DwTile<NB>::LDS > DxTile<(NB + 1) / 2>::LDS ? DwTile<NB>::LDS : DxTile<(NB + 1) / 2>::LDS;
 }
 
 // dWg and dbias: the parts of the tokens added in order.
@@ -464,11 +501,19 @@ int route_backward_blocks(const int E) {
     return 16;
 }
 
+int route_backward_columns(const int nb) {
+    int columns = 0;
+    (void)for_blocks(nb, [&]<int NB>() { columns = Tile<NB>::HT; return hipSuccess; });
+    return columns;
+}
+
 hipError_t route_backward_init() {
     hipError_t e = hipSuccess;
     for (int nb : {1, 2, 4, 6, 8, 10, 12, 16}) {
         const hipError_t r = for_blocks(nb, []<int NB>() {
-            return hipFuncSetAttribute((const void*)route_backward_products_kernel<NB>, hipFuncAttributeMaxDynamicSharedMemorySize, products_lds<NB>());
+            const hipError_t r = hipFuncSetAttribute((const void*)route_backward_products_kernel<NB, true>, hipFuncAttributeMaxDynamicSharedMemorySize, Tile<NB>::LDS);
+            if (r != hipSuccess) return r;
+            return hipFuncSetAttribute((const void*)route_backward_products_kernel<NB, false>, hipFuncAttributeMaxDynamicSharedMemorySize, Tile<NB>::LDS);
         });
         if (e == hipSuccess) e = r;
     }
@@ -484,8 +529,9 @@ hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st) {
     });
     if (e != hipSuccess) return e;
     e = for_blocks(a.nb, [&]<int NB>() {
-        const unsigned grid = (unsigned)(a.dw_tiles * a.splits + (a.dx ? a.dx_tiles * a.dx_parts : 0));
-        hipLaunchKernelGGL(route_backward_products_kernel<NB>, dim3(grid), dim3(512), products_lds<NB>(), st, a);
+        const dim3 grid(a.tiles * a.splits);
+        if (a.dx) hipLaunchKernelGGL((route_backward_products_kernel<NB, true>), grid, dim3(512), Tile<NB>::LDS, st, a);
+        else hipLaunchKernelGGL((route_backward_products_kernel<NB, false>), grid, dim3(512), Tile<NB>::LDS, st, a);
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;

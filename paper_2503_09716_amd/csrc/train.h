@@ -38,17 +38,15 @@ struct RouteBackwardArgs {
     float scale;
     int32_t nb, kb;            // blocks of 16 experts (as many as the kernel's variant takes), of 32 experts
     int32_t steps;             // blocks of 32 tokens
-    int32_t dw_tiles, splits, split_steps;    // dWg: tiles of H, parts of the tokens that are summed apart, blocks of 32 tokens to one
-    int32_t dx_tiles, dx_parts, dx_groups;    // dx: tiles of 256 tokens, parts of H, groups of 32 columns to one
+    int32_t tiles, splits, split_steps;   // tiles of H, parts of the tokens that dWg is summed over apart, blocks of 32 tokens to one
     char* zeros;               // 1 KiB that the first launch clears
     uint32_t* masks;           // [T / 32]: the tokens that count
-    char* dl_dx;               // [T / 16][hi, mid][kb] blocks: rows are tokens, steps experts
-    char* dl_dw;               // [T / 32][hi, mid, lo][nb] blocks: rows are experts, steps tokens
+    char* dl_blocks;           // [T / 32][hi, mid, lo][nb] blocks: rows are experts (dl_row), steps tokens
     char* wg_blocks;           // [H / 32][2][kb] blocks: row i of block b is h = 8 (i / 4) + 4 b + i % 4 of 32, steps are experts
     float* partial;            // [splits][H + 1][16 nb]: row H the sum of dl
 };
 int route_backward_blocks(int E);   // nb
-constexpr int ROUTE_BACKWARD_TILE = 256;   // columns of x to a workgroup of the dWg product
+int route_backward_columns(int nb);   // columns of x to a workgroup
 hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st);
 hipError_t launch_route_backward_empty(const moe_shape& s, float* dwg, float* dbias, hipStream_t st);
 hipError_t route_backward_init();
