@@ -149,35 +149,56 @@ __global__ __launch_bounds__(256) void route_backward_prep_kernel(const RouteBac
     if (blockIdx.x == 0 && threadIdx.x < 64) reinterpret_cast<u32x4*>(a.zeros)[threadIdx.x] = u32x4{0u, 0u, 0u, 0u};
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15;
     const int E = a.E, k = a.k;
+    // Both passes' rows and picks are asked for before either is computed with; a lane of a token's row holds one pick at a time.
+    float v[2][NV], add[2][NV], pick_dw[2];
+    int pick[2];
+    uint8_t kept[2];
+    int toks[2];
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {
-        const int lt = pass * 16 + wave * 4 + (lane >> 4), tok = blockIdx.x * PREP_TOKENS + lt, t = min(tok, a.T - 1);
-        const bool on = tok < a.T && (!a.keep || a.keep[t]);
-        float v[NV], g[NV];
-        load_row16<NV, WIDE>(v, a.logits, t, E, row, -INFINITY);
+        toks[pass] = blockIdx.x * PREP_TOKENS + pass * 16 + wave * 4 + (lane >> 4);
+        const size_t t = min(toks[pass], a.T - 1);
+        const size_t at = t * k + min(row, k - 1);
+        pick[pass] = a.idx[at];
+        pick_dw[pass] = a.dw[at];
+        load_row16<NV, WIDE>(v[pass], a.logits, t, E, row, -INFINITY);
+        if (a.dlogits) load_row16<NV, WIDE>(add[pass], a.dlogits, t, E, row, 0.f);
+        kept[pass] = a.keep ? a.keep[t] : 1;
+    }
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+        const int lt = pass * 16 + wave * 4 + (lane >> 4);
+        const bool on = toks[pass] < a.T && kept[pass];
+        float g[NV];
         uint32_t picked = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) g[i] = 0.f;
-        for (int j = 0; j < k; ++j) {
-            const int e = a.idx[(size_t)t * k + j];
-            const float d = a.dw[(size_t)t * k + j] * a.scale;
+        for (int j0 = 0; j0 < k; j0 += 16) {   // one round unless k > 16
+            if (j0 > 0) {
+                const size_t at = (size_t)min(toks[pass], a.T - 1) * k + min(j0 + row, k - 1);
+                pick[pass] = a.idx[at];
+                pick_dw[pass] = a.dw[at];
+            }
+            const int n = min(k - j0, 16);
+            for (int j = 0; j < n; ++j) {
+                const int e = __shfl(pick[pass], j, 16);
+                const float d = __shfl(pick_dw[pass], j, 16) * a.scale;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (row16_expert<WIDE>(row, i) == e) { g[i] = d; picked |= 1u << i; }
+                for (int i = 0; i < NV; ++i)
+                    if (row16_expert<WIDE>(row, i) == e) { g[i] = d; picked |= 1u << i; }
+            }
         }
         if (a.renorm)
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = picked >> i & 1 ? v[i] : -INFINITY;
-        softmax_row16<NV>(v);
+            for (int i = 0; i < NV; ++i) v[pass][i] = picked >> i & 1 ? v[pass][i] : -INFINITY;
+        softmax_row16<NV>(v[pass]);
         float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) s = fmaf(v[i], g[i], s);
+        for (int i = 0; i < NV; ++i) s = fmaf(v[pass][i], g[i], s);
         s = row16_sum(s);
-        float add[NV];
-        if (a.dlogits) load_row16<NV, WIDE>(add, a.dlogits, t, E, row, 0.f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const float d = v[i] * (g[i] - s) + (a.dlogits ? add[i] : 0.f);
+            const float d = v[pass][i] * (g[i] - s) + (a.dlogits ? add[pass][i] : 0.f);
             const int e = row16_expert<WIDE>(row, i);
             dl[lt][e] = on && e < E ? d : 0.f;
         }
@@ -458,18 +479,32 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
             *reinterpret_cast<f32x4*>(out + (size_t)a.H * (16 * NB) + (we * L::EB + eb) * 16 + 4 * (lane >> 4)) = bias[eb];
 }
 
-// dWg and dbias: the parts of the tokens added in order.
+// dWg and dbias: the parts of the tokens added in order, four experts to a thread.
 __global__ __launch_bounds__(256) void route_backward_sum_kernel(const RouteBackwardArgs a) {
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, n = (size_t)(a.H + 1) * a.E;
-    if (i >= n) return;
-    const size_t h = i / a.E, e = i - h * a.E, ld = 16 * a.nb;
-    float* const out = h < (size_t)a.H ? a.dwg + i : a.dbias ? a.dbias + e : nullptr;
+    const uint32_t per = 4 * a.nb, i = blockIdx.x * 256 + threadIdx.x;   // (H + 1) E < 2^30
+    const uint32_t h = i / per, e = (i - h * per) * 4;
+    if (h > (uint32_t)a.H || e >= (uint32_t)a.E) return;
+    float* const out = h < (uint32_t)a.H ? a.dwg + (size_t)h * a.E + e : a.dbias ? a.dbias + e : nullptr;
     if (!out) return;
-    const float* p = a.partial + h * ld + e;
-    float v = 0.f;
+    const float* p = a.partial + (size_t)h * (16 * a.nb) + e;
+    const size_t stride = (size_t)(a.H + 1) * 16 * a.nb;
+    const int n = min(4, a.E - (int)e);
+    f32x4 old = {0.f, 0.f, 0.f, 0.f};
+    if (a.accumulate)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) old[j] = out[j];
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int s = 0; s < a.splits; ++s) v += p[(size_t)s * (a.H + 1) * ld];
-    *out = a.accumulate ? *out + v : v;
+    for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * stride);
+    v += old;
+    if (n == 4 && ((uintptr_t)out & 15) == 0) {
+        *reinterpret_cast<f32x4*>(out) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) out[j] = v[j];
+    }
 }
 
 __global__ void route_backward_empty_kernel(const size_t n, const int E, float* dwg, float* dbias) {
@@ -535,7 +570,7 @@ hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st) {
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(route_backward_sum_kernel, dim3((unsigned)(((size_t)(a.H + 1) * a.E + 255) / 256)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(route_backward_sum_kernel, dim3((unsigned)(((size_t)(a.H + 1) * 4 * a.nb + 255) / 256)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
