@@ -104,9 +104,10 @@ __device__ __forceinline__ void read_transposed(bf16x8 (&f)[4], const lds_t p, c
 // the tokens lay the gate matrix out.
 constexpr int PREP_TOKENS = 32;
 
-// The expert (of 16) that lies e-th among those of tokens 8 g .. + 7 in a block of dl, and the other way round: what the transposing read
-// takes at a time of two neighbouring g lies in different banks.
-__device__ __forceinline__ int dl_row(const int e, const int g) { return e ^ ((g & 1) << 2); }
+// The expert (of 16) that lies e-th among those of tokens 8 g .. + 7 in a block of dl, and the other way round: neither what the
+// transposing read takes at a time of two neighbouring g (experts 0 .. 3 and 8 .. 11, or the others) nor what a 16-byte operand read does
+// (0 .. 3 and 12 .. 15 of the one, 4 .. 11 of the other) meets in a bank.
+__device__ __forceinline__ int dl_row(const int e, const int g) { return e ^ ((g & 1) * 12); }
 
 // v as bf16 pieces.
 __device__ __forceinline__ void split3(const float v, __bf16& hi, __bf16& mid, __bf16& lo) {
