@@ -853,7 +853,13 @@ RouteBackwardLayout route_backward_layout(const moe_shape& s) {
     L.tiles = (s.H + columns - 1) / columns;
     const int want = (L.nb <= 2 ? 512 : 256) / L.tiles;
     const int parts = want < 1 ? 1 : want < L.steps ? want : L.steps;
+    // ... but up to 4 blocks of tokens to a part, as the root of their number grows: each part writes a whole dWg that is read again (us with
+    // 1, 2, 3, 4 blocks: 1024 x 4096, 8 experts 14.8, 12.7, 13.9, 14.3; 1000 x 5120, 32 experts 20.0, 20.2, 17.2, 17.6; 256 x 2048, 64 experts
+    // 13.7, 15.2, 16.8, 18.9).
+    int least = (int)(sqrt((double)L.steps) / 3 + 0.5);
+    least = least < 1 ? 1 : least > 4 ? 4 : least;
     L.split_steps = (L.steps + parts - 1) / parts;
+    if (L.split_steps < least) L.split_steps = least;
     L.splits = (L.steps + L.split_steps - 1) / L.split_steps;
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
@@ -1355,8 +1361,13 @@ moe_status moe_route_backward(moe_ctx* c, const moe_shape* s, const void* x, con
     if (moe_status st = check_backward_ws(c, s, ws, ws_bytes)) return st;
     const RouteBackwardLayout L = route_backward_layout(*s);
     char* const w8 = (char*)ws;
+    // A launch for dl is saved where each workgroup computes it for few blocks of tokens, and reads its part of the gate matrix 16 bytes at a
+    // time (us with the launch, without: 256 x 512, 8 experts 13.7, 10.3; 3001 x 2048, 64 experts 26.3, 24.4; 6000 x 2048, 6 blocks of
+    // tokens, 26.6, 29.5; 256 x 2048, 63 experts, whose gate matrix it reads 2 bytes at a time, 16.2, 18.4).
+    const int wg_wide = s->E % 8 == 0 && !misaligned({wg}, 16);
+    const int own_dl = L.nb <= ROUTE_BACKWARD_OWN_BLOCKS && L.split_steps <= 4 && (wg_wide || !dx);
     const RouteBackwardArgs a{(const char*)x, (const char*)wg, logits, idx, dw, dlogits, keep, (char*)dx, dwg, dbias, s->T, s->H, s->E, s->top_k,
-                              s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.tiles, L.splits, L.split_steps, w8 + L.zeros,
+                              s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.tiles, L.splits, L.split_steps, own_dl, wg_wide, w8 + L.zeros,
                               (uint32_t*)(w8 + L.masks), w8 + L.dl_blocks, w8 + L.wg_blocks, (float*)(w8 + L.partial)};
     HIP_TRY(c, launch_route_backward(a, hs));
     return MOE_OK;

@@ -118,21 +118,77 @@ __device__ __forceinline__ void split3(const float v, __bf16& hi, __bf16& mid, _
 }
 
 // 16-byte piece p of wg_blocks.
-__device__ __forceinline__ void pack_gate_piece(const RouteBackwardArgs& a, const size_t p) {
+__device__ __forceinline__ u32x4 gate_piece(const RouteBackwardArgs& a, const size_t p) {
     const int lane = p & 63, i = lane & 15;
     const size_t blk = p >> 6;
     const int kb = (int)(blk % a.kb), b = (int)(blk / a.kb) & 1;
     const size_t h = blk / a.kb / 2 * 32 + 8 * (i >> 2) + 4 * b + (i & 3);
     const int e0 = kb * 32 + 8 * (lane >> 4);
     const uint16_t* const src = reinterpret_cast<const uint16_t*>(a.wg) + h * a.E;
-    uint32_t q[4];
+    if (a.wg_wide) return e0 < a.E ? *reinterpret_cast<const u32x4*>(src + e0) : u32x4{0u, 0u, 0u, 0u};
+    uint32_t v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int e = e0 + 2 * j;
-        q[j] = (e < a.E ? src[e] : 0u) | (e + 1 < a.E ? (uint32_t)src[e + 1] << 16 : 0u);
-    }
-    reinterpret_cast<u32x4*>(a.wg_blocks)[p] = u32x4{q[0], q[1], q[2], q[3]};
+    for (int j = 0; j < 8; ++j) v[j] = src[min(e0 + j, a.E - 1)];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = e0 + j < a.E ? v[j] : 0u;
+    return u32x4{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
 }
+
+// What a lane of a token's row reads: its logits and their gradients, one pick, whether the token counts.
+template <int NV>
+struct TokenRow {
+    float v[NV], add[NV], dw;
+    int token, pick;
+    uint8_t kept;
+    template <bool WIDE>
+    __device__ __forceinline__ void load(const RouteBackwardArgs& a, const int tok, const int row) {
+        token = tok;
+        const size_t t = min(tok, a.T - 1), at = t * a.k + min(row, a.k - 1);
+        pick = a.idx[at];
+        dw = a.dw[at];
+        load_row16<NV, WIDE>(v, a.logits, t, a.E, row, -INFINITY);
+        if (a.dlogits) load_row16<NV, WIDE>(add, a.dlogits, t, a.E, row, 0.f);
+        kept = a.keep ? a.keep[t] : 1;
+    }
+    __device__ __forceinline__ bool on(const RouteBackwardArgs& a) const { return token < a.T && kept; }
+    // v becomes dl, zero where the token does not count and past the experts
+    template <bool WIDE>
+    __device__ __forceinline__ void gradient(const RouteBackwardArgs& a, const int row) {
+        float g[NV];
+        uint32_t picked = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) g[i] = 0.f;
+        for (int j0 = 0; j0 < a.k; j0 += 16) {   // one round unless k > 16
+            if (j0 > 0) {
+                const size_t at = (size_t)min(token, a.T - 1) * a.k + min(j0 + row, a.k - 1);
+                pick = a.idx[at];
+                dw = a.dw[at];
+            }
+            const int n = min(a.k - j0, 16);
+            for (int j = 0; j < n; ++j) {
+                const int e = __shfl(pick, j, 16);
+                const float d = __shfl(dw, j, 16) * a.scale;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (row16_expert<WIDE>(row, i) == e) { g[i] = d; picked |= 1u << i; }
+            }
+        }
+        if (a.renorm)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] = picked >> i & 1 ? v[i] : -INFINITY;
+        softmax_row16<NV>(v);
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) s = fmaf(v[i], g[i], s);
+        s = row16_sum(s);
+        const bool counts = on(a);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const float d = v[i] * (g[i] - s) + (a.dlogits ? add[i] : 0.f);
+            v[i] = counts && row16_expert<WIDE>(row, i) < a.E ? d : 0.f;
+        }
+    }
+};
 
 template <int NV, bool WIDE>
 __global__ __launch_bounds__(256) void route_backward_prep_kernel(const RouteBackwardArgs a, const int token_blocks) {
@@ -142,68 +198,23 @@ __global__ __launch_bounds__(256) void route_backward_prep_kernel(const RouteBac
     if ((int)blockIdx.x >= token_blocks) {
         const size_t pieces = (size_t)a.H / 16 * a.kb * 64;
         const size_t p = (size_t)(blockIdx.x - token_blocks) * 256 + threadIdx.x;
-        if (p < pieces) pack_gate_piece(a, p);
+        if (p < pieces) reinterpret_cast<u32x4*>(a.wg_blocks)[p] = gate_piece(a, p);
         return;
     }
     if (threadIdx.x == 0) mask = 0;
     __syncthreads();
     if (blockIdx.x == 0 && threadIdx.x < 64) reinterpret_cast<u32x4*>(a.zeros)[threadIdx.x] = u32x4{0u, 0u, 0u, 0u};
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15;
-    const int E = a.E, k = a.k;
-    // Both passes' rows and picks are asked for before either is computed with; a lane of a token's row holds one pick at a time.
-    float v[2][NV], add[2][NV], pick_dw[2];
-    int pick[2];
-    uint8_t kept[2];
-    int toks[2];
+    TokenRow<NV> rows[2];   // both asked for before either is computed with
 #pragma unroll
-    for (int pass = 0; pass < 2; ++pass) {
-        toks[pass] = blockIdx.x * PREP_TOKENS + pass * 16 + wave * 4 + (lane >> 4);
-        const size_t t = min(toks[pass], a.T - 1);
-        const size_t at = t * k + min(row, k - 1);
-        pick[pass] = a.idx[at];
-        pick_dw[pass] = a.dw[at];
-        load_row16<NV, WIDE>(v[pass], a.logits, t, E, row, -INFINITY);
-        if (a.dlogits) load_row16<NV, WIDE>(add[pass], a.dlogits, t, E, row, 0.f);
-        kept[pass] = a.keep ? a.keep[t] : 1;
-    }
+    for (int pass = 0; pass < 2; ++pass) rows[pass].template load<WIDE>(a, blockIdx.x * PREP_TOKENS + pass * 16 + wave * 4 + (lane >> 4), row);
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {
         const int lt = pass * 16 + wave * 4 + (lane >> 4);
-        const bool on = toks[pass] < a.T && kept[pass];
-        float g[NV];
-        uint32_t picked = 0;
+        rows[pass].template gradient<WIDE>(a, row);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) g[i] = 0.f;
-        for (int j0 = 0; j0 < k; j0 += 16) {   // one round unless k > 16
-            if (j0 > 0) {
-                const size_t at = (size_t)min(toks[pass], a.T - 1) * k + min(j0 + row, k - 1);
-                pick[pass] = a.idx[at];
-                pick_dw[pass] = a.dw[at];
-            }
-            const int n = min(k - j0, 16);
-            for (int j = 0; j < n; ++j) {
-                const int e = __shfl(pick[pass], j, 16);
-                const float d = __shfl(pick_dw[pass], j, 16) * a.scale;
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (row16_expert<WIDE>(row, i) == e) { g[i] = d; picked |= 1u << i; }
-            }
-        }
-        if (a.renorm)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) v[pass][i] = picked >> i & 1 ? v[pass][i] : -INFINITY;
-        softmax_row16<NV>(v[pass]);
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) s = fmaf(v[pass][i], g[i], s);
-        s = row16_sum(s);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const float d = v[pass][i] * (g[i] - s) + (a.dlogits ? add[pass][i] : 0.f);
-            const int e = row16_expert<WIDE>(row, i);
-            dl[lt][e] = on && e < E ? d : 0.f;
-        }
-        if (on && row == 0) atomicOr(&mask, 1u << lt);
+        for (int i = 0; i < NV; ++i) dl[lt][row16_expert<WIDE>(row, i)] = rows[pass].v[i];
+        if (rows[pass].on(a) && row == 0) atomicOr(&mask, 1u << lt);
     }
     __syncthreads();
     if (threadIdx.x == 0) a.masks[blockIdx.x] = mask;
@@ -281,7 +292,27 @@ struct Tile {
 // Rows 0..3 and 8..11 (16..19 and 24..27, ...), which a transposing read takes at a time, in different 32-byte chunks of 256 bytes.
 __device__ __forceinline__ int swizzle(const int r) { return (r & 3) | ((r >> 1) & 4); }
 
-template <int NB, bool DX>
+// A page of zeros where no launch before could clear one.
+__device__ __align__(1024) const unsigned char zeros_page[1024] = {};
+
+// dl of token t (of 32) into the blocks of a stage: expert e's is lane e % 16's value e / 16.
+template <int NB>
+__device__ __forceinline__ void put_dl(const float (&v)[NB], const lds_t ds, const int t, const int row) {
+    typedef __attribute__((address_space(3))) __bf16* put_ptr_t;
+    const int g = t >> 3, at = (g * 16 + dl_row(row, g)) * 16 + (t & 7) * 2;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        __bf16 hi, mid, lo;
+        split3(v[i], hi, mid, lo);
+        *(put_ptr_t)(ds + i * 1024 + at) = hi;
+        *(put_ptr_t)(ds + (NB + i) * 1024 + at) = mid;
+        *(put_ptr_t)(ds + (2 * NB + i) * 1024 + at) = lo;
+    }
+}
+
+// OWN: the workgroup computes the dl of its tokens and lays out its part of the gate matrix by itself, so that the launch before is
+// saved; each of the tiles of H does it again.
+template <int NB, bool DX, bool OWN>
 __global__ __launch_bounds__(512) void route_backward_products_kernel(const RouteBackwardArgs a) {
     typedef Tile<NB> L;
     extern __shared__ char lds_raw[];
@@ -309,6 +340,15 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
         x_at[i] = (uint32_t)x_row[i] * (uint32_t)a.H * 2 + (uint32_t)(h0 + c * 8) * 2;
     }
     const bool inside = h0 + L::HT <= a.H;
+    auto issue_x = [&](const int step, const int stage) {   // OWN: no masks
+        const char* const xs = a.x + (size_t)step * 64 * a.H;
+#pragma unroll
+        for (int i = 0; i < L::XL; ++i) {
+            const int t = step * 32 + x_row[i];
+            const bool on = x_in[i] && t < a.T && (!a.keep || a.keep[t]);
+            load16_to_lds(on ? xs + x_at[i] : reinterpret_cast<const char*>(zeros_page) + lane * 16, lds + stage * L::STAGE + (wave + 8 * i) * 1024);
+        }
+    };
     auto issue = [&](const int step, const uint32_t mask, const int stage) {
         const lds_t base = lds + stage * L::STAGE + wave * 1024;
         const char* const xs = a.x + (size_t)step * 64 * a.H;
@@ -342,15 +382,21 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
         for (int b = 0; b < L::DB; ++b)
 #pragma unroll
             for (int kb = 0; kb < L::KB; ++kb) {
-                const size_t group = min(dh / 32 + b / 2, a.H / 32 - 1);
-                wg[b][kb] = reinterpret_cast<const bf16x8*>(a.wg_blocks)[((group * 2 + b % 2) * L::KB + kb) * 64 + lane];
+                const size_t group = min(dh / 32 + b / 2, a.H / 32 - 1), piece = ((group * 2 + b % 2) * L::KB + kb) * 64 + lane;
+                wg[b][kb] = OWN ? __builtin_bit_cast(bf16x8, gate_piece(a, piece)) : reinterpret_cast<const bf16x8*>(a.wg_blocks)[piece];
             }
 
     f32x4 acc[L::EB][L::HB] = {};
     f32x4 bias[L::EB] = {};
-    for (int i = 0; i < L::NS - 1; ++i) {
-        const int s = min(s0 + i, s1 - 1);
-        issue(s, masks[s], i);
+    TokenRow<NB> rows;   // OWN: this wavefront's four tokens of the step
+    if (OWN) {
+        rows.template load<false>(a, s0 * 32 + wave * 4 + (lane >> 4), lane & 15);
+        issue_x(s0, 0);
+    } else {
+        for (int i = 0; i < L::NS - 1; ++i) {
+            const int s = min(s0 + i, s1 - 1);
+            issue(s, masks[s], i);
+        }
     }
     // SUMS: dl's blocks are added up for dbias, too.
     auto steps = [&]<bool SUMS>() {
@@ -358,22 +404,33 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
 #pragma unroll
         for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
         int stage = 0;
-        uint32_t mask = masks[min(s0 + L::NS - 1, s1 - 1)];
+        uint32_t mask = OWN ? 0u : masks[min(s0 + L::NS - 1, s1 - 1)];
         for (int s = s0; s < s1; ++s) {
-            // Loads and stores retire in the order they were issued.  Behind this stage's loads there are those of NS - 2 stages and, from
-            // the ring's second round on, NS - 1 steps' stores (all tokens exist in every step but the last, and all columns or none).
-            if (DX && s - s0 >= L::NS - 1 && dh + L::DB * 16 <= a.H) {
-                if (L::MORE == 0 || wave < L::MORE) ring_wait<(L::NS - 2) * L::NL + (L::NS - 1) * L::STORES>();
-                else ring_wait<(L::NS - 2) * (L::NL - 1) + (L::NS - 1) * L::STORES>();
+            if constexpr (OWN) {
+                rows.template gradient<false>(a, lane & 15);
+                put_dl<NB>(rows.v, lds + stage * L::STAGE + 32 * L::ROW, wave * 4 + (lane >> 4), lane & 15);
+                ring_wait<0>();
+                ring_meet();
+                if (s + 1 < s1) {
+                    rows.template load<false>(a, (s + 1) * 32 + wave * 4 + (lane >> 4), lane & 15);
+                    issue_x(s + 1, 1 - stage);
+                }
             } else {
-                if (L::MORE == 0 || wave < L::MORE) ring_wait<(L::NS - 2) * L::NL>();
-                else ring_wait<(L::NS - 2) * (L::NL - 1)>();
+                // Loads and stores retire in the order they were issued.  Behind this stage's loads there are those of NS - 2 stages and, from
+                // the ring's second round on, NS - 1 steps' stores (all tokens exist in every step but the last, and all columns or none).
+                if (DX && s - s0 >= L::NS - 1 && dh + L::DB * 16 <= a.H) {
+                    if (L::MORE == 0 || wave < L::MORE) ring_wait<(L::NS - 2) * L::NL + (L::NS - 1) * L::STORES>();
+                    else ring_wait<(L::NS - 2) * (L::NL - 1) + (L::NS - 1) * L::STORES>();
+                } else {
+                    if (L::MORE == 0 || wave < L::MORE) ring_wait<(L::NS - 2) * L::NL>();
+                    else ring_wait<(L::NS - 2) * (L::NL - 1)>();
+                }
+                ring_meet();
+                int next = stage + L::NS - 1;
+                if (next >= L::NS) next -= L::NS;
+                issue(min(s + L::NS - 1, s1 - 1), mask, next);
+                mask = masks[min(s + L::NS, s1 - 1)];
             }
-            ring_meet();
-            int next = stage + L::NS - 1;
-            if (next >= L::NS) next -= L::NS;
-            issue(min(s + L::NS - 1, s1 - 1), mask, next);
-            mask = masks[min(s + L::NS, s1 - 1)];
             const lds_t xs = lds + stage * L::STAGE, ds = xs + 32 * L::ROW;
             {
                 // dl's blocks are read some ahead of the products that need them, the first of them before x's
@@ -458,7 +515,7 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
                     if (dh + 32 <= a.H && t < a.T) *reinterpret_cast<u32x4*>(a.dx + ((size_t)t * a.H + dh) * 2 + (lane >> 4) * 16) = o[0];
                 }
             }
-            if (++stage == L::NS) stage = 0;
+            if (++stage == (OWN ? 2 : L::NS)) stage = 0;
         }
     };
     const bool sums = ht == 0 && wh == 0;
@@ -543,31 +600,44 @@ int route_backward_columns(const int nb) {
     return columns;
 }
 
+template <int NB, bool OWN>
+constexpr int products_lds() {
+    return (OWN ? 2 : Tile<NB>::NS) * Tile<NB>::STAGE;
+}
+
+template <class F>
+hipError_t for_products(const int nb, const bool dx, const bool own, F&& f) {
+    return for_blocks(nb, [&]<int NB>() {
+        if constexpr (NB <= ROUTE_BACKWARD_OWN_BLOCKS)
+            if (own) return dx ? f.template operator()<NB, true, true>() : f.template operator()<NB, false, true>();
+        return dx ? f.template operator()<NB, true, false>() : f.template operator()<NB, false, false>();
+    });
+}
+
 hipError_t route_backward_init() {
     hipError_t e = hipSuccess;
-    for (int nb : {1, 2, 4, 6, 8, 10, 12, 16}) {
-        const hipError_t r = for_blocks(nb, []<int NB>() {
-            const hipError_t r = hipFuncSetAttribute((const void*)route_backward_products_kernel<NB, true>, hipFuncAttributeMaxDynamicSharedMemorySize, Tile<NB>::LDS);
-            if (r != hipSuccess) return r;
-            return hipFuncSetAttribute((const void*)route_backward_products_kernel<NB, false>, hipFuncAttributeMaxDynamicSharedMemorySize, Tile<NB>::LDS);
-        });
-        if (e == hipSuccess) e = r;
-    }
+    for (int nb : {1, 2, 4, 6, 8, 10, 12, 16})
+        for (int v = 0; v < 4 && e == hipSuccess; ++v)
+            e = for_products(nb, v & 1, v & 2, []<int NB, bool DX, bool OWN>() {
+                return hipFuncSetAttribute((const void*)route_backward_products_kernel<NB, DX, OWN>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           products_lds<NB, OWN>());
+            });
     return e;
 }
 
 hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st) {
-    const bool wide = wide_rows(a.E, {a.logits, a.dlogits ? a.dlogits : a.logits});
-    const unsigned pack = a.dx ? (unsigned)(((size_t)a.H / 16 * a.kb * 64 + 255) / 256) : 0u;
-    hipError_t e = for_row16(a.E, wide, [&]<int NV, bool WIDE>() {
-        hipLaunchKernelGGL((route_backward_prep_kernel<NV, WIDE>), dim3(a.steps + pack), dim3(256), 0, st, a, a.steps);
-        return hipGetLastError();
-    });
-    if (e != hipSuccess) return e;
-    e = for_blocks(a.nb, [&]<int NB>() {
-        const dim3 grid(a.tiles * a.splits);
-        if (a.dx) hipLaunchKernelGGL((route_backward_products_kernel<NB, true>), grid, dim3(512), Tile<NB>::LDS, st, a);
-        else hipLaunchKernelGGL((route_backward_products_kernel<NB, false>), grid, dim3(512), Tile<NB>::LDS, st, a);
+    hipError_t e;
+    if (!a.own_dl) {
+        const bool wide = wide_rows(a.E, {a.logits, a.dlogits ? a.dlogits : a.logits});
+        const unsigned pack = a.dx ? (unsigned)(((size_t)a.H / 16 * a.kb * 64 + 255) / 256) : 0u;
+        e = for_row16(a.E, wide, [&]<int NV, bool WIDE>() {
+            hipLaunchKernelGGL((route_backward_prep_kernel<NV, WIDE>), dim3(a.steps + pack), dim3(256), 0, st, a, a.steps);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) return e;
+    }
+    e = for_products(a.nb, a.dx != nullptr, a.own_dl, [&]<int NB, bool DX, bool OWN>() {
+        hipLaunchKernelGGL((route_backward_products_kernel<NB, DX, OWN>), dim3(a.tiles * a.splits), dim3(512), (products_lds<NB, OWN>()), st, a);
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;

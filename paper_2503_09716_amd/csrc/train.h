@@ -39,6 +39,8 @@ struct RouteBackwardArgs {
     int32_t nb, kb;            // blocks of 16 experts (as many as the kernel's variant takes), of 32 experts
     int32_t steps;             // blocks of 32 tokens
     int32_t tiles, splits, split_steps;   // tiles of H, parts of the tokens that dWg is summed over apart, blocks of 32 tokens to one
+    int32_t own_dl;            // 1: no launch for dl, the products' workgroups compute their tokens'
+    int32_t wg_wide;           // 1: the gate matrix can be read 16 bytes at a time
     char* zeros;               // 1 KiB that the first launch clears
     uint32_t* masks;           // [T / 32]: the tokens that count
     char* dl_blocks;           // [T / 32][hi, mid, lo][nb] blocks: rows are experts (dl_row), steps tokens
@@ -46,6 +48,7 @@ struct RouteBackwardArgs {
     float* partial;            // [splits][H + 1][16 nb]: row H the sum of dl
 };
 int route_backward_blocks(int E);   // nb
+constexpr int ROUTE_BACKWARD_OWN_BLOCKS = 6;   // nb up to which own_dl fits the registers
 int route_backward_columns(int nb);   // columns of x to a workgroup
 hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st);
 hipError_t launch_route_backward_empty(const moe_shape& s, float* dwg, float* dbias, hipStream_t st);
