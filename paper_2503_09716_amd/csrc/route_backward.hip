@@ -7,6 +7,8 @@
 // x and Wg are bf16, so a matrix instruction multiplies them exactly; dl is fp32 and goes in as a sum of bf16 pieces: hi + mid + lo
 // hold its 24 bits, and three products give dWg what products in fp32 would; dx is rounded to bf16 (8 bits), and the two pieces it
 // takes hold dl to 2^-17.
+#include <utility>
+
 #include "common.h"
 #include "router_rows.h"
 #include "train.h"
@@ -151,6 +153,12 @@ struct TokenRow {
         kept = a.keep ? a.keep[t] : 1;
     }
     __device__ __forceinline__ bool on(const RouteBackwardArgs& a) const { return token < a.T && kept; }
+    template <bool WIDE>
+    static __device__ __forceinline__ void take(float (&g)[NV], uint32_t& picked, const int row, const int e, const float d) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (row16_expert<WIDE>(row, i) == e) { g[i] = d; picked |= 1u << i; }
+    }
     // v becomes dl, zero where the token does not count and past the experts
     template <bool WIDE>
     __device__ __forceinline__ void gradient(const RouteBackwardArgs& a, const int row) {
@@ -165,13 +173,9 @@ struct TokenRow {
                 dw = a.dw[at];
             }
             const int n = min(a.k - j0, 16);
-            for (int j = 0; j < n; ++j) {
-                const int e = __shfl(pick, j, 16);
-                const float d = __shfl(dw, j, 16) * a.scale;
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (row16_expert<WIDE>(row, i) == e) { g[i] = d; picked |= 1u << i; }
-            }
+            [&]<int... J>(std::integer_sequence<int, J...>) {
+                ((J < n ? take<WIDE>(g, picked, row, dpp_move<0x150 + J>(pick), __int_as_float(dpp_move<0x150 + J>(__float_as_int(dw))) * a.scale) : (void)0), ...);
+            }(std::make_integer_sequence<int, 16>());   // row_newbcast: lane J's of the row
         }
         if (a.renorm)
 #pragma unroll
@@ -340,12 +344,17 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
         x_at[i] = (uint32_t)x_row[i] * (uint32_t)a.H * 2 + (uint32_t)(h0 + c * 8) * 2;
     }
     const bool inside = h0 + L::HT <= a.H;
-    auto issue_x = [&](const int step, const int stage) {   // OWN: no masks
+    // OWN: no masks, whether the rows count is read one step ahead
+    uint8_t x_kept[L::XL];
+    auto ask_kept = [&](const int step) {
+#pragma unroll
+        for (int i = 0; i < L::XL; ++i) x_kept[i] = a.keep ? a.keep[min(step * 32 + x_row[i], a.T - 1)] : 1;
+    };
+    auto issue_x = [&](const int step, const int stage) {
         const char* const xs = a.x + (size_t)step * 64 * a.H;
 #pragma unroll
         for (int i = 0; i < L::XL; ++i) {
-            const int t = step * 32 + x_row[i];
-            const bool on = x_in[i] && t < a.T && (!a.keep || a.keep[t]);
+            const bool on = x_in[i] && step * 32 + x_row[i] < a.T && x_kept[i];
             load16_to_lds(on ? xs + x_at[i] : reinterpret_cast<const char*>(zeros_page) + lane * 16, lds + stage * L::STAGE + (wave + 8 * i) * 1024);
         }
     };
@@ -391,7 +400,9 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
     TokenRow<NB> rows;   // OWN: this wavefront's four tokens of the step
     if (OWN) {
         rows.template load<false>(a, s0 * 32 + wave * 4 + (lane >> 4), lane & 15);
+        ask_kept(s0);
         issue_x(s0, 0);
+        ask_kept(s0 + 1);
     } else {
         for (int i = 0; i < L::NS - 1; ++i) {
             const int s = min(s0 + i, s1 - 1);
@@ -414,6 +425,7 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
                 if (s + 1 < s1) {
                     rows.template load<false>(a, (s + 1) * 32 + wave * 4 + (lane >> 4), lane & 15);
                     issue_x(s + 1, 1 - stage);
+                    ask_kept(s + 2);
                 }
             } else {
                 // Loads and stores retire in the order they were issued.  Behind this stage's loads there are those of NS - 2 stages and, from
@@ -553,8 +565,14 @@ __global__ __launch_bounds__(256) void route_backward_sum_kernel(const RouteBack
         for (int j = 0; j < 4; ++j)
             if (j < n) old[j] = out[j];
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * stride);
+    for (int s0 = 0; s0 < a.splits; s0 += 8) {   // eight in flight
+        f32x4 q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) q[u] = *reinterpret_cast<const f32x4*>(p + min(s0 + u, a.splits - 1) * stride);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (s0 + u < a.splits) v += q[u];
+    }
     v += old;
     if (n == 4 && ((uintptr_t)out & 15) == 0) {
         *reinterpret_cast<f32x4*>(out) = v;
