@@ -20,7 +20,9 @@ struct BalanceArgs {
     int32_t* done;
 };
 constexpr int BALANCE_COUNT_BLOCKS = 32, BALANCE_LOSS_BLOCKS = 256;
-constexpr int64_t BALANCE_ALONE = 4096;   // logits up to which one workgroup does all
+// One workgroup does all up to this many tokens and logits (us alone, in two launches: 256 tokens of 8 experts 6.0, 8.4; 512 8.7, 8.7;
+// 1024 14.0, 9.9; 128 of 64 experts 6.6, 9.8; 256 7.8, 10.1).
+constexpr int BALANCE_ALONE_TOKENS = 384, BALANCE_ALONE = 32768;
 hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t st);
 
 // The gradient of the logits travels in pieces of bf16 (hi + mid + lo = its 24 bits) in the order in which the matrix instructions
