@@ -15,7 +15,11 @@ template <bool F32, int N>
 struct Row {
     typedef uint32_t words __attribute__((ext_vector_type(N * (F32 ? 4 : 2) / 4)));
     words v;
-    __device__ __forceinline__ void load(const char* row, const int c) { v = reinterpret_cast<const words*>(row)[c]; }
+    template <bool NT>
+    __device__ __forceinline__ void load(const char* row, const int c) {
+        const words* const p = reinterpret_cast<const words*>(row) + c;
+        v = NT ? __builtin_nontemporal_load(p) : *p;
+    }
     __device__ __forceinline__ float operator[](const int i) const {
         return __uint_as_float(F32 ? v[i] : ((i & 1) ? v[i / 2] & 0xffff0000u : v[i / 2] << 16));
     }
@@ -23,7 +27,8 @@ struct Row {
 
 constexpr int AHEAD = 4;   // pieces of a row that a lane has in flight
 
-template <bool YF32, bool DF32, bool DY, int W>
+// LD, ST: y is read, dy written past the caches.
+template <bool YF32, bool DF32, bool DY, int W, bool LD, bool ST>
 __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __restrict__ dout, const char* __restrict__ y_perm,
                                                                 const int32_t* __restrict__ inv_perm, const float* __restrict__ w, const int k, const int H,
                                                                 float* __restrict__ dw, char* __restrict__ dy_perm) {
@@ -45,8 +50,8 @@ __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __re
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u) {
                     const int c = min(c0 + u * W * 64, n - 1);
-                    y[u].load(y_perm + at, c);
-                    g[u].load(d, c);
+                    y[u].template load<LD>(y_perm + at, c);
+                    g[u].template load<false>(d, c);
                 }
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u) {
@@ -59,13 +64,13 @@ __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __re
                             f32x4 o;
 #pragma unroll
                             for (int i = 0; i < 4; ++i) o[i] = wj * g[u][i];
-                            reinterpret_cast<f32x4*>(dy_perm + at)[c] = o;
+                            if (ST) __builtin_nontemporal_store(o, reinterpret_cast<f32x4*>(dy_perm + at) + c); else reinterpret_cast<f32x4*>(dy_perm + at)[c] = o;
                         } else {
                             typedef __bf16 bf16_n __attribute__((ext_vector_type(N)));
                             bf16_n o;
 #pragma unroll
                             for (int i = 0; i < N; ++i) o[i] = (__bf16)(wj * g[u][i]);
-                            reinterpret_cast<bf16_n*>(dy_perm + at)[c] = o;
+                            if (ST) __builtin_nontemporal_store(o, reinterpret_cast<bf16_n*>(dy_perm + at) + c); else reinterpret_cast<bf16_n*>(dy_perm + at)[c] = o;
                         }
                     }
                 }
@@ -93,19 +98,30 @@ __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __re
 
 hipError_t launch_combine_backward(const moe_shape& s, const void* dout, const void* y_perm, const int32_t* inv_perm, const float* w, float* dw,
                                    void* dy_perm, bool y_fp32, bool dout_fp32, hipStream_t st) {
-    const int64_t pairs = (int64_t)s.T * s.top_k;
+    const int64_t pairs = (int64_t)s.T * s.top_k, bytes = pairs * s.H * (y_fp32 ? 4 : 2);
     const bool split = pairs <= 2048 && s.H >= 1024;
-    auto run = [&]<bool Y, bool D, bool DY, int W>() {
+    // Past the caches, us without, loads, stores, both: 4096 tokens x 4096, k = 2, fp32 (134 MB) 61.7, 58.9, 59.4, 54.1; 32768 x 5120, k = 6, bf16
+    // (2 GB) 801, 811, 797, 795, without dy_perm 376, 359; 3001 x 2048, k = 6, fp32 (147 MB) without dy_perm 32.8, 28.4; 2000 x 2048, k = 6, bf16
+    // (49 MB) 22.1, 21.1, 17.6, 21.7.
+    const bool ld = !split && bytes > (int64_t)64 << 20, st_past = !split && dy_perm && bytes > (int64_t)16 << 20;
+    auto run = [&]<bool Y, bool D, bool DY, int W, bool LD, bool ST>() {
         const int rows = s.top_k < 16 / W ? s.top_k : 16 / W;
-        hipLaunchKernelGGL((combine_backward_kernel<Y, D, DY, W>), dim3(s.T), dim3(rows * W * 64), 0, st, (const char*)dout, (const char*)y_perm, inv_perm,
+        hipLaunchKernelGGL((combine_backward_kernel<Y, D, DY, W, LD, ST>), dim3(s.T), dim3(rows * W * 64), 0, st, (const char*)dout, (const char*)y_perm, inv_perm,
                            w, s.top_k, s.H, dw, (char*)dy_perm);
         return hipGetLastError();
     };
-    auto with_split = [&]<bool Y, bool D, bool DY>() {
-        return split ? run.template operator()<Y, D, DY, 4>() : run.template operator()<Y, D, DY, 1>();
+    auto with_policy = [&]<bool Y, bool D, bool DY>() {
+        if (split) return run.template operator()<Y, D, DY, 4, false, false>();
+        if constexpr (DY) {
+            if (ld) return run.template operator()<Y, D, true, 1, true, true>();
+            if (st_past) return run.template operator()<Y, D, true, 1, false, true>();
+        }
+        if constexpr (!DY)
+            if (ld) return run.template operator()<Y, D, false, 1, true, false>();
+        return run.template operator()<Y, D, DY, 1, false, false>();
     };
     auto with_dy = [&]<bool Y, bool D>() {
-        return dy_perm ? with_split.template operator()<Y, D, true>() : with_split.template operator()<Y, D, false>();
+        return dy_perm ? with_policy.template operator()<Y, D, true>() : with_policy.template operator()<Y, D, false>();
     };
     if (y_fp32) return dout_fp32 ? with_dy.operator()<true, true>() : with_dy.operator()<true, false>();
     return dout_fp32 ? with_dy.operator()<false, true>() : with_dy.operator()<false, false>();
