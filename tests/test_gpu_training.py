@@ -311,6 +311,46 @@ def test_route_backward_many_tokens(moe):
         check_route(s, False, 1.0, *run_route_backward(moe, s, False))
 
 
+@pytest.mark.parametrize("T,H,E,k", [(20000, 4096, 8, 2), (9001, 4096, 24, 2), (9000, 4160, 60, 6), (7003, 2112, 90, 6), (6000, 1984, 128, 8), (9002, 1088, 160, 6),
+                                     (5001, 2112, 192, 8), (4001, 1088, 256, 8)])
+def test_route_backward_rounds_of_the_ring(moe, T, H, E, k):
+    """Every width of the products with parts of many blocks of tokens, H that ends inside a tile, and the same bits every time."""
+    say("rounds", T, H, E, k)
+    s = route_inputs(T, H, E, k, T, padding=0.05)
+    first = run_route_backward(moe, s, True, 0.5)
+    check_route(s, True, 0.5, *first)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, run_route_backward(moe, s, True, 0.5)))
+    without = run_route_backward(moe, s, True, 0.5, dx=False)
+    assert torch.equal(without[1], first[1]) and torch.equal(without[2], first[2])
+
+
+@pytest.mark.parametrize("E", [20, 64, 160])
+def test_misaligned_rows(moe, E):
+    """Logits, their gradients and sums at addresses that are aligned to their elements only."""
+    T, H, k = 333, 192, 4
+    s = route_inputs(T, H, E, k, 30, padding=0.2)
+
+    def shifted(t):
+        out = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")[1:].view(t.shape)
+        return out.copy_(t)
+    want = run_route_backward(moe, s, False)
+    for name in ("logits", "dlogits", "dw", "idx", "wg", "keep"):
+        s[name] = shifted(s[name])
+    got = run_route_backward(moe, s, False)
+    check_route(s, False, 1.0, *got)
+    assert all(torch.allclose(a.float(), b.float(), rtol=1e-2, atol=1e-4) for a, b in zip(want, got))
+    shape = make_shape(T, H, 64, E, k, 0, False)
+    dwg, db = shifted(torch.zeros(H, E, device="cuda")), shifted(torch.zeros(E, device="cuda"))
+    moe.route_backward(shape, s["x"], s["wg"], s["logits"], s["idx"], s["dw"], s["dlogits"], s["keep"], None, dwg, db, False, moe.new_backward_workspace(shape))
+    assert torch.equal(dwg, got[1]) and torch.equal(db, got[2])
+    counts, loss, d = run_balance(moe, s["logits"], s["idx"], s["keep"])
+    r_counts, r_loss, r_d, loss_off, bound = balance_ref(s["logits"], s["idx"], s["keep"], 1e-2, 1e-3)
+    assert torch.equal(counts.long(), r_counts)
+    within("loss", loss, r_loss, loss_off)
+    within("dlogits", d, r_d, bound)
+
+
 @pytest.mark.parametrize("T,H,E", [(70, 128, 8), (700, 320, 64), (300, 192, 160)])
 @pytest.mark.parametrize("renorm", [True, False])
 def test_route_backward_padding_rows_may_hold_anything(moe, T, H, E, renorm):
@@ -731,3 +771,14 @@ def test_another_stream_and_a_graph(moe):
             step(moe, shape, s, b, made)
             torch.cuda.synchronize()
             assert all(torch.equal(b[n], want[n]) for n in OUTS)
+
+
+def test_the_example_learns():
+    """examples/tune_router.py: the layer's output nears the target and the tokens spread."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import tune_router
+    history = tune_router.tune(steps=30, tokens=1000, say=say)
+    assert torch.isfinite(history).all()
+    assert history[-1, 0] < 0.5 * history[0, 0] and history[-1, 1] < 0.7 * history[0, 1]
