@@ -136,6 +136,12 @@ __device__ __forceinline__ u32x4 gate_piece(const RouteBackwardArgs& a, const si
     return u32x4{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
 }
 
+// LDS accesses of a wavefront's lanes on either side keep their order.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // What a lane of a token's row reads: its logits and their gradients, one pick, whether the token counts.
 template <int NV>
 struct TokenRow {
@@ -153,30 +159,58 @@ struct TokenRow {
         kept = a.keep ? a.keep[t] : 1;
     }
     __device__ __forceinline__ bool on(const RouteBackwardArgs& a) const { return token < a.T && kept; }
-    template <bool WIDE>
-    static __device__ __forceinline__ void take(float (&g)[NV], uint32_t& picked, const int row, const int e, const float d) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (row16_expert<WIDE>(row, i) == e) { g[i] = d; picked |= 1u << i; }
+    // The next 16 picks of the row.
+    __device__ __forceinline__ void next_picks(const RouteBackwardArgs& a, const int j0, const int row) {
+        const size_t at = (size_t)min(token, a.T - 1) * a.k + min(j0 + row, a.k - 1);
+        pick = a.idx[at];
+        dw = a.dw[at];
     }
-    // v becomes dl, zero where the token does not count and past the experts
+    // Gradients of the weights at the lane's experts, 0 where they are not picked, and which are, by comparing every pick with every
+    // expert: for few experts.
     template <bool WIDE>
-    __device__ __forceinline__ void gradient(const RouteBackwardArgs& a, const int row) {
-        float g[NV];
+    __device__ __forceinline__ uint32_t picks(const RouteBackwardArgs& a, const int row, float (&g)[NV]) {
         uint32_t picked = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) g[i] = 0.f;
+        auto take = [&](const int e, const float d) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (row16_expert<WIDE>(row, i) == e) { g[i] = d; picked |= 1u << i; }
+        };
         for (int j0 = 0; j0 < a.k; j0 += 16) {   // one round unless k > 16
-            if (j0 > 0) {
-                const size_t at = (size_t)min(token, a.T - 1) * a.k + min(j0 + row, a.k - 1);
-                pick = a.idx[at];
-                dw = a.dw[at];
-            }
+            if (j0 > 0) next_picks(a, j0, row);
             const int n = min(a.k - j0, 16);
             [&]<int... J>(std::integer_sequence<int, J...>) {
-                ((J < n ? take<WIDE>(g, picked, row, dpp_move<0x150 + J>(pick), __int_as_float(dpp_move<0x150 + J>(__float_as_int(dw))) * a.scale) : (void)0), ...);
+                ((J < n ? take(dpp_move<0x150 + J>(pick), __int_as_float(dpp_move<0x150 + J>(__float_as_int(dw))) * a.scale) : (void)0), ...);
             }(std::make_integer_sequence<int, 16>());   // row_newbcast: lane J's of the row
         }
+        return picked;
+    }
+    // The same through a row of LDS that this wavefront has to itself, and the 16 lanes of a token among them.
+    template <bool WIDE>
+    __device__ __forceinline__ uint32_t picks(const RouteBackwardArgs& a, const int row, float (&g)[NV], float* const at) {
+        constexpr uint32_t NONE = 0xffffffffu, NOT_A_NUMBER = 0x7fc00000u;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) at[row16_expert<WIDE>(row, i)] = __uint_as_float(NONE);
+        wave_sync();
+        for (int j0 = 0; j0 < a.k; j0 += 16) {   // one round unless k > 16
+            if (j0 > 0) next_picks(a, j0, row);
+            const uint32_t d = __float_as_uint(dw * a.scale);
+            if (j0 + row < a.k && (uint32_t)pick < (uint32_t)a.E) at[pick] = __uint_as_float(d == NONE ? NOT_A_NUMBER : d);
+        }
+        wave_sync();
+        uint32_t picked = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t d = __float_as_uint(at[row16_expert<WIDE>(row, i)]);
+            g[i] = d == NONE ? 0.f : __uint_as_float(d);
+            picked |= d == NONE ? 0u : 1u << i;
+        }
+        return picked;
+    }
+    // v becomes dl, zero where the token does not count and past the experts
+    template <bool WIDE>
+    __device__ __forceinline__ void gradient(const RouteBackwardArgs& a, const int row, const float (&g)[NV], const uint32_t picked) {
         if (a.renorm)
 #pragma unroll
             for (int i = 0; i < NV; ++i) v[i] = picked >> i & 1 ? v[i] : -INFINITY;
@@ -215,7 +249,9 @@ __global__ __launch_bounds__(256) void route_backward_prep_kernel(const RouteBac
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {
         const int lt = pass * 16 + wave * 4 + (lane >> 4);
-        rows[pass].template gradient<WIDE>(a, row);
+        float g[NV];
+        const uint32_t picked = rows[pass].template picks<WIDE>(a, row, g, dl[lt]);
+        rows[pass].template gradient<WIDE>(a, row, g, picked);
 #pragma unroll
         for (int i = 0; i < NV; ++i) dl[lt][row16_expert<WIDE>(row, i)] = rows[pass].v[i];
         if (rows[pass].on(a) && row == 0) atomicOr(&mask, 1u << lt);
@@ -426,7 +462,9 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
         uint32_t mask = OWN ? 0u : masks[min(s0 + L::NS - 1, s1 - 1)];
         for (int s = s0; s < s1; ++s) {
             if constexpr (OWN) {
-                rows.template gradient<false>(a, lane & 15);
+                float g[NB];
+                const uint32_t picked = rows.template picks<false>(a, lane & 15, g);
+                rows.template gradient<false>(a, lane & 15, g, picked);
                 put_dl<NB>(rows.v, lds + stage * L::STAGE + 32 * L::ROW, wave * 4 + (lane >> 4), lane & 15);
                 ring_wait<0>();
                 ring_meet();
