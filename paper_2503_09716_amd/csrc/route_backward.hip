@@ -7,8 +7,6 @@
 // x and Wg are bf16, so a matrix instruction multiplies them exactly; dl is fp32 and goes in as a sum of bf16 pieces: hi + mid + lo
 // hold its 24 bits, and three products give dWg what products in fp32 would; dx is rounded to bf16 (8 bits), and the two pieces it
 // takes hold dl to 2^-17.
-#include <utility>
-
 #include "common.h"
 #include "router_rows.h"
 #include "train.h"
@@ -119,14 +117,10 @@ __device__ __forceinline__ void split3(const float v, __bf16& hi, __bf16& mid, _
     lo = (__bf16)(r - (float)mid);
 }
 
-// 16-byte piece p of wg_blocks.
-__device__ __forceinline__ u32x4 gate_piece(const RouteBackwardArgs& a, const size_t p) {
-    const int lane = p & 63, i = lane & 15;
-    const size_t blk = p >> 6;
-    const int kb = (int)(blk % a.kb), b = (int)(blk / a.kb) & 1;
-    const size_t h = blk / a.kb / 2 * 32 + 8 * (i >> 2) + 4 * b + (i & 3);
-    const int e0 = kb * 32 + 8 * (lane >> 4);
-    const uint16_t* const src = reinterpret_cast<const uint16_t*>(a.wg) + h * a.E;
+// The lane's 16 bytes of block b of 16 columns and kb of 32 experts, of the 32 columns from h on.
+__device__ __forceinline__ u32x4 gate_piece(const RouteBackwardArgs& a, const int h, const int b, const int kb, const int lane) {
+    const int i = lane & 15, e0 = kb * 32 + 8 * (lane >> 4);
+    const uint16_t* const src = reinterpret_cast<const uint16_t*>(a.wg) + (size_t)(h + 8 * (i >> 2) + 4 * b + (i & 3)) * a.E;
     if (a.wg_wide) return e0 < a.E ? *reinterpret_cast<const u32x4*>(src + e0) : u32x4{0u, 0u, 0u, 0u};
     uint32_t v[8];
 #pragma unroll
@@ -165,28 +159,8 @@ struct TokenRow {
         pick = a.idx[at];
         dw = a.dw[at];
     }
-    // Gradients of the weights at the lane's experts, 0 where they are not picked, and which are, by comparing every pick with every
-    // expert: for few experts.
-    template <bool WIDE>
-    __device__ __forceinline__ uint32_t picks(const RouteBackwardArgs& a, const int row, float (&g)[NV]) {
-        uint32_t picked = 0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) g[i] = 0.f;
-        auto take = [&](const int e, const float d) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (row16_expert<WIDE>(row, i) == e) { g[i] = d; picked |= 1u << i; }
-        };
-        for (int j0 = 0; j0 < a.k; j0 += 16) {   // one round unless k > 16
-            if (j0 > 0) next_picks(a, j0, row);
-            const int n = min(a.k - j0, 16);
-            [&]<int... J>(std::integer_sequence<int, J...>) {
-                ((J < n ? take(dpp_move<0x150 + J>(pick), __int_as_float(dpp_move<0x150 + J>(__float_as_int(dw))) * a.scale) : (void)0), ...);
-            }(std::make_integer_sequence<int, 16>());   // row_newbcast: lane J's of the row
-        }
-        return picked;
-    }
-    // The same through a row of LDS that this wavefront has to itself, and the 16 lanes of a token among them.
+    // Gradients of the weights at the lane's experts, 0 where they are not picked, and which are: by way of the token's row of LDS (to
+    // compare every pick with every expert takes five times the instructions).
     template <bool WIDE>
     __device__ __forceinline__ uint32_t picks(const RouteBackwardArgs& a, const int row, float (&g)[NV], float* const at) {
         constexpr uint32_t NONE = 0xffffffffu, NOT_A_NUMBER = 0x7fc00000u;
@@ -234,9 +208,9 @@ __global__ __launch_bounds__(256) void route_backward_prep_kernel(const RouteBac
     __shared__ float dl[PREP_TOKENS][LDS_E];
     __shared__ uint32_t mask;
     if ((int)blockIdx.x >= token_blocks) {
-        const size_t pieces = (size_t)a.H / 16 * a.kb * 64;
-        const size_t p = (size_t)(blockIdx.x - token_blocks) * 256 + threadIdx.x;
-        if (p < pieces) reinterpret_cast<u32x4*>(a.wg_blocks)[p] = gate_piece(a, p);
+        // a block of the gate matrix to a wavefront
+        const uint32_t blk = (blockIdx.x - token_blocks) * 4 + (threadIdx.x >> 6), kb = blk % a.kb, hb = blk / a.kb;
+        if (hb < (uint32_t)a.H / 16) reinterpret_cast<u32x4*>(a.wg_blocks)[(size_t)blk * 64 + (threadIdx.x & 63)] = gate_piece(a, hb / 2 * 32, hb & 1, kb, threadIdx.x & 63);
         return;
     }
     if (threadIdx.x == 0) mask = 0;
@@ -365,6 +339,8 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
     typedef Tile<NB> L;
     extern __shared__ char lds_raw[];
     const lds_t lds = (lds_t)lds_raw;
+    constexpr int PICK_ROW = 16 * NB + 1;
+    float* const scratch = reinterpret_cast<float*>(lds_raw + 2 * L::STAGE);   // OWN: a row for each of the 32 tokens' picks
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int id = xcd_place(blockIdx.x, a.tiles * a.splits);
     const int ht = id % a.tiles, split = id / a.tiles;
@@ -429,22 +405,25 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
     const int g = 2 * th + ((lane & 3) >> 1), e = 8 * ((lane >> 4) & 1) + ((lane & 15) >> 2);
     const int dl_lane = g * 256 + (lane & 1) * 8 + (NB > 1 ? (lane >> 5) * 1024 : 0);   // one block: its rows again, times zeros of the gate matrix
     const int dl_first = dl_lane + dl_row(e, g) * 16, dl_next = dl_lane + dl_row(e + 4, g) * 16;
+    TokenRow<NB> rows;   // OWN: this wavefront's four tokens of the step
+    if (OWN) {
+        rows.template load<false>(a, s0 * 32 + wave * 4 + (lane >> 4), lane & 15);
+        ask_kept(s0);
+    }
     bf16x8 wg[L::DB][L::KB];
     if (DX)
 #pragma unroll
         for (int b = 0; b < L::DB; ++b)
 #pragma unroll
             for (int kb = 0; kb < L::KB; ++kb) {
-                const size_t group = min(dh / 32 + b / 2, a.H / 32 - 1), piece = ((group * 2 + b % 2) * L::KB + kb) * 64 + lane;
-                wg[b][kb] = OWN ? __builtin_bit_cast(bf16x8, gate_piece(a, piece)) : reinterpret_cast<const bf16x8*>(a.wg_blocks)[piece];
+                const int h = min(dh + b / 2 * 32, a.H - 32);
+                wg[b][kb] = OWN ? __builtin_bit_cast(bf16x8, gate_piece(a, h, b % 2, kb, lane))
+                                : reinterpret_cast<const bf16x8*>(a.wg_blocks)[((size_t)(h / 16 + b % 2) * L::KB + kb) * 64 + lane];
             }
 
     f32x4 acc[L::EB][L::HB] = {};
     f32x4 bias[L::EB] = {};
-    TokenRow<NB> rows;   // OWN: this wavefront's four tokens of the step
     if (OWN) {
-        rows.template load<false>(a, s0 * 32 + wave * 4 + (lane >> 4), lane & 15);
-        ask_kept(s0);
         issue_x(s0, 0);
         ask_kept(s0 + 1);
     } else {
@@ -463,7 +442,7 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
         for (int s = s0; s < s1; ++s) {
             if constexpr (OWN) {
                 float g[NB];
-                const uint32_t picked = rows.template picks<false>(a, lane & 15, g);
+                const uint32_t picked = rows.template picks<false>(a, lane & 15, g, scratch + (wave * 4 + (lane >> 4)) * PICK_ROW);
                 rows.template gradient<false>(a, lane & 15, g, picked);
                 put_dl<NB>(rows.v, lds + stage * L::STAGE + 32 * L::ROW, wave * 4 + (lane >> 4), lane & 15);
                 ring_wait<0>();
@@ -595,9 +574,10 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
             *reinterpret_cast<f32x4*>(out + (size_t)a.H * (16 * NB) + (we * L::EB + eb) * 16 + 4 * (lane >> 4)) = bias[eb];
 }
 
-// dWg and dbias: the parts of the tokens added in order, four experts to a thread.
-__global__ __launch_bounds__(256) void route_backward_sum_kernel(const RouteBackwardArgs a) {
-    const uint32_t per = 4 * a.nb, i = blockIdx.x * 256 + threadIdx.x;   // (H + 1) E < 2^30
+// dWg and dbias: the parts of the tokens added in order, four experts to a thread.  Workgroups of one wavefront: short batches have few
+// threads here, and they are to be spread over all CUs.
+__global__ __launch_bounds__(64) void route_backward_sum_kernel(const RouteBackwardArgs a) {
+    const uint32_t per = 4 * a.nb, i = blockIdx.x * 64 + threadIdx.x;   // (H + 1) E < 2^30
     const uint32_t h = i / per, e = (i - h * per) * 4;
     if (h > (uint32_t)a.H || e >= (uint32_t)a.E) return;
     float* const out = h < (uint32_t)a.H ? a.dwg + (size_t)h * a.E + e : a.dbias ? a.dbias + e : nullptr;
@@ -666,7 +646,7 @@ int route_backward_columns(const int nb) {
 
 template <int NB, bool OWN>
 constexpr int products_lds() {
-    return (OWN ? 2 : Tile<NB>::NS) * Tile<NB>::STAGE;
+    return OWN ? 2 * Tile<NB>::STAGE + 32 * (16 * NB + 1) * 4 : Tile<NB>::NS * Tile<NB>::STAGE;
 }
 
 template <class F>
@@ -693,7 +673,7 @@ hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st) {
     hipError_t e;
     if (!a.own_dl) {
         const bool wide = wide_rows(a.E, {a.logits, a.dlogits ? a.dlogits : a.logits});
-        const unsigned pack = a.dx ? (unsigned)(((size_t)a.H / 16 * a.kb * 64 + 255) / 256) : 0u;
+        const unsigned pack = a.dx ? ((unsigned)a.H / 16 * a.kb + 3) / 4 : 0u;
         e = for_row16(a.E, wide, [&]<int NV, bool WIDE>() {
             hipLaunchKernelGGL((route_backward_prep_kernel<NV, WIDE>), dim3(a.steps + pack), dim3(256), 0, st, a, a.steps);
             return hipGetLastError();
@@ -705,7 +685,7 @@ hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st) {
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(route_backward_sum_kernel, dim3((unsigned)(((size_t)(a.H + 1) * 4 * a.nb + 255) / 256)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(route_backward_sum_kernel, dim3((unsigned)(((size_t)(a.H + 1) * 4 * a.nb + 63) / 64)), dim3(64), 0, st, a);
     return hipGetLastError();
 }
 
