@@ -820,8 +820,8 @@ struct BalanceLayout {
 };
 BalanceLayout balance_layout(const moe_shape& s) {
     BalanceLayout L;
-    // a workgroup of the counts takes at least 2048 picks, one of the loss 64 tokens at a time
-    int64_t n = ((int64_t)s.T * s.top_k + 2047) / 2048;
+    // a workgroup of the counts takes at least 1024 picks, one of the loss 64 tokens at a time
+    int64_t n = ((int64_t)s.T * s.top_k + 1023) / 1024;
     if (n > BALANCE_COUNT_BLOCKS) n = BALANCE_COUNT_BLOCKS;
     if (n < 1) n = 1;
     L.count_tokens = (int)((s.T + n - 1) / n);

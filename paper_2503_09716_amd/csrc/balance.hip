@@ -31,18 +31,19 @@ __device__ __forceinline__ int count_picks(int* hist, int* kept, const int32_t* 
     const int32_t* const p = idx + (size_t)t0 * k;
     const int n = (t1 - t0) * k;
     const int step = blockDim.x;
+    constexpr int AHEAD = 8;
     auto count = [&]<bool KEEP>() {
-        for (int i0 = threadIdx.x; i0 < n; i0 += 8 * step) {
-            uint32_t e[8];
-            uint8_t on[8];
+        for (int i0 = threadIdx.x; i0 < n; i0 += AHEAD * step) {
+            uint32_t e[AHEAD];
+            uint8_t on[AHEAD];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < AHEAD; ++u) {
                 const int i = min(i0 + u * step, n - 1);
                 e[u] = p[i];
                 on[u] = KEEP ? keep[t0 + i / k] : 1;
             }
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
+            for (int u = 0; u < AHEAD; ++u)
                 if (i0 + u * step < n && on[u] && e[u] < (uint32_t)E) atomicAdd(&hist[e[u]], 1);
         }
     };
@@ -92,14 +93,17 @@ __global__ __launch_bounds__(THREADS) void balance_loss_kernel(const BalanceArgs
         count_picks(hist, &kept, a.idx, a.keep, 0, a.T, E, a.k);
         if (threadIdx.x == 0) hist[E] = kept;
     } else {
-        for (int e = threadIdx.x; e <= E; e += THREADS) {
-            int c = 0;
+        // all threads read the partial histograms: one thread an expert, however many loads it has in flight, costs 3 us more
+        for (int e = threadIdx.x; e <= E; e += THREADS) hist[e] = 0;
+        __syncthreads();
+        const int total = a.count_blocks * (E + 1);
+        for (int i0 = threadIdx.x; i0 < total; i0 += 6 * THREADS) {
+            int c[6];
 #pragma unroll
-            for (int b = 0; b < BALANCE_COUNT_BLOCKS; ++b) {   // all in flight
-                const int v = a.partial_counts[min(b, a.count_blocks - 1) * (E + 1) + e];
-                c += b < a.count_blocks ? v : 0;
-            }
-            hist[e] = c;
+            for (int u = 0; u < 6; ++u) c[u] = a.partial_counts[min(i0 + u * THREADS, total - 1)];
+#pragma unroll
+            for (int u = 0; u < 6; ++u)
+                if (i0 + u * THREADS < total && c[u]) atomicAdd(&hist[(i0 + u * THREADS) % (E + 1)], c[u]);
         }
     }
     __syncthreads();
@@ -126,18 +130,19 @@ __global__ __launch_bounds__(THREADS) void balance_loss_kernel(const BalanceArgs
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = ahead[i];
         fetch(q + stride);
-        const float lse = softmax_row16<NV>(v);
-        float s = 0.f;
+        float z, s = 0.f;
+        const float top = exps_row16<NV>(v, z), rz = 1.0f / z, lse = top + logf(z);
 #pragma unroll
         for (int i = 0; i < NV; ++i) s = fmaf(v[i], o[i], s);
-        s = row16_sum(s);
+        s = row16_sum(s) * rz;
         if (on && row == 0) {
             sum_s += s;
             sum_z += (double)lse * lse;
         }
+        const float slope = rz * bal, at = rz * lse * zc;
         if (a.dlogits && tok < a.T) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = on ? v[i] * ((o[i] - s) * bal + lse * zc) : 0.f;
+            for (int i = 0; i < NV; ++i) v[i] = on ? v[i] * fmaf(o[i] - s, slope, at) : 0.f;
             store_row16<NV, WIDE>(v, a.dlogits, t, E, row);
         }
     }

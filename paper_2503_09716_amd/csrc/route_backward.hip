@@ -188,10 +188,11 @@ struct TokenRow {
         if (a.renorm)
 #pragma unroll
             for (int i = 0; i < NV; ++i) v[i] = picked >> i & 1 ? v[i] : -INFINITY;
-        softmax_row16<NV>(v);
-        float s = 0.f;
+        float z, s = 0.f;
+        exps_row16<NV>(v, z);
+        const float rz = 1.0f / z;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) s = fmaf(v[i], g[i], s);
+        for (int i = 0; i < NV; ++i) { v[i] *= rz; s = fmaf(v[i], g[i], s); }
         s = row16_sum(s);
         const bool counts = on(a);
 #pragma unroll

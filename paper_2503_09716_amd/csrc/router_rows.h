@@ -56,21 +56,18 @@ __device__ __forceinline__ float exp_nonpositive(float x) {
     return fmaf(e, lo * LN2, e);
 }
 
-// Logits to their softmax over the row; the logarithm of the sum of their exponentials.  Values of -inf get probability 0.
+// Logits to e^(logit - the largest); the sum of those in z.  The largest.  Values of -inf give 0.
 template <int NV>
-__device__ __forceinline__ float softmax_row16(float (&v)[NV]) {
+__device__ __forceinline__ float exps_row16(float (&v)[NV], float& z) {
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NV; ++i) m = fmaxf(m, v[i]);
     m = row16_max(m);
-    float z = 0.f;
+    z = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) { v[i] = exp_nonpositive(v[i] - m); z += v[i]; }
     z = row16_sum(z);
-    const float rz = 1.0f / z;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] *= rz;
-    return m + logf(z);
+    return m;
 }
 
 }  // namespace
