@@ -6,7 +6,15 @@
 //   dx = dl Wg^T,   dWg = x^T dl,   dbias = sum_t dl_t.
 // x and Wg are bf16, so a matrix instruction multiplies them exactly; dl is fp32 and goes in as a sum of bf16 pieces: hi + mid + lo
 // hold its 24 bits, and three products give dWg what products in fp32 would; dx is rounded to bf16 (8 bits), and the two pieces it
-// takes hold dl to 2^-17.
+// takes hold dl to 2^-17.  (Products in fp32 run at a sixteenth of the rate.)
+//
+// Three launches: dl and the gate matrix in operand order; both products; the sum of dWg's parts.  us (of which products):
+// 256 tokens x 512, 8 experts 10 (4.7; two launches), 3001 x 2048, 64 experts 23 (16; two launches), 16384 x 6144, 8 experts 91 (82: 403 MB at 4.9
+// TB/s, a copy of x takes 74), 32768 x 5120, 64 experts 160 (140; 124), 160 experts 246 to 270 by box (225 at 2.2 GHz: matrix units 55 % busy
+// with 268 GFLOP of bf16 products).  What keeps them from more there is that both wavefronts of a SIMD wait at the same time, after the
+// step's barrier and for operands from LDS (30 % of their cycles).  Two workgroups of four wavefronts to a CU, other priorities, one of
+// the two starting with the other product and three pieces of dl's operands in one wait: no gain; two tiles of their own for the
+// products, one after the other or in turn, 262 to 310.
 #include "common.h"
 #include "router_rows.h"
 #include "train.h"
