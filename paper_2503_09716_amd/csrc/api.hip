@@ -1361,11 +1361,11 @@ moe_status moe_route_backward(moe_ctx* c, const moe_shape* s, const void* x, con
     if (moe_status st = check_backward_ws(c, s, ws, ws_bytes)) return st;
     const RouteBackwardLayout L = route_backward_layout(*s);
     char* const w8 = (char*)ws;
-    // A launch for dl is saved where each workgroup computes it for few blocks of tokens, and reads its part of the gate matrix 16 bytes at a
-    // time (us with the launch, without: 256 x 512, 8 experts 13.7, 10.3; 3001 x 2048, 64 experts 26.3, 24.4; 6000 x 2048, 6 blocks of
-    // tokens, 26.6, 29.5; 256 x 2048, 63 experts, whose gate matrix it reads 2 bytes at a time, 16.2, 18.4).
+    // A launch for dl is saved where each workgroup computes it for few blocks of tokens, and can load its part of the gate matrix 16 bytes
+    // at a time (us with the launch, without: 256 x 512, 8 experts 13.7, 9.9; 3001 x 2048, 64 experts 26.3, 22.5; 6000 x 2048, 6 blocks of
+    // tokens, 26.6, 29.5).
     const int wg_wide = s->E % 8 == 0 && !misaligned({wg}, 16);
-    const int own_dl = L.nb <= ROUTE_BACKWARD_OWN_BLOCKS && L.split_steps <= 4 && (wg_wide || !dx);
+    const int own_dl = L.nb <= ROUTE_BACKWARD_OWN_BLOCKS && L.split_steps <= 4 && (!dx || !misaligned({wg}, 16));
     const RouteBackwardArgs a{(const char*)x, (const char*)wg, logits, idx, dw, dlogits, keep, (char*)dx, dwg, dbias, s->T, s->H, s->E, s->top_k,
                               s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.tiles, L.splits, L.split_steps, own_dl, wg_wide, w8 + L.zeros,
                               (uint32_t*)(w8 + L.masks), w8 + L.dl_blocks, w8 + L.wg_blocks, (float*)(w8 + L.partial)};

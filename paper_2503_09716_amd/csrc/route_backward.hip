@@ -420,7 +420,7 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
         ask_kept(s0);
     }
     bf16x8 wg[L::DB][L::KB];
-    if (DX)
+    auto load_gate = [&] {
 #pragma unroll
         for (int b = 0; b < L::DB; ++b)
 #pragma unroll
@@ -429,6 +429,39 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
                 wg[b][kb] = OWN ? __builtin_bit_cast(bf16x8, gate_piece(a, h, b % 2, kb, lane))
                                 : reinterpret_cast<const bf16x8*>(a.wg_blocks)[((size_t)(h / 16 + b % 2) * L::KB + kb) * 64 + lane];
             }
+    };
+    // Rows that do not start on 16 bytes: the tile's part of the gate matrix, which is one piece of memory, by way of LDS that is not in use
+    // yet (from memory 2 bytes at a time a tile of 63 experts took 5 us more).
+    auto stage_gate = [&] {
+        const lds_t area = lds + 32 * L::ROW;
+        static_assert(!OWN || 2 * L::STAGE - 32 * L::ROW >= L::HT * 16 * NB * 2);
+        const char* const src = a.wg + (size_t)h0 * a.E * 2;
+        const uint32_t bytes = (uint32_t)min(L::HT, a.H - h0) * a.E * 2;
+        for (uint32_t at = wave * 1024; at < bytes; at += 8192) {
+            const uint32_t here = at + lane * 16;
+            load16_to_lds(here < bytes ? src + here : reinterpret_cast<const char*>(zeros_page) + lane * 16, area + at);
+        }
+        ring_wait<0>();
+        ring_meet();
+        typedef __attribute__((address_space(3))) const uint16_t* element_t;
+#pragma unroll
+        for (int b = 0; b < L::DB; ++b)
+#pragma unroll
+            for (int kb = 0; kb < L::KB; ++kb) {
+                const int i = lane & 15, e0 = kb * 32 + 8 * (lane >> 4);
+                const element_t p = (element_t)area + (min(dh + b / 2 * 32, a.H - 32) - h0 + 8 * (i >> 2) + 4 * (b % 2) + (i & 3)) * a.E;
+                uint32_t v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = e0 + j < a.E ? p[min(e0 + j, a.E - 1)] : 0u;
+                wg[b][kb] = __builtin_bit_cast(bf16x8, u32x4{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16});
+            }
+        ring_wait<0>();
+        ring_meet();   // read before dl comes there
+    };
+    if constexpr (DX) {
+        if (OWN && !a.wg_wide) stage_gate();
+        else load_gate();
+    }
 
     f32x4 acc[L::EB][L::HB] = {};
     f32x4 bias[L::EB] = {};
