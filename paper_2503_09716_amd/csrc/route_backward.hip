@@ -268,6 +268,18 @@ __device__ __forceinline__ void ring_wait() {
     __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | 0x0070);  // vmcnt(N) lgkmcnt(0), gfx9 encoding
     asm volatile("" ::: "memory");
 }
+// ... at most the loads of `stages` stages, N or, where not `all`, FEW to a stage: a case for each number of stages up to MOST.
+template <int MOST, int N, int FEW>
+__device__ __forceinline__ void wait_stages(const int stages, const bool all) {
+    if constexpr (MOST >= 0) {
+        if (stages >= MOST) {
+            if (all) ring_wait<MOST * N>();
+            else ring_wait<MOST * FEW>();
+        } else {
+            wait_stages<MOST - 1, N, FEW>(stages, all);
+        }
+    }
+}
 __device__ __forceinline__ void ring_meet() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -469,10 +481,7 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
         issue_x(s0, 0);
         ask_kept(s0 + 1);
     } else {
-        for (int i = 0; i < L::NS - 1; ++i) {
-            const int s = min(s0 + i, s1 - 1);
-            issue(s, masks[s], i);
-        }
+        for (int s = s0; s < min(s0 + L::NS - 1, s1); ++s) issue(s, masks[s], s - s0);
     }
     // SUMS: dl's blocks are added up for dbias, too.
     auto steps = [&]<bool SUMS>() {
@@ -495,9 +504,12 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
                     ask_kept(s + 2);
                 }
             } else {
-                // Loads and stores retire in the order they were issued.  Behind this stage's loads there are those of NS - 2 stages and, from
-                // the ring's second round on, NS - 1 steps' stores (all tokens exist in every step but the last, and all columns or none).
-                if (DX && s - s0 >= L::NS - 1 && dh + L::DB * 16 <= a.H) {
+                // Loads and stores retire in the order they were issued.  Behind this stage's loads there are those of the stages that have
+                // been asked for since, NS - 2 or what is left, and, from the ring's second round on, NS - 1 steps' stores (all tokens exist in
+                // every step but the last, and all columns or none).
+                const int later = s1 - 1 - s;
+                if (later < L::NS - 2) wait_stages<L::NS - 3, L::NL, L::NL - 1>(later, L::MORE == 0 || wave < L::MORE);
+                else if (DX && s - s0 >= L::NS - 1 && dh + L::DB * 16 <= a.H) {
                     if (L::MORE == 0 || wave < L::MORE) ring_wait<(L::NS - 2) * L::NL + (L::NS - 1) * L::STORES>();
                     else ring_wait<(L::NS - 2) * (L::NL - 1) + (L::NS - 1) * L::STORES>();
                 } else {
@@ -505,9 +517,11 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
                     else ring_wait<(L::NS - 2) * (L::NL - 1)>();
                 }
                 ring_meet();
-                int next = stage + L::NS - 1;
-                if (next >= L::NS) next -= L::NS;
-                issue(min(s + L::NS - 1, s1 - 1), mask, next);
+                if (s + L::NS - 1 < s1) {
+                    int next = stage + L::NS - 1;
+                    if (next >= L::NS) next -= L::NS;
+                    issue(s + L::NS - 1, mask, next);
+                }
                 mask = masks[min(s + L::NS, s1 - 1)];
             }
             const lds_t xs = lds + stage * L::STAGE, ds = xs + 32 * L::ROW;
@@ -600,7 +614,6 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
     const bool sums = ht == 0 && wh == 0;
     if (sums) steps.template operator()<true>();
     else steps.template operator()<false>();
-    ring_wait<0>();   // no load may land in LDS that belongs to another workgroup
     float* const out = a.partial + (size_t)split * (a.H + 1) * (16 * NB);
 #pragma unroll
     for (int hb = 0; hb < L::HB; ++hb) {
