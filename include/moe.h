@@ -380,7 +380,7 @@ moe_status moe_combine_backward(moe_ctx* ctx, const moe_shape* shape, const void
 typedef struct {
     void* buffer;
     int32_t chunks;
-    int32_t in_place;
+    int32_t one_launch;
 } moe_gradient_list;
 
 /* Device bytes of a list of `tensors` tensors with elements[i] elements of 4 (is_fp32[i] = 1) or 2 bytes; 0 for invalid arguments. */

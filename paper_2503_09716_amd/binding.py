@@ -36,7 +36,7 @@ class MoeShape(C.Structure):
 
 
 class GradientListStruct(C.Structure):
-    _fields_ = [("buffer", C.c_void_p), ("chunks", C.c_int32), ("in_place", C.c_int32)]
+    _fields_ = [("buffer", C.c_void_p), ("chunks", C.c_int32), ("one_launch", C.c_int32)]
 
 
 class MoeError(RuntimeError):

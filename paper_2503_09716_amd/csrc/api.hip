@@ -1419,7 +1419,7 @@ moe_status moe_gradient_list_make(moe_ctx* c, int32_t tensors, const void* const
     moe_status st = MOE_OK;
     if (!e || !table) st = fail(c, MOE_E_ARG, "gradient_list: no host memory for %lld chunks", (long long)chunks);
     if (st == MOE_OK) {
-        int64_t n = 0, m = 0;
+        int64_t n = 0, m = 0, total = 0;
         bool in_place = false;
         for (int32_t i = 0; i < tensors; ++i) {
             if (elements[i] == 0) continue;
@@ -1427,6 +1427,7 @@ moe_status moe_gradient_list_make(moe_ctx* c, int32_t tensors, const void* const
             e[m++] = {(uintptr_t)grads[i], (uintptr_t)grads[i] + bytes, i};
             e[m++] = {(uintptr_t)outs[i], (uintptr_t)outs[i] + bytes, i};
             in_place = in_place || grads[i] == outs[i];
+            total += bytes;
             for (int64_t at = 0, end; at < bytes; at = end) {
                 end = at + CLIP_CHUNK - (at == 0 ? (int64_t)((uintptr_t)grads[i] & 127) : 0);
                 if (end > bytes) end = bytes;
@@ -1440,7 +1441,7 @@ moe_status moe_gradient_list_make(moe_ctx* c, int32_t tensors, const void* const
             r = hipMemcpyAsync((char*)buffer + align_up(CLIP_BLOCKS * sizeof(double)), table, n * sizeof(ClipChunk), hipMemcpyHostToDevice, (hipStream_t)stream);
         if (st == MOE_OK && r == hipSuccess) r = hipStreamSynchronize((hipStream_t)stream);
         if (r != hipSuccess) st = fail(c, MOE_E_HIP, "gradient_list: %s", hipGetErrorString(r));
-        if (st == MOE_OK) *list = moe_gradient_list{buffer, (int32_t)n, in_place ? 1 : 0};
+        if (st == MOE_OK) *list = moe_gradient_list{buffer, (int32_t)n, !in_place && n <= CLIP_FEW_CHUNKS && total <= CLIP_FEW_BYTES ? 1 : 0};
     }
     free(e);
     free(table);
@@ -1455,7 +1456,7 @@ moe_status moe_clip_gradients(moe_ctx* c, const moe_gradient_list* list, double 
     if (misaligned({norm}, 4)) return fail(c, MOE_E_ARG, "clip_gradients: misaligned pointer");
     HIP_TRY(c, hipSetDevice(c->device));
     const ClipArgs a{(const ClipChunk*)((char*)list->buffer + align_up(CLIP_BLOCKS * sizeof(double))), (double*)list->buffer, norm, max_norm, list->chunks,
-                     list->in_place};
+                     list->one_launch};
     HIP_TRY(c, launch_clip(a, (hipStream_t)stream));
     return MOE_OK;
 }

@@ -71,9 +71,11 @@ struct ClipArgs {
     double* partial;           // [CLIP_BLOCKS]
     float* norm;
     double max_norm;
-    int32_t n_chunks, in_place;   // in_place: an output is its own gradient
+    int32_t n_chunks, one_launch;
 };
 constexpr int CLIP_BLOCKS = 1024;
+// Lists that one launch takes: up to that many chunks and bytes, no output in place of its gradient.
+constexpr int CLIP_FEW_CHUNKS = 16, CLIP_FEW_BYTES = 384 << 10;
 hipError_t launch_clip(const ClipArgs& a, hipStream_t st);
 
 }  // namespace moe
