@@ -164,9 +164,9 @@ def _typed(t: Optional[torch.Tensor], dtype, numel: int):
     """_ptr of a tensor that the call reads or writes as `numel` elements of `dtype`."""
     if t is None:
         return None
-    assert t.dtype == dtype and t.numel() == numel, "tensor of %d elements of %s required" % (numel, dtype)
-    assert t.is_cuda and t.is_contiguous(), "device-resident contiguous tensor required"
-    return t.data_ptr()
+    if t.dtype is dtype and t.numel() == numel and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise AssertionError("device-resident contiguous tensor of %d elements of %s required" % (numel, dtype))
 
 
 def _raw_stream(device: int):

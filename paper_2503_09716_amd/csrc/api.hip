@@ -1366,8 +1366,11 @@ moe_status moe_route_backward(moe_ctx* c, const moe_shape* s, const void* x, con
     // tokens, 26.6, 29.5).
     const int wg_wide = s->E % 8 == 0 && !misaligned({wg}, 16);
     const int own_dl = L.nb <= ROUTE_BACKWARD_OWN_BLOCKS && L.split_steps <= 4 && (!dx || !misaligned({wg}, 16));
+    // The launch that sums the parts is saved where there is one (us with it, without: 32 x 512, 8 experts 10.0, 7.9); stores of 4 bytes
+    // cost more than it from 49 experts on (20 x 1024, 33 experts 11.6, 8.6; 32 x 2048, 64 experts 11, 12.8; 32 x 5120, 160 experts 20.7, 30.2).
+    const int direct = L.splits > 1 ? 0 : s->E % 4 == 0 && !misaligned({dwg}, 16) ? 2 : s->E <= 48 ? 1 : 0;
     const RouteBackwardArgs a{(const char*)x, (const char*)wg, logits, idx, dw, dlogits, keep, (char*)dx, dwg, dbias, s->T, s->H, s->E, s->top_k,
-                              s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.tiles, L.splits, L.split_steps, own_dl, wg_wide, w8 + L.zeros,
+                              s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.tiles, L.splits, L.split_steps, own_dl, direct, wg_wide, w8 + L.zeros,
                               (uint32_t*)(w8 + L.masks), w8 + L.dl_blocks, w8 + L.wg_blocks, (float*)(w8 + L.partial)};
     HIP_TRY(c, launch_route_backward(a, hs));
     return MOE_OK;

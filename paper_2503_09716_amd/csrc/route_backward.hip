@@ -614,19 +614,33 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
     const bool sums = ht == 0 && wh == 0;
     if (sums) steps.template operator()<true>();
     else steps.template operator()<false>();
-    float* const out = a.partial + (size_t)split * (a.H + 1) * (16 * NB);
+    // A single part is the sum: dWg and dbias at once.  Of several each goes to its place among the parts, in rows of 16 NB.
+    auto put = [&](const int h, const int e, f32x4 v) {
+        if (!a.direct) {
+            *reinterpret_cast<f32x4*>(a.partial + ((size_t)split * (a.H + 1) + h) * (16 * NB) + e) = v;
+            return;
+        }
+        float* const o = h < a.H ? a.dwg + (size_t)h * a.E + e : a.dbias ? a.dbias + e : nullptr;
+        if (!o || e >= a.E) return;
+        if (a.direct == 2 && h < a.H) {
+            if (a.accumulate) v += *reinterpret_cast<const f32x4*>(o);
+            *reinterpret_cast<f32x4*>(o) = v;
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (e + j < a.E) o[j] = a.accumulate ? v[j] + o[j] : v[j];
+    };
 #pragma unroll
     for (int hb = 0; hb < L::HB; ++hb) {
         const int h = h0 + (wh * L::HB + hb) * 16 + (lane & 15);
         if (h < a.H)
 #pragma unroll
-            for (int eb = 0; eb < L::EB; ++eb)
-                *reinterpret_cast<f32x4*>(out + (size_t)h * (16 * NB) + (we * L::EB + eb) * 16 + 4 * (lane >> 4)) = acc[eb][hb];
+            for (int eb = 0; eb < L::EB; ++eb) put(h, (we * L::EB + eb) * 16 + 4 * (lane >> 4), acc[eb][hb]);
     }
     if (sums && (lane & 15) == 0)
 #pragma unroll
-        for (int eb = 0; eb < L::EB; ++eb)
-            *reinterpret_cast<f32x4*>(out + (size_t)a.H * (16 * NB) + (we * L::EB + eb) * 16 + 4 * (lane >> 4)) = bias[eb];
+        for (int eb = 0; eb < L::EB; ++eb) put(a.H, (we * L::EB + eb) * 16 + 4 * (lane >> 4), bias[eb]);
 }
 
 // dWg and dbias: the parts of the tokens added in order, four experts to a thread.  Workgroups of one wavefront: short batches have few
@@ -740,6 +754,7 @@ hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st) {
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
+    if (a.direct) return hipSuccess;
     hipLaunchKernelGGL(route_backward_sum_kernel, dim3((unsigned)(((size_t)(a.H + 1) * 4 * a.nb + 63) / 64)), dim3(64), 0, st, a);
     return hipGetLastError();
 }

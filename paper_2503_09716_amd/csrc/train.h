@@ -42,6 +42,7 @@ struct RouteBackwardArgs {
     int32_t steps;             // blocks of 32 tokens
     int32_t tiles, splits, split_steps;   // tiles of H, parts of the tokens that dWg is summed over apart, blocks of 32 tokens to one
     int32_t own_dl;            // 1: no launch for dl, the products' workgroups compute their tokens'
+    int32_t direct;            // 1: the products write dWg and dbias themselves (one part), 2: dWg 16 bytes at a time
     int32_t wg_wide;           // 1: the gate matrix can be read 16 bytes at a time
     char* zeros;               // 1 KiB that the first launch clears
     uint32_t* masks;           // [T / 32]: the tokens that count

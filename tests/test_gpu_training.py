@@ -303,6 +303,25 @@ def test_route_backward(moe, T, H, E, k, renorm):
     assert torch.equal(dwg, dwg3)
 
 
+@pytest.mark.parametrize("E", [7, 30, 48, 64, 70, 130, 160])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_route_backward_one_block_of_tokens(moe, E, shift):
+    """Up to 32 tokens there is nothing to add up: dWg and dbias are written, or added to, in the products' launch, by 16 or by 4 bytes."""
+    for T, H in ((1, 64), (17, 576), (32, 320)):
+        s = route_inputs(T, H, E, 3, T + E)
+        shape = make_shape(T, H, 64, E, 3)
+        ws = moe.new_backward_workspace(shape)
+        at = lambda *n: torch.randn(math.prod(n) + shift, device="cuda")[shift:].view(n)
+        for accumulate in (False, True):
+            dx, dwg, db = torch.empty_like(s["x"]), at(H, E), at(E)
+            start = (dwg.clone(), db.clone()) if accumulate else None
+            moe.route_backward(shape, s["x"], s["wg"], s["logits"], s["idx"], s["dw"], s["dlogits"], None, dx, dwg, db, accumulate, ws)
+            check_route(s, True, 1.0, dx, dwg, db, start)
+        before = dwg.clone()
+        moe.route_backward(shape, s["x"], s["wg"], s["logits"], s["idx"], s["dw"], s["dlogits"], None, None, dwg, None, True, ws)
+        check_route(s, True, 1.0, None, dwg, None, (before, torch.zeros(E, device="cuda")))
+
+
 def test_route_backward_many_tokens(moe):
     """Long sums: each part of the tokens over several rounds of the ring, parts that end inside a block."""
     for T, H, E, k in ((20011, 320, 40, 4), (40003, 64, 8, 2), (12345, 256, 144, 6)):
