@@ -192,7 +192,7 @@ class Moe:
         if st != 0 or not h:
             raise MoeError(st, "moe_create failed on device %d" % device)
         self.h = h
-        self.options = {}   # what set_option was given
+        self.y_dtype, self.out_dtype = torch.float32, torch.bfloat16   # as options "y_fp32" and "out_fp32" have them
 
     def close(self):
         if getattr(self, "h", None):
@@ -211,7 +211,10 @@ class Moe:
 
     def set_option(self, key: str, value: int):
         self._check(self.lib.moe_set_option(self.h, key.encode(), int(value)))
-        self.options[key] = int(value)
+        if key == "y_fp32":
+            self.y_dtype = torch.float32 if value else torch.bfloat16
+        elif key == "out_fp32":
+            self.out_dtype = torch.float32 if value else torch.bfloat16
 
     def new_workspace(self, shape: MoeShape) -> torch.Tensor:
         n = workspace_bytes(shape)
@@ -293,9 +296,8 @@ class Moe:
     def combine_backward(self, shape, dout, y_perm, inv_perm, topk_w, dtopk_w, dy_perm):
         """dout as option "out_fp32" has it, y_perm and dy_perm (or None) as "y_fp32" has them."""
         T, H, R = shape.T, shape.H, shape.T * shape.top_k
-        f32, b16 = torch.float32, torch.bfloat16
-        y, o = (f32 if self.options.get(n, d) else b16 for n, d in (("y_fp32", 1), ("out_fp32", 0)))
-        self._check(self.lib.moe_combine_backward(self.h, C.byref(shape), _typed(dout, o, T * H), _typed(y_perm, y, R * H),
+        f32, y = torch.float32, self.y_dtype
+        self._check(self.lib.moe_combine_backward(self.h, C.byref(shape), _typed(dout, self.out_dtype, T * H), _typed(y_perm, y, R * H),
                                                   _typed(inv_perm, torch.int32, R), _typed(topk_w, f32, R), _typed(dtopk_w, f32, R),
                                                   _typed(dy_perm, y, R * H), _raw_stream(self.device)))
 
