@@ -838,26 +838,30 @@ BalanceLayout balance_layout(const moe_shape& s) {
     return L;
 }
 
+constexpr int DIRECT_ODD_EXPERTS = 48;   // up to which dWg is written 4 bytes at a time where it cannot be 16
 struct RouteBackwardLayout {
     int nb, kb, steps, tiles, splits, split_steps;
     size_t zeros, masks, dl_blocks, wg_blocks, partial, total;
 };
-RouteBackwardLayout route_backward_layout(const moe_shape& s) {
+RouteBackwardLayout route_backward_layout(const moe_shape& s, const bool own) {
     RouteBackwardLayout L;
     L.nb = route_backward_blocks(s.E);
     L.kb = (L.nb + 1) / 2;
     L.steps = (s.T + 31) / 32;
     if (L.steps < 1) L.steps = 1;
     // as many parts of the tokens as fill the CUs with workgroups (two to a CU up to 32 experts, whose ring is small)
-    const int columns = route_backward_columns(L.nb);
+    const int columns = route_backward_columns(L.nb, own);
     L.tiles = (s.H + columns - 1) / columns;
     const int want = (L.nb <= 2 ? 512 : 256) / L.tiles;
     const int parts = want < 1 ? 1 : want < L.steps ? want : L.steps;
     // ... but up to 4 blocks of tokens to a part, as the root of their number grows: each part writes a whole dWg that is read again (us with
     // 1, 2, 3, 4 blocks: 1024 x 4096, 8 experts 14.8, 12.7, 13.9, 14.3; 1000 x 5120, 32 experts 20.0, 20.2, 17.2, 17.6; 256 x 2048, 64 experts
-    // 13.7, 15.2, 16.8, 18.9).
+    // 13.7, 15.2, 16.8, 18.9, a tile of 256 columns).
     int least = (int)(sqrt((double)L.steps) / 3 + 0.5);
     least = least < 1 ? 1 : least > 4 ? 4 : least;
+    // Up to 4 blocks of tokens, 3 from 65 experts on, one part, which needs no sum (us with a part to a block, one part: 128 tokens x 4096, 8
+    // experts 11.1, 8.9, x 5120, 64 experts 11.4, 10.2, x 2048, 128 experts 13.2, 14.8; 96 tokens 12.7, 12.3; 160 tokens, 64 experts 10.7, 10.9).
+    if (L.steps <= (L.nb <= 4 ? 4 : 3) && (s.E % 4 == 0 || s.E <= DIRECT_ODD_EXPERTS)) least = L.steps;
     L.split_steps = (L.steps + parts - 1) / parts;
     if (L.split_steps < least) L.split_steps = least;
     L.splits = (L.steps + L.split_steps - 1) / L.split_steps;
@@ -873,8 +877,7 @@ RouteBackwardLayout route_backward_layout(const moe_shape& s) {
 }
 
 size_t backward_bytes(const moe_shape& s) {
-    const size_t a = balance_layout(s).total, b = route_backward_layout(s).total;
-    return a > b ? a : b;
+    return std::max({balance_layout(s).total, route_backward_layout(s, false).total, route_backward_layout(s, true).total});
 }
 
 const char* training_shape_problem(const moe_shape* s, moe_status* st) {
@@ -1359,16 +1362,19 @@ moe_status moe_route_backward(moe_ctx* c, const moe_shape* s, const void* x, con
         return MOE_OK;
     }
     if (moe_status st = check_backward_ws(c, s, ws, ws_bytes)) return st;
-    const RouteBackwardLayout L = route_backward_layout(*s);
+    RouteBackwardLayout L = route_backward_layout(*s, true);
     char* const w8 = (char*)ws;
     // A launch for dl is saved where each workgroup computes it for few blocks of tokens, and can load its part of the gate matrix 16 bytes
-    // at a time (us with the launch, without: 256 x 512, 8 experts 13.7, 9.9; 3001 x 2048, 64 experts 26.3, 22.5; 6000 x 2048, 6 blocks of
-    // tokens, 26.6, 29.5).
+    // at a time (us with the launch, without: 8 experts 256 x 512 13.7, 9.9, 4000 x 6144, 5 blocks, 25.5, 28.1; 64 experts 3001 x 2048, 6
+    // blocks, 24.3, 22.2, 3800 x 2048, 8 blocks, 25.6, 24.0; 96 experts 3000 x 2048, 6 blocks, 26.9, 25.6; 128 experts 2500 x 2048, 5 blocks, 29.1,
+    // 27.9, 3000 x 2048, 6 blocks, 28.8, 29.7; 160 experts 256 x 5120 27.7, 21.3, 900 x 5120, 5 blocks, 32.1, 30.2).
     const int wg_wide = s->E % 8 == 0 && !misaligned({wg}, 16);
-    const int own_dl = L.nb <= ROUTE_BACKWARD_OWN_BLOCKS && L.split_steps <= 4 && (!dx || !misaligned({wg}, 16));
+    const int most = L.nb <= 2 ? 4 : L.nb <= 4 ? 8 : 5;
+    const int own_dl = L.nb <= ROUTE_BACKWARD_OWN_BLOCKS && L.split_steps <= most && (!dx || !misaligned({wg}, 16));
+    if (!own_dl) L = route_backward_layout(*s, false);
     // The launch that sums the parts is saved where there is one (us with it, without: 32 x 512, 8 experts 10.0, 7.9); stores of 4 bytes
     // cost more than it from 49 experts on (20 x 1024, 33 experts 11.6, 8.6; 32 x 2048, 64 experts 11, 12.8; 32 x 5120, 160 experts 20.7, 30.2).
-    const int direct = L.splits > 1 ? 0 : s->E % 4 == 0 && !misaligned({dwg}, 16) ? 2 : s->E <= 48 ? 1 : 0;
+    const int direct = L.splits > 1 ? 0 : s->E % 4 == 0 && !misaligned({dwg}, 16) ? 2 : s->E <= DIRECT_ODD_EXPERTS ? 1 : 0;
     const RouteBackwardArgs a{(const char*)x, (const char*)wg, logits, idx, dw, dlogits, keep, (char*)dx, dwg, dbias, s->T, s->H, s->E, s->top_k,
                               s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.tiles, L.splits, L.split_steps, own_dl, direct, wg_wide, w8 + L.zeros,
                               (uint32_t*)(w8 + L.masks), w8 + L.dl_blocks, w8 + L.wg_blocks, (float*)(w8 + L.partial)};

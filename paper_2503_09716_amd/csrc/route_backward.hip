@@ -302,10 +302,12 @@ __device__ __forceinline__ int xcd_place(const int id, const int n) {
 //        columns of a token, two blocks whose rows are interleaved by fours.
 // So x is read and dx written side by side, dl is read once for both.  Rows of x past the end and of tokens that do not count come from
 // a page of zeros: their dl is zero, but what x holds there may be no number.
-// More than 160 experts take half the columns, or the accumulators and the gate matrix would not fit the registers.
-template <int NB>
+// More than 160 experts take half the columns, or the accumulators and the gate matrix would not fit the registers; so do short batches
+// of more than 32, for twice the workgroups to as many parts (us with 256, 128 columns: 64 experts 256 x 5120 15.9, 12.4, 1000 x 2048 17.0, 15.0,
+// 3001 x 2048 22.6, 21.7; 96 experts 1000 x 2048 21.0, 17.9).
+template <int NB, bool OWN>
 struct Tile {
-    static constexpr int HT = NB <= 10 ? 256 : 128;
+    static constexpr int HT = NB <= (OWN ? 2 : 10) ? 256 : 128;
     static constexpr int KB = (NB + 1) / 2;            // blocks of 32 experts
     static constexpr int WE = NB <= 2 ? 1 : NB <= 10 ? 2 : 4;   // wavefronts along the experts
     static constexpr int WH = 8 / WE;                  // and along the columns
@@ -357,7 +359,7 @@ __device__ __forceinline__ void store_dx(char* p, const u32x4 v) {
 // saved; each of the tiles of H does it again.
 template <int NB, bool DX, bool OWN>
 __global__ __launch_bounds__(512) void route_backward_products_kernel(const RouteBackwardArgs a) {
-    typedef Tile<NB> L;
+    typedef Tile<NB, OWN> L;
     extern __shared__ char lds_raw[];
     const lds_t lds = (lds_t)lds_raw;
     constexpr int PICK_ROW = 16 * NB + 1;
@@ -707,15 +709,15 @@ int route_backward_blocks(const int E) {
     return 16;
 }
 
-int route_backward_columns(const int nb) {
+int route_backward_columns(const int nb, const bool own) {
     int columns = 0;
-    (void)for_blocks(nb, [&]<int NB>() { columns = Tile<NB>::HT; return hipSuccess; });
+    (void)for_blocks(nb, [&]<int NB>() { columns = own ? Tile<NB, true>::HT : Tile<NB, false>::HT; return hipSuccess; });
     return columns;
 }
 
 template <int NB, bool OWN>
 constexpr int products_lds() {
-    return OWN ? 2 * Tile<NB>::STAGE + 32 * (16 * NB + 1) * 4 : Tile<NB>::NS * Tile<NB>::STAGE;
+    return OWN ? 2 * Tile<NB, OWN>::STAGE + 32 * (16 * NB + 1) * 4 : Tile<NB, OWN>::NS * Tile<NB, OWN>::STAGE;
 }
 
 template <class F>

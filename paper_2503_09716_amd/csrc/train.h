@@ -51,8 +51,8 @@ struct RouteBackwardArgs {
     float* partial;            // [splits][H + 1][16 nb]: row H the sum of dl
 };
 int route_backward_blocks(int E);   // nb
-constexpr int ROUTE_BACKWARD_OWN_BLOCKS = 6;   // nb up to which own_dl fits the registers
-int route_backward_columns(int nb);   // columns of x to a workgroup
+constexpr int ROUTE_BACKWARD_OWN_BLOCKS = 10;   // nb up to which own_dl is taken (12: 1000 x 2048, 180 experts 27.7 -> 29.9 us; 16 does not fit the registers)
+int route_backward_columns(int nb, bool own);   // columns of x to a workgroup
 hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st);
 hipError_t launch_route_backward_empty(const moe_shape& s, float* dwg, float* dbias, hipStream_t st);
 hipError_t route_backward_init();

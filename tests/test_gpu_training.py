@@ -322,6 +322,31 @@ def test_route_backward_one_block_of_tokens(moe, E, shift):
         check_route(s, True, 1.0, None, dwg, None, (before, torch.zeros(E, device="cuda")))
 
 
+@pytest.mark.parametrize("T,H,E", [(64, 512, 8), (128, 576, 20), (97, 320, 30), (127, 2112, 64), (96, 1088, 72), (95, 448, 160), (70, 192, 45), (66, 320, 63),
+                                   (128, 1088, 49), (129, 320, 64), (97, 192, 96)])
+@pytest.mark.parametrize("padding", [None, 0.3])
+def test_route_backward_few_blocks_of_tokens(moe, T, H, E, padding):
+    """Two to five blocks of tokens, of which one part is made or several, at once or to what is there, odd rows among them."""
+    say("few blocks", T, H, E, padding)
+    s = route_inputs(T, H, E, 2, T + E, padding=padding)
+    for start in (None, (torch.randn(H, E, device="cuda"), torch.randn(E, device="cuda"))):
+        out = run_route_backward(moe, s, False, 1.5, start=start)
+        check_route(s, False, 1.5, *out, start)
+        assert all(torch.equal(a, b) for a, b in zip(out, run_route_backward(moe, s, False, 1.5, start=start)))
+
+
+@pytest.mark.parametrize("T,H,E", [(3801, 2048, 64), (3201, 2112, 40), (1281, 5120, 61), (2500, 2048, 128), (2399, 2112, 80), (900, 5120, 160), (777, 4160, 121), (3001, 2048, 96)])
+def test_route_backward_parts_of_a_few_blocks(moe, T, H, E):
+    """The longest parts for which the products' workgroups compute dl, and parts one block longer, with and without dx."""
+    say("parts", T, H, E)
+    s = route_inputs(T, H, E, 6, T, padding=0.05)
+    first = run_route_backward(moe, s, True, 0.5)
+    check_route(s, True, 0.5, *first)
+    assert all(torch.equal(a, b) for a, b in zip(first, run_route_backward(moe, s, True, 0.5)))
+    without = run_route_backward(moe, s, True, 0.5, dx=False)
+    assert torch.equal(without[1], first[1]) and torch.equal(without[2], first[2])
+
+
 def test_route_backward_many_tokens(moe):
     """Long sums: each part of the tokens over several rounds of the ring, parts that end inside a block."""
     for T, H, E, k in ((20011, 320, 40, 4), (40003, 64, 8, 2), (12345, 256, 144, 6)):
