@@ -843,14 +843,14 @@ struct RouteBackwardLayout {
     int nb, kb, steps, tiles, splits, split_steps;
     size_t zeros, masks, dl_blocks, wg_blocks, partial, total;
 };
-RouteBackwardLayout route_backward_layout(const moe_shape& s, const bool own) {
+RouteBackwardLayout route_backward_layout(const moe_shape& s, const bool narrow) {
     RouteBackwardLayout L;
     L.nb = route_backward_blocks(s.E);
     L.kb = (L.nb + 1) / 2;
     L.steps = (s.T + 31) / 32;
     if (L.steps < 1) L.steps = 1;
     // as many parts of the tokens as fill the CUs with workgroups (two to a CU up to 32 experts, whose ring is small)
-    const int columns = route_backward_columns(L.nb, own);
+    const int columns = route_backward_columns(L.nb, narrow);
     L.tiles = (s.H + columns - 1) / columns;
     const int want = (L.nb <= 2 ? 512 : 256) / L.tiles;
     const int parts = want < 1 ? 1 : want < L.steps ? want : L.steps;
@@ -1365,18 +1365,22 @@ moe_status moe_route_backward(moe_ctx* c, const moe_shape* s, const void* x, con
     RouteBackwardLayout L = route_backward_layout(*s, true);
     char* const w8 = (char*)ws;
     // A launch for dl is saved where each workgroup computes it for few blocks of tokens, and can load its part of the gate matrix 16 bytes
-    // at a time (us with the launch, without: 8 experts 256 x 512 13.7, 9.9, 4000 x 6144, 5 blocks, 25.5, 28.1; 64 experts 3001 x 2048, 6
-    // blocks, 24.3, 22.2, 3800 x 2048, 8 blocks, 25.6, 24.0; 96 experts 3000 x 2048, 6 blocks, 26.9, 25.6; 128 experts 2500 x 2048, 5 blocks, 29.1,
-    // 27.9, 3000 x 2048, 6 blocks, 28.8, 29.7; 160 experts 256 x 5120 27.7, 21.3, 900 x 5120, 5 blocks, 32.1, 30.2).
+    // at a time (us with the launch, without: 8 experts 256 x 512 13.7, 9.9, 4000 x 6144, 5 blocks, 25.5, 28.1; 64 experts 3001 x 2048 26.3,
+    // 22.5, 6000 x 2048, 6 blocks, 26.6, 29.5; with narrow tiles 128 experts 2500 x 2048, 5 blocks, 29.1, 27.9, 3000 x 2048, 6 blocks, 28.8,
+    // 29.7; 160 experts 256 x 5120 27.7, 21.3, 900 x 5120, 5 blocks, 32.1, 30.2).
     const int wg_wide = s->E % 8 == 0 && !misaligned({wg}, 16);
-    const int most = L.nb <= 2 ? 4 : L.nb <= 4 ? 8 : 5;
-    const int own_dl = L.nb <= ROUTE_BACKWARD_OWN_BLOCKS && L.split_steps <= most && (!dx || !misaligned({wg}, 16));
-    if (!own_dl) L = route_backward_layout(*s, false);
+    const bool may = !dx || !misaligned({wg}, 16);
+    int narrow = L.nb > 2, own_dl = may && L.nb <= ROUTE_BACKWARD_OWN_NARROW && L.split_steps <= (narrow ? 5 : 4);
+    if (!own_dl && narrow) {
+        L = route_backward_layout(*s, false);
+        narrow = 0;
+        own_dl = may && L.nb <= ROUTE_BACKWARD_OWN_WIDE && L.split_steps <= 4;
+    }
     // The launch that sums the parts is saved where there is one (us with it, without: 32 x 512, 8 experts 10.0, 7.9); stores of 4 bytes
     // cost more than it from 49 experts on (20 x 1024, 33 experts 11.6, 8.6; 32 x 2048, 64 experts 11, 12.8; 32 x 5120, 160 experts 20.7, 30.2).
     const int direct = L.splits > 1 ? 0 : s->E % 4 == 0 && !misaligned({dwg}, 16) ? 2 : s->E <= DIRECT_ODD_EXPERTS ? 1 : 0;
     const RouteBackwardArgs a{(const char*)x, (const char*)wg, logits, idx, dw, dlogits, keep, (char*)dx, dwg, dbias, s->T, s->H, s->E, s->top_k,
-                              s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.tiles, L.splits, L.split_steps, own_dl, direct, wg_wide, w8 + L.zeros,
+                              s->renormalize, accumulate, s->routed_scale, L.nb, L.kb, L.steps, L.tiles, L.splits, L.split_steps, own_dl, narrow, direct, wg_wide, w8 + L.zeros,
                               (uint32_t*)(w8 + L.masks), w8 + L.dl_blocks, w8 + L.wg_blocks, (float*)(w8 + L.partial)};
     HIP_TRY(c, launch_route_backward(a, hs));
     return MOE_OK;

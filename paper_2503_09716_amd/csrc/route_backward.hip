@@ -8,8 +8,9 @@
 // hold its 24 bits, and three products give dWg what products in fp32 would; dx is rounded to bf16 (8 bits), and the two pieces it
 // takes hold dl to 2^-17.  (Products in fp32 run at a sixteenth of the rate.)
 //
-// Three launches: dl and the gate matrix in operand order; both products; the sum of dWg's parts.  us (of which products):
-// 256 tokens x 512, 8 experts 10 (4.7; two launches), 3001 x 2048, 64 experts 23 (16; two launches), 16384 x 6144, 8 experts 91 (82: 403 MB at 4.9
+// Three launches: dl and the gate matrix in operand order; both products; the sum of dWg's parts.  Short batches do without the first, up to
+// 128 tokens without the last.  us (of which products): 128 tokens x 4096, 8 experts 8.9 (one launch), 256 x 512, 8 experts 10.8 (4.7; two),
+// 256 x 5120, 160 experts 21 (two), 3001 x 2048, 64 experts 23 (16; two), 16384 x 6144, 8 experts 91 (82: 403 MB at 4.9
 // TB/s, a copy of x takes 74), 32768 x 5120, 64 experts 160 (140; 124), 160 experts 246 to 270 by box (225 at 2.2 GHz: matrix units 55 % busy
 // with 268 GFLOP of bf16 products).  What keeps them from more there is that both wavefronts of a SIMD wait at the same time, after the
 // step's barrier and for operands from LDS (30 % of their cycles).  Two workgroups of four wavefronts to a CU, other priorities, one of
@@ -302,12 +303,12 @@ __device__ __forceinline__ int xcd_place(const int id, const int n) {
 //        columns of a token, two blocks whose rows are interleaved by fours.
 // So x is read and dx written side by side, dl is read once for both.  Rows of x past the end and of tokens that do not count come from
 // a page of zeros: their dl is zero, but what x holds there may be no number.
-// More than 160 experts take half the columns, or the accumulators and the gate matrix would not fit the registers; so do short batches
-// of more than 32, for twice the workgroups to as many parts (us with 256, 128 columns: 64 experts 256 x 5120 15.9, 12.4, 1000 x 2048 17.0, 15.0,
-// 3001 x 2048 22.6, 21.7; 96 experts 1000 x 2048 21.0, 17.9).
-template <int NB, bool OWN>
+// More than 160 experts take half the columns, or the accumulators and the gate matrix would not fit the registers; so (NARROW) do short
+// batches of more than 32, for twice the workgroups to as many parts, as long as a part has up to 5 blocks of tokens (us with 256, 128
+// columns: 64 experts 256 x 5120 15.9, 12.4, 1000 x 2048 17.0, 15.0, 3001 x 2048, 6 blocks, padding 23.1, 23.9; 96 experts 1000 x 2048 21.0, 17.9).
+template <int NB, bool NARROW>
 struct Tile {
-    static constexpr int HT = NB <= (OWN ? 2 : 10) ? 256 : 128;
+    static constexpr int HT = NB <= 10 && !NARROW ? 256 : 128;
     static constexpr int KB = (NB + 1) / 2;            // blocks of 32 experts
     static constexpr int WE = NB <= 2 ? 1 : NB <= 10 ? 2 : 4;   // wavefronts along the experts
     static constexpr int WH = 8 / WE;                  // and along the columns
@@ -357,9 +358,9 @@ __device__ __forceinline__ void store_dx(char* p, const u32x4 v) {
 
 // OWN: the workgroup computes the dl of its tokens and lays out its part of the gate matrix by itself, so that the launch before is
 // saved; each of the tiles of H does it again.
-template <int NB, bool DX, bool OWN>
+template <int NB, bool DX, bool OWN, bool NARROW>
 __global__ __launch_bounds__(512) void route_backward_products_kernel(const RouteBackwardArgs a) {
-    typedef Tile<NB, OWN> L;
+    typedef Tile<NB, NARROW> L;
     extern __shared__ char lds_raw[];
     const lds_t lds = (lds_t)lds_raw;
     constexpr int PICK_ROW = 16 * NB + 1;
@@ -709,33 +710,36 @@ int route_backward_blocks(const int E) {
     return 16;
 }
 
-int route_backward_columns(const int nb, const bool own) {
+int route_backward_columns(const int nb, const bool narrow) {
     int columns = 0;
-    (void)for_blocks(nb, [&]<int NB>() { columns = own ? Tile<NB, true>::HT : Tile<NB, false>::HT; return hipSuccess; });
+    (void)for_blocks(nb, [&]<int NB>() { columns = narrow && NB > 2 ? Tile<NB, true>::HT : Tile<NB, false>::HT; return hipSuccess; });
     return columns;
 }
 
-template <int NB, bool OWN>
+template <int NB, bool OWN, bool NARROW>
 constexpr int products_lds() {
-    return OWN ? 2 * Tile<NB, OWN>::STAGE + 32 * (16 * NB + 1) * 4 : Tile<NB, OWN>::NS * Tile<NB, OWN>::STAGE;
+    typedef Tile<NB, NARROW> L;
+    return OWN ? 2 * L::STAGE + 32 * (16 * NB + 1) * 4 : L::NS * L::STAGE;
 }
 
 template <class F>
-hipError_t for_products(const int nb, const bool dx, const bool own, F&& f) {
+hipError_t for_products(const int nb, const bool dx, const bool own, const bool narrow, F&& f) {
     return for_blocks(nb, [&]<int NB>() {
-        if constexpr (NB <= ROUTE_BACKWARD_OWN_BLOCKS)
-            if (own) return dx ? f.template operator()<NB, true, true>() : f.template operator()<NB, false, true>();
-        return dx ? f.template operator()<NB, true, false>() : f.template operator()<NB, false, false>();
+        if constexpr (NB > 2 && NB <= ROUTE_BACKWARD_OWN_NARROW)
+            if (own && narrow) return dx ? f.template operator()<NB, true, true, true>() : f.template operator()<NB, false, true, true>();
+        if constexpr (NB <= ROUTE_BACKWARD_OWN_WIDE)
+            if (own) return dx ? f.template operator()<NB, true, true, false>() : f.template operator()<NB, false, true, false>();
+        return dx ? f.template operator()<NB, true, false, false>() : f.template operator()<NB, false, false, false>();
     });
 }
 
 hipError_t route_backward_init() {
     hipError_t e = hipSuccess;
     for (int nb : {1, 2, 4, 6, 8, 10, 12, 16})
-        for (int v = 0; v < 4 && e == hipSuccess; ++v)
-            e = for_products(nb, v & 1, v & 2, []<int NB, bool DX, bool OWN>() {
-                return hipFuncSetAttribute((const void*)route_backward_products_kernel<NB, DX, OWN>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                           products_lds<NB, OWN>());
+        for (int v = 0; v < 8 && e == hipSuccess; ++v)
+            e = for_products(nb, v & 1, v & 2, v & 4, []<int NB, bool DX, bool OWN, bool NARROW>() {
+                return hipFuncSetAttribute((const void*)route_backward_products_kernel<NB, DX, OWN, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           products_lds<NB, OWN, NARROW>());
             });
     return e;
 }
@@ -751,8 +755,9 @@ hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st) {
         });
         if (e != hipSuccess) return e;
     }
-    e = for_products(a.nb, a.dx != nullptr, a.own_dl, [&]<int NB, bool DX, bool OWN>() {
-        hipLaunchKernelGGL((route_backward_products_kernel<NB, DX, OWN>), dim3(a.tiles * a.splits), dim3(512), (products_lds<NB, OWN>()), st, a);
+    e = for_products(a.nb, a.dx != nullptr, a.own_dl, a.narrow, [&]<int NB, bool DX, bool OWN, bool NARROW>() {
+        hipLaunchKernelGGL((route_backward_products_kernel<NB, DX, OWN, NARROW>), dim3(a.tiles * a.splits), dim3(512), (products_lds<NB, OWN, NARROW>()),
+                           st, a);
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;

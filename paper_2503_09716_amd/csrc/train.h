@@ -42,6 +42,7 @@ struct RouteBackwardArgs {
     int32_t steps;             // blocks of 32 tokens
     int32_t tiles, splits, split_steps;   // tiles of H, parts of the tokens that dWg is summed over apart, blocks of 32 tokens to one
     int32_t own_dl;            // 1: no launch for dl, the products' workgroups compute their tokens'
+    int32_t narrow;            // 1: tiles of 128 columns (nb > 2, own_dl)
     int32_t direct;            // 1: the products write dWg and dbias themselves (one part), 2: dWg 16 bytes at a time
     int32_t wg_wide;           // 1: the gate matrix can be read 16 bytes at a time
     char* zeros;               // 1 KiB that the first launch clears
@@ -51,8 +52,10 @@ struct RouteBackwardArgs {
     float* partial;            // [splits][H + 1][16 nb]: row H the sum of dl
 };
 int route_backward_blocks(int E);   // nb
-constexpr int ROUTE_BACKWARD_OWN_BLOCKS = 10;   // nb up to which own_dl is taken (12: 1000 x 2048, 180 experts 27.7 -> 29.9 us; 16 does not fit the registers)
-int route_backward_columns(int nb, bool own);   // columns of x to a workgroup
+// nb up to which own_dl is taken, with narrow tiles (12: 1000 x 2048, 180 experts 27.7 -> 29.9 us; 16 does not fit the registers) and without (they
+// would not fit)
+constexpr int ROUTE_BACKWARD_OWN_NARROW = 10, ROUTE_BACKWARD_OWN_WIDE = 6;
+int route_backward_columns(int nb, bool narrow);   // columns of x to a workgroup
 hipError_t launch_route_backward(const RouteBackwardArgs& a, hipStream_t st);
 hipError_t launch_route_backward_empty(const moe_shape& s, float* dwg, float* dbias, hipStream_t st);
 hipError_t route_backward_init();
