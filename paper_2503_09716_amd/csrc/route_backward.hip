@@ -5,8 +5,9 @@
 // and without renormalisation p runs over all experts, so that every logit has a gradient.  Then
 //   dx = dl Wg^T,   dWg = x^T dl,   dbias = sum_t dl_t.
 // x and Wg are bf16, so a matrix instruction multiplies them exactly; dl is fp32 and goes in as a sum of bf16 pieces: hi + mid + lo
-// hold its 24 bits, and three products give dWg what products in fp32 would; dx is rounded to bf16 (8 bits), and the two pieces it
-// takes hold dl to 2^-17.  (Products in fp32 run at a sixteenth of the rate.)
+// hold its 24 bits, and three products give dWg and dx what products in fp32 would.  (Those run at a sixteenth of the rate.)  dx takes the
+// third piece, too, although it is rounded to bf16 afterwards: where the experts' terms cancel, what is left hangs on dl's last bits
+// (with hi + mid alone, 2^-17 of dl, 32768 x 5120, 160 experts took 260 us instead of 291).
 //
 // Three launches: dl and the gate matrix in operand order; both products; the sum of dWg's parts.  Short batches do without the first, up to
 // 128 tokens without the last.  us (of which products): 128 tokens x 4096, 8 experts 8.9 (one launch), 256 x 512, 8 experts 10.8 (4.7; two),
@@ -16,6 +17,8 @@
 // step's barrier and for operands from LDS (30 % of their cycles).  Two workgroups of four wavefronts to a CU, other priorities, one of
 // the two starting with the other product and three pieces of dl's operands in one wait: no gain; two tiles of their own for the
 // products, one after the other or in turn, 262 to 310.
+#include <utility>
+
 #include "common.h"
 #include "router_rows.h"
 #include "train.h"
@@ -46,21 +49,19 @@ __device__ __forceinline__ void load16_to_lds(const char* p, lds_t l) {
 // Columns of rows of bf16 in LDS as matrix operands.  ds_read_b64_tr_b16 takes four rows of 16 to a group of 16 lanes: lane i gives the
 // address of elements 4 (i % 4) .. + 3 of row i / 4 and gets column i.  Two of them make a lane's 8 steps.  Assembly with its own wait:
 // before the builtin the compiler waits for every direct load in flight.
-// Two operands: from p0 + A and q0 + A2, from p1 + B and q1 + B2.
-template <int A, int A2, int B, int B2>
-__device__ __forceinline__ void read_transposed(bf16x8& f0, bf16x8& f1, const lds_t p0, const lds_t q0, const lds_t p1, const lds_t q1) {
+// Two operands, from p0 and p1, the second half of each NEXT bytes behind its first.
+template <int NEXT>
+__device__ __forceinline__ void read_transposed(bf16x8 (&f)[2], const lds_t p0, const lds_t p1) {
 #if defined(__gfx950__)
     u32x2 a, b, c, d;
-    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%8\n\t"
-                 "ds_read_b64_tr_b16 %1, %5 offset:%9\n\t"
-                 "ds_read_b64_tr_b16 %2, %6 offset:%10\n\t"
-                 "ds_read_b64_tr_b16 %3, %7 offset:%11\n\t"
+    asm volatile("ds_read_b64_tr_b16 %0, %4\n\t"
+                 "ds_read_b64_tr_b16 %1, %4 offset:%6\n\t"
+                 "ds_read_b64_tr_b16 %2, %5\n\t"
+                 "ds_read_b64_tr_b16 %3, %5 offset:%6\n\t"
                  "s_waitcnt lgkmcnt(0)"
-                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
-                 : "v"((uint32_t)(uintptr_t)p0), "v"((uint32_t)(uintptr_t)q0), "v"((uint32_t)(uintptr_t)p1), "v"((uint32_t)(uintptr_t)q1), "n"(A), "n"(A2),
-                   "n"(B), "n"(B2) : "memory");
-    f0 = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
-    f1 = __builtin_bit_cast(bf16x8, u32x4{c[0], c[1], d[0], d[1]});
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d) : "v"((uint32_t)(uintptr_t)p0), "v"((uint32_t)(uintptr_t)p1), "n"(NEXT) : "memory");
+    f[0] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+    f[1] = __builtin_bit_cast(bf16x8, u32x4{c[0], c[1], d[0], d[1]});
 #endif
 }
 // Four operands, the second half of each NEXT bytes behind its first.
@@ -85,26 +86,23 @@ __device__ __forceinline__ void read_transposed(bf16x8 (&f)[4], const lds_t p0, 
     f[3] = __builtin_bit_cast(bf16x8, u32x4{h[0], h[1], i[0], i[1]});
 #endif
 }
-// Four operands, from p + A and q + A to p + D and q + D.
-template <int A, int B, int C, int D>
-__device__ __forceinline__ void read_transposed(bf16x8 (&f)[4], const lds_t p, const lds_t q) {
+// Three operands, from p + A and q + A to p + C and q + C.
+template <int A, int B, int C>
+__device__ __forceinline__ void read_transposed(bf16x8 (&f)[3], const lds_t p, const lds_t q) {
 #if defined(__gfx950__)
-    u32x2 a, b, c, d, e, g, h, i;
-    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%10\n\t"
-                 "ds_read_b64_tr_b16 %1, %9 offset:%10\n\t"
-                 "ds_read_b64_tr_b16 %2, %8 offset:%11\n\t"
-                 "ds_read_b64_tr_b16 %3, %9 offset:%11\n\t"
-                 "ds_read_b64_tr_b16 %4, %8 offset:%12\n\t"
-                 "ds_read_b64_tr_b16 %5, %9 offset:%12\n\t"
-                 "ds_read_b64_tr_b16 %6, %8 offset:%13\n\t"
-                 "ds_read_b64_tr_b16 %7, %9 offset:%13\n\t"
+    u32x2 a, b, c, d, e, g;
+    asm volatile("ds_read_b64_tr_b16 %0, %6 offset:%8\n\t"
+                 "ds_read_b64_tr_b16 %1, %7 offset:%8\n\t"
+                 "ds_read_b64_tr_b16 %2, %6 offset:%9\n\t"
+                 "ds_read_b64_tr_b16 %3, %7 offset:%9\n\t"
+                 "ds_read_b64_tr_b16 %4, %6 offset:%10\n\t"
+                 "ds_read_b64_tr_b16 %5, %7 offset:%10\n\t"
                  "s_waitcnt lgkmcnt(0)"
-                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d), "=&v"(e), "=&v"(g), "=&v"(h), "=&v"(i)
-                 : "v"((uint32_t)(uintptr_t)p), "v"((uint32_t)(uintptr_t)q), "n"(A), "n"(B), "n"(C), "n"(D) : "memory");
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d), "=&v"(e), "=&v"(g)
+                 : "v"((uint32_t)(uintptr_t)p), "v"((uint32_t)(uintptr_t)q), "n"(A), "n"(B), "n"(C) : "memory");
     f[0] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
     f[1] = __builtin_bit_cast(bf16x8, u32x4{c[0], c[1], d[0], d[1]});
     f[2] = __builtin_bit_cast(bf16x8, u32x4{e[0], e[1], g[0], g[1]});
-    f[3] = __builtin_bit_cast(bf16x8, u32x4{h[0], h[1], i[0], i[1]});
 #endif
 }
 
@@ -543,7 +541,7 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
                     const int f = swizzle(r);   // that of row r + 4, too
                     const int c = wh * L::HB;
                     auto at = [&](const int hb) { return p + (((c + hb) ^ f) << 5); };
-                    if constexpr (L::HB == 2) read_transposed<0, 4 * L::ROW, 0, 4 * L::ROW>(xf[0], xf[1], at(0), at(0), at(1), at(1));
+                    if constexpr (L::HB == 2) read_transposed<4 * L::ROW>(xf, at(0), at(1));
                     else read_transposed<4 * L::ROW>(xf, at(0), at(1), at(2), at(3));
                 }
 #pragma unroll
@@ -560,27 +558,15 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
             if (DX) {
                 f32x4 out[L::DB] = {};
                 const lds_t p = ds + dl_first, q4 = ds + dl_next;
-                auto two = [&]<int K>() {   // blocks K and K + 1 of 32 experts, mid and hi
-                    bf16x8 d[4];
-                    read_transposed<NB * 1024 + K * 2048, K * 2048, NB * 1024 + (K + 1) * 2048, (K + 1) * 2048>(d, p, q4);
+                auto block = [&]<int K>() {   // of 32 experts: lo, mid, hi
+                    bf16x8 d[3];
+                    read_transposed<2 * NB * 1024 + K * 2048, NB * 1024 + K * 2048, K * 2048>(d, p, q4);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-#pragma unroll
-                        for (int b = 0; b < L::DB; ++b) out[b] = mfma(wg[b][K + q / 2], d[q], out[b]);
-                };
-                auto one = [&]<int K>() {
-                    bf16x8 d[2];
-                    read_transposed<NB * 1024 + K * 2048, NB * 1024 + K * 2048, K * 2048, K * 2048>(d[0], d[1], p, q4, p, q4);
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
+                    for (int q = 0; q < 3; ++q)
 #pragma unroll
                         for (int b = 0; b < L::DB; ++b) out[b] = mfma(wg[b][K], d[q], out[b]);
                 };
-                if constexpr (L::KB >= 2) two.template operator()<0>();
-                if constexpr (L::KB >= 4) two.template operator()<2>();
-                if constexpr (L::KB >= 6) two.template operator()<4>();
-                if constexpr (L::KB >= 8) two.template operator()<6>();
-                if constexpr (L::KB % 2) one.template operator()<L::KB - 1>();
+                [&]<int... K>(std::integer_sequence<int, K...>) { (block.template operator()<K>(), ...); }(std::make_integer_sequence<int, L::KB>{});
                 u32x4 o[L::DB / 2];   // 8 columns of token lane % 16 in each group of 32
 #pragma unroll
                 for (int g = 0; g < L::DB / 2; ++g) {

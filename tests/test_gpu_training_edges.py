@@ -1,0 +1,35 @@
+"""Edges of the calls that train a router: what shows fewer bits than fp32, values at the ends of their types, ids that name no expert,
+and the variants that only large inputs take.  Bounds as in test_gpu_training.py."""
+import pytest
+import torch
+
+from test_gpu_training import BF16, U, moe, normal, generator, run_route_backward, say, within  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- gradient of the router ---------------------------------------------------------------------
+@pytest.mark.parametrize("T,H,E", [(33, 128, 8), (70, 192, 30), (100, 320, 64), (64, 576, 90), (90, 256, 128), (64, 128, 160), (45, 64, 192), (64, 192, 250),
+                                   (5300, 4096, 8), (5301, 4160, 27), (5300, 4096, 64), (5303, 4096, 90), (5300, 4096, 128), (5300, 4096, 160)])
+def test_dx_of_gradients_that_cancel_but_for_their_last_bits(moe, T, H, E):
+    """Two experts whose columns of the gate matrix are equal get dl and -dl rounded to 16 bits: dx is the rest, 2^-17 of dl at most, times
+    the column.  Six products and as many additions, each off by 2 U of the larger terms at most."""
+    say("cancelling", T, H, E)
+    gen = generator(T + E)
+    dl = normal(gen, (T,))
+    first = torch.randint(E, (T,), device="cuda", generator=gen)
+    second = (first + 1 + torch.randint(E - 1, (T,), device="cuda", generator=gen)) % E
+    hi = dl.bfloat16().float()
+    most = hi + (dl - hi).bfloat16().float()
+    d = torch.zeros((T, E), device="cuda")
+    d[torch.arange(T), first] = dl
+    d[torch.arange(T), second] = -most
+    column = normal(gen, (H,), torch.bfloat16)
+    s = {"x": normal(gen, (T, H), torch.bfloat16), "wg": column[:, None].expand(H, E).contiguous(), "logits": normal(gen, (T, E)),
+         "idx": torch.zeros((T, 1), dtype=torch.int32, device="cuda"), "dw": torch.zeros((T, 1), device="cuda"), "dlogits": d, "keep": None}
+    dx, _, _ = run_route_backward(moe, s, False)
+    rest = dl.double() - most.double()
+    assert (rest != 0).sum() > T // 4
+    size = dl.double().abs()[:, None] * column.double().abs()
+    want = rest[:, None] * column.double()
+    within("dx", dx, want, size * 12 * U + want.abs() * BF16 + 1e-38)
