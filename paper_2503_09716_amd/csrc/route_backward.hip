@@ -363,6 +363,7 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
     const lds_t lds = (lds_t)lds_raw;
     constexpr int PICK_ROW = 16 * NB + 1;
     float* const scratch = reinterpret_cast<float*>(lds_raw + 2 * L::STAGE);   // OWN: a row for each of the 32 tokens' picks
+    const lds_t counted = lds + 2 * L::STAGE + 32 * PICK_ROW * 4;   // OWN: [2 stages][8]: a bit for each of a wavefront's four tokens that counts
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int id = xcd_place(blockIdx.x, a.tiles * a.splits);
     const int ht = id % a.tiles, split = id / a.tiles;
@@ -492,11 +493,16 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
         int stage = 0;
         uint32_t mask = OWN ? 0u : masks[min(s0 + L::NS - 1, s1 - 1)];
         for (int s = s0; s < s1; ++s) {
+            const uint32_t count = OWN ? 0u : masks[s];   // the step's tokens that count
             if constexpr (OWN) {
                 float g[NB];
                 const uint32_t picked = rows.template picks<false>(a, lane & 15, g, scratch + (wave * 4 + (lane >> 4)) * PICK_ROW);
                 rows.template gradient<false>(a, lane & 15, g, picked);
                 put_dl<NB>(rows.v, lds + stage * L::STAGE + 32 * L::ROW, wave * 4 + (lane >> 4), lane & 15);
+                if (DX && a.keep) {
+                    const uint64_t on = __ballot(rows.on(a));
+                    counted[stage * 8 + wave] = (char)((on & 1) | (on >> 15 & 2) | (on >> 30 & 4) | (on >> 45 & 8));
+                }
                 ring_wait<0>();
                 ring_meet();
                 if (s + 1 < s1) {
@@ -574,6 +580,14 @@ __global__ __launch_bounds__(512) void route_backward_products_kernel(const Rout
 #pragma unroll
                     for (int r = 0; r < 4; ++r) { v[r] = (__bf16)out[2 * g][r]; v[4 + r] = (__bf16)out[2 * g + 1][r]; }
                     o[g] = __builtin_bit_cast(u32x4, v);
+                }
+                // A token that does not count has zeros for dl, but what the gate matrix holds may be no number.
+                if (OWN ? a.keep != nullptr : count != ~0u) {
+                    typedef __attribute__((address_space(3))) const uint32_t* word_ptr_t;
+                    const uint32_t four = OWN ? __builtin_amdgcn_readfirstlane(*(word_ptr_t)(counted + stage * 8 + th * 4)) : 0u;
+                    const bool on = (OWN ? four >> (2 * (lane & 12) + (lane & 3)) : count >> (th * 16 + (lane & 15))) & 1;
+#pragma unroll
+                    for (int g = 0; g < L::DB / 2; ++g) o[g] = on ? o[g] : u32x4{0u, 0u, 0u, 0u};
                 }
                 const int t0 = s * 32 + th * 16;
                 if constexpr (L::DB == 4) {
@@ -705,7 +719,7 @@ int route_backward_columns(const int nb, const bool narrow) {
 template <int NB, bool OWN, bool NARROW>
 constexpr int products_lds() {
     typedef Tile<NB, NARROW> L;
-    return OWN ? 2 * L::STAGE + 32 * (16 * NB + 1) * 4 : L::NS * L::STAGE;
+    return OWN ? 2 * L::STAGE + 32 * (16 * NB + 1) * 4 + 16 : L::NS * L::STAGE;
 }
 
 template <class F>

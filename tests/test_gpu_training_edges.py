@@ -3,7 +3,7 @@ and the variants that only large inputs take.  Bounds as in test_gpu_training.py
 import pytest
 import torch
 
-from test_gpu_training import BF16, U, moe, normal, generator, run_route_backward, say, within  # noqa: F401
+from test_gpu_training import BF16, U, generator, moe, normal, route_inputs, run_route_backward, say, within  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +33,26 @@ def test_dx_of_gradients_that_cancel_but_for_their_last_bits(moe, T, H, E):
     size = dl.double().abs()[:, None] * column.double().abs()
     want = rest[:, None] * column.double()
     within("dx", dx, want, size * 12 * U + want.abs() * BF16 + 1e-38)
+
+
+# tiles that compute dl by themselves, then those that do not, in every width
+PADDED = [(70, 128, 8), (333, 320, 27), (700, 320, 64), (300, 576, 90), (200, 192, 128), (300, 192, 160), (120, 128, 192), (200, 192, 250),
+          (5300, 4096, 8), (5301, 4160, 27), (2100, 4096, 64), (5303, 4096, 90), (2100, 4096, 128), (2100, 4160, 160)]
+
+
+@pytest.mark.parametrize("T,H,E", PADDED)
+def test_dx_of_padding_tokens_where_the_gate_matrix_is_not_finite(moe, T, H, E):
+    """Rows of padding tokens are zero whatever the gate matrix holds; elsewhere its columns keep to themselves."""
+    say("gate not finite", T, H, E)
+    s = route_inputs(T, H, E, 3, T + E, padding=0.3)
+    clean = run_route_backward(moe, s, True)
+    bad = torch.zeros(H, dtype=torch.bool, device="cuda")
+    s["wg"][::7, 1] = float("inf")
+    s["wg"][1::9, E - 1] = float("nan")
+    bad[::7] = True
+    bad[1::9] = True
+    dx, dwg, db = run_route_backward(moe, s, True)
+    off = ~s["keep"]
+    assert (dx[off] == 0).all()
+    assert torch.equal(dx[:, ~bad], clean[0][:, ~bad]) and not torch.isfinite(dx[s["keep"]][:, bad].float()).any()
+    assert torch.equal(dwg, clean[1]) and torch.equal(db, clean[2])
