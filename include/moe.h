@@ -354,7 +354,8 @@ moe_status moe_balance_loss(moe_ctx* ctx, const moe_shape* shape, const float* l
                             void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Gradient of moe_route.  With g the gradient of the weights (dtopk_w at a token's picks, 0 elsewhere) and p the softmax that they
- * are taken from (over all experts; with renormalize over the token's picks):
+ * are taken from (over all experts; with renormalize over the token's picks; ids outside [0,E) are no picks, and a token without any has
+ * dl = dlogits):
  *   dl = routed_scale * p * (g - sum_e p g) + dlogits,   dx = dl Wg^T,   dwg = x^T dl,   dbias = sum_t dl[t]
  * dl and the sums of dwg and dbias as fp32 has them; dx is rounded to bf16 once.  A gradient that is not finite comes out as not finite.
  *   x_bf16 [T,H], wg_bf16 [H,E] (logical layout whatever "gate_packed" says), logits [T,E] fp32 (with the bias, as moe_route gives them),

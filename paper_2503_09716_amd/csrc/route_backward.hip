@@ -192,9 +192,12 @@ struct TokenRow {
     // v becomes dl, zero where the token does not count and past the experts
     template <bool WIDE>
     __device__ __forceinline__ void gradient(const RouteBackwardArgs& a, const int row, const float (&g)[NV], const uint32_t picked) {
-        if (a.renorm)
+        if (a.renorm) {
+            // A row none of whose ids names an expert has no weights: any softmax will do, its gradients g are zero.
+            const float others = row16_max(picked) ? -INFINITY : 0.f;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = picked >> i & 1 ? v[i] : -INFINITY;
+            for (int i = 0; i < NV; ++i) v[i] = picked >> i & 1 ? v[i] : others;
+        }
         float z, s = 0.f;
         exps_row16<NV>(v, z);
         const float rz = 1.0f / z;

@@ -3,7 +3,7 @@ and the variants that only large inputs take.  Bounds as in test_gpu_training.py
 import pytest
 import torch
 
-from test_gpu_training import BF16, U, generator, moe, normal, route_inputs, run_route_backward, say, within  # noqa: F401
+from test_gpu_training import BF16, U, check_route, generator, moe, normal, route_inputs, run_route_backward, say, within  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +56,28 @@ def test_dx_of_padding_tokens_where_the_gate_matrix_is_not_finite(moe, T, H, E):
     assert (dx[off] == 0).all()
     assert torch.equal(dx[:, ~bad], clean[0][:, ~bad]) and not torch.isfinite(dx[s["keep"]][:, bad].float()).any()
     assert torch.equal(dwg, clean[1]) and torch.equal(db, clean[2])
+
+
+@pytest.mark.parametrize("T,H,E,k", [(50, 128, 8, 2), (400, 192, 40, 6), (300, 128, 130, 20), (90, 64, 200, 5), (5300, 4096, 8, 2)])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("dlogits", [True, False])
+def test_route_backward_ids_out_of_range(moe, T, H, E, k, renorm, dlogits):
+    """Ids that name no expert have no weight: the softmax over the picks is that over the others, and a row without any has the gradient
+    dlogits alone."""
+    say("ids out of range", T, H, E, k, renorm, dlogits)
+    s = route_inputs(T, H, E, k, T + E, dlogits=dlogits)
+    ref = {n: v if v is None else v.clone() for n, v in s.items()}
+    gen = generator(T)
+    some, none = torch.arange(T, device="cuda") % 3 == 0, torch.arange(T, device="cuda") % 5 == 0
+    out = torch.tensor([-1, E, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda")
+    wrong = out[torch.randint(4, (T, k), device="cuda", generator=gen)]
+    lost = torch.rand((T, k), device="cuda", generator=gen) < 0.4
+    lost &= some[:, None]
+    lost[:, 0] = False
+    lost |= none[:, None]
+    s["idx"] = torch.where(lost, wrong, s["idx"])
+    # the same picks in ids that exist: the row's first in place of a lost one, and weights without a gradient where all are lost
+    ref["idx"] = torch.where(lost, ref["idx"][:, :1], ref["idx"])
+    ref["dw"] = torch.where(lost, ref["dw"][:, :1], ref["dw"])
+    ref["dw"][none] = 0
+    check_route(ref, renorm, 1.5, *run_route_backward(moe, s, renorm, 1.5))
