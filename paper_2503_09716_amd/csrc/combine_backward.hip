@@ -1,8 +1,9 @@
 // Backward pass of the weighted combine: out_t = sum_j w_tj y_row(t,j) (+ y_shared_t) gives
 //   dw_tj = <y_row(t,j), dout_t>,   dy_row(t,j) = w_tj dout_t   (and dout_t itself for the shared experts).
 // HBM-bound: every row of y is read and, with dy_perm, written once.  W wavefronts take a pair's row; those of a token's pairs are one
-// workgroup, so that dout's row comes from memory once.  A row's product is added up in fp32 along each lane and then across
-// the lanes, once to a row: a thread that took a piece of all of a token's rows would end on a sum across lanes for every 8 elements of each.
+// workgroup, so that dout's row comes from memory once.  A row's product is added up in fp32 along each lane, in as many sums as a load has
+// elements (memory bounds the kernel either way, and a single sum of H / 64 terms was off by up to that many times more), and then across the
+// lanes, once to a row: a thread that took a piece of all of a token's rows would end on a sum across lanes for every 8 elements of each.
 // us: 3001 tokens x 2048, k = 6, fp32, weights alone 28.3 (172 MB at 6.1 TB/s), 4096 x 4096, k = 2, fp32 54.6 (302 MB at 5.5), 32768 x 5120,
 // k = 6, bf16 795 to 868 by box (4.4 GB at 5.5 to 5.0; a 1 GiB copy 5.1).
 #include "common.h"
@@ -44,6 +45,7 @@ __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __re
         const int j = j0 + r;
         float sum = 0.f;
         if (j < k) {
+            float sums[N] = {};
             const size_t p = (size_t)t * k + j, at = (size_t)inv_perm[p] * H * (YF32 ? 4 : 2);
             const float wj = DY ? w[p] : 0.f;
             for (int c0 = sub * 64 + lane; c0 < n; c0 += AHEAD * W * 64) {
@@ -60,7 +62,7 @@ __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __re
                     const int c = c0 + u * W * 64;
                     if (c >= n) break;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) sum = fmaf(y[u][i], g[u][i], sum);
+                    for (int i = 0; i < N; ++i) sums[i] = fmaf(y[u][i], g[u][i], sums[i]);
                     if (DY) {
                         if (YF32) {
                             f32x4 o;
@@ -77,7 +79,11 @@ __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __re
                     }
                 }
             }
-            sum = row16_sum(sum);
+#pragma unroll
+            for (int m = N / 2; m > 0; m /= 2)
+#pragma unroll
+                for (int i = 0; i < m; ++i) sums[i] += sums[i + m];
+            sum = row16_sum(sums[0]);
             sum += pair_f<16>(sum);
             sum += pair_f<32>(sum);
             if (W == 1 && lane == 0) dw[p] = sum;

@@ -3,7 +3,8 @@ and the variants that only large inputs take.  Bounds as in test_gpu_training.py
 import pytest
 import torch
 
-from test_gpu_training import BF16, U, check_route, generator, moe, normal, route_inputs, run_route_backward, say, within  # noqa: F401
+from test_gpu_training import (BF16, U, check_route, generator, moe, normal, route_inputs, run_combine_backward,  # noqa: F401
+                               run_route_backward, say, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +82,23 @@ def test_route_backward_ids_out_of_range(moe, T, H, E, k, renorm, dlogits):
     ref["dw"] = torch.where(lost, ref["dw"][:, :1], ref["dw"])
     ref["dw"][none] = 0
     check_route(ref, renorm, 1.5, *run_route_backward(moe, s, renorm, 1.5))
+
+
+# ---- gradient of the combine --------------------------------------------------------------------
+@pytest.mark.parametrize("y32", [True, False])
+@pytest.mark.parametrize("d32", [True, False])
+@pytest.mark.parametrize("dy", [True, False])
+def test_combine_backward_small_terms_behind_large_ones(moe, y32, d32, dy):
+    """Terms of 1 in the first elements of a row and small ones behind them, which a single sum along a lane loses one by one.  As many sums
+    to a lane as it has elements to a load, N: (H / 64 / N + 24) U of the sum of the terms."""
+    T, H, k = 700, 16384, 3
+    say("small terms", y32, d32, dy)
+    N = 4 if y32 or d32 else 8
+    f = {True: torch.float32, False: torch.bfloat16}
+    dout = torch.full((T, H), (2 if N == 4 else 6) * U, dtype=f[d32], device="cuda")
+    dout[:, :64 * N] = 1
+    y = torch.ones((T * k, H), dtype=f[y32], device="cuda")
+    inv = torch.randperm(T * k, device="cuda", generator=generator(1)).int()
+    dw, _ = run_combine_backward(moe, dout, y, inv, torch.ones((T, k), device="cuda"), dy=dy)
+    want = dout.double().sum(1, keepdim=True).expand(T, k)
+    within("dtopk_w", dw, want, want * (H / 64 / N + 24) * U)
