@@ -395,8 +395,9 @@ moe_status moe_gradient_list_make(moe_ctx* ctx, int32_t tensors, const void* con
                                   const int32_t* is_fp32, void* buffer, size_t buffer_bytes, moe_gradient_list* list, void* hip_stream);
 
 /* norm[0] = sqrt of the sum of all squares of the list's gradients (fp32 device out, formed in 64 bits);
- * out = grad * (norm > max_norm ? max_norm / norm : 1), rounded to the tensor's type.  max_norm >= 0 (infinity: the norm alone, and copies).
- * A norm that is NaN scales nothing, one that is infinite gives factor 0. */
+ * out = grad * (norm > max_norm ? max_norm / norm : 1), rounded to the tensor's type; norm and factor in 64 bits, also where norm[0] passes the
+ * range of fp32 and is infinite.  max_norm >= 0 (infinity: the norm alone, and copies).  Infinities among the gradients give factor 0, NaN
+ * scales nothing. */
 moe_status moe_clip_gradients(moe_ctx* ctx, const moe_gradient_list* list, double max_norm, float* norm, void* hip_stream);
 
 /* Profiling.  While enabled, every kernel group a call enqueues is bracketed by HIP events on

@@ -61,22 +61,30 @@ __device__ __forceinline__ double chunk_squares(const ClipChunk& c, const int me
     return s;
 }
 
+// min(1, max_norm / norm) as a product: where the norm passes the range of fp32 the factor can fall below it, though no gradient's product
+// with it does.  `rest` is 1, or 2^-126 where the factor would not be a normal number.
+struct Factor {
+    float first, rest;
+    __device__ __forceinline__ float operator()(const float g) const { return g * first * rest; }
+    __device__ __forceinline__ bool one() const { return first == 1.0f && rest == 1.0f; }
+};
+
 template <bool F32>
-__device__ __forceinline__ u32x4 scaled(const u32x4 v, const float scale) {
+__device__ __forceinline__ u32x4 scaled(const u32x4 v, const Factor scale) {
     if (F32) {
         u32x4 o;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(element(v, true, i) * scale);
+        for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(scale(element(v, true, i)));
         return o;
     }
     bf16x8 o;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = (__bf16)(element(v, false, i) * scale);
+    for (int i = 0; i < 8; ++i) o[i] = (__bf16)scale(element(v, false, i));
     return __builtin_bit_cast(u32x4, o);
 }
 
 template <bool F32, bool STREAM, int N>
-__device__ __forceinline__ void scale_chunk(const ClipChunk& c, const float scale) {
+__device__ __forceinline__ void scale_chunk(const ClipChunk& c, const Factor scale) {
     constexpr int PER = F32 ? 4 : 8, AHEAD = CLIP_CHUNK / 16 / N < 8 ? CLIP_CHUNK / 16 / N : 8;
     const int pieces = c.elements / PER;
     const GLOBAL u32x4_any* const p = (const GLOBAL u32x4_any*)c.src;
@@ -94,8 +102,8 @@ __device__ __forceinline__ void scale_chunk(const ClipChunk& c, const float scal
     const int rest = c.elements - pieces * PER;
     if ((int)threadIdx.x < rest) {
         const int i = pieces * PER + threadIdx.x;
-        if (F32) ((GLOBAL float*)c.dst)[i] = ((const GLOBAL float*)c.src)[i] * scale;
-        else ((GLOBAL __bf16*)c.dst)[i] = (__bf16)(bf16_bits_to_float(((const GLOBAL uint16_t*)c.src)[i]) * scale);
+        if (F32) ((GLOBAL float*)c.dst)[i] = scale(((const GLOBAL float*)c.src)[i]);
+        else ((GLOBAL __bf16*)c.dst)[i] = (__bf16)scale(bf16_bits_to_float(((const GLOBAL uint16_t*)c.src)[i]));
     }
 }
 
@@ -113,8 +121,10 @@ __device__ __forceinline__ double block_sum(double v) {
     return s;
 }
 
-__device__ __forceinline__ float factor(const ClipArgs& a, const double norm) {
-    return norm > a.max_norm ? (float)(a.max_norm / norm) : 1.0f;   // a norm that is no number scales nothing
+__device__ __forceinline__ Factor factor(const ClipArgs& a, const double norm) {
+    const double f = norm > a.max_norm ? a.max_norm / norm : 1.0;   // a norm that is no number scales nothing
+    const bool small = f < 0x1p-126;
+    return Factor{(float)(small ? f * 0x1p126 : f), small ? 0x1p-126f : 1.0f};
 }
 
 __global__ __launch_bounds__(THREADS) void clip_norm_kernel(const ClipArgs a) {
@@ -133,10 +143,10 @@ __global__ __launch_bounds__(THREADS) void clip_scale_kernel(const ClipArgs a, c
     for (int i = threadIdx.x; i < parts; i += THREADS) s += a.partial[i];
     const double norm = sqrt(block_sum<THREADS>(s));
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
-    const float scale = factor(a, norm);
+    const Factor scale = factor(a, norm);
     for (int i = a.n_chunks - 1 - (int)blockIdx.x; i >= 0; i -= gridDim.x) {
         const ClipChunk c = a.chunks[i];
-        if (scale == 1.0f && c.src == c.dst) continue;
+        if (scale.one() && c.src == c.dst) continue;
         if (i < a.n_chunks - KEPT_CHUNKS) {
             if (c.fp32) scale_chunk<true, true, THREADS>(c, scale);
             else scale_chunk<false, true, THREADS>(c, scale);
@@ -161,7 +171,7 @@ __global__ __launch_bounds__(FEW_THREADS) void clip_few_kernel(const ClipArgs a)
     }
     const double norm = sqrt(block_sum<FEW_THREADS>(s));
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
-    const float scale = factor(a, norm);
+    const Factor scale = factor(a, norm);
     if (mine.fp32) scale_chunk<true, false, FEW_THREADS>(mine, scale);
     else scale_chunk<false, false, FEW_THREADS>(mine, scale);
 }

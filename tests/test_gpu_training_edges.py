@@ -102,3 +102,25 @@ def test_combine_backward_small_terms_behind_large_ones(moe, y32, d32, dy):
     dw, _ = run_combine_backward(moe, dout, y, inv, torch.ones((T, k), device="cuda"), dy=dy)
     want = dout.double().sum(1, keepdim=True).expand(T, k)
     within("dtopk_w", dw, want, want * (H / 64 / N + 24) * U)
+
+
+# ---- clipping -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [4096, 200001])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_clip_gradients_by_factors_below_the_range_of_fp32(moe, dtype, n, in_place):
+    """The norm passes the range of fp32 and max_norm / norm falls below it; the gradients scaled by it do not."""
+    say("small factors", dtype, n, in_place)
+    norm = torch.zeros(1, device="cuda")
+    for size, limit in ((3e38, 1.0), (3e38, 1e-6), (1e37, 1e-12), (1e30, 1e-25), (3e38, 1e-33)):
+        g = torch.full((n,), size, dtype=dtype, device="cuda")
+        g[1::2] = -g[1::2]
+        g[5::16] = 1e-3
+        before = g.double()
+        out = g if in_place else torch.empty_like(g)
+        moe.clip_gradients(moe.gradient_list([g], [out]), limit, norm)
+        want = before.norm().item()
+        assert norm.item() == float("inf") if want > 3.5e38 else abs(norm.item() - want) <= 2 * U * want
+        want = before * (limit / want)
+        # products below 2^-126 are held to a step of 2^-149 (fp32) or 2^-133 (bf16), or are zero
+        within("out", out, want, want.abs() * (3 * U if dtype == torch.float32 else BF16 + 3 * U) + 2.0 ** -126)
