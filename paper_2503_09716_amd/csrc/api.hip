@@ -41,6 +41,7 @@ struct moe_ctx {
     bool y_fp32 = true;    // dtype of y_perm / y_shared in the staged calls
     int layer_y = -1;      // moe_layer's y_perm: 1 fp32, 0 bf16, -1 choose (its y_shared is always fp32)
     bool out_fp32 = false; // dtype of the layer output
+    hipError_t route_backward_ready = hipSuccess;   // what setting up moe_route_backward's kernels gave
     bool gate_packed = false;  // E > 16: the wg argument is already in the packed layout (moe_pack_gate)
     char* static_ws = nullptr;  // this device's address of `scratch`
     // Ring of device pointer tables [3][MAX_GROUPS] (W1p, W3p, W2p), each with a pinned host
@@ -952,7 +953,9 @@ moe_status moe_create(moe_ctx** out, int device) {
     moe_ctx* c = new moe_ctx();
     c->device = device;
     c->tab_shadow.assign(3 * MAX_GROUPS, nullptr);
-    bool ok = ffn_gemm_init() == hipSuccess && route_backward_init() == hipSuccess;
+    bool ok = ffn_gemm_init() == hipSuccess;
+    c->route_backward_ready = route_backward_init();
+    if (c->route_backward_ready != hipSuccess) (void)hipGetLastError();   // theirs alone: the other calls do not need these kernels
     ok = ok && hipGetSymbolAddress((void**)&c->static_ws, HIP_SYMBOL(scratch)) == hipSuccess && c->static_ws != nullptr &&
          ((uintptr_t)c->static_ws & 255) == 0;
     ok = ok && hipStreamCreateWithFlags(&c->copy_stream, hipStreamNonBlocking) == hipSuccess &&
@@ -1362,6 +1365,7 @@ moe_status moe_route_backward(moe_ctx* c, const moe_shape* s, const void* x, con
         return MOE_OK;
     }
     if (moe_status st = check_backward_ws(c, s, ws, ws_bytes)) return st;
+    HIP_TRY(c, c->route_backward_ready);
     RouteBackwardLayout L = route_backward_layout(*s, true);
     char* const w8 = (char*)ws;
     // A launch for dl is saved where each workgroup computes it for few blocks of tokens, and can load its part of the gate matrix 16 bytes

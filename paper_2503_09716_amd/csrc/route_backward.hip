@@ -738,12 +738,19 @@ hipError_t for_products(const int nb, const bool dx, const bool own, const bool 
 
 hipError_t route_backward_init() {
     hipError_t e = hipSuccess;
-    for (int nb : {1, 2, 4, 6, 8, 10, 12, 16})
-        for (int v = 0; v < 8 && e == hipSuccess; ++v)
-            e = for_products(nb, v & 1, v & 2, v & 4, []<int NB, bool DX, bool OWN, bool NARROW>() {
-                return hipFuncSetAttribute((const void*)route_backward_products_kernel<NB, DX, OWN, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                           products_lds<NB, OWN, NARROW>());
-            });
+    auto set = [&](const int nb, const bool own, const bool narrow) {
+        for (const bool dx : {false, true})
+            if (e == hipSuccess)
+                e = for_products(nb, dx, own, narrow, []<int NB, bool DX, bool OWN, bool NARROW>() {
+                    return hipFuncSetAttribute((const void*)route_backward_products_kernel<NB, DX, OWN, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                               products_lds<NB, OWN, NARROW>());
+                });
+    };
+    for (int nb : {1, 2, 4, 6, 8, 10, 12, 16}) {
+        set(nb, false, false);
+        if (nb <= ROUTE_BACKWARD_OWN_WIDE) set(nb, true, false);
+        if (nb > 2 && nb <= ROUTE_BACKWARD_OWN_NARROW) set(nb, true, true);
+    }
     return e;
 }
 
