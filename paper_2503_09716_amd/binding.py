@@ -7,6 +7,7 @@ library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import List, Optional, Sequence
 
@@ -160,13 +161,18 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _typed(t: Optional[torch.Tensor], dtype, numel: int):
-    """_ptr of a tensor that the call reads or writes as `numel` elements of `dtype`."""
+def _typed(t: Optional[torch.Tensor], dtype, shape, device: int):
+    """_ptr of a tensor that the call reads or writes as `shape` of `dtype` on its device.  Flat tensors and other leading dimensions will do,
+    rows of another length will not."""
     if t is None:
         return None
-    if t.dtype is dtype and t.numel() == numel and t.is_cuda and t.is_contiguous():
+    if t.dtype is dtype and (t.shape == shape or _same_rows(t, shape)) and t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
-    raise AssertionError("device-resident contiguous tensor of %d elements of %s required" % (numel, dtype))
+    raise AssertionError("contiguous tensor of %s, %s, on cuda:%d required" % (list(shape), dtype, device))
+
+
+def _same_rows(t, shape) -> bool:
+    return t.numel() == math.prod(shape) and (len(shape) == 1 or t.dim() < 2 or t.shape[-1] == shape[-1])
 
 
 def _raw_stream(device: int):
@@ -277,29 +283,29 @@ class Moe:
 
     def balance_loss(self, shape, logits, topk_idx, keep, balance_coef, z_coef, counts, loss, dlogits, workspace):
         """keep: bool [T] or None; dlogits: fp32 [T, E] or None."""
-        T, E = shape.T, shape.E
-        self._check(self.lib.moe_balance_loss(self.h, C.byref(shape), _typed(logits, torch.float32, T * E),
-                                              _typed(topk_idx, torch.int32, T * shape.top_k), _typed(keep, torch.bool, T),
-                                              balance_coef, z_coef, _typed(counts, torch.int32, E), _typed(loss, torch.float32, 2),
-                                              _typed(dlogits, torch.float32, T * E), _ptr(workspace), workspace.numel(), _raw_stream(self.device)))
+        T, E, d = shape.T, shape.E, self.device
+        self._check(self.lib.moe_balance_loss(self.h, C.byref(shape), _typed(logits, torch.float32, (T, E), d),
+                                              _typed(topk_idx, torch.int32, (T, shape.top_k), d), _typed(keep, torch.bool, (T,), d),
+                                              balance_coef, z_coef, _typed(counts, torch.int32, (E,), d), _typed(loss, torch.float32, (2,), d),
+                                              _typed(dlogits, torch.float32, (T, E), d), _ptr(workspace), workspace.numel(), _raw_stream(d)))
 
     def route_backward(self, shape, x, wg, logits, topk_idx, dtopk_w, dlogits, keep, dx, dwg, dbias, accumulate, workspace):
         """dlogits, keep (bool [T]), dx and dbias may be None."""
-        T, H, E, R = shape.T, shape.H, shape.E, shape.T * shape.top_k
+        T, H, E, k, d = shape.T, shape.H, shape.E, shape.top_k, self.device
         f32, b16 = torch.float32, torch.bfloat16
-        self._check(self.lib.moe_route_backward(self.h, C.byref(shape), _typed(x, b16, T * H), _typed(wg, b16, H * E),
-                                                _typed(logits, f32, T * E), _typed(topk_idx, torch.int32, R), _typed(dtopk_w, f32, R),
-                                                _typed(dlogits, f32, T * E), _typed(keep, torch.bool, T), _typed(dx, b16, T * H),
-                                                _typed(dwg, f32, H * E), _typed(dbias, f32, E), 1 if accumulate else 0,
-                                                _ptr(workspace), workspace.numel(), _raw_stream(self.device)))
+        self._check(self.lib.moe_route_backward(self.h, C.byref(shape), _typed(x, b16, (T, H), d), _typed(wg, b16, (H, E), d),
+                                                _typed(logits, f32, (T, E), d), _typed(topk_idx, torch.int32, (T, k), d),
+                                                _typed(dtopk_w, f32, (T, k), d), _typed(dlogits, f32, (T, E), d), _typed(keep, torch.bool, (T,), d),
+                                                _typed(dx, b16, (T, H), d), _typed(dwg, f32, (H, E), d), _typed(dbias, f32, (E,), d),
+                                                1 if accumulate else 0, _ptr(workspace), workspace.numel(), _raw_stream(d)))
 
     def combine_backward(self, shape, dout, y_perm, inv_perm, topk_w, dtopk_w, dy_perm):
         """dout as option "out_fp32" has it, y_perm and dy_perm (or None) as "y_fp32" has them."""
-        T, H, R = shape.T, shape.H, shape.T * shape.top_k
-        f32, y = torch.float32, self.y_dtype
-        self._check(self.lib.moe_combine_backward(self.h, C.byref(shape), _typed(dout, self.out_dtype, T * H), _typed(y_perm, y, R * H),
-                                                  _typed(inv_perm, torch.int32, R), _typed(topk_w, f32, R), _typed(dtopk_w, f32, R),
-                                                  _typed(dy_perm, y, R * H), _raw_stream(self.device)))
+        T, H, k, d = shape.T, shape.H, shape.top_k, self.device
+        f32, y, R = torch.float32, self.y_dtype, T * k
+        self._check(self.lib.moe_combine_backward(self.h, C.byref(shape), _typed(dout, self.out_dtype, (T, H), d), _typed(y_perm, y, (R, H), d),
+                                                  _typed(inv_perm, torch.int32, (R,), d), _typed(topk_w, f32, (T, k), d),
+                                                  _typed(dtopk_w, f32, (T, k), d), _typed(dy_perm, y, (R, H), d), _raw_stream(d)))
 
     def gradient_list(self, grads: Sequence[torch.Tensor], outs: Sequence[torch.Tensor]) -> GradientList:
         """The tensors (fp32 or bf16) that clip_gradients takes together; outs[i] receives grads[i] scaled and may be it."""
@@ -307,7 +313,7 @@ class Moe:
         assert len(grads) == len(outs)
         for g, o in zip(grads, outs):
             assert g.dtype in (torch.float32, torch.bfloat16) and o.dtype == g.dtype and o.numel() == g.numel()
-            assert g.is_cuda and o.is_cuda and g.is_contiguous() and o.is_contiguous()
+            assert g.get_device() == o.get_device() == self.device and g.is_contiguous() and o.is_contiguous()
         n = len(grads)
         sizes = (C.c_int64 * n)(*[g.numel() for g in grads])
         types = (C.c_int32 * n)(*[int(g.dtype == torch.float32) for g in grads])
@@ -318,7 +324,7 @@ class Moe:
         return GradientList(struct, buffer, grads, outs)
 
     def clip_gradients(self, gradients: GradientList, max_norm: float, norm):
-        self._check(self.lib.moe_clip_gradients(self.h, C.byref(gradients.struct), max_norm, _typed(norm, torch.float32, 1), _raw_stream(self.device)))
+        self._check(self.lib.moe_clip_gradients(self.h, C.byref(gradients.struct), max_norm, _typed(norm, torch.float32, (1,), self.device), _raw_stream(self.device)))
 
     # ---- fused call --------------------------------------------------------------------
     def layer(self, shape, x, wg, bias, w1p, w3p, w2p, out, workspace, tables=None):

@@ -3,6 +3,8 @@ and the variants that only large inputs take.  Bounds as in test_gpu_training.py
 import pytest
 import torch
 
+from paper_2503_09716_amd import make_shape
+
 from test_gpu_training import (BF16, U, check_route, generator, moe, normal, route_inputs, run_combine_backward,  # noqa: F401
                                run_route_backward, say, within)
 
@@ -124,3 +126,24 @@ def test_clip_gradients_by_factors_below_the_range_of_fp32(moe, dtype, n, in_pla
         want = before * (limit / want)
         # products below 2^-126 are held to a step of 2^-149 (fp32) or 2^-133 (bf16), or are zero
         within("out", out, want, want.abs() * (3 * U if dtype == torch.float32 else BF16 + 3 * U) + 2.0 ** -126)
+
+
+def test_transposed_shapes_are_refused(moe):
+    """A matrix of as many elements whose rows have another length."""
+    T, H, E, k = 40, 128, 8, 2
+    s = route_inputs(T, H, E, k, 1)
+    shape, ws = make_shape(T, H, 64, E, k), moe.new_backward_workspace(make_shape(T, H, 64, E, k))
+    dwg = torch.zeros((H, E), device="cuda")
+    call = lambda s, dwg: moe.route_backward(shape, s["x"], s["wg"], s["logits"], s["idx"], s["dw"], None, None, None, dwg, None, False, ws)
+    call(s, dwg)
+    call(s, dwg.view(-1))
+    for name in ("x", "wg", "logits", "idx", "dw"):
+        wrong = dict(s)
+        wrong[name] = s[name].t().contiguous()
+        with pytest.raises(AssertionError):
+            call(wrong, dwg)
+    with pytest.raises(AssertionError):
+        call(s, dwg.view(E, H))
+    with pytest.raises(AssertionError):
+        moe.balance_loss(shape, s["logits"].t().contiguous(), s["idx"], None, 1.0, 0.0, torch.zeros(E, dtype=torch.int32, device="cuda"),
+                         torch.zeros(2, device="cuda"), None, ws)
