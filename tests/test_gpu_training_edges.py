@@ -5,7 +5,7 @@ import torch
 
 from paper_2503_09716_amd import make_shape
 
-from test_gpu_training import (BF16, U, check_route, generator, moe, normal, route_inputs, run_combine_backward,  # noqa: F401
+from test_gpu_training import (BF16, U, check_clip, check_route, combine_inputs, generator, moe, normal, route_inputs, run_combine_backward,  # noqa: F401
                                run_route_backward, say, within)
 
 pytestmark = pytest.mark.gpu
@@ -106,6 +106,24 @@ def test_combine_backward_small_terms_behind_large_ones(moe, y32, d32, dy):
     within("dtopk_w", dw, want, want * (H / 64 / N + 24) * U)
 
 
+@pytest.mark.parametrize("d32", [True, False])
+@pytest.mark.parametrize("T,H,k", [(1501, 5120, 5), (40001, 192, 5)])
+def test_combine_backward_of_bf16_rows_past_the_cache(moe, T, H, k, d32):
+    """y in bf16 of more than 64 MiB, which is read past the caches, with the rows' gradient, which is written past them, and without."""
+    say("bf16 rows", T, H, k, d32)
+    dout, y, inv, w = combine_inputs(T, H, k, 5, False, d32)
+    assert y.numel() * 2 > 64 << 20
+    dw, dy = run_combine_backward(moe, dout, y, inv, w)
+    rows = inv.long()
+    terms = y.double()[rows].view(T, k, H) * dout.double()[:, None, :]
+    within("dtopk_w", dw, terms.sum(2), terms.abs().sum(2) * (H / 64 + 24) * U + 1e-38)
+    want = torch.empty(y.shape, dtype=torch.float64, device="cuda")
+    want[rows] = (w.double()[:, :, None] * dout.double()[:, None, :]).view(T * k, H)
+    within("dy_perm", dy, want, want.abs() * (BF16 + 2 * U) + 1e-38)
+    only, _ = run_combine_backward(moe, dout, y, inv, w, dy=False)
+    assert torch.equal(only, dw)
+
+
 # ---- clipping -----------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n", [4096, 200001])
@@ -127,7 +145,46 @@ def test_clip_gradients_by_factors_below_the_range_of_fp32(moe, dtype, n, in_pla
         # products below 2^-126 are held to a step of 2^-149 (fp32) or 2^-133 (bf16), or are zero
         within("out", out, want, want.abs() * (3 * U if dtype == torch.float32 else BF16 + 3 * U) + 2.0 ** -126)
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("first", [torch.float32, torch.bfloat16])
+def test_clip_gradients_of_lists_past_the_cache(moe, in_place, first):
+    """More chunks than what is kept in the memory-side cache between the passes (245 MB of 32 KiB each), of both types on both sides of
+    that border, with odd lengths and starts."""
+    say("long list", in_place, first)
+    second = torch.bfloat16 if first == torch.float32 else torch.float32
+    gen = generator(3)
+    sizes = [3000001, 777, 5000003, 45000007, 30000001, 1, 3000005, 40000003]
+    dtypes = [first, second, second, torch.float32, torch.bfloat16, first, second, first]
+    shifted = lambda n, dtype, by: torch.empty(n + by, dtype=dtype, device="cuda")[by:]
+    grads = [shifted(n, d, 1 + i % 3).normal_(generator=gen) for i, (n, d) in enumerate(zip(sizes, dtypes))]
+    before = [g.clone() for g in grads]
+    outs = grads if in_place else [shifted(n, d, i % 2) for i, (n, d) in enumerate(zip(sizes, dtypes))]
+    made = moe.gradient_list(grads, outs)
+    assert made.struct.chunks > 9500
+    norm = torch.zeros(1, device="cuda")
+    for ratio in (3.0, 0.3):
+        limit = ratio * sum(sizes) ** 0.5
+        moe.clip_gradients(made, limit, norm)
+        check_clip(grads, outs, before, norm, limit)
 
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_clip_gradients_of_a_few_elements(moe, dtype, in_place):
+    """Lists of one to nine elements whose norm is known, scaled and not."""
+    for n in (1, 2, 3, 9):
+        for share in (0.3, 0.999, 1.0, 1.5):
+            g = torch.arange(1, n + 1, device="cuda").to(dtype) * -0.75
+            before = g.clone()
+            out = g if in_place else torch.empty_like(g)
+            made, norm = moe.gradient_list([g], [out]), torch.zeros(1, device="cuda")
+            limit = share * before.double().norm().item()
+            moe.clip_gradients(made, limit, norm)
+            check_clip([g], [out], [before], norm, limit)
+            assert share >= 1 or not torch.equal(out, before) or (dtype == torch.bfloat16 and share > 0.99)
+
+
+# ---- refusals -----------------------------------------------------------------------------------
 def test_transposed_shapes_are_refused(moe):
     """A matrix of as many elements whose rows have another length."""
     T, H, E, k = 40, 128, 8, 2
