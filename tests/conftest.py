@@ -21,6 +21,8 @@ def _has_gpu() -> bool:
 
 
 def pytest_collection_modifyitems(config, items):
+    # What compares times comes last: one that a busy machine fails must not keep the others from running under -x.
+    items.sort(key=lambda it: it.path.name == "test_gpu_profile.py")
     if _has_gpu():
         return
     skip = pytest.mark.skip(reason="no GPU in this process")
