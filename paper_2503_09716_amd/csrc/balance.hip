@@ -201,7 +201,8 @@ hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t st) {
         return hipGetLastError();
     }
     const bool wide = wide_rows(a.E, {a.logits, a.dlogits ? a.dlogits : a.logits});
-    const bool alone = a.T <= BALANCE_ALONE_TOKENS && a.T * a.E <= BALANCE_ALONE;
+    const int row = (a.E + 63) & ~63;
+    const bool alone = a.T <= BALANCE_ALONE_TOKENS && a.T * row <= BALANCE_ALONE_LOGITS && a.T * (row + a.k) <= BALANCE_ALONE;
     if (!alone) hipLaunchKernelGGL(balance_count_kernel, dim3(a.count_blocks), dim3(THREADS), 0, st, a);
     return for_row16(a.E, wide, [&]<int NV, bool WIDE>() {
         if (alone) hipLaunchKernelGGL((balance_loss_kernel<NV, WIDE, true>), dim3(1), dim3(THREADS), 0, st, a);

@@ -20,9 +20,11 @@ struct BalanceArgs {
     int32_t* done;
 };
 constexpr int BALANCE_COUNT_BLOCKS = 32, BALANCE_LOSS_BLOCKS = 256;
-// One workgroup does all up to this many tokens and logits (us alone, in two launches: 256 tokens of 8 experts 6.0, 8.4; 512 8.7, 8.7;
-// 1024 14.0, 9.9; 128 of 64 experts 6.6, 9.8; 256 7.8, 10.1).
-constexpr int BALANCE_ALONE_TOKENS = 384, BALANCE_ALONE = 32768;
+// One workgroup does all up to this many tokens, logits (in rows as wide as the kernel takes them), and logits and picks together.  us in one
+// workgroup, in two launches: 256 tokens of 8 experts, k = 2 6.5, 9.4; 384 of 8 7.1, 9.3; 448 of 64, k = 8 10.0, 9.4; 384 of 64, k = 8 9.0, 9.5;
+// k = 64 10.3, 9.5; 320, k = 64 9.4, 9.6; 384 of 48, k = 48 10.2, 9.5; 256 of 128, k = 8 9.1, 9.3; k = 64 9.8, 9.4; 320 of 85, k = 8 10.8, 9.5;
+// 128 of 256, k = 64 8.7, 10.4.
+constexpr int BALANCE_ALONE_TOKENS = 384, BALANCE_ALONE_LOGITS = 32768, BALANCE_ALONE = 40960;
 hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t st);
 
 // The gradient of the logits travels in pieces of bf16 (hi + mid + lo = its 24 bits) in the order in which the matrix instructions

@@ -5,10 +5,25 @@ import torch
 
 from paper_2503_09716_amd import make_shape
 
-from test_gpu_training import (BF16, U, check_clip, check_route, combine_inputs, generator, moe, normal, route_inputs, run_combine_backward,  # noqa: F401
-                               run_route_backward, say, within)
+from test_gpu_training import (BF16, U, balance_inputs, balance_ref, check_clip, check_route, combine_inputs, generator, moe, normal, route_inputs, run_balance,  # noqa: F401
+                               run_combine_backward, run_route_backward, say, within)
 
 pytestmark = pytest.mark.gpu
+
+
+# ---- balance loss -------------------------------------------------------------------------------
+@pytest.mark.parametrize("T,E,k", [(384, 64, 42), (384, 63, 43), (385, 8, 2), (384, 33, 2), (256, 128, 32), (256, 65, 33), (320, 85, 8), (170, 129, 1),
+                                   (171, 191, 1), (128, 256, 64), (129, 255, 30)])
+@pytest.mark.parametrize("padding", [None, 0.25])
+def test_balance_loss_at_the_limit_of_one_workgroup(moe, T, E, k, padding):
+    """Tokens, and logits with picks, for which one workgroup does all, and a few more."""
+    say("balance", T, E, k, padding)
+    logits, idx, keep = balance_inputs(T, E, k, T + E, padding=padding)
+    counts, loss, d = run_balance(moe, logits, idx, keep)
+    r_counts, r_loss, r_d, loss_off, bound = balance_ref(logits, idx, keep, 1e-2, 1e-3)
+    assert torch.equal(counts.long(), r_counts)
+    within("loss", loss, r_loss, loss_off)
+    within("dlogits", d, r_d, bound)
 
 
 # ---- gradient of the router ---------------------------------------------------------------------
