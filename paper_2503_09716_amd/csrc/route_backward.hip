@@ -305,8 +305,10 @@ __device__ __forceinline__ int xcd_place(const int id, const int n) {
 // So x is read and dx written side by side, dl is read once for both.  Rows of x past the end and of tokens that do not count come from
 // a page of zeros: their dl is zero, but what x holds there may be no number.
 // More than 160 experts take half the columns, or the accumulators and the gate matrix would not fit the registers; so (NARROW) do short
-// batches of more than 32, for twice the workgroups to as many parts, as long as a part has up to 5 blocks of tokens (us with 256, 128
-// columns: 64 experts 256 x 5120 15.9, 12.4, 1000 x 2048 17.0, 15.0, 3001 x 2048, 6 blocks, padding 23.1, 23.9; 96 experts 1000 x 2048 21.0, 17.9).
+// batches of more than 32, for twice the workgroups to as many parts, as long as a part has up to 5 blocks of tokens.  us with 256, 128
+// columns: 64 experts 256 x 5120 15.9, 12.4, 1000 x 2048 17.0, 15.0; 96 experts 1000 x 2048 21.0, 17.9.  At 6 blocks two ways to measure disagree,
+// with and without padding: 3001 x 2048, 64 experts, inputs that change from call to call 19.9, 20.2, with padding 20.2, 21.3; the same buffers
+// again and again, from a graph, 24.3, 23.3 and 25.1, 24.2.  The former is taken for what programs do.
 template <int NB, bool NARROW>
 struct Tile {
     static constexpr int HT = NB <= 10 && !NARROW ? 256 : 128;

@@ -76,6 +76,18 @@ def test_dx_of_padding_tokens_where_the_gate_matrix_is_not_finite(moe, T, H, E):
     assert torch.equal(dwg, clean[1]) and torch.equal(db, clean[2])
 
 
+@pytest.mark.parametrize("T,H,E", [(2560, 2048, 64), (2561, 2048, 40), (2560, 2048, 96), (2561, 2048, 96), (4096, 4096, 8), (4097, 4096, 24), (9500, 640, 33),
+                                   (3584, 2048, 64)])
+@pytest.mark.parametrize("padding", [None, 0.1])
+def test_route_backward_longest_parts_without_a_launch_for_dl(moe, T, H, E, padding):
+    """As many blocks of tokens to a part as workgroups compute dl for, and one more."""
+    say("longest parts", T, H, E, padding)
+    s = route_inputs(T, H, E, 4, T, padding=padding)
+    first = run_route_backward(moe, s, True, 0.5)
+    check_route(s, True, 0.5, *first)
+    assert all(torch.equal(a, b) for a, b in zip(first, run_route_backward(moe, s, True, 0.5)))
+
+
 @pytest.mark.parametrize("T,H,E,k", [(50, 128, 8, 2), (400, 192, 40, 6), (300, 128, 130, 20), (90, 64, 200, 5), (5300, 4096, 8, 2)])
 @pytest.mark.parametrize("renorm", [True, False])
 @pytest.mark.parametrize("dlogits", [True, False])
