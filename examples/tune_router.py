@@ -45,7 +45,7 @@ class Layer:
         self.y_perm, self.y_shared = torch.empty((T * k, H), **f32), torch.empty((T, H), **f32) if Ns else None
         self.out = torch.empty((T, H), **f32)
         self.h, self.ws, self.back = moe.new_h_scratch(shape), moe.new_workspace(shape), moe.new_backward_workspace(shape)
-        self.dtopk_w, self.dlogits, self.dx = torch.empty((T, k), **f32), torch.empty((T, E), **f32), torch.empty((T, H), dtype=torch.bfloat16, device="cuda")
+        self.dtopk_w, self.dlogits = torch.empty((T, k), **f32), torch.empty((T, E), **f32)
         self.counts, self.loss = torch.empty(E, **i32), torch.empty(2, **f32)
         self.dwg, self.dbias = torch.empty((H, E), **f32), torch.empty(E, **f32)
 
@@ -58,11 +58,11 @@ class Layer:
         return self.out
 
     def backward(self, x, wg, keep, dout):
-        """Gradients of <dout, out> and of the balance losses in dwg, dbias and dx (through the router alone)."""
+        """Gradients of <dout, out> and of the balance losses in dwg and dbias.  Nothing before the layer is tuned: no gradient of x."""
         m, s = self.moe, self.shape
         m.combine_backward(s, dout, self.y_perm, self.inv_perm, self.topk_w, self.dtopk_w, None)
         m.balance_loss(s, self.logits, self.topk_idx, keep, BALANCE_COEF, Z_COEF, self.counts, self.loss, self.dlogits, self.back)
-        m.route_backward(s, x, wg, self.logits, self.topk_idx, self.dtopk_w, self.dlogits, keep, self.dx, self.dwg, self.dbias, False, self.back)
+        m.route_backward(s, x, wg, self.logits, self.topk_idx, self.dtopk_w, self.dlogits, keep, None, self.dwg, self.dbias, False, self.back)
 
 
 def tune(steps=60, tokens=3000, seed=0, lr=0.02, say=print):

@@ -326,8 +326,9 @@ moe_status moe_layer_views(const moe_shape* shape, void* workspace, int32_t** to
                            int32_t** expert_offsets, int32_t** inv_perm);
 
 /* ---- Training a router --------------------------------------------------------------------
- * What a program needs beside the calls above to tune the gate matrix (and bias) of a layer whose experts stay as they are, and, with
- * the gradients that leave here, the tensors around it.  In the order of a step: moe_route (with logits), moe_permute,
+ * What a program needs beside the calls above to tune the gate matrix (and bias) of a layer whose experts stay as they are.  There is no
+ * gradient of moe_grouped_ffn: dx below is the router's share of the layer's gradient of x, and a program that passes gradients on to the
+ * layers before adds the experts' share, which it forms from dy_perm by itself.  In the order of a step: moe_route (with logits), moe_permute,
  * moe_grouped_ffn, moe_combine; then moe_combine_backward, moe_balance_loss, moe_route_backward, and moe_clip_gradients over all
  * tensors.  Conventions as above; the calls record no profiling intervals.  Every gradient is that of the call's outputs as written
  * here, sums are fp32 or wider, and the same inputs give the same bits.

@@ -11,9 +11,9 @@
 // that finds the last workgroup), then one pass over the logits with a token in a row of 16 lanes.  The last workgroup of the second
 // launch adds the workgroups' partial losses in order, in 64 bits.  Few tokens: one workgroup does it all.
 // Bound by latency: each launch is a chain of two or three memory round trips, and the gradient waits for all counts.  us (of which
-// counts, loss): 256 tokens of 8 experts 6.4 (alone), 5003 of 64 11.1 (4.9, 6.6), 32768 of 160 17.8 (3.7, 14: 42 MB at 3 TB/s, half of it spent on
-// 350 vector instructions for every four tokens).  A workgroup to a CU: with two the last one's wait for all partial losses outgrows
-// what the second saves (20.8).
+// counts, loss): 256 tokens of 8 experts 6.4 (alone), 5003 of 64 11.1 (5.0, 6.4), 32768 of 160 17.7 (3.9, 14: 42 MB at 3 TB/s, half of it spent on
+// 350 vector instructions for every four tokens); without the gradient 6.1, 10.8, 15.1.  A workgroup to
+// a CU: with two the last one's wait for all partial losses outgrows what the second saves (20.8).
 #include "common.h"
 #include "router_rows.h"
 #include "train.h"
@@ -168,8 +168,8 @@ __global__ __launch_bounds__(THREADS) void balance_loss_kernel(const BalanceArgs
     }
     if (ALONE || wave != 0) return;
     // The last workgroup to get here adds up what all have written.  The partial losses are atomic stores past the L2, complete when the
-    // count goes up, and atomic loads past it read them: no fence, which would write this XCD's L2 back with all of dlogits in it
-    // (32768 tokens, 160 experts: 41 us instead of 28).
+    // count goes up, and atomic loads past it read them: no fence at agent scope, which would write this XCD's L2 back with all of dlogits in
+    // it (32768 tokens, 160 experts: 18.6 us instead of 17.6).
     __builtin_amdgcn_s_waitcnt(0);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     int before = 0;

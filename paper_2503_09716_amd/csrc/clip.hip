@@ -1,7 +1,8 @@
 // Norm of all gradients of a list, and the gradients scaled down to a norm: out = g min(1, max_norm / sqrt(sum g^2)).
 // HBM-bound: one pass for the norm, one to read and write.  Chunks of at most 32 KiB of one tensor (the list's table) are dealt to the
 // workgroups; squares are formed and added up in 64 bits, so that no gradient in the range of its type overflows or vanishes (in fp32 the
-// pass takes as long), and added up in a fixed order.  Small lists are one launch.
+// pass takes as long), and added up in a fixed order.  Small lists are one launch, unless an output is in place (32 to 512 KB out of place 4.5 to
+// 7.6 us, in place 7.7).
 // The second pass goes through the chunks from the last to the first: the last 245 MB that the first read are still in the memory-side
 // cache.  All else goes past the caches, the outputs too, and so does not displace them (1.16 GB, us: 635 with ordinary loads and stores,
 // 611 with the stores past the caches, 551 with everything past them, 540 as it is; 360 MB 198, 172, 172, 161).

@@ -4,7 +4,7 @@
 // workgroup, so that dout's row comes from memory once.  A row's product is added up in fp32 along each lane, in as many sums as a load has
 // elements (memory bounds the kernel either way, and a single sum of H / 64 terms was off by up to that many times more), and then across the
 // lanes, once to a row: a thread that took a piece of all of a token's rows would end on a sum across lanes for every 8 elements of each.
-// us: 3001 tokens x 2048, k = 6, fp32, weights alone 28.3 (172 MB at 6.1 TB/s), 4096 x 4096, k = 2, fp32 54.6 (302 MB at 5.5), 32768 x 5120,
+// us: 3001 tokens x 2048, k = 6, fp32, weights alone 28.8 (172 MB at 6.0 TB/s), 4096 x 4096, k = 2, fp32 54.6 (302 MB at 5.5), 32768 x 5120,
 // k = 6, bf16 795 to 868 by box (4.4 GB at 5.5 to 5.0; a 1 GiB copy 5.1).
 #include "common.h"
 #include "topk.h"
