@@ -4,7 +4,7 @@
 // workgroup, so that dout's row comes from memory once.  A row's product is added up in fp32 along each lane, in as many sums as a load has
 // elements (memory bounds the kernel either way, and a single sum of H / 64 terms was off by up to that many times more), and then across the
 // lanes, once to a row: a thread that took a piece of all of a token's rows would end on a sum across lanes for every 8 elements of each.
-// us: 3001 tokens x 2048, k = 6, fp32, weights alone 28.8 (172 MB at 6.0 TB/s), 4096 x 4096, k = 2, fp32 54.6 (302 MB at 5.5), 32768 x 5120,
+// us: 3001 tokens x 2048, k = 6, fp32, weights alone 27.0 (172 MB at 6.4 TB/s), 4096 x 4096, k = 2, fp32 54.6 (302 MB at 5.5), 32768 x 5120,
 // k = 6, bf16 795 to 868 by box (4.4 GB at 5.5 to 5.0; a 1 GiB copy 5.1).
 #include "common.h"
 #include "topk.h"
@@ -28,8 +28,6 @@ struct Row {
     }
 };
 
-constexpr int AHEAD = 4;   // pieces of a row that a lane has in flight
-
 // LD, ST: y is read, dy written past the caches.
 template <bool YF32, bool DF32, bool DY, int W, bool LD, bool ST>
 __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __restrict__ dout, const char* __restrict__ y_perm,
@@ -48,17 +46,23 @@ __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __re
             float sums[N] = {};
             const size_t p = (size_t)t * k + j, at = (size_t)inv_perm[p] * H * (YF32 ? 4 : 2);
             const float wj = DY ? w[p] : 0.f;
-            for (int c0 = sub * 64 + lane; c0 < n; c0 += AHEAD * W * 64) {
-                Row<YF32, N> y[AHEAD];
-                Row<DF32, N> g[AHEAD];
+            // A pieces of the row, all in flight before the first is used: the compiler would move each load behind the branch that needs it
+            // (3001 x 2048, k = 6, fp32, weights alone 28.9 us).  As many as the row has, for short ones (20000 x 192, k = 6 with four at a time
+            // 66.7 us, one by one 60.7, so 47.6).
+            auto pieces = [&]<int A>(const int c0) {
+                Row<YF32, N> y[A];
+                Row<DF32, N> g[A];
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
+                for (int u = 0; u < A; ++u) {
                     const int c = min(c0 + u * W * 64, n - 1);
                     y[u].template load<LD>(y_perm + at, c);
                     g[u].template load<false>(d, c);
                 }
+                if constexpr (A > 1)
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
+                    for (int u = 0; u < A; ++u) asm volatile("" : "+v"(y[u].v), "+v"(g[u].v));
+#pragma unroll
+                for (int u = 0; u < A; ++u) {
                     const int c = c0 + u * W * 64;
                     if (c >= n) break;
 #pragma unroll
@@ -78,7 +82,14 @@ __global__ __launch_bounds__(1024) void combine_backward_kernel(const char* __re
                         }
                     }
                 }
+            };
+            int c0 = sub * 64;   // of the wavefront's first lane
+            for (; c0 + 3 * W * 64 < n; c0 += 4 * W * 64) pieces.template operator()<4>(c0 + lane);
+            if (c0 + W * 64 < n) {
+                pieces.template operator()<2>(c0 + lane);
+                c0 += 2 * W * 64;
             }
+            if (c0 < n) pieces.template operator()<1>(c0 + lane);
 #pragma unroll
             for (int m = N / 2; m > 0; m /= 2)
 #pragma unroll
