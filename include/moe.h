@@ -358,7 +358,8 @@ moe_status moe_balance_loss(moe_ctx* ctx, const moe_shape* shape, const float* l
  * are taken from (over all experts; with renormalize over the token's picks; ids outside [0,E) are no picks, and a token without any has
  * dl = dlogits):
  *   dl = routed_scale * p * (g - sum_e p g) + dlogits,   dx = dl Wg^T,   dwg = x^T dl,   dbias = sum_t dl[t]
- * dl and the sums of dwg and dbias as fp32 has them; dx is rounded to bf16 once.  A gradient that is not finite comes out as not finite.
+ * dl (its elements to 2^-134 at best) and the sums of dwg and dbias as fp32 has them; dx is rounded to bf16 once.  A gradient that is not
+ * finite comes out as not finite.
  *   x_bf16 [T,H], wg_bf16 [H,E] (logical layout whatever "gate_packed" says), logits [T,E] fp32 (with the bias, as moe_route gives them),
  *   topk_idx [T,k] int32 (distinct ids in a row), dtopk_w [T,k] fp32, dlogits_or_null [T,E] fp32: device in
  *   dx_or_null [T,H] bf16, dwg [H,E] fp32, dbias_or_null [E] fp32: device out; with accumulate = 1 dwg and dbias are added to (each

@@ -117,9 +117,9 @@ constexpr int PREP_TOKENS = 32;
 // (0 .. 3 and 12 .. 15 of the one, 4 .. 11 of the other) meets in a bank.
 __device__ __forceinline__ int dl_row(const int e, const int g) { return e ^ ((g & 1) * 12); }
 
-// v as bf16 pieces.
+// v as bf16 pieces.  hi is cut off: rounded, it could pass the type's range next to the end of fp32's.
 __device__ __forceinline__ void split3(const float v, __bf16& hi, __bf16& mid, __bf16& lo) {
-    hi = (__bf16)v;
+    hi = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(v) >> 16));
     const float r = v - (float)hi;
     mid = (__bf16)r;
     lo = (__bf16)(r - (float)mid);

@@ -53,6 +53,32 @@ def test_dx_of_gradients_that_cancel_but_for_their_last_bits(moe, T, H, E):
     within("dx", dx, want, size * 12 * U + want.abs() * BF16 + 1e-38)
 
 
+@pytest.mark.parametrize("T,H,E", [(40, 128, 8), (70, 192, 60), (64, 192, 250), (5300, 4096, 8)])
+def test_route_backward_of_gradients_at_the_ends_of_fp32(moe, T, H, E):
+    """dl next to the largest number, and below the smallest normal one, which is held to 2^-134; a token each, so that nothing is added up."""
+    say("ends of fp32", T, H, E)
+    gen = generator(T + E)
+    most = torch.finfo(torch.float32).max
+    s = {"x": torch.full((T, H), 2.0 ** -30, dtype=torch.bfloat16, device="cuda"), "wg": torch.full((H, E), 2.0 ** -30, dtype=torch.bfloat16, device="cuda"),
+         "logits": normal(gen, (T, E)), "idx": torch.zeros((T, 1), dtype=torch.int32, device="cuda"), "dw": torch.zeros((T, 1), device="cuda"),
+         "dlogits": torch.zeros((T, E), device="cuda"), "keep": None}
+    values = torch.tensor([most, -most, 3.395e38, -3.3895e38, 3.38e38, 1.0], device="cuda")
+    s["dlogits"][torch.arange(6), torch.arange(6)] = values
+    dx, dwg, db = run_route_backward(moe, s, False)
+    want = values.double() * 2.0 ** -30
+    within("dwg", dwg[:, :6], want.expand(H, 6), want.abs() * 2 * U)
+    within("dbias", db[:6], values.double(), values.double().abs() * 2 * U)
+    within("dx", dx[:6], want[:, None].expand(6, H), want.abs()[:, None] * (BF16 + 2 * U))
+    assert (dwg[:, 6:] == 0).all() and (db[6:] == 0).all() and (dx[6:] == 0).all()
+    s["x"].fill_(1.0)
+    s["dlogits"].zero_()
+    small = torch.tensor([1.0, -1.9999999, 1.5, 1.0000001], device="cuda") * torch.tensor([2.0 ** -e for e in (109, 112, 120, 126)], device="cuda")
+    s["dlogits"][torch.arange(4), torch.arange(4)] = small
+    _, dwg, db = run_route_backward(moe, s, False)
+    within("small dwg", dwg[:, :4], small.double().expand(H, 4), torch.full((1,), 2.0 ** -134, dtype=torch.float64, device="cuda"))
+    within("small dbias", db[:4], small.double(), torch.full((1,), 2.0 ** -134, dtype=torch.float64, device="cuda"))
+
+
 # tiles that compute dl by themselves, then those that do not, in every width
 PADDED = [(70, 128, 8), (333, 320, 27), (700, 320, 64), (300, 576, 90), (200, 192, 128), (300, 192, 160), (120, 128, 192), (200, 192, 250),
           (5300, 4096, 8), (5301, 4160, 27), (2100, 4096, 64), (5303, 4096, 90), (2100, 4096, 128), (2100, 4160, 160)]
