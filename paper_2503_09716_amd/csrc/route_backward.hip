@@ -13,7 +13,7 @@
 // 128 tokens (96 from 65 experts on) do without the last, too, unless their rows of dWg can only be written 4 bytes at a time and are longer than
 // 48 experts.  us (of which products): 128 tokens x 4096, 8 experts 8.9 (one launch), 256 x 512, 8 experts 10.8 (4.7; two), 256 x 5120,
 // 160 experts 21.5 (two), 3001 x 2048, 64 experts 20 (16.7; two), 16384 x 6144, 8 experts 91 (82: 403 MB at 4.9 TB/s, a copy of x takes 74), 32768 x
-// 5120, 64 experts 162 (matrix units 47 % busy; a copy of x takes 124), 160 experts 291 to 298 by box (267: matrix units 64 % busy with 322 GFLOP of
+// 5120, 64 experts 162 (matrix units 47 % busy; a copy of x takes 124), 160 experts 286 to 298 by box (267: matrix units 64 % busy with 322 GFLOP of
 // bf16 products, 1.2 PFLOP/s); without dx 16384 x 6144, 8 experts 48, 32768 x 5120, 160 experts 165.  What keeps them from more there is that both
 // wavefronts of a SIMD wait at the same time, after the step's barrier and for operands from LDS (30 % of their cycles).  While dx took two
 // pieces of dl (262): two workgroups of four wavefronts to a CU, other priorities, one of the two starting with the other product: no gain; two
