@@ -190,7 +190,7 @@ def prepare(case, seed):
             s.q = moe.new_fp4_rows(*s.x.shape)
             moe.fp4_quantize(s.x, s.q)
             s.weights = [[moe.fp4_pack_weight(w) for w in ws] for ws in s.weights]
-            s.tables = moe.fp4_tables(*s.weights)
+            s.list = moe.weight_list(*s.weights)
             s.out = torch.empty((rows, case["N"]), dtype=torch.float32 if case["fp32"] else torch.bfloat16, device="cuda")
             s.workspace = moe.new_fp4_workspace(rows, case["E"])
         else:
@@ -200,7 +200,7 @@ def prepare(case, seed):
             s.wg = moe.pack_gate(s.shape, s.wg)
             pack = moe.fp4_pack_weight if case["fp4"] else moe.pack_weight
             s.weights = [[pack(w) for w in ws] for ws in s.weights]
-            s.tables = moe.tables(*s.weights)
+            s.list = moe.weight_list(*s.weights)
             s.out, s.workspace = torch.empty_like(s.x), moe.new_few_workspace(s.shape)
     elif case["op"] == "few":
         s.weights = [torch.stack(ws) for ws in s.weights]
@@ -235,7 +235,7 @@ def _silu(g):
 def _run_product(s):
     case = s.case
     if own:
-        s.moe.fp4_grouped_product(s.q, s.row_token, s.offsets, s.tables, s.out, s.workspace)
+        s.moe.fp4_grouped_product(s.q, s.row_token, s.offsets, s.list, s.out, s.workspace, gated=case["gated"])
         return {"out": s.out}
     out, at = [], 0
     for e, n in enumerate(s.counts):
@@ -251,7 +251,7 @@ def _run_product(s):
 def _run_few(s):
     case = s.case
     if own:
-        s.moe.layer_few(s.shape, s.x, s.wg, s.bias, s.tables, case["fp4"], s.out, s.workspace)
+        s.moe.layer_few(s.shape, s.x, s.wg, s.bias, s.list, s.out, s.workspace)
         return {"out": s.out}
     x = s.x.float()
     logits = x @ s.wg.float()
