@@ -182,23 +182,23 @@ def prepare(case, seed):
         from paper_2503_09716_amd import Moe, make_shape
         s.moe = moe = Moe(0)
         if case["op"] == "rows":
-            s.q, s.out = moe.new_fp4_rows(case["rows"], case["cols"]), torch.empty(s.x.shape, dtype=torch.bfloat16, device="cuda")
+            s.q, s.out = moe.new_mx_rows(case["rows"], case["cols"]), torch.empty(s.x.shape, dtype=torch.bfloat16, device="cuda")
         elif case["op"] == "weight":
-            s.packed, s.out = moe.new_fp4_weight(case["K"], case["N"]), torch.empty_like(s.w)
+            s.packed, s.out = moe.new_mx_weight(case["K"], case["N"]), torch.empty_like(s.w)
         elif case["op"] == "product":
             rows = case["T"] * case["k"]
-            s.q = moe.new_fp4_rows(*s.x.shape)
-            moe.fp4_quantize(s.x, s.q)
-            s.weights = [[moe.fp4_pack_weight(w) for w in ws] for ws in s.weights]
+            s.q = moe.new_mx_rows(*s.x.shape)
+            moe.mx_quantize(s.x, s.q)
+            s.weights = [[moe.mx_pack_weight(w) for w in ws] for ws in s.weights]
             s.list = moe.weight_list(*s.weights)
             s.out = torch.empty((rows, case["N"]), dtype=torch.float32 if case["fp32"] else torch.bfloat16, device="cuda")
-            s.workspace = moe.new_fp4_workspace(rows, case["E"])
+            s.workspace = moe.new_mx_workspace(rows, case["E"])
         else:
             T, H, F, E, k = (case[n] for n in ("T", "H", "F", "E", "k"))
             s.shape = make_shape(T, H, F, E, k, case["shared"], case["renorm"])
             moe.set_option("gate_packed", 1)
             s.wg = moe.pack_gate(s.shape, s.wg)
-            pack = moe.fp4_pack_weight if case["fp4"] else moe.pack_weight
+            pack = moe.mx_pack_weight if case["fp4"] else moe.pack_weight
             s.weights = [[pack(w) for w in ws] for ws in s.weights]
             s.list = moe.weight_list(*s.weights)
             s.out, s.workspace = torch.empty_like(s.x), moe.new_few_workspace(s.shape)
@@ -214,16 +214,16 @@ def run(s):
 
 def _run_rows(s):
     if own:
-        s.moe.fp4_quantize(s.x, s.q)
-        s.moe.fp4_dequantize(s.q, s.out)
+        s.moe.mx_quantize(s.x, s.q)
+        s.moe.mx_dequantize(s.q, s.out)
         return {"values": s.out}
     return {"values": _to_fp4(s.x).bfloat16()}
 
 
 def _run_weight(s):
     if own:
-        s.moe.fp4_pack_weight(s.w, s.packed)
-        s.moe.fp4_unpack_weight(s.packed, s.out)
+        s.moe.mx_pack_weight(s.w, s.packed)
+        s.moe.mx_unpack_weight(s.packed, s.out)
         return {"values": s.out}
     return {"values": _to_fp4(s.w.t().contiguous()).t().bfloat16().contiguous()}
 
@@ -235,7 +235,7 @@ def _silu(g):
 def _run_product(s):
     case = s.case
     if own:
-        s.moe.fp4_grouped_product(s.q, s.row_token, s.offsets, s.list, s.out, s.workspace, gated=case["gated"])
+        s.moe.mx_grouped_product(s.q, s.row_token, s.offsets, s.list, s.out, s.workspace, gated=case["gated"])
         return {"out": s.out}
     out, at = [], 0
     for e, n in enumerate(s.counts):
