@@ -402,6 +402,73 @@ moe_status moe_gradient_list_make(moe_ctx* ctx, int32_t tensors, const void* con
  * scales nothing. */
 moe_status moe_clip_gradients(moe_ctx* ctx, const moe_gradient_list* list, double max_norm, float* norm, void* hip_stream);
 
+/* ---- 4-bit expert weights -----------------------------------------------------------------
+ * MXFP4: 32 neighbours along the contraction dimension share a scale 2^s, s = max(floor(log2 of their largest magnitude) - 2, -127),
+ * and each of them is held as the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives times that scale (ties to the even of
+ * these eight, counted from 0; beyond 6 scales: 6).  4.25 bits a value.  A block that holds an infinity or NaN is NaN throughout.  Values
+ * that are in MXFP4 already, under whatever scales, come back as they are (down to 2^-128).
+ * With experts in this form a layer needs 0.27 of the memory, and of the bytes that a decode step reads.  For large batches:
+ * moe_route, moe_permute, moe_mx_quantize of x, moe_mx_grouped_product (gate and up), moe_mx_quantize of h,
+ * moe_mx_grouped_product (down), moe_combine.  For a few tokens: moe_layer_few.  The calls record no profiling intervals.
+ *  - Quantised rows (moe_mx_rows_bytes bytes): codes [rows][64 * ceil(cols / 128)] bytes in the order of the columns, two to a byte, low
+ *    half first, zero past cols; then from the next multiple of 256 bytes scales [rows][16 * ceil(cols / 512)], s + 127 as a byte (255:
+ *    NaN), column block b (of 32) of a row at byte 16 * (b / 16) + 4 * (b % 4) + b / 4 % 4, 127 past cols.
+ *  - Packed weights (moe_mx_weight_bytes bytes), from the transposed matrix W[n][k]: codes in blocks of 16 rows x 128 k = 1 KiB, ordered
+ *    [cols/16][ceil(rows/128)], inside a block as in moe_pack_weight's (row r at bytes 64r, its 16-byte piece c, k = 32c .. 32c+31, at slot
+ *    c ^ ((4 - r/4) & 3)); then from the next multiple of 256 bytes scales [cols/16][ceil(rows/512)][16 rows][16], in a row as above.
+ *  - Limits: rows of x of any number, contraction and output dimensions multiples of 32, every buffer below 4 GiB but the output of a product. */
+
+/* Bytes of `rows` quantised rows of `cols` columns, and of a packed weight matrix [rows = contraction, cols]; 0 for invalid sizes. */
+size_t moe_mx_rows_bytes(int32_t rows, int32_t cols);
+size_t moe_mx_weight_bytes(int32_t rows, int32_t cols);
+
+/* Quantises the rows of x [rows, cols] (bf16, or fp32 with is_fp32 = 1), blocks along the columns, and gives the values back (exact in
+ * bf16 and fp32).  x, out: device, 16-byte aligned; q: device, 256-byte aligned, moe_mx_rows_bytes bytes. */
+moe_status moe_mx_quantize(moe_ctx* ctx, const void* x, int32_t is_fp32, int32_t rows, int32_t cols, void* q, void* hip_stream);
+moe_status moe_mx_dequantize(moe_ctx* ctx, const void* q, int32_t rows, int32_t cols, void* out, int32_t out_fp32, void* hip_stream);
+
+/* One-time quantisation and packing of a weight: w_logical [rows, cols] bf16 (device, 4-byte aligned; rows = contraction dimension, along
+ * which the blocks lie) -> w_packed (device, 256-byte aligned, moe_mx_weight_bytes bytes); and its values back as bf16 [rows, cols]. */
+moe_status moe_mx_pack_weight(moe_ctx* ctx, const void* w_logical, int32_t rows, int32_t cols, void* w_packed, void* hip_stream);
+moe_status moe_mx_unpack_weight(moe_ctx* ctx, const void* w_packed, int32_t rows, int32_t cols, void* w_logical, void* hip_stream);
+
+/* A list of expert matrices that stay where they are, made once: `matrices` (1 .. 3) matrices of each of `experts` experts.  The struct and
+ * the device buffer are the caller's; the fields are the library's.  Nothing is copied or looked up when a call uses it, so calls
+ * can be captured into graphs. */
+typedef struct {
+    void* buffer;
+    int32_t experts;
+    int32_t matrices;
+    int32_t fp4;
+} moe_weight_list;
+
+/* Device bytes of a list; 0 for invalid arguments (1 <= experts <= 256). */
+size_t moe_weight_list_bytes(int32_t experts, int32_t matrices);
+
+/* Fills `list` and its buffer (device, 256-byte aligned, MOE_E_WORKSPACE if too small).  weights: HOST array of matrices * experts DEVICE
+ * pointers, 16-byte aligned, the first matrix of every expert, then the second ones: made by moe_mx_pack_weight (fp4 = 1) or
+ * moe_pack_weight (fp4 = 0).  SYNCHRONISES hip_stream. */
+moe_status moe_weight_list_make(moe_ctx* ctx, int32_t experts, int32_t matrices, const void* const* weights, int32_t fp4, void* buffer,
+                                size_t buffer_bytes, moe_weight_list* list, void* hip_stream);
+
+/* Bytes of device workspace for moe_mx_grouped_product with up to `rows` rows in `experts` groups; 0 for invalid arguments. */
+size_t moe_mx_workspace_bytes(int32_t rows, int32_t experts);
+
+/* Grouped product of quantised rows with MXFP4 matrices; fp32 accumulation, rounded once at the end.  Row r of group e (expert_offsets[e] <=
+ * r < expert_offsets[e + 1] <= rows) is multiplied with expert e's matrices: W = the list's matrix number `first`, with gated = 1 also
+ * the next one, W':
+ *   gated = 0: out[r,:] = x_r W        gated = 1: out[r,:] = silu(x_r W) * (x_r W')
+ * where x_r is row r of xq, or row row_index[r] of xq (moe_permute's row_token: xq are then the tokens' rows).
+ *   xq: moe_mx_quantize of x_rows rows of K columns; row_index_or_null [rows] int32, expert_offsets [E+1] int32: device in, not validated
+ *   list: MXFP4 matrices of K rows and N columns
+ *   out [rows, N] bf16, or fp32 with out_fp32 = 1: device out, 16-byte aligned.  Rows from expert_offsets[E] on are left as they were.
+ *   workspace: device, 256-byte aligned, moe_mx_workspace_bytes(rows, list->experts) bytes
+ * rows = 0 is valid and enqueues nothing. */
+moe_status moe_mx_grouped_product(moe_ctx* ctx, int32_t rows, int32_t K, int32_t N, const void* xq, int32_t x_rows,
+                                   const int32_t* row_index_or_null, const int32_t* expert_offsets, const moe_weight_list* list,
+                                   int32_t first, int32_t gated, void* out, int32_t out_fp32, void* workspace, size_t workspace_bytes,
+                                   void* hip_stream);
+
 /* Profiling.  While enabled, every kernel group a call enqueues is bracketed by HIP events on
  * the call's stream.  moe_profile_read waits for the recorded events, adds the elapsed
  * milliseconds per stage into ms_sum[MOE_STAGE_COUNT] and the number of intervals into

@@ -27,6 +27,8 @@ EXPORTS = [
     "moe_layer_streamed", "moe_stream_stats", "moe_estimate_streamed_ms", "moe_accumulate", "moe_layer_chunked",
     "moe_backward_workspace_bytes", "moe_balance_loss", "moe_route_backward", "moe_combine_backward",
     "moe_gradient_list_bytes", "moe_gradient_list_make", "moe_clip_gradients",
+    "moe_mx_rows_bytes", "moe_mx_weight_bytes", "moe_mx_quantize", "moe_mx_dequantize", "moe_mx_pack_weight", "moe_mx_unpack_weight",
+    "moe_weight_list_bytes", "moe_weight_list_make", "moe_mx_workspace_bytes", "moe_mx_grouped_product",
     "moe_profile_enable", "moe_profile_read", "moe_profile_read_intervals", "moe_profile_mfma_ceiling",
 ]
 
@@ -38,6 +40,10 @@ class MoeShape(C.Structure):
 
 class GradientListStruct(C.Structure):
     _fields_ = [("buffer", C.c_void_p), ("chunks", C.c_int32), ("one_launch", C.c_int32)]
+
+
+class WeightListStruct(C.Structure):
+    _fields_ = [("buffer", C.c_void_p), ("experts", C.c_int32), ("matrices", C.c_int32), ("fp4", C.c_int32)]
 
 
 class MoeError(RuntimeError):
@@ -106,8 +112,19 @@ def load_library():
     lib.moe_gradient_list_bytes.restype = C.c_size_t
     lib.moe_gradient_list_make.argtypes = [C.c_void_p, C.c_int32, tab, tab, i64s, i32s, vp, C.c_size_t, C.POINTER(GradientListStruct), vp]
     lib.moe_clip_gradients.argtypes = [C.c_void_p, C.POINTER(GradientListStruct), C.c_double, f32p, vp]
+    i32, ls = C.c_int32, C.POINTER(WeightListStruct)
+    for name in ("moe_mx_rows_bytes", "moe_mx_weight_bytes", "moe_weight_list_bytes", "moe_mx_workspace_bytes"):
+        getattr(lib, name).argtypes = [i32, i32]
+        getattr(lib, name).restype = C.c_size_t
+    lib.moe_mx_quantize.argtypes = [C.c_void_p, vp, i32, i32, i32, vp, vp]
+    lib.moe_mx_dequantize.argtypes = [C.c_void_p, vp, i32, i32, vp, i32, vp]
+    lib.moe_mx_pack_weight.argtypes = [C.c_void_p, vp, i32, i32, vp, vp]
+    lib.moe_mx_unpack_weight.argtypes = [C.c_void_p, vp, i32, i32, vp, vp]
+    lib.moe_weight_list_make.argtypes = [C.c_void_p, i32, i32, tab, i32, vp, C.c_size_t, ls, vp]
+    lib.moe_mx_grouped_product.argtypes = [C.c_void_p, i32, i32, i32, vp, i32, i32p, i32p, ls, i32, i32, vp, i32, vp, C.c_size_t, vp]
     for name in EXPORTS:
-        if name not in ("moe_backward_workspace_bytes", "moe_gradient_list_bytes",
+        if name not in ("moe_backward_workspace_bytes", "moe_gradient_list_bytes", "moe_mx_rows_bytes", "moe_mx_weight_bytes",
+                        "moe_weight_list_bytes", "moe_mx_workspace_bytes",
                         "moe_destroy", "moe_last_error", "moe_workspace_bytes", "moe_h_scratch_bytes", "moe_gate_packed_bytes",
                         "moe_estimate_streamed_ms"):
             getattr(lib, name).restype = C.c_int
@@ -175,6 +192,10 @@ def _same_rows(t, shape) -> bool:
     return t.numel() == math.prod(shape) and (len(shape) == 1 or t.dim() < 2 or t.shape[-1] == shape[-1])
 
 
+def _float_type(t: torch.Tensor):
+    return torch.float32 if t.dtype is torch.float32 else torch.bfloat16
+
+
 def _raw_stream(device: int):
     """The device's current stream; torch.cuda.current_stream() makes an object for it, which takes longer than a small kernel's launch."""
     return torch._C._cuda_getCurrentRawStream(device)
@@ -185,6 +206,21 @@ class GradientList:
 
     def __init__(self, struct: GradientListStruct, buffer: torch.Tensor, grads, outs):
         self.struct, self.buffer, self.grads, self.outs = struct, buffer, grads, outs
+
+
+class MxRows:
+    """Rows in MXFP4 (Moe.mx_quantize): `rows` of `cols` values in one opaque buffer."""
+
+    def __init__(self, rows: int, cols: int, buffer: torch.Tensor):
+        self.rows, self.cols, self.buffer = rows, cols, buffer
+
+
+class WeightList:
+    """Expert matrices that calls find through a device table made once (Moe.weight_list): keeps them and the table alive."""
+
+    def __init__(self, struct: WeightListStruct, buffer: torch.Tensor, weights):
+        self.struct, self.buffer, self.weights = struct, buffer, weights
+        self.bytes = [ws[0].numel() * ws[0].element_size() for ws in weights]   # of a matrix, by its number
 
 
 class Moe:
@@ -325,6 +361,78 @@ class Moe:
 
     def clip_gradients(self, gradients: GradientList, max_norm: float, norm):
         self._check(self.lib.moe_clip_gradients(self.h, C.byref(gradients.struct), max_norm, _typed(norm, torch.float32, (1,), self.device), _raw_stream(self.device)))
+
+    # ---- 4-bit expert weights --------------------------------------------------------------
+    def new_mx_rows(self, rows: int, cols: int) -> MxRows:
+        n = int(self.lib.moe_mx_rows_bytes(rows, cols))
+        if n == 0 and not (rows == 0 and cols > 0 and cols % 32 == 0):
+            raise MoeError(1, "rows of columns that are no multiple of 32, or 4 GiB of them")
+        return MxRows(rows, cols, torch.empty(n, dtype=torch.uint8, device="cuda:%d" % self.device))
+
+    def new_mx_weight(self, rows: int, cols: int) -> torch.Tensor:
+        n = int(self.lib.moe_mx_weight_bytes(rows, cols))
+        if n == 0:
+            raise MoeError(1, "a matrix whose rows or columns are no multiple of 32, or of 4 GiB")
+        return torch.empty(n, dtype=torch.uint8, device="cuda:%d" % self.device)
+
+    def mx_quantize(self, x, q: MxRows):
+        """x: bf16 or fp32 [rows, cols]."""
+        self._check(self.lib.moe_mx_quantize(self.h, _typed(x, _float_type(x), (q.rows, q.cols), self.device), int(x.dtype is torch.float32), q.rows, q.cols,
+                                              q.buffer.data_ptr(), _raw_stream(self.device)))
+
+    def mx_dequantize(self, q: MxRows, out):
+        """out: bf16 or fp32 [rows, cols]."""
+        self._check(self.lib.moe_mx_dequantize(self.h, q.buffer.data_ptr(), q.rows, q.cols, _typed(out, _float_type(out), (q.rows, q.cols), self.device),
+                                                int(out.dtype is torch.float32), _raw_stream(self.device)))
+
+    def mx_pack_weight(self, w: torch.Tensor, packed: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Logical bf16 [K, N] weight -> MXFP4 (opaque 1-D uint8 tensor, `packed` if given)."""
+        rows, cols = w.shape
+        if packed is None:
+            packed = self.new_mx_weight(rows, cols)
+        n = int(self.lib.moe_mx_weight_bytes(rows, cols))
+        self._check(self.lib.moe_mx_pack_weight(self.h, _typed(w, torch.bfloat16, (rows, cols), self.device), rows, cols,
+                                                 _typed(packed, torch.uint8, (n,), self.device), _raw_stream(self.device)))
+        return packed
+
+    def mx_unpack_weight(self, packed: torch.Tensor, out: torch.Tensor) -> torch.Tensor:
+        """The values of a packed weight as a logical bf16 [K, N] matrix, in `out`."""
+        rows, cols = out.shape
+        n = int(self.lib.moe_mx_weight_bytes(rows, cols))
+        self._check(self.lib.moe_mx_unpack_weight(self.h, _typed(packed, torch.uint8, (n,), self.device), rows, cols,
+                                                   _typed(out, torch.bfloat16, (rows, cols), self.device), _raw_stream(self.device)))
+        return out
+
+    def weight_list(self, *weights: Sequence[torch.Tensor]) -> WeightList:
+        """One to three matrices of each expert (first all experts' first, ...), packed by mx_pack_weight (uint8) or pack_weight (bf16)."""
+        weights = [list(ws) for ws in weights]
+        kind = weights[0][0].dtype
+        assert kind in (torch.uint8, torch.bfloat16)
+        for ws in weights:
+            assert len(ws) == len(weights[0]) and all(w.dtype is kind and w.numel() == ws[0].numel() and w.get_device() == self.device for w in ws)
+        experts, matrices = len(weights[0]), len(weights)
+        buffer = torch.empty(int(self.lib.moe_weight_list_bytes(experts, matrices)), dtype=torch.uint8, device="cuda:%d" % self.device)
+        struct = WeightListStruct()
+        self._check(self.lib.moe_weight_list_make(self.h, experts, matrices, _table([w for ws in weights for w in ws]), int(kind is torch.uint8),
+                                                  _ptr(buffer), buffer.numel(), C.byref(struct), _raw_stream(self.device)))
+        return WeightList(struct, buffer, weights)
+
+    def new_mx_workspace(self, rows: int, experts: int) -> torch.Tensor:
+        """Workspace of mx_grouped_product."""
+        n = int(self.lib.moe_mx_workspace_bytes(rows, experts))
+        if n == 0:
+            raise MoeError(1, "invalid number of rows or experts")
+        return torch.empty(n, dtype=torch.uint8, device="cuda:%d" % self.device)
+
+    def mx_grouped_product(self, q: MxRows, row_index, expert_offsets, weights: WeightList, out, workspace, gated: bool = False, first: int = 0):
+        """out: bf16 or fp32 [rows, N]; row_index: int32 [rows] or None; weights: matrices number `first` and, gated, the next of each expert."""
+        d, (rows, N) = self.device, out.shape
+        n = int(self.lib.moe_mx_weight_bytes(q.cols, N))
+        assert all(b == n for b in weights.bytes[first:first + 1 + bool(gated)]), "matrices of %d x %d in MXFP4 required" % (q.cols, N)
+        self._check(self.lib.moe_mx_grouped_product(self.h, rows, q.cols, N, q.buffer.data_ptr(), q.rows, _typed(row_index, torch.int32, (rows,), d),
+                                                     _typed(expert_offsets, torch.int32, (weights.struct.experts + 1,), d), C.byref(weights.struct),
+                                                     first, int(gated), _typed(out, _float_type(out), (rows, N), d), int(out.dtype is torch.float32),
+                                                     _ptr(workspace), workspace.numel(), _raw_stream(d)))
 
     # ---- fused call --------------------------------------------------------------------
     def layer(self, shape, x, wg, bias, w1p, w3p, w2p, out, workspace, tables=None):

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "common.h"
+#include "fp4.h"
 #include "train.h"
 
 using namespace moe;
@@ -942,6 +943,43 @@ int64_t tensor_chunks(uintptr_t src, int64_t bytes) {
     return ((int64_t)(src & 127) + bytes + CLIP_CHUNK - 1) / CLIP_CHUNK;
 }
 
+// Why rows x K cannot be held in MXFP4 (any_rows: rows of x, of any number), or nullptr.
+const char* fp4_size_problem(int64_t rows, int64_t K, bool any_rows) {
+    if (K < 32 || K % 32 || rows < 0 || (!any_rows && (rows < 32 || rows % 32)))
+        return any_rows ? "columns must be a positive multiple of 32" : "rows and columns must be positive multiples of 32";
+    if (fp4_bytes(rows, K) >= (int64_t)1 << 32) return "quantised it reaches 4 GiB";
+    return nullptr;
+}
+const char* fp4_weight_problem(int64_t K, int64_t N) {
+    if (const char* why = fp4_size_problem(N, K, false)) return why;
+    return K * N * 2 >= (int64_t)1 << 32 ? "a matrix reaches 4 GiB" : nullptr;
+}
+moe_status fp4_status(int64_t K, int64_t N) { return K < 32 || K % 32 || N < 32 || N % 32 ? MOE_E_ARG : MOE_E_UNSUPPORTED; }
+
+moe_status check_fp4_rows(moe_ctx* c, const char* what, const void* x, int32_t is_fp32, int32_t rows, int32_t cols, const void* q) {
+    if (is_fp32 != 0 && is_fp32 != 1) return fail(c, MOE_E_ARG, "%s: the type must be 0 or 1", what);
+    if (rows < 0) return fail(c, MOE_E_ARG, "%s: rows must be >= 0", what);
+    if (const char* why = fp4_size_problem(rows, cols, true)) return fail(c, fp4_status(cols, 32), "%s: %s", what, why);
+    if ((int64_t)rows * cols * (is_fp32 ? 4 : 2) >= (int64_t)1 << 36) return fail(c, MOE_E_UNSUPPORTED, "%s: x reaches 64 GiB", what);
+    if (rows == 0) return MOE_OK;
+    if (!x || !q || x == q) return fail(c, MOE_E_ARG, "%s: NULL or aliased buffers", what);
+    if (misaligned({x}, 16) || misaligned({q}, 256)) return fail(c, MOE_E_ARG, "%s: misaligned pointer", what);
+    return MOE_OK;
+}
+
+moe_status check_fp4_weight(moe_ctx* c, const char* what, const void* w, int32_t rows, int32_t cols, const void* packed) {
+    if (const char* why = fp4_weight_problem(rows, cols)) return fail(c, fp4_status(rows, cols), "%s: %s", what, why);
+    if (!w || !packed || w == packed) return fail(c, MOE_E_ARG, "%s: NULL or aliased buffers", what);
+    if (misaligned({w}, 4) || misaligned({packed}, 256)) return fail(c, MOE_E_ARG, "%s: misaligned pointer", what);
+    return MOE_OK;
+}
+
+moe_status check_list(moe_ctx* c, const char* what, const moe_weight_list* list) {
+    if (!list || !list->buffer || list->experts < 1 || list->experts > MAX_GROUPS || list->matrices < 1 || list->matrices > 3)
+        return fail(c, MOE_E_ARG, "%s: NULL pointer or a list that was not made", what);
+    return MOE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1475,6 +1513,122 @@ moe_status moe_clip_gradients(moe_ctx* c, const moe_gradient_list* list, double 
     const ClipArgs a{(const ClipChunk*)((char*)list->buffer + align_up(CLIP_BLOCKS * sizeof(double))), (double*)list->buffer, norm, max_norm, list->chunks,
                      list->one_launch};
     HIP_TRY(c, launch_clip(a, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+size_t moe_mx_rows_bytes(int32_t rows, int32_t cols) { return fp4_size_problem(rows, cols, true) ? 0 : (size_t)fp4_bytes(rows, cols); }
+
+size_t moe_mx_weight_bytes(int32_t rows, int32_t cols) { return fp4_weight_problem(rows, cols) ? 0 : (size_t)fp4_bytes(cols, rows); }
+
+moe_status moe_mx_quantize(moe_ctx* c, const void* x, int32_t is_fp32, int32_t rows, int32_t cols, void* q, void* stream) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    if (moe_status st = check_fp4_rows(c, "mx_quantize", x, is_fp32, rows, cols, q)) return st;
+    if (rows == 0) return MOE_OK;
+    HIP_TRY(c, hipSetDevice(c->device));
+    HIP_TRY(c, launch_fp4_quantize(x, is_fp32 != 0, rows, cols, q, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+moe_status moe_mx_dequantize(moe_ctx* c, const void* q, int32_t rows, int32_t cols, void* out, int32_t out_fp32, void* stream) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    if (moe_status st = check_fp4_rows(c, "mx_dequantize", out, out_fp32, rows, cols, q)) return st;
+    if (rows == 0) return MOE_OK;
+    HIP_TRY(c, hipSetDevice(c->device));
+    HIP_TRY(c, launch_fp4_dequantize(q, rows, cols, out, out_fp32 != 0, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+moe_status moe_mx_pack_weight(moe_ctx* c, const void* w, int32_t rows, int32_t cols, void* packed, void* stream) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    if (moe_status st = check_fp4_weight(c, "mx_pack_weight", w, rows, cols, packed)) return st;
+    HIP_TRY(c, hipSetDevice(c->device));
+    HIP_TRY(c, launch_fp4_pack(w, rows, cols, packed, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+moe_status moe_mx_unpack_weight(moe_ctx* c, const void* packed, int32_t rows, int32_t cols, void* w, void* stream) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    if (moe_status st = check_fp4_weight(c, "mx_unpack_weight", w, rows, cols, packed)) return st;
+    HIP_TRY(c, hipSetDevice(c->device));
+    HIP_TRY(c, launch_fp4_unpack(packed, rows, cols, w, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+size_t moe_weight_list_bytes(int32_t experts, int32_t matrices) {
+    if (experts < 1 || experts > MAX_GROUPS || matrices < 1 || matrices > 3) return 0;
+    return align_up((size_t)experts * matrices * sizeof(void*));
+}
+
+moe_status moe_weight_list_make(moe_ctx* c, int32_t experts, int32_t matrices, const void* const* weights, int32_t fp4, void* buffer,
+                                size_t buffer_bytes, moe_weight_list* list, void* stream) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    const size_t need = moe_weight_list_bytes(experts, matrices);
+    if (need == 0) return fail(c, MOE_E_ARG, "weight_list: 1 to %d experts and 1 to 3 matrices required", MAX_GROUPS);
+    if (!weights || !buffer || !list) return fail(c, MOE_E_ARG, "weight_list: NULL pointer");
+    if (fp4 != 0 && fp4 != 1) return fail(c, MOE_E_ARG, "weight_list: fp4 must be 0 or 1");
+    if (misaligned({buffer}, 256)) return fail(c, MOE_E_ARG, "weight_list: buffer must be 256-byte aligned");
+    if (buffer_bytes < need) return fail(c, MOE_E_WORKSPACE, "weight_list: buffer %zu bytes < required %zu", buffer_bytes, need);
+    for (int i = 0; i < experts * matrices; ++i) {
+        if (!weights[i]) return fail(c, MOE_E_ARG, "weight_list: pointer %d is NULL", i);
+        if (misaligned({weights[i]}, 16)) return fail(c, MOE_E_ARG, "weight_list: pointer %d is misaligned", i);
+    }
+    HIP_TRY(c, hipSetDevice(c->device));
+    HIP_TRY(c, hipMemcpyAsync(buffer, weights, (size_t)experts * matrices * sizeof(void*), hipMemcpyHostToDevice, (hipStream_t)stream));
+    HIP_TRY(c, hipStreamSynchronize((hipStream_t)stream));
+    *list = moe_weight_list{buffer, experts, matrices, fp4};
+    return MOE_OK;
+}
+
+size_t moe_mx_workspace_bytes(int32_t rows, int32_t experts) {
+    return rows < 0 || experts < 1 || experts > MAX_GROUPS ? 0 : fp4_layout(rows, experts).total;
+}
+
+moe_status moe_mx_grouped_product(moe_ctx* c, int32_t rows, int32_t K, int32_t N, const void* xq, int32_t x_rows, const int32_t* row_index,
+                                   const int32_t* offsets, const moe_weight_list* list, int32_t first, int32_t gated, void* out,
+                                   int32_t out_fp32, void* ws, size_t ws_bytes, void* stream) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    if (rows < 0 || x_rows < 0) return fail(c, MOE_E_ARG, "mx_grouped_product: rows must be >= 0");
+    if (const char* why = fp4_weight_problem(K, N)) return fail(c, fp4_status(K, N), "mx_grouped_product: %s", why);
+    if (const char* why = fp4_size_problem(x_rows, K, true)) return fail(c, MOE_E_UNSUPPORTED, "mx_grouped_product: %s", why);
+    if ((gated != 0 && gated != 1) || (out_fp32 != 0 && out_fp32 != 1)) return fail(c, MOE_E_ARG, "mx_grouped_product: gated and out_fp32 must be 0 or 1");
+    if (moe_status st = check_list(c, "mx_grouped_product", list)) return st;
+    if (!list->fp4) return fail(c, MOE_E_ARG, "mx_grouped_product: the list is not of MXFP4 matrices");
+    if (first < 0 || first + gated >= list->matrices) return fail(c, MOE_E_ARG, "mx_grouped_product: the list has no matrix %d", (int)(first + gated));
+    if (rows == 0) return MOE_OK;
+    if (!xq || !offsets || !out) return fail(c, MOE_E_ARG, "mx_grouped_product: NULL pointer");
+    if (row_index ? x_rows == 0 : x_rows < rows) return fail(c, MOE_E_ARG, "mx_grouped_product: xq has fewer rows than the product");
+    if (misaligned({xq}, 256) || misaligned({out}, 16) || misaligned({row_index, offsets}, 4))
+        return fail(c, MOE_E_ARG, "mx_grouped_product: misaligned pointer");
+    if (!ws) return fail(c, MOE_E_ARG, "workspace is NULL");
+    if ((uintptr_t)ws & 255) return fail(c, MOE_E_ARG, "workspace must be 256-byte aligned");
+    const Fp4Layout L = fp4_layout(rows, list->experts);
+    if (ws_bytes < L.total) return fail(c, MOE_E_WORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, L.total);
+    HIP_TRY(c, hipSetDevice(c->device));
+    Fp4Product p = {};
+    p.codes = (const char*)xq;
+    p.scales = p.codes + fp4_scales_at(x_rows, K);
+    p.row_index = row_index;
+    p.wa = (const void* const*)list->buffer + (size_t)first * list->experts;
+    p.wb = p.wa + (gated ? list->experts : 0);
+    p.out = (char*)out;
+    p.offsets = offsets;
+    p.plan = (PlanHeader*)((char*)ws + L.plan);
+    p.descs = (TileDesc*)((char*)ws + L.descs);
+    p.rows = rows;
+    p.E = list->experts;
+    p.K = K;
+    p.N = N;
+    p.sub_tiles = (int32_t)fp4_sub_tiles(K);
+    p.groups = (int32_t)fp4_groups(K);
+    p.out_fp32 = out_fp32;
+    p.scales_at = (uint32_t)fp4_scales_at(N, K);
+    HIP_TRY(c, launch_fp4_product(p, gated != 0, (hipStream_t)stream));
     return MOE_OK;
 }
 
