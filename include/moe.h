@@ -469,6 +469,21 @@ moe_status moe_mx_grouped_product(moe_ctx* ctx, int32_t rows, int32_t K, int32_t
                                    int32_t first, int32_t gated, void* out, int32_t out_fp32, void* workspace, size_t workspace_bytes,
                                    void* hip_stream);
 
+/* The whole layer for a few tokens (T <= 16, top_k <= 16), in two launches, or three where the gate matrix is above 256 KiB (one more unless
+ * it is packed): moe_layer's formula,
+ *   out[t] = sum over the picks e of w[t,e] * ( silu(x_t W1_e) * (x_t W3_e) ) W2_e + sum over the shared experts of the same without w,
+ * on matrices of moe_pack_weight or in MXFP4.  Nothing is rounded to fewer bits than its input has but out, once: logits, weights and sums are fp32,
+ * and h enters the second product with 16 of its bits.  Results differ from moe_layer's in the last bits (it rounds h to bf16); the same
+ * inputs give the same bits, but the order of a token's sums depends on which experts the other tokens pick.
+ *   x_bf16 [T,H], wg_bf16 [H,E] (packed under option "gate_packed"), gate_bias [E] fp32 or NULL: device in; x 16-byte aligned
+ *   list: three matrices (gate, up, down) of each of the E + num_shared experts
+ *   out [T,H] bf16 (fp32 under "out_fp32" = 1): device out, 16-byte aligned, not x
+ *   workspace: device, 256-byte aligned, moe_few_workspace_bytes(shape) bytes (0: a shape outside the limits)
+ * H <= 32768 and F <= 65536.  T = 0 is valid and enqueues nothing.  A batch of more tokens is MOE_E_UNSUPPORTED. */
+size_t moe_few_workspace_bytes(const moe_shape* shape);
+moe_status moe_layer_few(moe_ctx* ctx, const moe_shape* shape, const void* x_bf16, const void* wg_bf16, const float* gate_bias,
+                         const moe_weight_list* list, void* out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Profiling.  While enabled, every kernel group a call enqueues is bracketed by HIP events on
  * the call's stream.  moe_profile_read waits for the recorded events, adds the elapsed
  * milliseconds per stage into ms_sum[MOE_STAGE_COUNT] and the number of intervals into

@@ -28,7 +28,7 @@ EXPORTS = [
     "moe_backward_workspace_bytes", "moe_balance_loss", "moe_route_backward", "moe_combine_backward",
     "moe_gradient_list_bytes", "moe_gradient_list_make", "moe_clip_gradients",
     "moe_mx_rows_bytes", "moe_mx_weight_bytes", "moe_mx_quantize", "moe_mx_dequantize", "moe_mx_pack_weight", "moe_mx_unpack_weight",
-    "moe_weight_list_bytes", "moe_weight_list_make", "moe_mx_workspace_bytes", "moe_mx_grouped_product",
+    "moe_weight_list_bytes", "moe_weight_list_make", "moe_mx_workspace_bytes", "moe_mx_grouped_product", "moe_few_workspace_bytes", "moe_layer_few",
     "moe_profile_enable", "moe_profile_read", "moe_profile_read_intervals", "moe_profile_mfma_ceiling",
 ]
 
@@ -122,8 +122,11 @@ def load_library():
     lib.moe_mx_unpack_weight.argtypes = [C.c_void_p, vp, i32, i32, vp, vp]
     lib.moe_weight_list_make.argtypes = [C.c_void_p, i32, i32, tab, i32, vp, C.c_size_t, ls, vp]
     lib.moe_mx_grouped_product.argtypes = [C.c_void_p, i32, i32, i32, vp, i32, i32p, i32p, ls, i32, i32, vp, i32, vp, C.c_size_t, vp]
+    lib.moe_few_workspace_bytes.argtypes = [sp]
+    lib.moe_few_workspace_bytes.restype = C.c_size_t
+    lib.moe_layer_few.argtypes = [C.c_void_p, sp, vp, vp, f32p, ls, vp, vp, C.c_size_t, vp]
     for name in EXPORTS:
-        if name not in ("moe_backward_workspace_bytes", "moe_gradient_list_bytes", "moe_mx_rows_bytes", "moe_mx_weight_bytes",
+        if name not in ("moe_few_workspace_bytes", "moe_backward_workspace_bytes", "moe_gradient_list_bytes", "moe_mx_rows_bytes", "moe_mx_weight_bytes",
                         "moe_weight_list_bytes", "moe_mx_workspace_bytes",
                         "moe_destroy", "moe_last_error", "moe_workspace_bytes", "moe_h_scratch_bytes", "moe_gate_packed_bytes",
                         "moe_estimate_streamed_ms"):
@@ -433,6 +436,23 @@ class Moe:
                                                      _typed(expert_offsets, torch.int32, (weights.struct.experts + 1,), d), C.byref(weights.struct),
                                                      first, int(gated), _typed(out, _float_type(out), (rows, N), d), int(out.dtype is torch.float32),
                                                      _ptr(workspace), workspace.numel(), _raw_stream(d)))
+
+    def new_few_workspace(self, shape: MoeShape) -> torch.Tensor:
+        """Workspace of layer_few."""
+        n = int(self.lib.moe_few_workspace_bytes(C.byref(shape)))
+        if n == 0:
+            raise MoeError(2, "a shape outside the limits of layer_few")
+        return torch.empty(n, dtype=torch.uint8, device="cuda:%d" % self.device)
+
+    def layer_few(self, shape, x, wg, bias, weights: WeightList, out, workspace):
+        """The whole layer for up to 16 tokens; weights: weight_list of the gate, up and down matrices, bf16 or MXFP4."""
+        T, H, F, E, d = shape.T, shape.H, shape.F, shape.E, self.device
+        fp4 = weights.struct.fp4
+        want = [int(self.lib.moe_mx_weight_bytes(*s)) if fp4 else 2 * H * F for s in ((H, F), (H, F), (F, H))]
+        assert weights.bytes == want, "three matrices of %d x %d, %d x %d and %d x %d required" % (H, F, H, F, F, H)
+        self._check(self.lib.moe_layer_few(self.h, C.byref(shape), _typed(x, torch.bfloat16, (T, H), d), _ptr(wg), _typed(bias, torch.float32, (E,), d),
+                                           C.byref(weights.struct), _typed(out, self.out_dtype, (T, H), d), _ptr(workspace), workspace.numel(),
+                                           _raw_stream(d)))
 
     # ---- fused call --------------------------------------------------------------------
     def layer(self, shape, x, wg, bias, w1p, w3p, w2p, out, workspace, tables=None):

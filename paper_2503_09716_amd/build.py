@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoe_mi355.so")
 SOURCES = ["api.hip", "route.hip", "permute.hip", "ffn_gemm.hip", "ffn_small.hip", "combine.hip", "stream.hip", "profile.hip",
-           "balance.hip", "route_backward.hip", "combine_backward.hip", "clip.hip", "fp4_quantize.hip", "fp4_product.hip"]
+           "balance.hip", "route_backward.hip", "combine_backward.hip", "clip.hip", "fp4_quantize.hip", "fp4_product.hip", "few.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument",
          "-Wno-unknown-attributes"]
@@ -27,7 +27,7 @@ def _stale(target: str, deps) -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     headers = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "plan.h"), os.path.join(CSRC, "topk.h"), os.path.join(CSRC, "train.h"),
-               os.path.join(CSRC, "router_rows.h"), os.path.join(CSRC, "fp4.h"), os.path.join(ROOT, "include", "moe.h")]
+               os.path.join(CSRC, "router_rows.h"), os.path.join(CSRC, "fp4.h"), os.path.join(CSRC, "few.h"), os.path.join(ROOT, "include", "moe.h")]
     jobs = []
     for src in SOURCES:
         s = os.path.join(CSRC, src)

@@ -6,9 +6,11 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <vector>
 
 #include "common.h"
+#include "few.h"
 #include "fp4.h"
 #include "train.h"
 
@@ -943,6 +945,31 @@ int64_t tensor_chunks(uintptr_t src, int64_t bytes) {
     return ((int64_t)(src & 127) + bytes + CLIP_CHUNK - 1) / CLIP_CHUNK;
 }
 
+const char* few_shape_problem(const moe_shape* s, moe_status* st) {
+    if (const char* why = shape_problem(s, st)) return why;
+    *st = MOE_E_UNSUPPORTED;
+    if (s->T > FEW_TOKENS || s->top_k > FEW_TOP_K) return "T <= 16 and top_k <= 16 required";
+    if (s->H > 32768 || s->F > 65536) return "H <= 32768 and F <= 65536 required";
+    *st = MOE_OK;
+    return nullptr;
+}
+
+struct FewLayout {
+    size_t idx, logits, gate, h, total;
+};
+FewLayout few_layout(const moe_shape& s) {
+    FewLayout L;
+    size_t o = 0;
+    auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
+    const size_t ep = (size_t)route_gemm_config(s).ep;
+    L.idx = take((size_t)s.T * s.top_k * 4);
+    L.logits = take((size_t)s.T * ep * 4);
+    L.gate = take(ep * s.H * 2);
+    L.h = take(few_h_bytes(s));
+    L.total = std::max<size_t>(o, 256);
+    return L;
+}
+
 // Why rows x K cannot be held in MXFP4 (any_rows: rows of x, of any number), or nullptr.
 const char* fp4_size_problem(int64_t rows, int64_t K, bool any_rows) {
     if (K < 32 || K % 32 || rows < 0 || (!any_rows && (rows < 32 || rows % 32)))
@@ -1629,6 +1656,61 @@ moe_status moe_mx_grouped_product(moe_ctx* c, int32_t rows, int32_t K, int32_t N
     p.out_fp32 = out_fp32;
     p.scales_at = (uint32_t)fp4_scales_at(N, K);
     HIP_TRY(c, launch_fp4_product(p, gated != 0, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+size_t moe_few_workspace_bytes(const moe_shape* s) {
+    moe_status st;
+    return few_shape_problem(s, &st) ? 0 : few_layout(*s).total;
+}
+
+moe_status moe_layer_few(moe_ctx* c, const moe_shape* s, const void* x, const void* wg, const float* bias, const moe_weight_list* list, void* out,
+                         void* ws, size_t ws_bytes, void* stream) {
+    if (!c) return MOE_E_ARG;
+    c->err[0] = 0;
+    moe_status st;
+    if (const char* why = few_shape_problem(s, &st)) return fail(c, st, "layer_few: %s", why);
+    if (moe_status bad = check_list(c, "layer_few", list)) return bad;
+    if (list->experts != s->E + s->num_shared || list->matrices != 3)
+        return fail(c, MOE_E_ARG, "layer_few: a list of 3 matrices of %d experts required", (int)(s->E + s->num_shared));
+    if (s->T == 0) return MOE_OK;   // an empty batch: nothing to do
+    if (!x || !wg || !out) return fail(c, MOE_E_ARG, "layer_few: NULL pointer");
+    if (x == out) return fail(c, MOE_E_ARG, "layer_few: out must not be x");
+    if (misaligned({x, out}, 16) || misaligned({wg}, c->gate_packed ? 16 : 2) || misaligned({bias}, 4)) return fail(c, MOE_E_ARG, "layer_few: misaligned pointer");
+    if (!ws) return fail(c, MOE_E_ARG, "workspace is NULL");
+    if ((uintptr_t)ws & 255) return fail(c, MOE_E_ARG, "workspace must be 256-byte aligned");
+    const FewLayout L = few_layout(*s);
+    if (ws_bytes < L.total) return fail(c, MOE_E_WORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, L.total);
+    HIP_TRY(c, hipSetDevice(c->device));
+    char* const w8 = (char*)ws;
+    hipStream_t hs = (hipStream_t)stream;
+    const char* packed = (const char*)wg;
+    if (!c->gate_packed) {
+        HIP_TRY(c, launch_pack_weight(wg, s->H, s->E, route_gemm_config(*s).ep, w8 + L.gate, hs));
+        packed = w8 + L.gate;
+    }
+    FewArgs a = {};
+    a.x = (const char*)x;
+    a.wg = packed;
+    a.bias = bias;
+    a.ep = route_gemm_config(*s).ep;
+    if (!few_routes_inside(*s)) a.logits = a.logits_out = (float*)(w8 + L.logits);
+    a.weights = (const void* const*)list->buffer;
+    a.idx = (int32_t*)(w8 + L.idx);
+    a.h = w8 + L.h;
+    a.out = (char*)out;
+    a.T = s->T;
+    a.H = s->H;
+    a.F = s->F;
+    a.E = s->E;
+    a.k = s->top_k;
+    a.Ns = s->num_shared;
+    a.renorm = s->renormalize;
+    a.scale = s->routed_scale;
+    a.out_fp32 = c->out_fp32;
+    a.up_scales_at = (uint32_t)fp4_scales_at(s->F, s->H);
+    a.down_scales_at = (uint32_t)fp4_scales_at(s->H, s->F);
+    HIP_TRY(c, launch_few(a, list->fp4 != 0, hs));
     return MOE_OK;
 }
 

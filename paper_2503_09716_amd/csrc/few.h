@@ -1,0 +1,26 @@
+// The whole layer for up to 16 tokens (few.hip): arguments and launchers.
+#pragma once
+#include "common.h"
+
+namespace moe {
+
+constexpr int FEW_TOKENS = 16, FEW_TOP_K = 16;
+
+struct FewArgs {
+    const char *x, *wg;                  // tokens; packed gate matrix
+    const float *bias, *logits;          // bias: or nullptr; logits [T][ep]: computed by a launch before, or nullptr
+    float* logits_out;                   // that launch's
+    const void* const* weights;          // device table of packed matrices [3][E + Ns]
+    int32_t* idx;                        // [T * k]
+    char* h;                             // [T * k + Ns * T] rows of F: 8 values as bf16, then what that leaves of them as bf16
+    char* out;
+    int32_t T, H, F, E, k, Ns, ep, renorm, out_fp32;
+    float scale;
+    uint32_t up_scales_at, down_scales_at;   // MXFP4: of a matrix, its scales
+};
+size_t few_h_bytes(const moe_shape& s);
+hipError_t launch_few(const FewArgs& a, bool fp4, hipStream_t st);
+bool few_routes_inside(const moe_shape& s);   // no launch for the logits
+hipError_t few_init();
+
+}  // namespace moe
