@@ -45,6 +45,7 @@ struct moe_ctx {
     int layer_y = -1;      // moe_layer's y_perm: 1 fp32, 0 bf16, -1 choose (its y_shared is always fp32)
     bool out_fp32 = false; // dtype of the layer output
     hipError_t route_backward_ready = hipSuccess;   // what setting up moe_route_backward's kernels gave
+    hipError_t fp4_product_ready = hipSuccess;      // the same of moe_mx_grouped_product's
     bool gate_packed = false;  // E > 16: the wg argument is already in the packed layout (moe_pack_gate)
     char* static_ws = nullptr;  // this device's address of `scratch`
     // Ring of device pointer tables [3][MAX_GROUPS] (W1p, W3p, W2p), each with a pinned host
@@ -1021,6 +1022,8 @@ moe_status moe_create(moe_ctx** out, int device) {
     bool ok = ffn_gemm_init() == hipSuccess;
     c->route_backward_ready = route_backward_init();
     if (c->route_backward_ready != hipSuccess) (void)hipGetLastError();   // theirs alone: the other calls do not need these kernels
+    c->fp4_product_ready = fp4_product_init();
+    if (c->fp4_product_ready != hipSuccess) (void)hipGetLastError();
     ok = ok && hipGetSymbolAddress((void**)&c->static_ws, HIP_SYMBOL(scratch)) == hipSuccess && c->static_ws != nullptr &&
          ((uintptr_t)c->static_ws & 255) == 0;
     ok = ok && hipStreamCreateWithFlags(&c->copy_stream, hipStreamNonBlocking) == hipSuccess &&
@@ -1637,6 +1640,7 @@ moe_status moe_mx_grouped_product(moe_ctx* c, int32_t rows, int32_t K, int32_t N
     const Fp4Layout L = fp4_layout(rows, list->experts);
     if (ws_bytes < L.total) return fail(c, MOE_E_WORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, L.total);
     HIP_TRY(c, hipSetDevice(c->device));
+    HIP_TRY(c, c->fp4_product_ready);
     Fp4Product p = {};
     p.codes = (const char*)xq;
     p.scales = p.codes + fp4_scales_at(x_rows, K);

@@ -21,6 +21,5 @@ struct FewArgs {
 size_t few_h_bytes(const moe_shape& s);
 hipError_t launch_few(const FewArgs& a, bool fp4, hipStream_t st);
 bool few_routes_inside(const moe_shape& s);   // no launch for the logits
-hipError_t few_init();
 
 }  // namespace moe

@@ -38,12 +38,13 @@ struct Fp4Product {
     int32_t rows, E, K, N, sub_tiles, groups;
     int32_t out_fp32;
     uint32_t scales_at;           // of a weight matrix: its scales, from its start
-    int32_t n_tiles, max_mtiles;
+    int32_t n_tiles, max_mtiles, group_m;
 };
 struct Fp4Layout {
     size_t plan, descs, total;
 };
 Fp4Layout fp4_layout(int64_t rows, int E);
+hipError_t fp4_product_init();
 hipError_t launch_fp4_product(const Fp4Product& p, bool gated, hipStream_t st);
 
 }  // namespace moe
