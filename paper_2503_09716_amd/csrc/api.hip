@@ -1630,6 +1630,8 @@ moe_status moe_mx_grouped_product(moe_ctx* c, int32_t rows, int32_t K, int32_t N
     if (moe_status st = check_list(c, "mx_grouped_product", list)) return st;
     if (!list->fp4) return fail(c, MOE_E_ARG, "mx_grouped_product: the list is not of MXFP4 matrices");
     if (first < 0 || first + gated >= list->matrices) return fail(c, MOE_E_ARG, "mx_grouped_product: the list has no matrix %d", (int)(first + gated));
+    if (fp4_tiles(rows, list->experts, N, gated != 0) > 0x7fffffff || (int64_t)256 * N * 4 >= (int64_t)1 << 31)
+        return fail(c, MOE_E_UNSUPPORTED, "mx_grouped_product: too many rows or columns");
     if (rows == 0) return MOE_OK;
     if (!xq || !offsets || !out) return fail(c, MOE_E_ARG, "mx_grouped_product: NULL pointer");
     if (row_index ? x_rows == 0 : x_rows < rows) return fail(c, MOE_E_ARG, "mx_grouped_product: xq has fewer rows than the product");

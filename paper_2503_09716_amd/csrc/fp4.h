@@ -44,6 +44,7 @@ struct Fp4Layout {
     size_t plan, descs, total;
 };
 Fp4Layout fp4_layout(int64_t rows, int E);
+int64_t fp4_tiles(int64_t rows, int E, int64_t N, bool gated);   // workgroups at most
 hipError_t fp4_product_init();
 hipError_t launch_fp4_product(const Fp4Product& p, bool gated, hipStream_t st);
 

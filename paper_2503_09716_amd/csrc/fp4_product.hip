@@ -3,6 +3,7 @@
 //   plain: out[r, n] = sum_k x[r, k] W_e[k, n]        gated: out[r, n] = silu(x[r] . Wa_e[n]) * (x[r] . Wb_e[n])
 // for the rows r of group e.  v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 x 128 by 128 x 16 values in 16 cycles, four times what
 // the bf16 form does, and takes one scale for 32 values of a row.
+#include <algorithm>
 #include <initializer_list>
 #include <type_traits>
 
@@ -12,104 +13,33 @@
 namespace moe {
 namespace {
 
-constexpr int DIRECT_ROWS = 64;
-
-__device__ __forceinline__ f32x4 mfma_fp4(const i32x4 a, const i32x4 b, const f32x4 c, const uint32_t sa, const uint32_t sb) {
-#if defined(__gfx950__)
-    typedef int i32x8 __attribute__((ext_vector_type(8)));
-    const i32x8 x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)sa, 0, (int)sb);
-#else
-    return c;
-#endif
-}
-
 __device__ __forceinline__ float silu_times(const float g, const float u) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u; }
 
 __global__ __launch_bounds__(256) void fp4_plan_kernel(const PlanArgs p) { plan_list(p, 0, p.offsets); }
 
-// One wavefront: 16 columns of up to 64 rows of one group over the whole of K, straight from memory.  W is the row operand: a
-// lane has four neighbouring columns of one row.
-template <bool GATED>
-__global__ __launch_bounds__(256) void fp4_direct_kernel(const Fp4Product p) {
-    constexpr int XB = DIRECT_ROWS / 16, WM = GATED ? 2 : 1;
-    const int lane = threadIdx.x & 63, rl = lane & 15, g = lane >> 4;
-    const int mt = blockIdx.x / p.n_tiles;
-    const int n16 = (blockIdx.x - mt * p.n_tiles) * 4 + (threadIdx.x >> 6);
-    if (mt >= p.plan->n_gate_up || n16 * 16 >= p.N) return;
-    TileDesc d = p.descs[mt];
-    d.nrows &= TILE_ROWS_MASK;
-    const char* w[2];
-    const char* ws[2];
-#pragma unroll
-    for (int m = 0; m < WM; ++m) {
-        const char* const base = (const char*)(m == 0 ? p.wa : p.wb)[d.group];
-        w[m] = base + (size_t)n16 * p.sub_tiles * 1024 + rl * 64 + ((g ^ block_swizzle(rl)) << 4);
-        ws[m] = base + p.scales_at + (size_t)n16 * p.groups * 256 + rl * 16 + g * 4;
-    }
-    const char *x[XB], *xs[XB];
-#pragma unroll
-    for (int i = 0; i < XB; ++i) {
-        const int r = d.row0 + min(i * 16 + rl, d.nrows - 1);
-        const size_t at = p.row_index ? p.row_index[r] : r;
-        x[i] = p.codes + at * p.sub_tiles * 64 + g * 16;
-        xs[i] = p.scales + at * p.groups * 16 + g * 4;
-    }
-    f32x4 acc[WM][XB];
-#pragma unroll
-    for (int m = 0; m < WM; ++m)
-#pragma unroll
-        for (int i = 0; i < XB; ++i) acc[m][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    uint32_t sw[WM], sx[XB];
-    for (int t = 0; t < p.sub_tiles; ++t) {
-        if ((t & 3) == 0) {
-#pragma unroll
-            for (int m = 0; m < WM; ++m) sw[m] = *reinterpret_cast<const uint32_t*>(ws[m] + (t >> 2) * 256);
-#pragma unroll
-            for (int i = 0; i < XB; ++i) sx[i] = *reinterpret_cast<const uint32_t*>(xs[i] + (t >> 2) * 16);
-        }
-        i32x4 a[WM], b[XB];
-#pragma unroll
-        for (int m = 0; m < WM; ++m) a[m] = *reinterpret_cast<const i32x4*>(w[m] + (size_t)t * 1024);
-#pragma unroll
-        for (int i = 0; i < XB; ++i) b[i] = *reinterpret_cast<const i32x4*>(x[i] + t * 64);
-#pragma unroll
-        for (int m = 0; m < WM; ++m)
-#pragma unroll
-            for (int i = 0; i < XB; ++i) acc[m][i] = mfma_fp4(a[m], b[i], acc[m][i], sw[m], sx[i]);
-#pragma unroll
-        for (int m = 0; m < WM; ++m) sw[m] >>= 8;
-#pragma unroll
-        for (int i = 0; i < XB; ++i) sx[i] >>= 8;
-    }
-    const int esz = p.out_fp32 ? 4 : 2;
-#pragma unroll
-    for (int i = 0; i < XB; ++i) {
-        if (i * 16 + rl >= d.nrows) continue;
-        char* const at = p.out + ((size_t)(d.row0 + i * 16 + rl) * p.N + n16 * 16 + g * 4) * esz;
-        f32x4 v = acc[0][i];
-        if (GATED)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = silu_times(v[q], acc[WM - 1][i][q]);
-        if (p.out_fp32) {
-            *reinterpret_cast<f32x4*>(at) = v;
-        } else {
-            bf16x4 o;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = (__bf16)v[q];
-            *reinterpret_cast<bf16x4*>(at) = o;
-        }
-    }
-}
-
 // ---- tiles ---------------------------------------------------------------------------------
-// A workgroup of four wavefronts (one to a SIMD) multiplies up to 256 rows of x with 256 rows of W (gated: 128 of each matrix, so that the
-// gate meets its up value in registers) in sub-tiles of 128 along K.  Codes go from memory straight into a ring of four LDS stages of
-// 64-byte rows, three sub-tiles ahead; a row's 16 scale bytes of a group of four sub-tiles into a ring of two.  Each wavefront has all rows
-// of x and 64 of W: 256 accumulators.  A fragment is read from the next stage right after its last use, and one barrier a sub-tile hands the ring over.
-constexpr int ROWB = 64, NS = 4, TILE_ROWS = 256, WROWS = 256;
-constexpr int SCALE_X = TILE_ROWS * 16, SCALE_STAGE = SCALE_X + WROWS * 16;
-constexpr int TILE_LDS = NS * (TILE_ROWS + WROWS) * ROWB + 2 * SCALE_STAGE;
+// A workgroup multiplies up to ROWS rows of x with 256 rows of W (gated: 128 of each matrix, so that the gate meets its up value in registers) in
+// sub-tiles of 128 along K.  Codes go from memory straight into a ring of NS LDS stages of 64-byte rows, NS - 1 sub-tiles ahead; a row's 16
+// scale bytes of a group of four sub-tiles into places of their own.  A fragment is read from the next stage right after its last use, and one
+// barrier a sub-tile hands the ring over.  Two forms:
+struct Long {    // long batches: one workgroup of eight wavefronts to a CU, which takes every 256th tile and asks for the next one's first sub-tiles behind the
+                 // last ones of its own
+    static constexpr int NW = 8, NS = 4, ROWS = 256, MW = 2, SCALES = 2;   // MW: wavefronts side by side along x
+    static constexpr bool NEXT = true;
+};
+struct Short {   // short and ragged ones: two workgroups of four wavefronts to a CU, one tile each
+    static constexpr int NW = 4, NS = 3, ROWS = 128, MW = 1, SCALES = 1;
+    static constexpr bool NEXT = false;
+};
+constexpr int ROWB = 64, WROWS = 256;
+template <class C>
+struct Ring {
+    static constexpr int X = C::ROWS * ROWB, STAGE = X + WROWS * ROWB;
+    static constexpr int SCALE_X = C::ROWS * 16, SCALE_STAGE = SCALE_X + WROWS * 16;
+    static constexpr int BYTES = C::NS * STAGE + C::SCALES * SCALE_STAGE;
+    static constexpr int XL = C::ROWS / 16 / C::NW, WL = WROWS / 16 / C::NW;   // loads of a sub-tile per wavefront, of a tile of full height
+};
+static_assert(Ring<Long>::BYTES <= 160 * 1024 && Ring<Short>::BYTES <= 80 * 1024, "LDS");
 
 typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
@@ -129,20 +59,23 @@ __device__ __forceinline__ void load_lds(const __amdgpu_buffer_rsrc_t rsrc, lptr
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, l, 16, voff, soff, 0, 0);
 #endif
 }
+template <bool NT>
 __device__ __forceinline__ void store_b128(const __amdgpu_buffer_rsrc_t rsrc, const uint32_t voff, const u32x4 v) {
 #if defined(__gfx950__)
-    __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, voff, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, voff, 0, NT ? 2 : 0);
 #endif
 }
+template <bool NT>
 __device__ __forceinline__ void store_b32(const __amdgpu_buffer_rsrc_t rsrc, const uint32_t voff, const float v) {
 #if defined(__gfx950__)
-    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rsrc, voff, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rsrc, voff, 0, NT ? 2 : 0);
 #endif
 }
+template <bool NT>
 __device__ __forceinline__ void store_bf16(const __amdgpu_buffer_rsrc_t rsrc, const uint32_t voff, const float v) {
 #if defined(__gfx950__)
     const __bf16 b = (__bf16)v;
-    __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, b), rsrc, voff, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, b), rsrc, voff, 0, NT ? 2 : 0);
 #endif
 }
 // Lanes 16..31 and 48..63 of a and lanes 0..15 and 32..47 of b change places; both halves as one piece.
@@ -167,6 +100,21 @@ __device__ __forceinline__ void mfma_tile(f32x4& c, const i32x4& a, const i32x4&
                  : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
 #endif
 }
+// The same on an accumulator of zeros.
+__device__ __forceinline__ void mfma_tile_first(f32x4& c, const i32x4& a, const i32x4& b, const uint32_t sa, const uint32_t sb) {
+#if defined(__gfx950__)
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, 0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+                 : "=a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+#endif
+}
+// Here, not earlier: left alone all accumulators are copied ahead of the first store.
+__device__ __forceinline__ float read_acc(const float& a) {
+    float v = 0.f;
+#if defined(__gfx950__)
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a) : "memory");
+#endif
+    return v;
+}
 __device__ __forceinline__ void mfma_drain() {
 #if defined(__gfx950__)
     asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
@@ -182,233 +130,22 @@ __device__ __forceinline__ void ring_sync() {
     asm volatile("" ::: "memory");
 }
 
-template <int TI, bool GATED>
-__device__ __forceinline__ void tile_product(const Fp4Product& p, const TileDesc d, const int n_tile, char* lds) {
-    constexpr int NW = 4, BM = TI * 32, XB = 2 * TI, WB = 4, WBH = 2;
-    constexpr int NLX = (BM / 16 + NW - 1) / NW, XBYTES = NLX * NW * 1024, NL = NLX + WROWS / 16 / NW, STAGE = NL * NW * 1024;
-    constexpr int BN = GATED ? 128 : WROWS;
-    constexpr int NL0 = XB * NL / (2 * XB);   // loads of a sub-tile issued before its hand-over
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rl = lane & 15, g = lane >> 4;
-    const int N = p.N, n0 = n_tile * BN, KT = p.sub_tiles;
-    lds_t const ring = (lds_t)lds, scale_ring = ring + NS * STAGE;
+// A tile: what its loads need, one tile ahead of its use.
+template <class C>
+struct TileLoads {
+    const char *w_at, *u_at;                    // the matrix (gated: gate, up)
+    uint32_t x[Ring<C>::XL], w[Ring<C>::WL], xs, ws;   // offsets of this lane's pieces
+    int row0, nrows, n0;
+    bool any;
+};
 
-    // loads: rows of x, then blocks of W, each wave every fourth
-    const int lrow = lane >> 2, lpiece = (lane & 3) ^ block_swizzle(lrow);
-    uint32_t loff[NL];
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-        const int q = i * NW + wave;
-        if (i < NLX) {
-            const int r = d.row0 + min(q * 16 + lrow, d.nrows - 1);   // rows past the end are the last one again
-            const uint32_t at = p.row_index ? p.row_index[r] : r;
-            loff[i] = at * (uint32_t)(KT * 64) + (uint32_t)(lpiece * 16);
-        } else {
-            const int qw = q - NLX * NW, grp = min((n0 >> 4) + (GATED ? (qw & 7) : qw), (N >> 4) - 1);
-            loff[i] = (uint32_t)grp * (uint32_t)(KT * 1024) + (uint32_t)(lane * 16);
-        }
-    }
-    uint32_t xs_off, ws_off;
-    {
-        const int r = d.row0 + min(wave * 64 + lane, d.nrows - 1);
-        xs_off = (uint32_t)(p.row_index ? p.row_index[r] : r) * (uint32_t)(p.groups * 16);
-        const int wr = wave * 64 + lane, n = min(n0 + (GATED ? (wr & 127) : wr), N - 1);
-        ws_off = p.scales_at + (uint32_t)(n >> 4) * (uint32_t)(p.groups * 256) + (uint32_t)((n & 15) * 16);
-    }
-    const __amdgpu_buffer_rsrc_t rs_x = rsrc_of(p.codes), rs_xs = rsrc_of(p.scales), rs_w = rsrc_of(p.wa[d.group]), rs_u = rsrc_of((GATED ? p.wb : p.wa)[d.group]);
-    const __amdgpu_buffer_rsrc_t rs_ws = GATED && wave >= 2 ? rs_u : rs_w;
-    int koff_x = 0, koff_w = 0;
-    auto issue_one = [&](const int i, const int stage) __attribute__((always_inline)) {
-        lptr_t dst = (lptr_t)(ring + stage * STAGE + (i * NW + wave) * 1024);
-        if (i < NLX) load_lds(rs_x, dst, loff[i], koff_x);
-        else if (GATED && (i - NLX) * NW >= 8) load_lds(rs_u, dst, loff[i], koff_w);
-        else load_lds(rs_w, dst, loff[i], koff_w);
-    };
-    auto issue_scales = [&](const int q) __attribute__((always_inline)) {
-        lds_t const dst = scale_ring + (q & 1) * SCALE_STAGE + wave * 1024;
-        load_lds(rs_xs, (lptr_t)dst, xs_off, q * 16);
-        load_lds(rs_ws, (lptr_t)(dst + SCALE_X), ws_off, q * 256);
-    };
-
-    const uint32_t offX = (uint32_t)(rl * ROWB + ((g ^ block_swizzle(rl)) << 4));
-    const uint32_t offW = offX + (uint32_t)(XBYTES + wave * (GATED ? 32 : 64) * ROWB);
-    const uint32_t offSX = (uint32_t)(rl * 16 + g * 4), offSW = offSX + (uint32_t)(SCALE_X + wave * (GATED ? 32 : 64) * 16);
-    auto w_row = [](const int hf, const int jj) __attribute__((always_inline)) { return GATED ? hf * 128 + jj * 16 : (hf * WBH + jj) * 16; };
-
-    f32x4 acc[WB][XB];
-#pragma unroll
-    for (int j = 0; j < WB; ++j)
-#pragma unroll
-        for (int i = 0; i < XB; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[j][i][r] = 0.f;
-    i32x4 xf[XB], wA[WBH], wB[WBH];
-    uint32_t sx[XB], sw[WB], sx_next[XB], sw_next[WB];
-    auto read_x = [&](const int stage, const int i) __attribute__((always_inline)) { xf[i] = *(lfrag_t)(ring + stage * STAGE + offX + i * 16 * ROWB); };
-    auto read_w = [&](const int stage, const int hf, const int jj) __attribute__((always_inline)) {
-        const i32x4 v = *(lfrag_t)(ring + stage * STAGE + offW + w_row(hf, jj) * ROWB);
-        if (hf == 0) wA[jj] = v;
-        else wB[jj] = v;
-    };
-    auto read_scales = [&](const int q) __attribute__((always_inline)) {
-        lds_t const from = scale_ring + (q & 1) * SCALE_STAGE;
-#pragma unroll
-        for (int i = 0; i < XB; ++i) sx_next[i] = *(lword_t)(from + offSX + i * 256);
-#pragma unroll
-        for (int j = 0; j < WB; ++j) sw_next[j] = *(lword_t)(from + offSW + w_row(j / WBH, j % WBH) * 16);
-    };
-
-    // Half HF of a sub-tile: XB groups of two matrix instructions with one block of x.
-    auto part = [&](auto hf_tag, auto rd_tag, auto ld_tag, const int cur, const int nxt, const int ld_stage) __attribute__((always_inline)) {
-        constexpr int HF = decltype(hf_tag)::value;
-        constexpr bool RD = decltype(rd_tag)::value, LD = decltype(ld_tag)::value;
-#pragma unroll
-        for (int i = 0; i < XB; ++i) {
-#pragma unroll
-            for (int jj = 0; jj < WBH; ++jj) {
-                const int j = HF * WBH + jj;
-                const i32x4 w = HF == 0 ? wA[jj] : wB[jj];
-                if (GATED) mfma_tile(acc[j][i], w, xf[i], sw[j], sx[i]);
-                else mfma_tile(acc[j][i], xf[i], w, sx[i], sw[j]);
-            }
-            if (HF == 1 && RD) read_x(nxt, i);
-            if (i < WBH && (HF == 0 || RD)) read_w(HF == 0 ? cur : nxt, HF == 0 ? 1 : 0, i);
-            if (LD) {
-                constexpr int G = 2 * XB;
-                const int q = HF * XB + i;
-#pragma unroll
-                for (int l = (q * NL) / G; l < ((q + 1) * NL) / G; ++l) issue_one(l, ld_stage);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-    using T_ = std::true_type;
-    using F_ = std::false_type;
-    using H0 = std::integral_constant<int, 0>;
-    using H1 = std::integral_constant<int, 1>;
-    // Sub-tile t; its scales are byte 0 of sx and sw.
-    auto sub_tile = [&](auto rd_tag, auto ld_tag, const int t, auto sync) __attribute__((always_inline)) {
-        if ((t & 3) == 0) {
-#pragma unroll
-            for (int i = 0; i < XB; ++i) sx[i] = sx_next[i];
-#pragma unroll
-            for (int j = 0; j < WB; ++j) sw[j] = sw_next[j];
-            if (t + 4 < KT) issue_scales((t >> 2) + 1);
-        } else {
-#pragma unroll
-            for (int i = 0; i < XB; ++i) sx[i] >>= 8;
-#pragma unroll
-            for (int j = 0; j < WB; ++j) sw[j] >>= 8;
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_nop 3" ::: "memory");   // between those and the first matrix instruction
-        const int cur = t % NS, nxt = (t + 1) % NS, ld = (t + NS - 1) % NS;
-        part(H0{}, rd_tag, ld_tag, cur, nxt, ld);
-        sync();
-        // the scales of the next group came in during this one's first sub-tile
-        if ((t & 3) == 3 && t + 1 < KT) read_scales((t >> 2) + 1);
-        part(H1{}, rd_tag, ld_tag, cur, nxt, ld);
-    };
-
-    issue_scales(0);
-#pragma unroll
-    for (int s = 0; s < NS - 1; ++s) {
-        if (s < KT) {
-#pragma unroll
-            for (int i = 0; i < NL; ++i) issue_one(i, s);
-            koff_x += 64;
-            koff_w += 1024;
-        }
-    }
-    if (KT >= NS - 1) ring_sync<(NS - 2) * NL>();
-    else ring_sync<0>();
-    read_scales(0);
-#pragma unroll
-    for (int i = 0; i < XB; ++i) {
-        read_x(0, i);
-        if (i < WBH) read_w(0, 0, i);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    int t = 0;
-    for (; t + NS - 1 < KT; ++t) {
-        // Scales may be among the loads that are younger than sub-tile t + 1, which then waits for a few more than it has to.
-        sub_tile(T_{}, T_{}, t, [] __attribute__((always_inline)) { ring_sync<(NS - 3) * NL + NL0>(); });
-        koff_x += 64;
-        koff_w += 1024;
-    }
-    auto drain = [] __attribute__((always_inline)) { ring_sync<0>(); };
-    for (; t < KT - 1; ++t) sub_tile(T_{}, F_{}, t, drain);
-    sub_tile(F_{}, F_{}, t, drain);
-
-    mfma_drain();
-    __builtin_amdgcn_sched_barrier(0);
-    if (GATED) {
-        // W is the row operand: a lane has the four columns 4g .. 4g+3 of row rl of a block; lanes 16 apart swap halves of two blocks, so that each has
-        // 16 bytes of a row and a store covers 16 rows x 64 bytes.
-        const uint32_t rowbytes = (uint32_t)N * (p.out_fp32 ? 4u : 2u);
-        const __amdgpu_buffer_rsrc_t rs_o = rsrc_of(p.out + (size_t)d.row0 * rowbytes, (uint32_t)d.nrows * rowbytes);
-        const int col = n0 + wave * 32;
-        if (col >= N) return;   // N is a multiple of 32
-#pragma unroll
-        for (int i = 0; i < XB; ++i) {
-            float v[2][4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) v[j][q] = silu_times(acc[j][i][q], acc[WBH + j][i][q]);
-            const int row = i * 16 + rl;
-            const bool ok = row < d.nrows;
-            if (p.out_fp32) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    store_b128(rs_o, ok ? (uint32_t)row * rowbytes + (uint32_t)(col + j * 16 + g * 4) * 4u : 0xFFFFFFF0u,
-                               u32x4{__float_as_uint(v[j][0]), __float_as_uint(v[j][1]), __float_as_uint(v[j][2]), __float_as_uint(v[j][3])});
-            } else {
-                u32x2 o[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const bf16x4 b = {(__bf16)v[j][0], (__bf16)v[j][1], (__bf16)v[j][2], (__bf16)v[j][3]};
-                    o[j] = __builtin_bit_cast(u32x2, b);
-                }
-                // lane g: block g & 1, columns 8 (g >> 1) .. + 7 of it
-                store_b128(rs_o, ok ? (uint32_t)row * rowbytes + (uint32_t)(col + (g & 1) * 16 + (g >> 1) * 8) * 2u : 0xFFFFFFF0u, swap_rows16(o[0], o[1]));
-            }
-            if (i % 2) __builtin_amdgcn_sched_barrier(0);
-        }
-    } else {
-        // x is the row operand: a lane has column rl of a block and rows 4g .. 4g+3; a store covers 4 rows x 64 bytes (fp32)
-        auto store_tile = [&](auto f32_tag) __attribute__((always_inline)) {
-            constexpr bool F32 = decltype(f32_tag)::value;
-            constexpr int esz = F32 ? 4 : 2;
-            const uint32_t rowbytes = (uint32_t)N * (uint32_t)esz;
-            uint32_t vcol[WB][4];
-#pragma unroll
-            for (int j = 0; j < WB; ++j) {
-                const int col = n0 + wave * 64 + j * 16 + rl;
-                const uint32_t base = col < N ? (uint32_t)(g * 4) * rowbytes + (uint32_t)col * esz : 0x80000000u;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) vcol[j][r] = base + (uint32_t)r * rowbytes;
-            }
-#pragma unroll
-            for (int i = 0; i < XB; ++i) {
-                const int left = min(max(d.nrows - i * 16, 0), 16);
-                const __amdgpu_buffer_rsrc_t rs_o = rsrc_of(p.out + (size_t)(d.row0 + i * 16) * rowbytes, (uint32_t)left * rowbytes);
-#pragma unroll
-                for (int j = 0; j < WB; ++j)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float v;   // read here, not earlier: left alone all accumulators are copied ahead of the first store
-                        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[j][i][r]) : "memory");
-                        if (F32) store_b32(rs_o, vcol[j][r], v);
-                        else store_bf16(rs_o, vcol[j][r], v);
-                    }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        };
-        if (p.out_fp32) store_tile(T_{});
-        else store_tile(F_{});
-    }
+// Through the scalar cache: what the launch before left, at an address that is the same for the wavefront.
+template <class T>
+__device__ __forceinline__ T scalar_load(const T* ptr) {
+    return *(const __attribute__((address_space(4))) T*)(uintptr_t)ptr;
 }
+
+__device__ __forceinline__ int row_of(const Fp4Product& p, const int r) { return p.row_index ? p.row_index[r] : r; }
 
 // Workgroup id -> position in the order of the tiles: ids are dealt to the 8 XCDs in turn; inside each whole round of 256 tiles an XCD gets a run of 32.
 __device__ __forceinline__ int tile_order(const int wg, const int total) {
@@ -417,11 +154,13 @@ __device__ __forceinline__ int tile_order(const int wg, const int total) {
     return (wg - r) + (r & 7) * 32 + (r >> 3);
 }
 
+// The tile at place `at` of the launch: its descriptor (nrows = 0: there is none) and columns.
 template <bool GATED>
-__global__ __launch_bounds__(256, 1) void fp4_tile_kernel(const Fp4Product p) {
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const int count = p.plan->n_gate_up, n_run = p.plan->n_run_up;
-    const int L = tile_order(blockIdx.x, count * p.n_tiles);
+__device__ __forceinline__ TileDesc tile_at(const Fp4Product& p, const int count, const int n_run, const int at, int& n0) {
+    TileDesc d = {0, 0, 0, 0};
+    n0 = 0;
+    if (at >= count * p.n_tiles) return d;
+    const int L = tile_order(at, count * p.n_tiles);
     int mt, n_tile;
     if (L < n_run * p.n_tiles) {   // group_m m-tiles side by side along n: they share panels of W, and those along n panels of x
         const int per = p.group_m * p.n_tiles, sr = L / per, rem = L - sr * per;
@@ -433,25 +172,405 @@ __global__ __launch_bounds__(256, 1) void fp4_tile_kernel(const Fp4Product p) {
         mt = n_run + rem / p.n_tiles;
         n_tile = rem - (mt - n_run) * p.n_tiles;
     }
-    if (mt >= count) return;
-    TileDesc d = p.descs[mt];
+    const i32x4 v = scalar_load((const i32x4*)p.descs + __builtin_amdgcn_readfirstlane(mt));
+    d = TileDesc{v[0], v[1], v[2], v[3]};
     d.nrows &= TILE_ROWS_MASK;
-    const int blocks = (d.nrows + 31) >> 5;
-    if (blocks > 7) tile_product<8, GATED>(p, d, n_tile, lds);
-    else if (blocks > 6) tile_product<7, GATED>(p, d, n_tile, lds);
-    else if (blocks > 5) tile_product<6, GATED>(p, d, n_tile, lds);
-    else if (blocks > 4) tile_product<5, GATED>(p, d, n_tile, lds);
-    else if (blocks > 3) tile_product<4, GATED>(p, d, n_tile, lds);
-    else if (blocks > 2) tile_product<3, GATED>(p, d, n_tile, lds);
-    else if (blocks > 1) tile_product<2, GATED>(p, d, n_tile, lds);
-    else tile_product<1, GATED>(p, d, n_tile, lds);
+    n0 = n_tile * (GATED ? 128 : WROWS);
+    return d;
+}
+
+// Rows of x for the four pieces that this lane loads of a sub-tile, and for its scales; rows past the end are the last one again.
+template <class C>
+struct TileRows {
+    int x[Ring<C>::XL], xs;
+};
+template <class C>
+__device__ __forceinline__ TileRows<C> tile_rows(const Fp4Product& p, const TileDesc& d, const int lane, const int wave) {
+    TileRows<C> r = {};
+    if (d.nrows == 0) return r;
+#pragma unroll
+    for (int i = 0; i < Ring<C>::XL; ++i) r.x[i] = row_of(p, d.row0 + min((i * C::NW + wave) * 16 + (lane >> 2), d.nrows - 1));
+    r.xs = row_of(p, d.row0 + min((wave & 3) * 64 + lane, d.nrows - 1));
+    return r;
+}
+
+template <bool GATED>
+__device__ __forceinline__ void tile_weights(const Fp4Product& p, const TileDesc& d, const char*& w_at, const char*& u_at) {
+    const int group = __builtin_amdgcn_readfirstlane(d.group);
+    w_at = scalar_load((const char* const*)p.wa + group);
+    u_at = GATED ? scalar_load((const char* const*)p.wb + group) : w_at;
+}
+
+template <class C, bool GATED>
+__device__ __forceinline__ TileLoads<C> tile_loads(const Fp4Product& p, const TileDesc& d, const int n0, const TileRows<C>& rows, const char* w_at,
+                                                   const char* u_at, const int lane, const int wave) {
+    TileLoads<C> t;
+    t.row0 = d.row0;
+    t.nrows = d.nrows;
+    t.n0 = n0;
+    t.any = d.nrows > 0;
+    t.w_at = w_at;
+    t.u_at = u_at;
+    const int lrow = lane >> 2, lpiece = (lane & 3) ^ block_swizzle(lrow);
+#pragma unroll
+    for (int i = 0; i < Ring<C>::XL; ++i) t.x[i] = (uint32_t)rows.x[i] * (uint32_t)(p.sub_tiles * 64) + (uint32_t)(lpiece * 16);
+#pragma unroll
+    for (int i = 0; i < Ring<C>::WL; ++i) {
+        const int qw = i * C::NW + wave, block = min((n0 >> 4) + (GATED ? (qw & 7) : qw), (p.N >> 4) - 1);
+        t.w[i] = (uint32_t)block * (uint32_t)(p.sub_tiles * 1024) + (uint32_t)(lane * 16);
+    }
+    const int wr = (wave & 3) * 64 + lane, n = min(n0 + (GATED ? (wr & 127) : wr), p.N - 1);
+    t.xs = (uint32_t)rows.xs * (uint32_t)(p.groups * 16);
+    t.ws = p.scales_at + (uint32_t)(n >> 4) * (uint32_t)(p.groups * 256) + (uint32_t)((n & 15) * 16);
+    return t;
+}
+
+template <class C>
+__device__ __forceinline__ void load_x(const TileLoads<C>& t, const __amdgpu_buffer_rsrc_t rs_x, lds_t stage, const int wave, const int i, const int sub) {
+    load_lds(rs_x, (lptr_t)(stage + (i * C::NW + wave) * 1024), t.x[i], sub * 64);
+}
+template <class C, bool GATED>
+__device__ __forceinline__ void load_w(const TileLoads<C>& t, lds_t stage, const int wave, const int i, const int sub) {
+    load_lds(rsrc_of(GATED && i * 2 >= Ring<C>::WL ? t.u_at : t.w_at), (lptr_t)(stage + Ring<C>::X + (i * C::NW + wave) * 1024), t.w[i], sub * 1024);
+}
+// 64 rows of x or W to a wavefront: with eight of them one of the two, with four up to both.
+template <class C, bool GATED>
+__device__ __forceinline__ void load_scales(const TileLoads<C>& t, const __amdgpu_buffer_rsrc_t rs_xs, lds_t stage, const int wave, const int q) {
+    const int part = wave & 3;
+    if (wave < 4 && part * 64 < C::ROWS) load_lds(rs_xs, (lptr_t)(stage + part * 1024), t.xs, q * 16);
+    if (C::NW == 4 || wave >= 4)
+        load_lds(rsrc_of(GATED && part >= 2 ? t.u_at : t.w_at), (lptr_t)(stage + Ring<C>::SCALE_X + part * 1024), t.ws, q * 256);
+}
+// A whole sub-tile of a tile whose height the caller does not know.
+template <class C, bool GATED>
+__device__ __forceinline__ void load_sub_tile(const TileLoads<C>& t, const __amdgpu_buffer_rsrc_t rs_x, lds_t stage, const int wave, const int sub) {
+#pragma unroll
+    for (int i = 0; i < Ring<C>::XL; ++i)
+        if (i == 0 || i * C::NW * 16 < t.nrows) load_x<C>(t, rs_x, stage, wave, i, sub);
+#pragma unroll
+    for (int i = 0; i < Ring<C>::WL; ++i) load_w<C, GATED>(t, stage, wave, i, sub);
+}
+
+// A tile of TI * 32 rows: MW x 4 wavefronts, each with XB blocks of 16 rows of x and four of W (gated: two of each matrix).
+constexpr int WB = 4, WBH = 2;
+template <class C, int TI>
+struct Grid {
+    static constexpr int XB = 2 * TI / C::MW;
+    static __device__ __forceinline__ int x_row(const int wave) { return (wave >> 2) * XB * 16; }
+    // of the first of its rows of W (gated: in the gate's half, and as far into the other one)
+    static __device__ __forceinline__ int w_row(const int wave, const bool gated) { return (wave & 3) * (gated ? 32 : 64); }
+};
+
+// Multiplies tile t, whose first sub-tiles and scales are in the ring from stages `base` and `sbase` on.  NEXT: asks for the first ones of the next tile
+// behind the last ones of its own; when it returns, those have landed for every wavefront.
+template <class C, int TI, bool GATED>
+__device__ __forceinline__ void multiply(const Fp4Product& p, const TileLoads<C>& t, const TileLoads<C>& next, const __amdgpu_buffer_rsrc_t rs_x,
+                                         const __amdgpu_buffer_rsrc_t rs_xs, lds_t ring, const int base, const int sbase,
+                                         f32x4 (&acc)[WB][Grid<C, TI>::XB]) {
+    constexpr int XB = Grid<C, TI>::XB, NS = C::NS, STAGE = Ring<C>::STAGE;
+    constexpr int NLX = (2 * TI + C::NW - 1) / C::NW, NL = NLX + Ring<C>::WL;   // loads of a sub-tile per wavefront
+    constexpr int NL0 = XB * NL / (2 * XB);                                     // of them, those issued before the hand-over
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rl = lane & 15, g = lane >> 4;
+    const int KT = p.sub_tiles;
+    lds_t const scale_ring = ring + NS * STAGE;
+    const int x_row = Grid<C, TI>::x_row(wave), wn_row = Grid<C, TI>::w_row(wave, GATED);
+    const uint32_t off = (uint32_t)(rl * ROWB + ((g ^ block_swizzle(rl)) << 4)), offS = (uint32_t)(rl * 16 + g * 4);
+    const uint32_t offX = off + (uint32_t)(x_row * ROWB), offW = off + (uint32_t)(Ring<C>::X + wn_row * ROWB);
+    const uint32_t offSX = offS + (uint32_t)(x_row * 16), offSW = offS + (uint32_t)(Ring<C>::SCALE_X + wn_row * 16);
+    auto w_row = [](const int hf, const int jj) __attribute__((always_inline)) { return GATED ? hf * 128 + jj * 16 : (hf * WBH + jj) * 16; };
+    auto stage_of = [&](const int s) __attribute__((always_inline)) { return ring + (int)((uint32_t)(base + s) % NS) * STAGE; };
+    auto scales_of = [&](const int q) __attribute__((always_inline)) { return scale_ring + (int)((uint32_t)(sbase + q) % C::SCALES) * Ring<C>::SCALE_STAGE; };
+
+    i32x4 xf[XB], wA[WBH], wB[WBH];
+    uint32_t sx[XB], sw[WB], sx_next[XB], sw_next[WB];
+    auto read_x = [&](lds_t stage, const int i) __attribute__((always_inline)) { xf[i] = *(lfrag_t)(stage + offX + i * 16 * ROWB); };
+    auto read_w = [&](lds_t stage, const int hf, const int jj) __attribute__((always_inline)) {
+        const i32x4 v = *(lfrag_t)(stage + offW + w_row(hf, jj) * ROWB);
+        if (hf == 0) wA[jj] = v;
+        else wB[jj] = v;
+    };
+    auto read_scales = [&](const int q) __attribute__((always_inline)) {
+        lds_t const from = scales_of(q);
+#pragma unroll
+        for (int i = 0; i < XB; ++i) sx_next[i] = *(lword_t)(from + offSX + i * 256);
+#pragma unroll
+        for (int j = 0; j < WB; ++j) sw_next[j] = *(lword_t)(from + offSW + w_row(j / WBH, j % WBH) * 16);
+    };
+
+    // Half HF of sub-tile s: XB groups of two matrix instructions with one block of x.  RD: fragments of the next sub-tile are read, LD: sub-tile s + NS - 1 is
+    // asked for, spread over the groups.
+    auto part = [&](auto hf_tag, auto first_tag, auto rd_tag, auto ld_tag, const int s) __attribute__((always_inline)) {
+        constexpr int HF = decltype(hf_tag)::value;
+        constexpr bool FIRST = decltype(first_tag)::value, RD = decltype(rd_tag)::value, LD = decltype(ld_tag)::value;
+        lds_t const cur = stage_of(s), nxt = stage_of(s + 1), ahead = stage_of(s + NS - 1);
+#pragma unroll
+        for (int i = 0; i < XB; ++i) {
+#pragma unroll
+            for (int jj = 0; jj < WBH; ++jj) {
+                const int j = HF * WBH + jj;
+                const i32x4 w = HF == 0 ? wA[jj] : wB[jj];
+                if (FIRST && GATED) mfma_tile_first(acc[j][i], w, xf[i], sw[j], sx[i]);
+                else if (FIRST) mfma_tile_first(acc[j][i], xf[i], w, sx[i], sw[j]);
+                else if (GATED) mfma_tile(acc[j][i], w, xf[i], sw[j], sx[i]);
+                else mfma_tile(acc[j][i], xf[i], w, sx[i], sw[j]);
+            }
+            if (HF == 1 && RD) read_x(nxt, i);
+            constexpr int PER = (WBH + XB - 1) / XB;
+            if (HF == 0 || RD)
+#pragma unroll
+                for (int jj = i * PER; jj < (i + 1) * PER && jj < WBH; ++jj) read_w(HF == 0 ? cur : nxt, HF == 0 ? 1 : 0, jj);
+            if (LD) {
+                constexpr int G = 2 * XB;
+                const int q = HF * XB + i;
+#pragma unroll
+                for (int l = (q * NL) / G; l < ((q + 1) * NL) / G; ++l) {
+
+                    if (l < NLX) load_x<C>(t, rs_x, ahead, wave, l, s + NS - 1);
+                    else load_w<C, GATED>(t, ahead, wave, l - NLX, s + NS - 1);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    using T_ = std::true_type;
+    using F_ = std::false_type;
+    using H0 = std::integral_constant<int, 0>;
+    using H1 = std::integral_constant<int, 1>;
+    // Sub-tile s; its scales are byte 0 of sx and sw.
+    auto sub_tile = [&](auto first_tag, auto rd_tag, auto ld_tag, const int s, auto sync) __attribute__((always_inline)) {
+        if (decltype(first_tag)::value || (s & 3) == 0) {
+#pragma unroll
+            for (int i = 0; i < XB; ++i) sx[i] = sx_next[i];
+#pragma unroll
+            for (int j = 0; j < WB; ++j) sw[j] = sw_next[j];
+            if (C::SCALES == 2 && s + 4 < KT) load_scales<C, GATED>(t, rs_xs, scales_of((s >> 2) + 1), wave, (s >> 2) + 1);
+        } else {
+#pragma unroll
+            for (int i = 0; i < XB; ++i) sx[i] >>= 8;
+#pragma unroll
+            for (int j = 0; j < WB; ++j) sw[j] >>= 8;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 3" ::: "memory");   // between those and the first matrix instruction
+        part(H0{}, first_tag, rd_tag, ld_tag, s);
+        sync();
+        // one place for scales: free once every wavefront is here
+        if (C::SCALES == 1 && (s & 3) == 0 && s + 4 < KT) load_scales<C, GATED>(t, rs_xs, scales_of(0), wave, (s >> 2) + 1);
+        // the scales of the next group came in during this one's first sub-tile
+        if ((s & 3) == 3 && s + 1 < KT) read_scales((s >> 2) + 1);
+        part(H1{}, first_tag, rd_tag, ld_tag, s);
+    };
+
+    read_scales(0);
+#pragma unroll
+    for (int i = 0; i < XB; ++i) {
+        constexpr int PER = (WBH + XB - 1) / XB;
+        read_x(stage_of(0), i);
+#pragma unroll
+        for (int jj = i * PER; jj < (i + 1) * PER && jj < WBH; ++jj) read_w(stage_of(0), 0, jj);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    int s = 0;
+    // Scales may be among the loads that are younger than sub-tile s + 1, which then waits for a few more than it has to.
+    auto steady = [] __attribute__((always_inline)) { ring_sync<(NS - 3) * NL + NL0>(); };
+    // The last NS - 1 sub-tiles.  NEXT: in the stages that come free, the next tile's first ones.  Behind sub-tile KT - 1 are at least the
+    // AFTER loads of the next tile's first sub-tile that every height has, or nothing.
+    constexpr int AFTER = Ring<C>::WL + 1;
+    static_assert(!C::NEXT || NS == 4, "what is waited for below");
+    auto ask_next = [&] __attribute__((always_inline)) {
+        const int ahead = s + NS - 1 - KT;
+        if (C::NEXT && next.any && ahead >= 0 && ahead < KT) {
+            if (ahead == 0) load_scales<C, GATED>(next, rs_xs, scales_of(p.groups), wave, 0);
+            load_sub_tile<C, GATED>(next, rs_x, stage_of(KT + ahead), wave, ahead);
+        }
+    };
+    auto late = [&] __attribute__((always_inline)) {
+        if (C::NEXT && s == KT - 3) ring_sync<NL>();
+        else if (C::NEXT && next.any && KT >= NS) ring_sync<AFTER>();
+        else ring_sync<0>();
+    };
+    if (KT >= NS) {
+        sub_tile(T_{}, T_{}, T_{}, 0, steady);
+        for (s = 1; s + NS - 1 < KT; ++s) sub_tile(F_{}, T_{}, T_{}, s, steady);
+    } else {   // all of it is there
+        ask_next();
+        sub_tile(T_{}, T_{}, F_{}, 0, late);
+        s = 1;
+    }
+    for (; s < KT - 1; ++s) {
+        ask_next();
+        sub_tile(F_{}, T_{}, F_{}, s, late);
+    }
+    if (s < KT) {
+        ask_next();
+        sub_tile(F_{}, F_{}, F_{}, s, [] __attribute__((always_inline)) {});
+    }
+    if (C::NEXT) {
+        if (next.any && KT < NS - 1) {   // KT = 1, 2: the sub-tiles above never came to the next tile's first one
+            load_scales<C, GATED>(next, rs_xs, scales_of(p.groups), wave, 0);
+            load_sub_tile<C, GATED>(next, rs_x, stage_of(KT), wave, 0);
+        }
+        ring_sync<0>();
+    }
+}
+
+template <class C, int TI, bool GATED, bool NT>
+__device__ __forceinline__ void store_tile(const Fp4Product& p, const TileLoads<C>& t, f32x4 (&acc)[WB][Grid<C, TI>::XB]) {
+    constexpr int XB = Grid<C, TI>::XB;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rl = lane & 15, g = lane >> 4;
+    const int N = p.N, x_row = Grid<C, TI>::x_row(wave), wn_row = Grid<C, TI>::w_row(wave, GATED);
+    mfma_drain();
+    __builtin_amdgcn_sched_barrier(0);
+    if (GATED) {
+        // W is the row operand: a lane has the four columns 4g .. 4g+3 of row rl of a block; lanes 16 apart swap halves of two blocks, so that each has
+        // 16 bytes of a row and a store covers 16 rows x 64 bytes.
+        const uint32_t rowbytes = (uint32_t)N * (p.out_fp32 ? 4u : 2u);
+        const __amdgpu_buffer_rsrc_t rs_o = rsrc_of(p.out + (size_t)t.row0 * rowbytes, (uint32_t)t.nrows * rowbytes);
+        const int col = t.n0 + wn_row;
+        if (col < N) {   // N is a multiple of 32
+#pragma unroll
+            for (int i = 0; i < XB; ++i) {
+                float v[2][4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[j][q] = silu_times(read_acc(acc[j][i][q]), read_acc(acc[WBH + j][i][q]));
+                const int row = x_row + i * 16 + rl;
+                const bool ok = row < t.nrows;
+                if (p.out_fp32) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        store_b128<NT>(rs_o, ok ? (uint32_t)row * rowbytes + (uint32_t)(col + j * 16 + g * 4) * 4u : 0xFFFFFFF0u,
+                                   u32x4{__float_as_uint(v[j][0]), __float_as_uint(v[j][1]), __float_as_uint(v[j][2]), __float_as_uint(v[j][3])});
+                } else {
+                    u32x2 o[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const bf16x4 b = {(__bf16)v[j][0], (__bf16)v[j][1], (__bf16)v[j][2], (__bf16)v[j][3]};
+                        o[j] = __builtin_bit_cast(u32x2, b);
+                    }
+                    // lane g: block g & 1, columns 8 (g >> 1) .. + 7 of it
+                    store_b128<NT>(rs_o, ok ? (uint32_t)row * rowbytes + (uint32_t)(col + (g & 1) * 16 + (g >> 1) * 8) * 2u : 0xFFFFFFF0u, swap_rows16(o[0], o[1]));
+                }
+                if (i % 2) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    } else {
+        // x is the row operand: a lane has column rl of a block and rows 4g .. 4g+3; a store covers 4 rows x 64 bytes (fp32)
+        auto store = [&](auto f32_tag) __attribute__((always_inline)) {
+            constexpr bool F32 = decltype(f32_tag)::value;
+            constexpr int esz = F32 ? 4 : 2;
+            const uint32_t rowbytes = (uint32_t)N * (uint32_t)esz;
+            uint32_t vcol[WB][4];
+#pragma unroll
+            for (int j = 0; j < WB; ++j) {
+                const int col = t.n0 + wn_row + j * 16 + rl;
+                const uint32_t base = col < N ? (uint32_t)(g * 4) * rowbytes + (uint32_t)col * esz : 0x80000000u;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) vcol[j][r] = base + (uint32_t)r * rowbytes;
+            }
+#pragma unroll
+            for (int i = 0; i < XB; ++i) {
+                const int r0 = x_row + i * 16, left = min(max(t.nrows - r0, 0), 16);
+                const __amdgpu_buffer_rsrc_t rs_o = rsrc_of(p.out + (size_t)(t.row0 + r0) * rowbytes, (uint32_t)left * rowbytes);
+#pragma unroll
+                for (int j = 0; j < WB; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float v = read_acc(acc[j][i][r]);
+                        if (F32) store_b32<NT>(rs_o, vcol[j][r], v);
+                        else store_bf16<NT>(rs_o, vcol[j][r], v);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        if (p.out_fp32) store(std::true_type{});
+        else store(std::false_type{});
+    }
+}
+
+// NEXT: the next tile's descriptor and offsets are there, and its first three sub-tiles on their way, when the present one ends.
+template <class C, bool GATED, bool NT>
+__global__ __launch_bounds__(C::NW * 64, 2) void fp4_tile_kernel(const Fp4Product p) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int count = scalar_load(&p.plan->n_gate_up), n_run = scalar_load(&p.plan->n_run_up), KT = p.sub_tiles;
+    lds_t const ring = (lds_t)lds, scale_ring = ring + C::NS * Ring<C>::STAGE;
+    const __amdgpu_buffer_rsrc_t rs_x = rsrc_of(p.codes), rs_xs = rsrc_of(p.scales);
+    int at = blockIdx.x, n0, n0_next = 0, n0_after = 0, n0_last = 0, base = 0, sbase = 0;
+    const TileDesc d = tile_at<GATED>(p, count, n_run, at, n0);
+    if (d.nrows == 0) return;
+    const char *w_at, *u_at;
+    tile_weights<GATED>(p, d, w_at, u_at);
+    TileLoads<C> t = tile_loads<C, GATED>(p, d, n0, tile_rows<C>(p, d, lane, wave), w_at, u_at, lane, wave), next;
+    load_scales<C, GATED>(t, rs_xs, scale_ring, wave, 0);
+    for (int s = 0; s < C::NS - 1 && s < KT; ++s) load_sub_tile<C, GATED>(t, rs_x, ring + s * Ring<C>::STAGE, wave, s);
+    next.any = false;
+    TileDesc after = {0, 0, 0, 0};   // two tiles on
+    if (C::NEXT) {
+        const TileDesc d_next = tile_at<GATED>(p, count, n_run, at += gridDim.x, n0_next);
+        tile_weights<GATED>(p, d_next, w_at, u_at);
+        next = tile_loads<C, GATED>(p, d_next, n0_next, tile_rows<C>(p, d_next, lane, wave), w_at, u_at, lane, wave);
+        after = tile_at<GATED>(p, count, n_run, at += gridDim.x, n0_after);
+    }
+    ring_sync<0>();
+    for (;;) {
+        TileRows<C> rows;
+        TileDesc last;
+        at += gridDim.x;
+        auto run = [&](auto ti_tag) __attribute__((always_inline)) {
+            constexpr int TI = decltype(ti_tag)::value;
+            f32x4 acc[WB][Grid<C, TI>::XB];
+            multiply<C, TI, GATED>(p, t, next, rs_x, rs_xs, ring, base, sbase, acc);
+            if (C::NEXT) {   // on their way while this tile is stored
+                tile_weights<GATED>(p, after, w_at, u_at);
+                last = tile_at<GATED>(p, count, n_run, at, n0_last);
+                rows = tile_rows<C>(p, after, lane, wave);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            store_tile<C, TI, GATED, NT>(p, t, acc);
+        };
+        const int blocks = (t.nrows + 31) >> 5;
+        if constexpr (C::ROWS > 128) {
+            if (blocks > 7) run(std::integral_constant<int, 8>{});
+            else if (blocks > 6) run(std::integral_constant<int, 7>{});
+            else if (blocks > 5) run(std::integral_constant<int, 6>{});
+            else if (blocks > 4) run(std::integral_constant<int, 5>{});
+        }
+        if (blocks <= 4) {
+            if (blocks > 3) run(std::integral_constant<int, 4>{});
+            else if (blocks > 2) run(std::integral_constant<int, 3>{});
+            else if (blocks > 1) run(std::integral_constant<int, 2>{});
+            else run(std::integral_constant<int, 1>{});
+        }
+        if (!C::NEXT || !next.any) return;
+        base += KT;
+        sbase += p.groups;
+        t = next;
+        next = tile_loads<C, GATED>(p, after, n0_after, rows, w_at, u_at, lane, wave);
+        after = last;
+        n0_after = n0_last;
+    }
+}
+
+template <class C, bool NT>
+void launch_tiles(const Fp4Product& p, const bool gated, const dim3 grid, hipStream_t st) {
+    if (gated) hipLaunchKernelGGL((fp4_tile_kernel<C, true, NT>), grid, dim3(C::NW * 64), Ring<C>::BYTES, st, p);
+    else hipLaunchKernelGGL((fp4_tile_kernel<C, false, NT>), grid, dim3(C::NW * 64), Ring<C>::BYTES, st, p);
+}
+
+template <class C, bool NT>
+hipError_t set_lds() {
+    const auto to = hipFuncAttributeMaxDynamicSharedMemorySize;
+    if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&fp4_tile_kernel<C, true, NT>), to, Ring<C>::BYTES)) return e;
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&fp4_tile_kernel<C, false, NT>), to, Ring<C>::BYTES);
 }
 
 }  // namespace
 
 hipError_t fp4_product_init() {
-    for (const void* k : {reinterpret_cast<const void*>(&fp4_tile_kernel<true>), reinterpret_cast<const void*>(&fp4_tile_kernel<false>)})
-        if (const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, TILE_LDS)) return e;
+    for (const auto f : {set_lds<Long, false>, set_lds<Long, true>, set_lds<Short, false>, set_lds<Short, true>})
+        if (const hipError_t e = f()) return e;
     return hipSuccess;
 }
 
@@ -459,33 +578,40 @@ Fp4Layout fp4_layout(int64_t rows, int E) {
     Fp4Layout L;
     L.plan = 0;
     L.descs = 256;
-    L.total = L.descs + (((size_t)(rows / DIRECT_ROWS + E) * sizeof(TileDesc) + 255) & ~(size_t)255);
+    L.total = L.descs + (((size_t)(rows / Short::ROWS + E) * sizeof(TileDesc) + 255) & ~(size_t)255);
     return L;
 }
 
+int64_t fp4_tiles(int64_t rows, int E, int64_t N, bool gated) { return (rows / Short::ROWS + E) * ((N + (gated ? 127 : 255)) / (gated ? 128 : 256)); }
+
 hipError_t launch_fp4_product(const Fp4Product& args, bool gated, hipStream_t st) {
     Fp4Product p = args;
-    const bool tiles = p.rows > 2 * DIRECT_ROWS;
-    const int tm = tiles ? TILE_ROWS : DIRECT_ROWS, bn = tiles ? (gated ? 128 : WROWS) : 64;
+    const int bn = gated ? 128 : WROWS;
+    p.n_tiles = (p.N + bn - 1) / bn;
+    // tiles that even groups would have in either form
+    const int64_t per = (p.rows + p.E - 1) / p.E, groups = std::min(p.E, p.rows);
+    const int64_t long_tiles = groups * ((per + Long::ROWS - 1) / Long::ROWS) * p.n_tiles, short_tiles = groups * ((per + Short::ROWS - 1) / Short::ROWS) * p.n_tiles;
+    const bool is_long = (per > 100 && long_tiles >= 256) || (short_tiles <= 256 && p.sub_tiles >= 32);
+    const bool nt = (int64_t)p.rows * p.N * (p.out_fp32 ? 4 : 2) > (int64_t)256 << 20;
     PlanArgs a = {};
     a.offsets = p.offsets;
     a.E = p.E;
-    a.tm_up = tm;
-    a.nt_up = p.n_tiles = (p.N + bn - 1) / bn;
-    a.tails_last_up = tiles;
+    a.tm_up = is_long ? Long::ROWS : Short::ROWS;
+    a.nt_up = p.n_tiles;
+    a.tails_last_up = 1;
     a.small_tiles = 1;
     a.e_hi = p.E;
     a.plan = p.plan;
     a.descs_up = p.descs;
     p.group_m = 8;
-    p.max_mtiles = p.rows / tm + p.E;
+    p.max_mtiles = p.rows / a.tm_up + p.E;
     hipLaunchKernelGGL(fp4_plan_kernel, dim3(1), dim3(256), 0, st, a);
     if (const hipError_t e = hipGetLastError()) return e;
-    const dim3 grid((unsigned)(p.max_mtiles * p.n_tiles));
-    if (tiles && gated) hipLaunchKernelGGL(fp4_tile_kernel<true>, grid, dim3(256), TILE_LDS, st, p);
-    else if (tiles) hipLaunchKernelGGL(fp4_tile_kernel<false>, grid, dim3(256), TILE_LDS, st, p);
-    else if (gated) hipLaunchKernelGGL(fp4_direct_kernel<true>, grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL(fp4_direct_kernel<false>, grid, dim3(256), 0, st, p);
+    const dim3 all((unsigned)(p.max_mtiles * p.n_tiles)), cus(std::min(all.x, 256u));
+    if (is_long && nt) launch_tiles<Long, true>(p, gated, cus, st);
+    else if (is_long) launch_tiles<Long, false>(p, gated, cus, st);
+    else if (nt) launch_tiles<Short, true>(p, gated, all, st);
+    else launch_tiles<Short, false>(p, gated, all, st);
     return hipGetLastError();
 }
 

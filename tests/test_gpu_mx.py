@@ -237,6 +237,26 @@ def test_products(moe, counts, K, N, gated):
     p.check(torch.bfloat16)
 
 
+@pytest.mark.parametrize("gated,N", [(True, 4128), (False, 8224)])
+@pytest.mark.parametrize("K", [32, 160, 288, 416, 544, 672, 1152, 2080])
+def test_products_of_long_batches(moe, K, N, gated):
+    """Several tiles to a workgroup, of all heights, with contractions from one sub-tile on."""
+    p = Product(moe, [1500, 0, 250, 230, 180, 2100, 3, 33, 70, 100, 150, 770], K, N, gated, seed=K, tokens=2000 if gated else 0)
+    p.check(torch.float32 if K % 64 else torch.bfloat16)
+
+
+def test_products_of_few_rows_with_a_long_contraction(moe):
+    for counts in ([3, 0, 120], [128, 256]):
+        Product(moe, counts, 5152, 320, False).check(torch.float32)
+        Product(moe, counts, 4096, 160, True).check(torch.float32)
+
+
+def test_outputs_larger_than_the_caches(moe):
+    """256 MiB and more are stored past the caches."""
+    Product(moe, [9000, 7500], 96, 4352, False).check(torch.float32)
+    Product(moe, [20000, 12000], 64, 4352, True).check(torch.bfloat16)
+
+
 @pytest.mark.parametrize("gated", [False, True])
 @pytest.mark.parametrize("counts,tokens", [([5, 0, 9], 6), ([300, 280], 200), ([1], 1)])
 def test_products_of_gathered_rows(moe, counts, tokens, gated):
