@@ -37,7 +37,7 @@ struct Ring {
     static constexpr int X = C::ROWS * ROWB, STAGE = X + WROWS * ROWB;
     static constexpr int SCALE_X = C::ROWS * 16, SCALE_STAGE = SCALE_X + WROWS * 16;
     static constexpr int BYTES = C::NS * STAGE + C::SCALES * SCALE_STAGE;
-    static constexpr int XL = C::ROWS / 16 / C::NW, WL = WROWS / 16 / C::NW;   // loads of a sub-tile per wavefront, of a tile of full height
+    static constexpr int XL = C::ROWS / 16 / C::NW, WL = WROWS / 16 / C::NW, SL = 8 / C::NW;   // loads of a sub-tile per wavefront, of a tile of full height
 };
 static_assert(Ring<Long>::BYTES <= 160 * 1024 && Ring<Short>::BYTES <= 80 * 1024, "LDS");
 
@@ -63,19 +63,6 @@ template <bool NT>
 __device__ __forceinline__ void store_b128(const __amdgpu_buffer_rsrc_t rsrc, const uint32_t voff, const u32x4 v) {
 #if defined(__gfx950__)
     __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, voff, 0, NT ? 2 : 0);
-#endif
-}
-template <bool NT>
-__device__ __forceinline__ void store_b32(const __amdgpu_buffer_rsrc_t rsrc, const uint32_t voff, const float v) {
-#if defined(__gfx950__)
-    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rsrc, voff, 0, NT ? 2 : 0);
-#endif
-}
-template <bool NT>
-__device__ __forceinline__ void store_bf16(const __amdgpu_buffer_rsrc_t rsrc, const uint32_t voff, const float v) {
-#if defined(__gfx950__)
-    const __bf16 b = (__bf16)v;
-    __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, b), rsrc, voff, 0, NT ? 2 : 0);
 #endif
 }
 // Lanes 16..31 and 48..63 of a and lanes 0..15 and 32..47 of b change places; both halves as one piece.
@@ -134,7 +121,7 @@ __device__ __forceinline__ void ring_sync() {
 template <class C>
 struct TileLoads {
     const char *w_at, *u_at;                    // the matrix (gated: gate, up)
-    uint32_t x[Ring<C>::XL], w[Ring<C>::WL], xs, ws;   // offsets of this lane's pieces
+    uint32_t x[Ring<C>::XL], w[Ring<C>::WL], sc[Ring<C>::SL];   // offsets of this lane's pieces
     int row0, nrows, n0;
     bool any;
 };
@@ -220,8 +207,8 @@ __device__ __forceinline__ TileLoads<C> tile_loads(const Fp4Product& p, const Ti
         t.w[i] = (uint32_t)block * (uint32_t)(p.sub_tiles * 1024) + (uint32_t)(lane * 16);
     }
     const int wr = (wave & 3) * 64 + lane, n = min(n0 + (GATED ? (wr & 127) : wr), p.N - 1);
-    t.xs = (uint32_t)rows.xs * (uint32_t)(p.groups * 16);
-    t.ws = p.scales_at + (uint32_t)(n >> 4) * (uint32_t)(p.groups * 256) + (uint32_t)((n & 15) * 16);
+    t.sc[Ring<C>::SL - 1] = p.scales_at + (uint32_t)(n >> 4) * (uint32_t)(p.groups * 256) + (uint32_t)((n & 15) * 16);
+    if (Ring<C>::SL == 2 || wave < 4) t.sc[0] = (uint32_t)rows.xs * (uint32_t)(p.groups * 16);
     return t;
 }
 
@@ -237,9 +224,9 @@ __device__ __forceinline__ void load_w(const TileLoads<C>& t, lds_t stage, const
 template <class C, bool GATED>
 __device__ __forceinline__ void load_scales(const TileLoads<C>& t, const __amdgpu_buffer_rsrc_t rs_xs, lds_t stage, const int wave, const int q) {
     const int part = wave & 3;
-    if (wave < 4 && part * 64 < C::ROWS) load_lds(rs_xs, (lptr_t)(stage + part * 1024), t.xs, q * 16);
+    if (wave < 4 && part * 64 < C::ROWS) load_lds(rs_xs, (lptr_t)(stage + part * 1024), t.sc[0], q * 16);
     if (C::NW == 4 || wave >= 4)
-        load_lds(rsrc_of(GATED && part >= 2 ? t.u_at : t.w_at), (lptr_t)(stage + Ring<C>::SCALE_X + part * 1024), t.ws, q * 256);
+        load_lds(rsrc_of(GATED && part >= 2 ? t.u_at : t.w_at), (lptr_t)(stage + Ring<C>::SCALE_X + part * 1024), t.sc[Ring<C>::SL - 1], q * 256);
 }
 // A whole sub-tile of a tile whose height the caller does not know.
 template <class C, bool GATED>
@@ -309,10 +296,8 @@ __device__ __forceinline__ void multiply(const Fp4Product& p, const TileLoads<C>
             for (int jj = 0; jj < WBH; ++jj) {
                 const int j = HF * WBH + jj;
                 const i32x4 w = HF == 0 ? wA[jj] : wB[jj];
-                if (FIRST && GATED) mfma_tile_first(acc[j][i], w, xf[i], sw[j], sx[i]);
-                else if (FIRST) mfma_tile_first(acc[j][i], xf[i], w, sx[i], sw[j]);
-                else if (GATED) mfma_tile(acc[j][i], w, xf[i], sw[j], sx[i]);
-                else mfma_tile(acc[j][i], xf[i], w, sx[i], sw[j]);
+                if (FIRST) mfma_tile_first(acc[j][i], w, xf[i], sw[j], sx[i]);
+                else mfma_tile(acc[j][i], w, xf[i], sw[j], sx[i]);
             }
             if (HF == 1 && RD) read_x(nxt, i);
             constexpr int PER = (WBH + XB - 1) / XB;
@@ -421,71 +406,43 @@ __device__ __forceinline__ void store_tile(const Fp4Product& p, const TileLoads<
     const int N = p.N, x_row = Grid<C, TI>::x_row(wave), wn_row = Grid<C, TI>::w_row(wave, GATED);
     mfma_drain();
     __builtin_amdgcn_sched_barrier(0);
-    if (GATED) {
-        // W is the row operand: a lane has the four columns 4g .. 4g+3 of row rl of a block; lanes 16 apart swap halves of two blocks, so that each has
-        // 16 bytes of a row and a store covers 16 rows x 64 bytes.
-        const uint32_t rowbytes = (uint32_t)N * (p.out_fp32 ? 4u : 2u);
-        const __amdgpu_buffer_rsrc_t rs_o = rsrc_of(p.out + (size_t)t.row0 * rowbytes, (uint32_t)t.nrows * rowbytes);
-        const int col = t.n0 + wn_row;
-        if (col < N) {   // N is a multiple of 32
+    // W is the row operand: a lane has the four columns 4g .. 4g+3 of row rl of a block.  fp32: 16 bytes of a row; bf16: lanes 16 apart swap halves of two
+    // blocks for that.  A store covers 16 rows x 64 bytes.
+    const uint32_t rowbytes = (uint32_t)N * (p.out_fp32 ? 4u : 2u);
+    const __amdgpu_buffer_rsrc_t rs_o = rsrc_of(p.out + (size_t)t.row0 * rowbytes, (uint32_t)t.nrows * rowbytes);
+    constexpr int BLOCKS = GATED ? WBH : WB;   // of 16 columns
 #pragma unroll
-            for (int i = 0; i < XB; ++i) {
-                float v[2][4];
+    for (int b = 0; b < BLOCKS; b += 2) {
+        const int col = t.n0 + wn_row + b * 16;
+        if (col >= N) break;   // N is a multiple of 32
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+        for (int i = 0; i < XB; ++i) {
+            f32x4 v[2];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) v[j][q] = silu_times(read_acc(acc[j][i][q]), read_acc(acc[WBH + j][i][q]));
-                const int row = x_row + i * 16 + rl;
-                const bool ok = row < t.nrows;
-                if (p.out_fp32) {
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        store_b128<NT>(rs_o, ok ? (uint32_t)row * rowbytes + (uint32_t)(col + j * 16 + g * 4) * 4u : 0xFFFFFFF0u,
-                                   u32x4{__float_as_uint(v[j][0]), __float_as_uint(v[j][1]), __float_as_uint(v[j][2]), __float_as_uint(v[j][3])});
-                } else {
-                    u32x2 o[2];
+                for (int q = 0; q < 4; ++q)
+                    v[j][q] = GATED ? silu_times(read_acc(acc[b + j][i][q]), read_acc(acc[(WBH + b + j) % WB][i][q])) : read_acc(acc[b + j][i][q]);
+            const int row = x_row + i * 16 + rl;
+            // rows past the end get an offset that the descriptor drops
+            auto offset = [&](const int c, const uint32_t size) __attribute__((always_inline)) {
+                return row < t.nrows ? (uint32_t)row * rowbytes + (uint32_t)c * size : 0xFFFFFFF0u;
+            };
+            if (p.out_fp32) {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const bf16x4 b = {(__bf16)v[j][0], (__bf16)v[j][1], (__bf16)v[j][2], (__bf16)v[j][3]};
-                        o[j] = __builtin_bit_cast(u32x2, b);
-                    }
-                    // lane g: block g & 1, columns 8 (g >> 1) .. + 7 of it
-                    store_b128<NT>(rs_o, ok ? (uint32_t)row * rowbytes + (uint32_t)(col + (g & 1) * 16 + (g >> 1) * 8) * 2u : 0xFFFFFFF0u, swap_rows16(o[0], o[1]));
+                for (int j = 0; j < 2; ++j) store_b128<NT>(rs_o, offset(col + j * 16 + g * 4, 4), __builtin_bit_cast(u32x4, v[j]));
+            } else {
+                u32x2 o[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const bf16x4 w = {(__bf16)v[j][0], (__bf16)v[j][1], (__bf16)v[j][2], (__bf16)v[j][3]};
+                    o[j] = __builtin_bit_cast(u32x2, w);
                 }
-                if (i % 2) __builtin_amdgcn_sched_barrier(0);
+                // lane g: block g & 1, columns 8 (g >> 1) .. + 7 of it
+                store_b128<NT>(rs_o, offset(col + (g & 1) * 16 + (g >> 1) * 8, 2), swap_rows16(o[0], o[1]));
             }
+            if (i % 2) __builtin_amdgcn_sched_barrier(0);
         }
-    } else {
-        // x is the row operand: a lane has column rl of a block and rows 4g .. 4g+3; a store covers 4 rows x 64 bytes (fp32)
-        auto store = [&](auto f32_tag) __attribute__((always_inline)) {
-            constexpr bool F32 = decltype(f32_tag)::value;
-            constexpr int esz = F32 ? 4 : 2;
-            const uint32_t rowbytes = (uint32_t)N * (uint32_t)esz;
-            uint32_t vcol[WB][4];
-#pragma unroll
-            for (int j = 0; j < WB; ++j) {
-                const int col = t.n0 + wn_row + j * 16 + rl;
-                const uint32_t base = col < N ? (uint32_t)(g * 4) * rowbytes + (uint32_t)col * esz : 0x80000000u;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) vcol[j][r] = base + (uint32_t)r * rowbytes;
-            }
-#pragma unroll
-            for (int i = 0; i < XB; ++i) {
-                const int r0 = x_row + i * 16, left = min(max(t.nrows - r0, 0), 16);
-                const __amdgpu_buffer_rsrc_t rs_o = rsrc_of(p.out + (size_t)(t.row0 + r0) * rowbytes, (uint32_t)left * rowbytes);
-#pragma unroll
-                for (int j = 0; j < WB; ++j)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float v = read_acc(acc[j][i][r]);
-                        if (F32) store_b32<NT>(rs_o, vcol[j][r], v);
-                        else store_bf16<NT>(rs_o, vcol[j][r], v);
-                    }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        };
-        if (p.out_fp32) store(std::true_type{});
-        else store(std::false_type{});
     }
 }
 
@@ -592,7 +549,9 @@ hipError_t launch_fp4_product(const Fp4Product& args, bool gated, hipStream_t st
     const int64_t per = (p.rows + p.E - 1) / p.E, groups = std::min(p.E, p.rows);
     const int64_t long_tiles = groups * ((per + Long::ROWS - 1) / Long::ROWS) * p.n_tiles, short_tiles = groups * ((per + Short::ROWS - 1) / Short::ROWS) * p.n_tiles;
     const bool is_long = (per > 100 && long_tiles >= 256) || (short_tiles <= 256 && p.sub_tiles >= 32);
-    const bool nt = (int64_t)p.rows * p.N * (p.out_fp32 ? 4 : 2) > (int64_t)256 << 20;
+    // Outputs past the L2s where the contraction is short and they are most of what moves (64 experts, 16000 tokens, us: gate/up of K = 2048 336 -> 309,
+    // down of K = 1408, bf16 281 -> 188, fp32 313 -> 260); where it is long they displace little (8 experts, K = 4096, 3000 tokens 381 -> 397).
+    const bool nt = p.sub_tiles <= 16;
     PlanArgs a = {};
     a.offsets = p.offsets;
     a.E = p.E;
