@@ -121,7 +121,8 @@ __device__ __forceinline__ void ring_sync() {
 template <class C>
 struct TileLoads {
     const char *w_at, *u_at;                    // the matrix (gated: gate, up)
-    uint32_t x[Ring<C>::XL], w[Ring<C>::WL], sc[Ring<C>::SL];   // offsets of this lane's pieces
+    uint32_t x[Ring<C>::XL], sc[Ring<C>::SL];   // offsets of this lane's pieces
+    int w[Ring<C>::WL];                         // and of this wavefront's blocks of W
     int row0, nrows, n0;
     bool any;
 };
@@ -130,6 +131,15 @@ struct TileLoads {
 template <class T>
 __device__ __forceinline__ T scalar_load(const T* ptr) {
     return *(const __attribute__((address_space(4))) T*)(uintptr_t)ptr;
+}
+
+// The lane's number, anew: what is computed from it then stays where it is needed and does not take registers around the loop over the tiles.
+__device__ __forceinline__ int fresh_lane() {
+    int lane = threadIdx.x & 63;
+#if defined(__gfx950__)
+    asm volatile("" : "+v"(lane));
+#endif
+    return lane;
 }
 
 __device__ __forceinline__ int row_of(const Fp4Product& p, const int r) { return p.row_index ? p.row_index[r] : r; }
@@ -204,7 +214,7 @@ __device__ __forceinline__ TileLoads<C> tile_loads(const Fp4Product& p, const Ti
 #pragma unroll
     for (int i = 0; i < Ring<C>::WL; ++i) {
         const int qw = i * C::NW + wave, block = min((n0 >> 4) + (GATED ? (qw & 7) : qw), (p.N >> 4) - 1);
-        t.w[i] = (uint32_t)block * (uint32_t)(p.sub_tiles * 1024) + (uint32_t)(lane * 16);
+        t.w[i] = block * p.sub_tiles * 1024;
     }
     const int wr = (wave & 3) * 64 + lane, n = min(n0 + (GATED ? (wr & 127) : wr), p.N - 1);
     t.sc[Ring<C>::SL - 1] = p.scales_at + (uint32_t)(n >> 4) * (uint32_t)(p.groups * 256) + (uint32_t)((n & 15) * 16);
@@ -218,7 +228,7 @@ __device__ __forceinline__ void load_x(const TileLoads<C>& t, const __amdgpu_buf
 }
 template <class C, bool GATED>
 __device__ __forceinline__ void load_w(const TileLoads<C>& t, lds_t stage, const int wave, const int i, const int sub) {
-    load_lds(rsrc_of(GATED && i * 2 >= Ring<C>::WL ? t.u_at : t.w_at), (lptr_t)(stage + Ring<C>::X + (i * C::NW + wave) * 1024), t.w[i], sub * 1024);
+    load_lds(rsrc_of(GATED && i * 2 >= Ring<C>::WL ? t.u_at : t.w_at), (lptr_t)(stage + Ring<C>::X + (i * C::NW + wave) * 1024), (uint32_t)(threadIdx.x & 63) * 16u, t.w[i] + sub * 1024);
 }
 // 64 rows of x or W to a wavefront: with eight of them one of the two, with four up to both.
 template <class C, bool GATED>
@@ -257,7 +267,7 @@ __device__ __forceinline__ void multiply(const Fp4Product& p, const TileLoads<C>
     constexpr int XB = Grid<C, TI>::XB, NS = C::NS, STAGE = Ring<C>::STAGE;
     constexpr int NLX = (2 * TI + C::NW - 1) / C::NW, NL = NLX + Ring<C>::WL;   // loads of a sub-tile per wavefront
     constexpr int NL0 = XB * NL / (2 * XB);                                     // of them, those issued before the hand-over
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rl = lane & 15, g = lane >> 4;
+    const int lane = fresh_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rl = lane & 15, g = lane >> 4;
     const int KT = p.sub_tiles;
     lds_t const scale_ring = ring + NS * STAGE;
     const int x_row = Grid<C, TI>::x_row(wave), wn_row = Grid<C, TI>::w_row(wave, GATED);
@@ -309,7 +319,6 @@ __device__ __forceinline__ void multiply(const Fp4Product& p, const TileLoads<C>
                 const int q = HF * XB + i;
 #pragma unroll
                 for (int l = (q * NL) / G; l < ((q + 1) * NL) / G; ++l) {
-
                     if (l < NLX) load_x<C>(t, rs_x, ahead, wave, l, s + NS - 1);
                     else load_w<C, GATED>(t, ahead, wave, l - NLX, s + NS - 1);
                 }
@@ -323,12 +332,12 @@ __device__ __forceinline__ void multiply(const Fp4Product& p, const TileLoads<C>
     using H1 = std::integral_constant<int, 1>;
     // Sub-tile s; its scales are byte 0 of sx and sw.
     auto sub_tile = [&](auto first_tag, auto rd_tag, auto ld_tag, const int s, auto sync) __attribute__((always_inline)) {
+        if (C::SCALES == 2 && (s & 3) == 0 && s + 4 < KT) load_scales<C, GATED>(t, rs_xs, scales_of((s >> 2) + 1), wave, (s >> 2) + 1);
         if (decltype(first_tag)::value || (s & 3) == 0) {
 #pragma unroll
             for (int i = 0; i < XB; ++i) sx[i] = sx_next[i];
 #pragma unroll
             for (int j = 0; j < WB; ++j) sw[j] = sw_next[j];
-            if (C::SCALES == 2 && s + 4 < KT) load_scales<C, GATED>(t, rs_xs, scales_of((s >> 2) + 1), wave, (s >> 2) + 1);
         } else {
 #pragma unroll
             for (int i = 0; i < XB; ++i) sx[i] >>= 8;
@@ -341,7 +350,7 @@ __device__ __forceinline__ void multiply(const Fp4Product& p, const TileLoads<C>
         sync();
         // one place for scales: free once every wavefront is here
         if (C::SCALES == 1 && (s & 3) == 0 && s + 4 < KT) load_scales<C, GATED>(t, rs_xs, scales_of(0), wave, (s >> 2) + 1);
-        // the scales of the next group came in during this one's first sub-tile
+        // the scales of the next group came in since this one's first sub-tile
         if ((s & 3) == 3 && s + 1 < KT) read_scales((s >> 2) + 1);
         part(H1{}, first_tag, rd_tag, ld_tag, s);
     };
@@ -395,42 +404,38 @@ __device__ __forceinline__ void multiply(const Fp4Product& p, const TileLoads<C>
             load_scales<C, GATED>(next, rs_xs, scales_of(p.groups), wave, 0);
             load_sub_tile<C, GATED>(next, rs_x, stage_of(KT), wave, 0);
         }
-        ring_sync<0>();
     }
+    if (C::NEXT || !GATED) ring_sync<0>();   // store_tile writes into the ring
 }
 
 template <class C, int TI, bool GATED, bool NT>
-__device__ __forceinline__ void store_tile(const Fp4Product& p, const TileLoads<C>& t, f32x4 (&acc)[WB][Grid<C, TI>::XB]) {
+__device__ __forceinline__ void store_tile(const Fp4Product& p, const TileLoads<C>& t, lds_t spare, f32x4 (&acc)[WB][Grid<C, TI>::XB]) {
     constexpr int XB = Grid<C, TI>::XB;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rl = lane & 15, g = lane >> 4;
+    const int lane = fresh_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rl = lane & 15, g = lane >> 4;
     const int N = p.N, x_row = Grid<C, TI>::x_row(wave), wn_row = Grid<C, TI>::w_row(wave, GATED);
     mfma_drain();
     __builtin_amdgcn_sched_barrier(0);
-    // W is the row operand: a lane has the four columns 4g .. 4g+3 of row rl of a block.  fp32: 16 bytes of a row; bf16: lanes 16 apart swap halves of two
-    // blocks for that.  A store covers 16 rows x 64 bytes.
+    // W is the row operand: a lane has the four columns 4g .. 4g+3 of row rl of a block.  Rows past the end get an offset that the descriptor drops.
     const uint32_t rowbytes = (uint32_t)N * (p.out_fp32 ? 4u : 2u);
     const __amdgpu_buffer_rsrc_t rs_o = rsrc_of(p.out + (size_t)t.row0 * rowbytes, (uint32_t)t.nrows * rowbytes);
-    constexpr int BLOCKS = GATED ? WBH : WB;   // of 16 columns
-#pragma unroll
-    for (int b = 0; b < BLOCKS; b += 2) {
-        const int col = t.n0 + wn_row + b * 16;
-        if (col >= N) break;   // N is a multiple of 32
+    auto offset = [&](const int row, const int col, const bool ok) __attribute__((always_inline)) {
+        return ok && row < t.nrows ? (uint32_t)row * rowbytes + (uint32_t)col * (p.out_fp32 ? 4u : 2u) : 0xFFFFFFF0u;
+    };
+    const int col0 = t.n0 + wn_row;
+    if constexpr (GATED) {
+        // fp32: 16 bytes of a row; bf16: lanes 16 apart swap halves of two blocks for that.  A store covers 16 rows x 64 bytes.
+        if (col0 >= N) return;   // N is a multiple of 32
 #pragma unroll
         for (int i = 0; i < XB; ++i) {
             f32x4 v[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    v[j][q] = GATED ? silu_times(read_acc(acc[b + j][i][q]), read_acc(acc[(WBH + b + j) % WB][i][q])) : read_acc(acc[b + j][i][q]);
+                for (int q = 0; q < 4; ++q) v[j][q] = silu_times(read_acc(acc[j][i][q]), read_acc(acc[WBH + j][i][q]));
             const int row = x_row + i * 16 + rl;
-            // rows past the end get an offset that the descriptor drops
-            auto offset = [&](const int c, const uint32_t size) __attribute__((always_inline)) {
-                return row < t.nrows ? (uint32_t)row * rowbytes + (uint32_t)c * size : 0xFFFFFFF0u;
-            };
             if (p.out_fp32) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) store_b128<NT>(rs_o, offset(col + j * 16 + g * 4, 4), __builtin_bit_cast(u32x4, v[j]));
+                for (int j = 0; j < 2; ++j) store_b128<NT>(rs_o, offset(row, col0 + j * 16 + g * 4, true), __builtin_bit_cast(u32x4, v[j]));
             } else {
                 u32x2 o[2];
 #pragma unroll
@@ -439,9 +444,37 @@ __device__ __forceinline__ void store_tile(const Fp4Product& p, const TileLoads<
                     o[j] = __builtin_bit_cast(u32x2, w);
                 }
                 // lane g: block g & 1, columns 8 (g >> 1) .. + 7 of it
-                store_b128<NT>(rs_o, offset(col + (g & 1) * 16 + (g >> 1) * 8, 2), swap_rows16(o[0], o[1]));
+                store_b128<NT>(rs_o, offset(row, col0 + (g & 1) * 16 + (g >> 1) * 8, true), swap_rows16(o[0], o[1]));
             }
             if (i % 2) __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+        // Whole lines: 16 rows x 64 columns at a time through 4 KiB of LDS that only this wavefront's loads fill, as four pieces of four rows; 16-byte
+        // pieces of a row at slot piece ^ row, so that neither way has bank conflicts.  A store covers 4 rows x 256 bytes (fp32) or 8 x 128.
+        typedef __attribute__((address_space(3))) f32x4* lpiece_t;
+        auto place = [&](const int row, const int piece) __attribute__((always_inline)) {
+            return (lpiece_t)(spare + (row >> 2) * C::NW * 1024 + (row & 3) * 256 + ((piece ^ row) << 4));
+        };
+#pragma unroll
+        for (int i = 0; i < XB; ++i) {
+#pragma unroll
+            for (int j = 0; j < WB; ++j) *place(rl, j * 4 + g) = f32x4{read_acc(acc[j][i][0]), read_acc(acc[j][i][1]), read_acc(acc[j][i][2]), read_acc(acc[j][i][3])};
+            if (p.out_fp32) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = q * 4 + (lane >> 4), col = col0 + (lane & 15) * 4;
+                    store_b128<NT>(rs_o, offset(x_row + i * 16 + r, col, col < N), __builtin_bit_cast(u32x4, *place(r, lane & 15)));
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int r = q * 8 + (lane >> 3), piece = (lane & 7) * 2, col = col0 + piece * 4;
+                    const f32x4 lo = *place(r, piece), hi = *place(r, piece + 1);
+                    const bf16x8 w = {(__bf16)lo[0], (__bf16)lo[1], (__bf16)lo[2], (__bf16)lo[3], (__bf16)hi[0], (__bf16)hi[1], (__bf16)hi[2], (__bf16)hi[3]};
+                    store_b128<NT>(rs_o, offset(x_row + i * 16 + r, col, col < N), __builtin_bit_cast(u32x4, w));
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
@@ -482,10 +515,11 @@ __global__ __launch_bounds__(C::NW * 64, 2) void fp4_tile_kernel(const Fp4Produc
             if (C::NEXT) {   // on their way while this tile is stored
                 tile_weights<GATED>(p, after, w_at, u_at);
                 last = tile_at<GATED>(p, count, n_run, at, n0_last);
-                rows = tile_rows<C>(p, after, lane, wave);
+                rows = tile_rows<C>(p, after, fresh_lane(), wave);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            store_tile<C, TI, GATED, NT>(p, t, acc);
+            // the stage that comes free last, at the places of this wavefront's own loads
+            store_tile<C, TI, GATED, NT>(p, t, ring + (int)((uint32_t)(base + KT + C::NS - 1) % C::NS) * Ring<C>::STAGE + wave * 1024, acc);
         };
         const int blocks = (t.nrows + 31) >> 5;
         if constexpr (C::ROWS > 128) {
@@ -504,7 +538,7 @@ __global__ __launch_bounds__(C::NW * 64, 2) void fp4_tile_kernel(const Fp4Produc
         base += KT;
         sbase += p.groups;
         t = next;
-        next = tile_loads<C, GATED>(p, after, n0_after, rows, w_at, u_at, lane, wave);
+        next = tile_loads<C, GATED>(p, after, n0_after, rows, w_at, u_at, fresh_lane(), wave);
         after = last;
         n0_after = n0_last;
     }
@@ -545,13 +579,17 @@ hipError_t launch_fp4_product(const Fp4Product& args, bool gated, hipStream_t st
     Fp4Product p = args;
     const int bn = gated ? 128 : WROWS;
     p.n_tiles = (p.N + bn - 1) / bn;
-    // tiles that even groups would have in either form
+    // Which form, by the tiles that even groups would have (us, short and long; rows per group): 64 experts, K = 2048, gated 94 rows 45, 46, 281 89, 91, 750 196,
+    // 187; K = 1408 94 26, 30, 281 60, 54; 160 experts, K = 1536 37 154, 152, 112 202, 189, 600 740, 626; 8 experts, K = 4096, gated 100 104, 114, 250 176,
+    // 186, 750 438, 407.  Few tiles: a CU has one workgroup in either form, and a long contraction is better off with the deeper ring (8 experts, K = 14336, 25 rows
+    // 86, 47), a short one with lower tiles (K = 512, 750 rows 14.2, 14.5).
     const int64_t per = (p.rows + p.E - 1) / p.E, groups = std::min(p.E, p.rows);
     const int64_t long_tiles = groups * ((per + Long::ROWS - 1) / Long::ROWS) * p.n_tiles, short_tiles = groups * ((per + Short::ROWS - 1) / Short::ROWS) * p.n_tiles;
     const bool is_long = (per > 100 && long_tiles >= 256) || (short_tiles <= 256 && p.sub_tiles >= 32);
-    // Outputs past the L2s where the contraction is short and they are most of what moves (64 experts, 16000 tokens, us: gate/up of K = 2048 336 -> 309,
-    // down of K = 1408, bf16 281 -> 188, fp32 313 -> 260); where it is long they displace little (8 experts, K = 4096, 3000 tokens 381 -> 397).
-    const bool nt = p.sub_tiles <= 16;
+    // Outputs go past the L2s, where they would displace what tiles share (us, without and with: down of K = 1408, 64 experts, 16000 tokens, bf16 230, 195, fp32
+    // 287, 249; K = 1536, 160 experts, 16000 593, 538; gate/up of K = 2048 339, 326, of K = 5120, 160 experts, 3000 tokens 306, 288), but for gated ones of a
+    // long contraction and tall groups, which are few bytes for their time, in half lines (K = 4096, 8 experts, 16000 tokens 1828, 1852).
+    const bool nt = !gated || p.sub_tiles <= 16 || per <= 128;
     PlanArgs a = {};
     a.offsets = p.offsets;
     a.E = p.E;
