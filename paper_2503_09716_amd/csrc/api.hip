@@ -956,7 +956,7 @@ const char* few_shape_problem(const moe_shape* s, moe_status* st) {
 }
 
 struct FewLayout {
-    size_t idx, logits, gate, h, total;
+    size_t idx, arrived, logits, gate, h, partial, total;
 };
 FewLayout few_layout(const moe_shape& s) {
     FewLayout L;
@@ -964,9 +964,11 @@ FewLayout few_layout(const moe_shape& s) {
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
     const size_t ep = (size_t)route_gemm_config(s).ep;
     L.idx = take((size_t)s.T * s.top_k * 4);
+    L.arrived = take((size_t)(s.H / DOWN_COLUMNS) * 4);
     L.logits = take((size_t)s.T * ep * 4);
     L.gate = take(ep * s.H * 2);
     L.h = take(few_h_bytes(s));
+    L.partial = take(few_partial_bytes(s));
     L.total = std::max<size_t>(o, 256);
     return L;
 }
@@ -1704,6 +1706,9 @@ moe_status moe_layer_few(moe_ctx* c, const moe_shape* s, const void* x, const vo
     a.weights = (const void* const*)list->buffer;
     a.idx = (int32_t*)(w8 + L.idx);
     a.h = w8 + L.h;
+    a.partial = (float*)(w8 + L.partial);
+    a.arrived = (int32_t*)(w8 + L.arrived);
+    a.shares = few_shares(*s, list->fp4 != 0);
     a.out = (char*)out;
     a.T = s->T;
     a.H = s->H;

@@ -5,6 +5,7 @@
 namespace moe {
 
 constexpr int FEW_TOKENS = 16, FEW_TOP_K = 16;
+constexpr int DOWN_COLUMNS = 64, FEW_SHARES = 32;   // columns of a workgroup of the down launch; workgroups to the same columns at most
 
 struct FewArgs {
     const char *x, *wg;                  // tokens; packed gate matrix
@@ -13,12 +14,17 @@ struct FewArgs {
     const void* const* weights;          // device table of packed matrices [3][E + Ns]
     int32_t* idx;                        // [T * k]
     char* h;                             // [T * k + Ns * T] rows of F: 8 values as bf16, then what that leaves of them as bf16
+    float* partial;                      // [H / 64][shares][16][64]
+    int32_t* arrived;                    // [H / 64]: workgroups that have left theirs; cleared by the launch before
     char* out;
+    int32_t shares;                      // workgroups to the same columns
     int32_t T, H, F, E, k, Ns, ep, renorm, out_fp32;
     float scale;
     uint32_t up_scales_at, down_scales_at;   // MXFP4: of a matrix, its scales
 };
 size_t few_h_bytes(const moe_shape& s);
+size_t few_partial_bytes(const moe_shape& s);
+int few_shares(const moe_shape& s, bool fp4);
 hipError_t launch_few(const FewArgs& a, bool fp4, hipStream_t st);
 bool few_routes_inside(const moe_shape& s);   // no launch for the logits
 

@@ -18,6 +18,12 @@
 namespace moe {
 namespace {
 
+// Said to be global memory: after loads through a generic pointer the compiler waits for every load in flight.
+typedef const __attribute__((address_space(1))) u32x4* gpiece_t;
+typedef const __attribute__((address_space(1))) uint32_t* gword_t;
+__device__ __forceinline__ u32x4 load_piece(const char* at) { return *(gpiece_t)(uintptr_t)at; }
+__device__ __forceinline__ uint32_t load_word(const char* at) { return *(gword_t)(uintptr_t)at; }
+
 constexpr int WAVES = 8;
 constexpr int LOGIT_STRIDE = 256;
 
@@ -46,6 +52,13 @@ __device__ __forceinline__ bf16x8 weight_part(const u32x4 piece, const float sca
 __device__ __forceinline__ float scale_of(const uint32_t four, const int t) {
     const uint32_t byte = four >> (8 * (t & 3)) & 255u;
     return __uint_as_float(byte == 255u ? 0x7fc00000u : byte << 23);
+}
+
+// A pointer that is the same for the wavefront, to global memory.
+__device__ __forceinline__ const char* uniform(const char* ptr) {
+    const uint64_t v = (uint64_t)ptr;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (const char*)(((uint64_t)hi << 32) | lo);
 }
 
 // Where the picks of the tokens sit: pick[e][t] = j of token t's pick e, or -1; the experts that have any, ascending.
@@ -140,13 +153,19 @@ __device__ __forceinline__ void select(const FewArgs& p, const float* logits, co
     }
 }
 
+// Gate and up, and the router before them.  A workgroup takes 32 columns of both matrices of a picked or shared expert at a time, its wavefronts every
+// eighth sub-tile of the contraction (eight together read consecutive blocks), and their sums meet in LDS.  The loads of the next steps, the
+// next columns' among them, are on their way while one is multiplied.
 template <bool FP4>
 __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
-    __shared__ float logits[FEW_TOKENS * LOGIT_STRIDE];
+    // the logits and their parts, then the wavefronts' sums (two places in turn: one barrier each)
+    __shared__ __attribute__((aligned(16))) float room[2][WAVES][2][2][256];
     __shared__ __attribute__((aligned(16))) Picks picks;
     __shared__ int32_t idx[FEW_TOKENS * FEW_TOP_K];
     __shared__ float w[FEW_TOKENS * FEW_TOP_K];
-    __shared__ float part[WAVES][256];
+    __shared__ const char* matrix[2][256];
+    float* const logits = &room[0][0][0][0][0];
+    float(*const part)[256] = room[1][0][0];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rl = lane & 15, g = lane >> 4;
     if (!p.logits) {
         // up to 8 blocks of 16 experts side by side; what wavefronts are left share the contraction, and are added in order
@@ -183,148 +202,251 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
     }
     __syncthreads();
     gather_picks(picks, idx, p.T, p.k, p.E);
-    if (blockIdx.x == 0)
+    if (blockIdx.x == 0) {
         for (int i = tid; i < p.T * p.k; i += WAVES * 64) p.idx[i] = idx[i];
+        for (int i = tid; i < p.H / DOWN_COLUMNS; i += WAVES * 64) p.arrived[i] = 0;
+    }
 
-    const int units = p.F >> 4, experts = p.E + p.Ns;
-    const int KT = FP4 ? (p.H + 127) >> 7 : p.H >> 5, groups = (p.H + 511) >> 9;
+    const int units = p.F >> 5, experts = p.E + p.Ns, n_active = __builtin_amdgcn_readfirstlane(picks.n);
+    const int KT = FP4 ? (p.H + 127) >> 7 : p.H >> 5, groups = (p.H + 511) >> 9, steps = (KT + WAVES - 1) / WAVES;
+    const int items = (n_active + p.Ns) * units, mine = items > (int)blockIdx.x ? (items - 1 - blockIdx.x) / gridDim.x + 1 : 0;
+    // the matrices of the picked and shared experts, by their place in the list
+    for (int i = tid; i < 2 * (n_active + p.Ns); i += WAVES * 64) {
+        const int at = i >> 1, e = at < n_active ? picks.active[at] : p.E + at - n_active;
+        matrix[i & 1][at] = (const char*)p.weights[(i & 1) * experts + e];
+    }
+    __syncthreads();
     const char* const xa = p.x + (size_t)min(rl, p.T - 1) * p.H * 2 + g * (FP4 ? 64 : 16);
-    constexpr int DEPTH = FP4 ? 4 : 8, PARTS = FP4 ? 4 : 1, XSTEP = FP4 ? 256 : 64;
-    for (int item = blockIdx.x * WAVES + wave; item < (picks.n + p.Ns) * units; item += gridDim.x * WAVES) {
-        const int a = item / units, unit = item - a * units;
-        const int e = a < picks.n ? picks.active[a] : p.E + a - picks.n;
-        const char* const w1 = (const char*)p.weights[e];
-        const char* const w3 = (const char*)p.weights[experts + e];
-        const size_t at = (size_t)unit * KT * 1024 + rl * 64 + ((g ^ block_swizzle(rl)) << 4);
-        const size_t sat = (size_t)p.up_scales_at + (size_t)unit * groups * 256 + rl * 16 + g * 4;
-        f32x4 ag = {0.f, 0.f, 0.f, 0.f}, au = {0.f, 0.f, 0.f, 0.f};
-        for (int t0 = 0; t0 < KT; t0 += DEPTH) {
-            u32x4 a1[DEPTH], a3[DEPTH], b[DEPTH][PARTS];
-            uint32_t s1 = 0, s3 = 0;
-            if (FP4) {
-                s1 = *reinterpret_cast<const uint32_t*>(w1 + sat + (t0 >> 2) * 256);
-                s3 = *reinterpret_cast<const uint32_t*>(w3 + sat + (t0 >> 2) * 256);
+    const uint32_t lane_w = (uint32_t)(rl * 64 + ((g ^ block_swizzle(rl)) << 4)), lane_s = (uint32_t)(rl * 16 + g * 4);
+    constexpr int DEPTH = FP4 ? 2 : 4, PARTS = FP4 ? 4 : 1, XSTEP = FP4 ? 256 : 64;
+    u32x4 a[DEPTH][2][2], x[DEPTH][PARTS];
+    uint32_t sc[DEPTH][2][2];
+    // what is asked for next: step `ls` of item blockIdx.x + li * gridDim.x, its expert's matrices and columns
+    int li = 0, ls = 0;
+    const char *lw[2] = {nullptr, nullptr};
+    auto load = [&](const int slot) __attribute__((always_inline)) {
+        if (li >= mine) return;
+        const int item = blockIdx.x + li * gridDim.x, at = item / units, unit = item - at * units;
+        if (ls == 0) {
+            lw[0] = uniform(matrix[0][at]);
+            lw[1] = uniform(matrix[1][at]);
+        }
+        const int t = wave + ls * WAVES;
+        if (t < KT) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int block = unit * 2 + c;
+                    a[slot][m][c] = load_piece(lw[m] + ((size_t)block * KT + t) * 1024 + lane_w);
+                    if (FP4) sc[slot][m][c] = load_word(lw[m] + p.up_scales_at + ((size_t)block * groups + (t >> 2)) * 256 + lane_s);
+                }
+#pragma unroll
+            for (int f = 0; f < PARTS; ++f) {
+                // past H (a multiple of 64) the weights are zero; x there is not read
+                const bool in = !FP4 || t * 128 + g * 32 < p.H;
+                x[slot][f] = in ? load_piece(xa + (size_t)t * XSTEP + f * 16) : u32x4{0u, 0u, 0u, 0u};
             }
+        }
+        if (++ls == steps) { ls = 0; ++li; }
+    };
 #pragma unroll
-            for (int u = 0; u < DEPTH; ++u) {
-                const int t = min(t0 + u, KT - 1);
-                a1[u] = *reinterpret_cast<const u32x4*>(w1 + at + (size_t)t * 1024);
-                a3[u] = *reinterpret_cast<const u32x4*>(w3 + at + (size_t)t * 1024);
+    for (int u = 0; u < DEPTH; ++u) load(u);
+    f32x4 acc[2][2] = {};
+    int i = 0, s = 0;   // item and step that are multiplied next
+    while (i < mine) {
 #pragma unroll
-                for (int f = 0; f < PARTS; ++f) {
-                    // past H (a multiple of 64) the weights are zero; x there is not read
-                    const bool in = t0 + u < KT && (!FP4 || t * 128 + g * 32 < p.H);
-                    b[u][f] = in ? *reinterpret_cast<const u32x4*>(xa + (size_t)t * XSTEP + f * 16) : u32x4{0u, 0u, 0u, 0u};
+        for (int u = 0; u < DEPTH; ++u) {
+            if (i >= mine) break;
+            if (wave + s * WAVES < KT) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const float scale = FP4 ? scale_of(sc[u][m][c], wave) : 0.f;
+#pragma unroll
+                        for (int f = 0; f < PARTS; ++f) acc[m][c] = mfma(weight_part<FP4>(a[u][m][c], scale, f), __builtin_bit_cast(bf16x8, x[u][f]), acc[m][c]);
+                    }
+            }
+            load(u);
+            if (++s < steps) continue;
+            // the item's last step: lane (rl, g) has columns 4 g + r of 16 of token rl
+            float(*const sums)[2][2][256] = room[i & 1];
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    *reinterpret_cast<f32x4*>(&sums[wave][m][c][rl * 16 + 4 * g]) = acc[m][c];
+                    acc[m][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+            __syncthreads();
+            {
+                const int item = blockIdx.x + i * gridDim.x, at = item / units, unit = item - at * units;
+                const int e = at < n_active ? picks.active[at] : p.E + at - n_active;
+                const int t = tid >> 5, c = tid >> 4 & 1, n = tid & 15;   // token, half and column of the unit
+                int row = -1;
+                float weight = 1.f;
+                if (t < p.T) {
+                    if (at >= n_active) row = p.T * (p.k + at - n_active) + t;
+                    else if (picks.pick[e][t] >= 0) {
+                        row = t * p.k + picks.pick[e][t];
+                        weight = w[row];
+                    }
+                }
+                if (row >= 0) {
+                    float gate = 0.f, up = 0.f;
+#pragma unroll
+                    for (int q = 0; q < WAVES; ++q) {
+                        gate += sums[q][0][c][t * 16 + n];
+                        up += sums[q][1][c][t * 16 + n];
+                    }
+                    const float v = weight * (gate / (1.0f + __expf(-gate)) * up);
+                    const __bf16 hi = (__bf16)v;
+                    char* const to = p.h + ((size_t)row * (p.F >> 3) + unit * 4 + c * 2 + (n >> 3)) * 32 + (n & 7) * 2;
+                    *reinterpret_cast<__bf16*>(to) = hi;
+                    *reinterpret_cast<__bf16*>(to + 16) = __builtin_isfinite((float)hi) ? (__bf16)(v - (float)hi) : (__bf16)0.0f;
                 }
             }
-#pragma unroll
-            for (int u = 0; u < DEPTH; ++u) {
-                if (t0 + u >= KT) break;
-                const float c1 = FP4 ? scale_of(s1, u) : 0.f, c3 = FP4 ? scale_of(s3, u) : 0.f;
-#pragma unroll
-                for (int f = 0; f < PARTS; ++f) {
-                    ag = mfma(weight_part<FP4>(a1[u], c1, f), __builtin_bit_cast(bf16x8, b[u][f]), ag);
-                    au = mfma(weight_part<FP4>(a3[u], c3, f), __builtin_bit_cast(bf16x8, b[u][f]), au);
-                }
-            }
+            s = 0;
+            ++i;
         }
-        // columns 16 unit + 4 g + r of token rl
-        int row = -1;
-        float weight = 1.f;
-        if (rl < p.T) {
-            if (a >= picks.n) row = p.T * (p.k + a - picks.n) + rl;
-            else if (picks.pick[e][rl] >= 0) {
-                row = rl * p.k + picks.pick[e][rl];
-                weight = w[row];
-            }
-        }
-        if (row < 0) continue;
-        bf16x4 hi, lo;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float v = weight * (ag[r] / (1.0f + __expf(-ag[r])) * au[r]);
-            hi[r] = (__bf16)v;
-            lo[r] = __builtin_isfinite((float)hi[r]) ? (__bf16)(v - (float)hi[r]) : (__bf16)0.0f;
-        }
-        char* const to = p.h + ((size_t)row * (p.F >> 3) + unit * 2 + (g >> 1)) * 32 + (g & 1) * 8;
-        *reinterpret_cast<bf16x4*>(to) = hi;
-        *reinterpret_cast<bf16x4*>(to + 16) = lo;
     }
 }
 
+// Down: 64 columns to a workgroup, and a share of all sub-tiles of all picked and shared experts, one after the other; its wavefronts take every eighth of
+// them.  The shares' sums meet in the workgroup that comes last, which adds them in order: no workgroup waits for another.  Sums and
+// counter pass by the L2s, each of which only its own XCD sees.
 template <bool FP4>
 __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
     __shared__ __attribute__((aligned(16))) Picks picks;
-    __shared__ float part[WAVES][256];
+    __shared__ __attribute__((aligned(16))) float sums[WAVES][4][256];
+    __shared__ const char* matrix[256];
+    __shared__ int last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rl = lane & 15, g = lane >> 4;
     gather_picks(picks, p.idx, p.T, p.k, p.E);
-    const int unit = blockIdx.x, experts = p.E + p.Ns;
+    const int n_active = __builtin_amdgcn_readfirstlane(picks.n), experts = p.E + p.Ns;
+    for (int i = tid; i < n_active + p.Ns; i += WAVES * 64)
+        matrix[i] = (const char*)p.weights[2 * experts + (i < n_active ? picks.active[i] : p.E + i - n_active)];
+    __syncthreads();
+    const int share = blockIdx.x % p.shares, columns = blockIdx.x / p.shares;
     const int KT = FP4 ? (p.F + 127) >> 7 : p.F >> 5, groups = (p.F + 511) >> 9;
-    const size_t at = (size_t)unit * KT * 1024 + rl * 64 + ((g ^ block_swizzle(rl)) << 4);
-    const size_t sat = (size_t)p.down_scales_at + (size_t)unit * groups * 256 + rl * 16 + g * 4;
-    constexpr int DEPTH = FP4 ? 2 : 8, PARTS = FP4 ? 4 : 1, HSTEP = FP4 ? 512 : 128;
-    // all experts' sub-tiles one after the other, cut evenly over the wavefronts
-    const int total = (picks.n + p.Ns) * KT;
-    const int from = (int)((int64_t)total * wave / WAVES), to = (int)((int64_t)total * (wave + 1) / WAVES);
-    // each expert's sum by itself: a token that did not pick it takes nothing from it, not even what is not a number
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f}, sum = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = from; c0 < to; c0 += DEPTH) {
-        u32x4 a[DEPTH], hi[DEPTH][PARTS], lo[DEPTH][PARTS];
-        uint32_t s[DEPTH];
-        bool picked[DEPTH];
+    constexpr int DEPTH = FP4 ? 2 : 4, PARTS = FP4 ? 4 : 1, HSTEP = FP4 ? 512 : 128, NB = DOWN_COLUMNS / 16;
+    const uint32_t lane_w = (uint32_t)(rl * 64 + ((g ^ block_swizzle(rl)) << 4)), lane_s = (uint32_t)(rl * 16 + g * 4);
+    const int total = (n_active + p.Ns) * KT;
+    const int from = (int)((int64_t)total * share / p.shares), to = (int)((int64_t)total * (share + 1) / p.shares);
+    u32x4 a[DEPTH][NB], hi[DEPTH][PARTS], lo[DEPTH][PARTS];
+    uint32_t sc[DEPTH][NB];
+    int expert[DEPTH];       // which in the list; -1: none
+    bool picked[DEPTH];
+    int lc = from + wave, le = lc / KT, lt = lc - le * KT;   // sub-tile lt of the le-th expert is asked for next
+    auto load = [&](const int slot) __attribute__((always_inline)) {
+        expert[slot] = -1;
+        picked[slot] = false;
+        if (lc >= to) return;
+        expert[slot] = le;
+        const char* const w2 = uniform(matrix[le]);
 #pragma unroll
-        for (int u = 0; u < DEPTH; ++u) {
-            const int c = min(c0 + u, to - 1), i = c / KT, t = c - i * KT;
-            const int e = i < picks.n ? picks.active[i] : p.E + i - picks.n;
-            const char* const w2 = (const char*)p.weights[2 * experts + e];
-            a[u] = *reinterpret_cast<const u32x4*>(w2 + at + (size_t)t * 1024);
-            s[u] = FP4 ? *reinterpret_cast<const uint32_t*>(w2 + sat + (t >> 2) * 256) >> (8 * (t & 3)) : 0u;
-            int row = -1;
-            if (rl < p.T && c0 + u < to) {
-                if (i >= picks.n) row = p.T * (p.k + i - picks.n) + rl;
-                else if (picks.pick[e][rl] >= 0) row = rl * p.k + picks.pick[e][rl];
-            }
-            picked[u] = row >= 0;
-            if (FP4 && t * 128 + g * 32 >= p.F) row = -1;
-            const char* const from_h = p.h + (size_t)max(row, 0) * p.F * 4 + (size_t)t * HSTEP + g * (FP4 ? 128 : 32);
-#pragma unroll
-            for (int f = 0; f < PARTS; ++f) {
-                hi[u][f] = row >= 0 ? *reinterpret_cast<const u32x4*>(from_h + f * 32) : u32x4{0u, 0u, 0u, 0u};
-                lo[u][f] = row >= 0 ? *reinterpret_cast<const u32x4*>(from_h + f * 32 + 16) : u32x4{0u, 0u, 0u, 0u};
-            }
+        for (int c = 0; c < NB; ++c) {
+            const int block = columns * NB + c;
+            a[slot][c] = load_piece(w2 + ((size_t)block * KT + lt) * 1024 + lane_w);
+            if (FP4) sc[slot][c] = load_word(w2 + p.down_scales_at + ((size_t)block * groups + (lt >> 2)) * 256 + lane_s) >> (8 * (lt & 3));
         }
+        int row = -1;
+        if (rl < p.T) {
+            if (le >= n_active) row = p.T * (p.k + le - n_active) + rl;
+            else if (const int j = picks.pick[picks.active[le]][rl]; j >= 0) row = rl * p.k + j;
+        }
+        picked[slot] = row >= 0;
+        const bool in = row >= 0 && (!FP4 || lt * 128 + g * 32 < p.F);
+        const char* const from_h = p.h + (size_t)max(row, 0) * p.F * 4 + (size_t)lt * HSTEP + g * (FP4 ? 128 : 32);
+#pragma unroll
+        for (int f = 0; f < PARTS; ++f) {
+            hi[slot][f] = in ? load_piece(from_h + f * 32) : u32x4{0u, 0u, 0u, 0u};
+            lo[slot][f] = in ? load_piece(from_h + f * 32 + 16) : u32x4{0u, 0u, 0u, 0u};
+        }
+        lc += WAVES;
+        for (lt += WAVES; lt >= KT; lt -= KT) ++le;
+    };
+#pragma unroll
+    for (int u = 0; u < DEPTH; ++u) load(u);
+    // each expert's sum by itself: a token that did not pick it takes nothing from it, not even what is not a number
+    f32x4 acc[NB] = {}, sum[NB] = {};
+    int now = expert[0];
+    bool now_picked = picked[0];
+    auto flush = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+            if (now_picked) sum[c] += acc[c];
+            acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    for (bool more = expert[0] >= 0; more;) {
 #pragma unroll
         for (int u = 0; u < DEPTH; ++u) {
-            if (c0 + u >= to) break;
-            const float scale = FP4 ? scale_of(s[u], 0) : 0.f;
+            if (expert[u] < 0) { more = false; break; }
+            if (expert[u] != now) {
+                flush();
+                now = expert[u];
+                now_picked = picked[u];
+            }
 #pragma unroll
-            for (int f = 0; f < PARTS; ++f) {
-                const bf16x8 v = weight_part<FP4>(a[u], scale, f);
-                acc = mfma(v, __builtin_bit_cast(bf16x8, hi[u][f]), acc);
-                acc = mfma(v, __builtin_bit_cast(bf16x8, lo[u][f]), acc);
+            for (int c = 0; c < NB; ++c) {
+                const float scale = FP4 ? scale_of(sc[u][c], 0) : 0.f;
+#pragma unroll
+                for (int f = 0; f < PARTS; ++f) {
+                    const bf16x8 v = weight_part<FP4>(a[u][c], scale, f);
+                    acc[c] = mfma(v, __builtin_bit_cast(bf16x8, hi[u][f]), acc[c]);
+                    acc[c] = mfma(v, __builtin_bit_cast(bf16x8, lo[u][f]), acc[c]);
+                }
             }
-            if (c0 + u == to - 1 || (c0 + u + 1) % KT == 0) {
-                if (picked[u]) sum += acc;
-                acc = f32x4{0.f, 0.f, 0.f, 0.f};
-            }
+            load(u);
         }
     }
+    flush();
 #pragma unroll
-    for (int r = 0; r < 4; ++r) part[wave][rl * 16 + 4 * g + r] = sum[r];
+    for (int c = 0; c < NB; ++c) *reinterpret_cast<f32x4*>(&sums[wave][c][rl * 16 + 4 * g]) = sum[c];
     __syncthreads();
-    const int t = tid >> 4;
-    if (t >= p.T) return;
-    float v = 0.f;
+    // thread: columns n and n + 32 of a token
+    const int t = tid >> 5, n = tid & 31;
+    float v[2] = {0.f, 0.f};
 #pragma unroll
-    for (int q = 0; q < WAVES; ++q) v += part[q][tid];
-    const size_t o = (size_t)t * p.H + unit * 16 + (tid & 15);
-    if (p.out_fp32) *reinterpret_cast<float*>(p.out + o * 4) = v;
-    else *reinterpret_cast<__bf16*>(p.out + o * 2) = (__bf16)v;
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int q = 0; q < WAVES; ++q) v[j] += sums[q][j * 2 + (n >> 4)][t * 16 + (n & 15)];
+    if (p.shares > 1) {
+        float* const mine = p.partial + ((size_t)columns * p.shares + share) * (FEW_TOKENS * DOWN_COLUMNS);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) __hip_atomic_store(&mine[t * DOWN_COLUMNS + j * 32 + n], v[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): they have arrived
+        __syncthreads();
+        if (tid == 0) last = __hip_atomic_fetch_add(&p.arrived[columns], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.shares - 1;
+        __syncthreads();
+        if (!last) return;
+        const float* const all = p.partial + (size_t)columns * p.shares * (FEW_TOKENS * DOWN_COLUMNS);
+        v[0] = v[1] = 0.f;
+        for (int q = 0; q < p.shares; ++q)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                v[j] += __hip_atomic_load(&all[(size_t)q * (FEW_TOKENS * DOWN_COLUMNS) + t * DOWN_COLUMNS + j * 32 + n], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (t >= p.T) return;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const size_t o = (size_t)t * p.H + columns * DOWN_COLUMNS + j * 32 + n;
+        if (p.out_fp32) *reinterpret_cast<float*>(p.out + o * 4) = v[j];
+        else *reinterpret_cast<__bf16*>(p.out + o * 2) = (__bf16)v[j];
+    }
 }
 
 }  // namespace
 
+int few_shares(const moe_shape& s, bool fp4) {
+    const int64_t active = std::min<int64_t>(s.E, (int64_t)s.T * s.top_k) + s.num_shared, sub_tiles = active * ((s.F + (fp4 ? 127 : 31)) / (fp4 ? 128 : 32));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 512 / (s.H / DOWN_COLUMNS), (sub_tiles + WAVES - 1) / WAVES}));
+}
+
 size_t few_h_bytes(const moe_shape& s) { return (size_t)s.T * (s.top_k + s.num_shared) * s.F * 4; }
+size_t few_partial_bytes(const moe_shape& s) { return (size_t)(s.H / DOWN_COLUMNS) * FEW_SHARES * FEW_TOKENS * DOWN_COLUMNS * 4; }
 
 bool few_routes_inside(const moe_shape& s) { return (int64_t)s.E * s.H * 2 <= 256 << 10; }
 
@@ -333,8 +455,8 @@ hipError_t launch_few(const FewArgs& a, bool fp4, hipStream_t st) {
         hipLaunchKernelGGL(few_logits_kernel, dim3((unsigned)((a.E + 15) / 16)), dim3(WAVES * 64), 0, st, a);
         if (const hipError_t e = hipGetLastError()) return e;
     }
-    const int64_t active = std::min<int64_t>(a.E, (int64_t)a.T * a.k) + a.Ns, items = active * (a.F / 16);
-    const dim3 up((unsigned)std::min<int64_t>(512, (items + WAVES - 1) / WAVES)), down((unsigned)(a.H / 16)), block(WAVES * 64);
+    const int64_t active = std::min<int64_t>(a.E, (int64_t)a.T * a.k) + a.Ns, items = active * (a.F / 32);
+    const dim3 up((unsigned)std::min<int64_t>(512, items)), down((unsigned)(a.H / DOWN_COLUMNS * a.shares)), block(WAVES * 64);
     if (fp4) hipLaunchKernelGGL(few_up_kernel<true>, up, block, 0, st, a);
     else hipLaunchKernelGGL(few_up_kernel<false>, up, block, 0, st, a);
     if (const hipError_t e = hipGetLastError()) return e;
