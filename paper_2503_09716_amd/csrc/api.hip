@@ -956,14 +956,14 @@ const char* few_shape_problem(const moe_shape* s, moe_status* st) {
 }
 
 struct FewLayout {
-    size_t idx, arrived, logits, gate, h, partial, total;
+    size_t picks, arrived, logits, gate, h, partial, total;
 };
 FewLayout few_layout(const moe_shape& s) {
     FewLayout L;
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
     const size_t ep = (size_t)route_gemm_config(s).ep;
-    L.idx = take((size_t)s.T * s.top_k * 4);
+    L.picks = take(sizeof(Picks));
     L.arrived = take((size_t)(s.H / DOWN_COLUMNS) * 4);
     L.logits = take((size_t)s.T * ep * 4);
     L.gate = take(ep * s.H * 2);
@@ -1704,11 +1704,12 @@ moe_status moe_layer_few(moe_ctx* c, const moe_shape* s, const void* x, const vo
     a.ep = route_gemm_config(*s).ep;
     if (!few_routes_inside(*s)) a.logits = a.logits_out = (float*)(w8 + L.logits);
     a.weights = (const void* const*)list->buffer;
-    a.idx = (int32_t*)(w8 + L.idx);
+    a.picks = (Picks*)(w8 + L.picks);
     a.h = w8 + L.h;
     a.partial = (float*)(w8 + L.partial);
     a.arrived = (int32_t*)(w8 + L.arrived);
     a.shares = few_shares(*s, list->fp4 != 0);
+    a.nt = (double)list->experts * 3 * s->H * s->F * (list->fp4 ? 0.53125 : 2.0) > (double)(256 << 20);
     a.out = (char*)out;
     a.T = s->T;
     a.H = s->H;

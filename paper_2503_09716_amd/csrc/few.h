@@ -7,17 +7,25 @@ namespace moe {
 constexpr int FEW_TOKENS = 16, FEW_TOP_K = 16;
 constexpr int DOWN_COLUMNS = 64, FEW_SHARES = 32;   // columns of a workgroup of the down launch; workgroups to the same columns at most
 
+// Where the picks of the tokens sit: pick[e][t] = j of token t's pick e, or -1; the experts that have any, ascending.
+struct alignas(16) Picks {
+    int8_t pick[256][FEW_TOKENS];
+    int16_t active[256];
+    int32_t n;
+};
+
 struct FewArgs {
     const char *x, *wg;                  // tokens; packed gate matrix
     const float *bias, *logits;          // bias: or nullptr; logits [T][ep]: computed by a launch before, or nullptr
     float* logits_out;                   // that launch's
     const void* const* weights;          // device table of packed matrices [3][E + Ns]
-    int32_t* idx;                        // [T * k]
+    Picks* picks;                        // from the first launch to the second
     char* h;                             // [T * k + Ns * T] rows of F: 8 values as bf16, then what that leaves of them as bf16
     float* partial;                      // [H / 64][shares][16][64]
     int32_t* arrived;                    // [H / 64]: workgroups that have left theirs; cleared by the launch before
     char* out;
     int32_t shares;                      // workgroups to the same columns
+    int32_t nt;                          // 1: weights past the caches
     int32_t T, H, F, E, k, Ns, ep, renorm, out_fp32;
     float scale;
     uint32_t up_scales_at, down_scales_at;   // MXFP4: of a matrix, its scales

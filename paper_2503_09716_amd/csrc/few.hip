@@ -21,7 +21,10 @@ namespace {
 // Said to be global memory: after loads through a generic pointer the compiler waits for every load in flight.
 typedef const __attribute__((address_space(1))) u32x4* gpiece_t;
 typedef const __attribute__((address_space(1))) uint32_t* gword_t;
-__device__ __forceinline__ u32x4 load_piece(const char* at) { return *(gpiece_t)(uintptr_t)at; }
+template <bool NT = false>
+__device__ __forceinline__ u32x4 load_piece(const char* at) {
+    return NT ? __builtin_nontemporal_load((gpiece_t)(uintptr_t)at) : *(gpiece_t)(uintptr_t)at;
+}
 __device__ __forceinline__ uint32_t load_word(const char* at) { return *(gword_t)(uintptr_t)at; }
 
 constexpr int WAVES = 8;
@@ -61,16 +64,8 @@ __device__ __forceinline__ const char* uniform(const char* ptr) {
     return (const char*)(((uint64_t)hi << 32) | lo);
 }
 
-// Where the picks of the tokens sit: pick[e][t] = j of token t's pick e, or -1; the experts that have any, ascending.
-struct Picks {
-    int8_t pick[256][FEW_TOKENS];
-    int16_t active[256];
-    int32_t n;
-};
-
-// By a whole workgroup of at least 256 threads, from idx [T][k] in LDS or global memory.
-template <class Idx>
-__device__ __forceinline__ void gather_picks(Picks& s, const Idx idx, const int T, const int k, const int E) {
+// By a whole workgroup of at least 256 threads, from idx [T][k] in LDS.
+__device__ __forceinline__ void gather_picks(Picks& s, const int32_t* idx, const int T, const int k, const int E) {
     __shared__ int wave_count[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int e = tid; e < E; e += blockDim.x) *reinterpret_cast<u32x4*>(s.pick[e]) = u32x4{~0u, ~0u, ~0u, ~0u};
@@ -156,17 +151,21 @@ __device__ __forceinline__ void select(const FewArgs& p, const float* logits, co
 // Gate and up, and the router before them.  A workgroup takes 32 columns of both matrices of a picked or shared expert at a time, its wavefronts every
 // eighth sub-tile of the contraction (eight together read consecutive blocks), and their sums meet in LDS.  The loads of the next steps, the
 // next columns' among them, are on their way while one is multiplied.
-template <bool FP4>
+template <bool FP4, bool NT>
 __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
     // the logits and their parts, then the wavefronts' sums (two places in turn: one barrier each)
     __shared__ __attribute__((aligned(16))) float room[2][WAVES][2][2][256];
     __shared__ __attribute__((aligned(16))) Picks picks;
     __shared__ int32_t idx[FEW_TOKENS * FEW_TOP_K];
     __shared__ float w[FEW_TOKENS * FEW_TOP_K];
-    __shared__ const char* matrix[2][256];
+    __shared__ const char* matrix[2][256];   // of every expert
     float* const logits = &room[0][0][0][0][0];
     float(*const part)[256] = room[1][0][0];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rl = lane & 15, g = lane >> 4;
+    const int experts = p.E + p.Ns;
+    if (tid < 256)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) matrix[m][tid] = (const char*)p.weights[m * experts + min(tid, experts - 1)];
     if (!p.logits) {
         // up to 8 blocks of 16 experts side by side; what wavefronts are left share the contraction, and are added in order
         const int blocks = (p.E + 15) >> 4;
@@ -203,19 +202,14 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
     __syncthreads();
     gather_picks(picks, idx, p.T, p.k, p.E);
     if (blockIdx.x == 0) {
-        for (int i = tid; i < p.T * p.k; i += WAVES * 64) p.idx[i] = idx[i];
+        const uint32_t* const from = reinterpret_cast<const uint32_t*>(&picks);
+        for (int i = tid; i < (int)sizeof(Picks) / 4; i += WAVES * 64) reinterpret_cast<uint32_t*>(p.picks)[i] = from[i];
         for (int i = tid; i < p.H / DOWN_COLUMNS; i += WAVES * 64) p.arrived[i] = 0;
     }
 
-    const int units = p.F >> 5, experts = p.E + p.Ns, n_active = __builtin_amdgcn_readfirstlane(picks.n);
+    const int units = p.F >> 5, n_active = __builtin_amdgcn_readfirstlane(picks.n);
     const int KT = FP4 ? (p.H + 127) >> 7 : p.H >> 5, groups = (p.H + 511) >> 9, steps = (KT + WAVES - 1) / WAVES;
     const int items = (n_active + p.Ns) * units, mine = items > (int)blockIdx.x ? (items - 1 - blockIdx.x) / gridDim.x + 1 : 0;
-    // the matrices of the picked and shared experts, by their place in the list
-    for (int i = tid; i < 2 * (n_active + p.Ns); i += WAVES * 64) {
-        const int at = i >> 1, e = at < n_active ? picks.active[at] : p.E + at - n_active;
-        matrix[i & 1][at] = (const char*)p.weights[(i & 1) * experts + e];
-    }
-    __syncthreads();
     const char* const xa = p.x + (size_t)min(rl, p.T - 1) * p.H * 2 + g * (FP4 ? 64 : 16);
     const uint32_t lane_w = (uint32_t)(rl * 64 + ((g ^ block_swizzle(rl)) << 4)), lane_s = (uint32_t)(rl * 16 + g * 4);
     constexpr int DEPTH = FP4 ? 2 : 4, PARTS = FP4 ? 4 : 1, XSTEP = FP4 ? 256 : 64;
@@ -228,8 +222,9 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
         if (li >= mine) return;
         const int item = blockIdx.x + li * gridDim.x, at = item / units, unit = item - at * units;
         if (ls == 0) {
-            lw[0] = uniform(matrix[0][at]);
-            lw[1] = uniform(matrix[1][at]);
+            const int e = at < n_active ? picks.active[at] : p.E + at - n_active;
+            lw[0] = uniform(matrix[0][e]);
+            lw[1] = uniform(matrix[1][e]);
         }
         const int t = wave + ls * WAVES;
         if (t < KT) {
@@ -238,7 +233,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const int block = unit * 2 + c;
-                    a[slot][m][c] = load_piece(lw[m] + ((size_t)block * KT + t) * 1024 + lane_w);
+                    a[slot][m][c] = load_piece<NT>(lw[m] + ((size_t)block * KT + t) * 1024 + lane_w);
                     if (FP4) sc[slot][m][c] = load_word(lw[m] + p.up_scales_at + ((size_t)block * groups + (t >> 2)) * 256 + lane_s);
                 }
 #pragma unroll
@@ -316,18 +311,19 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
 // Down: 64 columns to a workgroup, and a share of all sub-tiles of all picked and shared experts, one after the other; its wavefronts take every eighth of
 // them.  The shares' sums meet in the workgroup that comes last, which adds them in order: no workgroup waits for another.  Sums and
 // counter pass by the L2s, each of which only its own XCD sees.
-template <bool FP4>
+template <bool FP4, bool NT>
 __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
     __shared__ __attribute__((aligned(16))) Picks picks;
     __shared__ __attribute__((aligned(16))) float sums[WAVES][4][256];
-    __shared__ const char* matrix[256];
+    __shared__ const char* matrix[256];   // of every expert
     __shared__ int last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rl = lane & 15, g = lane >> 4;
-    gather_picks(picks, p.idx, p.T, p.k, p.E);
-    const int n_active = __builtin_amdgcn_readfirstlane(picks.n), experts = p.E + p.Ns;
-    for (int i = tid; i < n_active + p.Ns; i += WAVES * 64)
-        matrix[i] = (const char*)p.weights[2 * experts + (i < n_active ? picks.active[i] : p.E + i - n_active)];
+    const int experts = p.E + p.Ns;
+    if (tid < 256) matrix[tid] = (const char*)p.weights[2 * experts + min(tid, experts - 1)];
+    const u32x4* const from_up = reinterpret_cast<const u32x4*>(p.picks);
+    for (int i = tid; i < (int)sizeof(Picks) / 16; i += WAVES * 64) reinterpret_cast<u32x4*>(&picks)[i] = from_up[i];
     __syncthreads();
+    const int n_active = __builtin_amdgcn_readfirstlane(picks.n);
     const int share = blockIdx.x % p.shares, columns = blockIdx.x / p.shares;
     const int KT = FP4 ? (p.F + 127) >> 7 : p.F >> 5, groups = (p.F + 511) >> 9;
     constexpr int DEPTH = FP4 ? 2 : 4, PARTS = FP4 ? 4 : 1, HSTEP = FP4 ? 512 : 128, NB = DOWN_COLUMNS / 16;
@@ -344,17 +340,18 @@ __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
         picked[slot] = false;
         if (lc >= to) return;
         expert[slot] = le;
-        const char* const w2 = uniform(matrix[le]);
+        const int e = __builtin_amdgcn_readfirstlane(le < n_active ? picks.active[le] : p.E + le - n_active);
+        const char* const w2 = uniform(matrix[e]);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
             const int block = columns * NB + c;
-            a[slot][c] = load_piece(w2 + ((size_t)block * KT + lt) * 1024 + lane_w);
+            a[slot][c] = load_piece<NT>(w2 + ((size_t)block * KT + lt) * 1024 + lane_w);
             if (FP4) sc[slot][c] = load_word(w2 + p.down_scales_at + ((size_t)block * groups + (lt >> 2)) * 256 + lane_s) >> (8 * (lt & 3));
         }
         int row = -1;
         if (rl < p.T) {
             if (le >= n_active) row = p.T * (p.k + le - n_active) + rl;
-            else if (const int j = picks.pick[picks.active[le]][rl]; j >= 0) row = rl * p.k + j;
+            else if (const int j = picks.pick[e][rl]; j >= 0) row = rl * p.k + j;
         }
         picked[slot] = row >= 0;
         const bool in = row >= 0 && (!FP4 || lt * 128 + g * 32 < p.F);
@@ -424,10 +421,20 @@ __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
         if (!last) return;
         const float* const all = p.partial + (size_t)columns * p.shares * (FEW_TOKENS * DOWN_COLUMNS);
         v[0] = v[1] = 0.f;
-        for (int q = 0; q < p.shares; ++q)
+        constexpr int AHEAD = 8;   // loads on their way
+        for (int q0 = 0; q0 < p.shares; q0 += AHEAD) {
+            float u[AHEAD][2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-                v[j] += __hip_atomic_load(&all[(size_t)q * (FEW_TOKENS * DOWN_COLUMNS) + t * DOWN_COLUMNS + j * 32 + n], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    u[q][j] = __hip_atomic_load(&all[(size_t)min(q0 + q, p.shares - 1) * (FEW_TOKENS * DOWN_COLUMNS) + t * DOWN_COLUMNS + j * 32 + n],
+                                                __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) v[j] += q0 + q < p.shares ? u[q][j] : 0.f;
+        }
     }
     if (t >= p.T) return;
 #pragma unroll
@@ -442,13 +449,13 @@ __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
 
 int few_shares(const moe_shape& s, bool fp4) {
     const int64_t active = std::min<int64_t>(s.E, (int64_t)s.T * s.top_k) + s.num_shared, sub_tiles = active * ((s.F + (fp4 ? 127 : 31)) / (fp4 ? 128 : 32));
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 512 / (s.H / DOWN_COLUMNS), (sub_tiles + WAVES - 1) / WAVES}));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 256 / (s.H / DOWN_COLUMNS), (sub_tiles + WAVES - 1) / WAVES}));
 }
 
 size_t few_h_bytes(const moe_shape& s) { return (size_t)s.T * (s.top_k + s.num_shared) * s.F * 4; }
 size_t few_partial_bytes(const moe_shape& s) { return (size_t)(s.H / DOWN_COLUMNS) * FEW_SHARES * FEW_TOKENS * DOWN_COLUMNS * 4; }
 
-bool few_routes_inside(const moe_shape& s) { return (int64_t)s.E * s.H * 2 <= 256 << 10; }
+bool few_routes_inside(const moe_shape& s) { return (int64_t)((s.E + 15) / 16) * s.H * 32 <= 128 << 10; }
 
 hipError_t launch_few(const FewArgs& a, bool fp4, hipStream_t st) {
     if (a.logits) {
@@ -457,11 +464,17 @@ hipError_t launch_few(const FewArgs& a, bool fp4, hipStream_t st) {
     }
     const int64_t active = std::min<int64_t>(a.E, (int64_t)a.T * a.k) + a.Ns, items = active * (a.F / 32);
     const dim3 up((unsigned)std::min<int64_t>(512, items)), down((unsigned)(a.H / DOWN_COLUMNS * a.shares)), block(WAVES * 64);
-    if (fp4) hipLaunchKernelGGL(few_up_kernel<true>, up, block, 0, st, a);
-    else hipLaunchKernelGGL(few_up_kernel<false>, up, block, 0, st, a);
-    if (const hipError_t e = hipGetLastError()) return e;
-    if (fp4) hipLaunchKernelGGL(few_down_kernel<true>, down, block, 0, st, a);
-    else hipLaunchKernelGGL(few_down_kernel<false>, down, block, 0, st, a);
+#define FEW(FP4_, NT_)                                                                      \
+    do {                                                                                    \
+        hipLaunchKernelGGL((few_up_kernel<FP4_, NT_>), up, block, 0, st, a);                \
+        if (const hipError_t e = hipGetLastError()) return e;                               \
+        hipLaunchKernelGGL((few_down_kernel<FP4_, NT_>), down, block, 0, st, a);            \
+    } while (0)
+    if (fp4 && a.nt) FEW(true, true);
+    else if (fp4) FEW(true, false);
+    else if (a.nt) FEW(false, true);
+    else FEW(false, false);
+#undef FEW
     return hipGetLastError();
 }
 
