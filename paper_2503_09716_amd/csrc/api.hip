@@ -45,6 +45,7 @@ struct moe_ctx {
     int layer_y = -1;      // moe_layer's y_perm: 1 fp32, 0 bf16, -1 choose (its y_shared is always fp32)
     bool out_fp32 = false; // dtype of the layer output
     hipError_t route_backward_ready = hipSuccess;   // what setting up moe_route_backward's kernels gave
+    hipError_t few_ready = hipSuccess;              // the same of moe_layer_few's
     hipError_t fp4_product_ready = hipSuccess;      // the same of moe_mx_grouped_product's
     bool gate_packed = false;  // E > 16: the wg argument is already in the packed layout (moe_pack_gate)
     char* static_ws = nullptr;  // this device's address of `scratch`
@@ -956,7 +957,7 @@ const char* few_shape_problem(const moe_shape* s, moe_status* st) {
 }
 
 struct FewLayout {
-    size_t picks, arrived, logits, gate, h, partial, total;
+    size_t picks, arrived, logits, gate, x_copy, h, partial, total;
 };
 FewLayout few_layout(const moe_shape& s) {
     FewLayout L;
@@ -964,9 +965,10 @@ FewLayout few_layout(const moe_shape& s) {
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
     const size_t ep = (size_t)route_gemm_config(s).ep;
     L.picks = take(sizeof(Picks));
-    L.arrived = take((size_t)(s.H / DOWN_COLUMNS) * 4);
+    L.arrived = take((size_t)(s.H / 16) * 4);
     L.logits = take((size_t)s.T * ep * 4);
     L.gate = take(ep * s.H * 2);
+    L.x_copy = take(few_x_in_lds(s) ? 0 : few_x_bytes(s));
     L.h = take(few_h_bytes(s));
     L.partial = take(few_partial_bytes(s));
     L.total = std::max<size_t>(o, 256);
@@ -1025,6 +1027,8 @@ moe_status moe_create(moe_ctx** out, int device) {
     c->route_backward_ready = route_backward_init();
     if (c->route_backward_ready != hipSuccess) (void)hipGetLastError();   // theirs alone: the other calls do not need these kernels
     c->fp4_product_ready = fp4_product_init();
+    c->few_ready = few_init();
+    if (c->few_ready != hipSuccess) (void)hipGetLastError();
     if (c->fp4_product_ready != hipSuccess) (void)hipGetLastError();
     ok = ok && hipGetSymbolAddress((void**)&c->static_ws, HIP_SYMBOL(scratch)) == hipSuccess && c->static_ws != nullptr &&
          ((uintptr_t)c->static_ws & 255) == 0;
@@ -1690,6 +1694,7 @@ moe_status moe_layer_few(moe_ctx* c, const moe_shape* s, const void* x, const vo
     const FewLayout L = few_layout(*s);
     if (ws_bytes < L.total) return fail(c, MOE_E_WORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, L.total);
     HIP_TRY(c, hipSetDevice(c->device));
+    HIP_TRY(c, c->few_ready);
     char* const w8 = (char*)ws;
     hipStream_t hs = (hipStream_t)stream;
     const char* packed = (const char*)wg;
@@ -1708,6 +1713,11 @@ moe_status moe_layer_few(moe_ctx* c, const moe_shape* s, const void* x, const vo
     a.h = w8 + L.h;
     a.partial = (float*)(w8 + L.partial);
     a.arrived = (int32_t*)(w8 + L.arrived);
+    a.x_copy = w8 + L.x_copy;
+    a.x_in_lds = few_x_in_lds(*s);
+    a.x_bytes = (int32_t)few_x_bytes(*s);
+    a.h_row = few_h_row(*s);
+    a.down_columns = few_down_columns(*s, list->fp4 != 0);
     a.shares = few_shares(*s, list->fp4 != 0);
     a.nt = (double)list->experts * 3 * s->H * s->F * (list->fp4 ? 0.53125 : 2.0) > (double)(256 << 20);
     a.out = (char*)out;

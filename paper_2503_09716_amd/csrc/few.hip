@@ -87,37 +87,49 @@ __device__ __forceinline__ void gather_picks(Picks& s, const int32_t* idx, const
     __syncthreads();
 }
 
-// Logits of 16 experts (block nb) by one wavefront over the sub-tiles first, first + step, ..: lane (rl, g) gets tokens 4g .. 4g+3 of expert rl.
-__device__ __forceinline__ f32x4 logits_of(const FewArgs& p, const int nb, const int first, const int step) {
+// x in LDS or as a copy in memory, so that what one load of a wavefront takes is consecutive: pieces of 8 values in the order [step][part][row][g], where
+// piece (step, part, g) of a row is what lane group g multiplies in that part of that step (MXFP4: values 128 step + 32 g + 8 part on, bf16:
+// 32 step + 8 g on).  `row_pieces`: rows that it holds.
+template <bool FP4>
+__device__ __forceinline__ int x_place(const int piece, const int row, const int rows) {   // piece: of the row, in its own order
+    const int step_part = FP4 ? (piece >> 4) * 4 + (piece & 3) : piece >> 2, g = FP4 ? piece >> 2 & 3 : piece & 3;
+    return ((step_part * rows + row) * 4 + g) * 16;
+}
+
+// Logits of 16 experts (block nb) by one wavefront over the blocks of 32 first, first + step, ..: lane (rl, g) gets tokens 4g .. 4g+3 of expert rl.
+// x_of(s): the lane's piece of block s.
+template <class X>
+__device__ __forceinline__ f32x4 logits_of(const FewArgs& p, const int nb, const int first, const int step, const X x_of) {
     const int lane = threadIdx.x & 63, rl = lane & 15, g = lane >> 4;
-    const char* const xa = p.x + (size_t)min(rl, p.T - 1) * p.H * 2 + g * 16;
     const char* const wb = p.wg + (size_t)nb * (p.H >> 5) * 1024 + rl * 64 + ((g ^ block_swizzle(rl)) << 4);
     const int KS = p.H >> 5;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    constexpr int AHEAD = 8;
+    constexpr int AHEAD = 16;
     for (int s0 = first; s0 < KS; s0 += step * AHEAD) {
-        bf16x8 a[AHEAD], b[AHEAD];
+        u32x4 b[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int s = s0 + u * step;
-            if (s < KS) {   // wave-uniform
-                a[u] = *reinterpret_cast<const bf16x8*>(xa + (size_t)s * 64);
-                b[u] = *reinterpret_cast<const bf16x8*>(wb + (size_t)s * 1024);
-            } else {
-                a[u] = b[u] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-            }
-        }
+        for (int u = 0; u < AHEAD; ++u) b[u] = load_piece(wb + (size_t)min(s0 + u * step, KS - 1) * 1024);
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) acc = mfma(a[u], b[u], acc);
+        for (int u = 0; u < AHEAD; ++u)
+            if (s0 + u * step < KS) acc = mfma(__builtin_bit_cast(bf16x8, x_of(s0 + u * step)), __builtin_bit_cast(bf16x8, b[u]), acc);
     }
     return acc;
 }
 
-// A large gate matrix: one workgroup to 16 experts, K cut over its wavefronts, sums in wave order.
+// A large gate matrix, or more x than LDS holds: one workgroup to 16 experts, K cut over its wavefronts, sums in wave order; those behind them
+// copy x.
+template <bool FP4>
 __global__ __launch_bounds__(WAVES * 64) void few_logits_kernel(const FewArgs p) {
     __shared__ float part[WAVES][256];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const f32x4 acc = logits_of(p, blockIdx.x, wave, WAVES);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int blocks = (p.E + 15) >> 4;
+    if ((int)blockIdx.x >= blocks) {
+        const int pieces = p.H >> 3, i = (blockIdx.x - blocks) * WAVES * 64 + tid, row = i / pieces, piece = i - row * pieces;
+        if (row < p.T) *reinterpret_cast<u32x4*>(p.x_copy + x_place<FP4>(piece, row, p.T)) = load_piece(p.x + (size_t)i * 16);
+        return;
+    }
+    const char* const xa = p.x + (size_t)min(lane & 15, p.T - 1) * p.H * 2 + (lane >> 4) * 16;
+    const f32x4 acc = logits_of(p, blockIdx.x, wave, WAVES, [&](const int s) __attribute__((always_inline)) { return load_piece(xa + (size_t)s * 64); });
 #pragma unroll
     for (int r = 0; r < 4; ++r) part[wave][(4 * (lane >> 4) + r) * 16 + (lane & 15)] = acc[r];
     __syncthreads();
@@ -148,24 +160,42 @@ __device__ __forceinline__ void select(const FewArgs& p, const float* logits, co
     }
 }
 
-// Gate and up, and the router before them.  A workgroup takes 32 columns of both matrices of a picked or shared expert at a time, its wavefronts every
-// eighth sub-tile of the contraction (eight together read consecutive blocks), and their sums meet in LDS.  The loads of the next steps, the
-// next columns' among them, are on their way while one is multiplied.
-template <bool FP4, bool NT>
+// h: row [step][part][hi, lo][g] of pieces of 8, as x above.
+template <bool FP4>
+__device__ __forceinline__ int h_place(const int f) {   // byte of the high half of value f; the low half 64 bytes on
+    return FP4 ? (f >> 7) * 512 + (f >> 3 & 3) * 128 + (f >> 5 & 3) * 16 + (f & 7) * 2 : (f >> 5) * 128 + (f >> 3 & 3) * 16 + (f & 7) * 2;
+}
+
+// A contraction is cut into tasks of four steps (MXFP4: 512, one dword of scales to a lane; bf16: 128).
+constexpr int TASK = 4;
+
+// Gate and up, and the router before them.  An item is 32 columns of both matrices of a picked or shared expert; the tasks of a workgroup's items, one
+// after the other, go to its wavefronts in turn, and after each round the sums of eight tasks meet in LDS, where every thread adds up one
+// column of a token in the order of the tasks.  Loads run a task ahead.  XLDS: x is in LDS.
+template <bool FP4, bool NT, bool XLDS>
 __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
-    // the logits and their parts, then the wavefronts' sums (two places in turn: one barrier each)
+    extern __shared__ __attribute__((aligned(16))) char x_lds[];
+    // the logits and their parts, then the wavefronts' sums (two places in turn: one barrier a round)
     __shared__ __attribute__((aligned(16))) float room[2][WAVES][2][2][256];
-    __shared__ __attribute__((aligned(16))) Picks picks;
+    __shared__ Picks picks;
     __shared__ int32_t idx[FEW_TOKENS * FEW_TOP_K];
     __shared__ float w[FEW_TOKENS * FEW_TOP_K];
     __shared__ const char* matrix[2][256];   // of every expert
     float* const logits = &room[0][0][0][0][0];
     float(*const part)[256] = room[1][0][0];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rl = lane & 15, g = lane >> 4;
-    const int experts = p.E + p.Ns;
+    const int experts = p.E + p.Ns, x_row = min(rl, p.T - 1);
     if (tid < 256)
 #pragma unroll
         for (int m = 0; m < 2; ++m) matrix[m][tid] = (const char*)p.weights[m * experts + min(tid, experts - 1)];
+    if (XLDS) {
+        const int pieces = p.H >> 3;
+        for (int i = tid; i < p.T * pieces; i += WAVES * 64) {
+            const int row = i / pieces, piece = i - row * pieces;
+            *reinterpret_cast<u32x4*>(x_lds + x_place<FP4>(piece, row, p.T)) = load_piece(p.x + (size_t)i * 16);
+        }
+        __syncthreads();
+    }
     if (!p.logits) {
         // up to 8 blocks of 16 experts side by side; what wavefronts are left share the contraction, and are added in order
         const int blocks = (p.E + 15) >> 4;
@@ -173,7 +203,9 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
         while (per > 1 && WAVES / per < blocks) per >>= 1;
         const int beside = WAVES / per, share = wave / beside;
         for (int nb = wave - share * beside; nb < blocks; nb += beside) {
-            const f32x4 acc = logits_of(p, nb, share, per);
+            const f32x4 acc = logits_of(p, nb, share, per, [&](const int s) __attribute__((always_inline)) {
+                return *reinterpret_cast<const u32x4*>(x_lds + x_place<FP4>(s * 4 + g, x_row, p.T));
+            });
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 if (per == 1) logits[(4 * g + r) * LOGIT_STRIDE + nb * 16 + rl] = acc[r];
@@ -204,117 +236,131 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
     if (blockIdx.x == 0) {
         const uint32_t* const from = reinterpret_cast<const uint32_t*>(&picks);
         for (int i = tid; i < (int)sizeof(Picks) / 4; i += WAVES * 64) reinterpret_cast<uint32_t*>(p.picks)[i] = from[i];
-        for (int i = tid; i < p.H / DOWN_COLUMNS; i += WAVES * 64) p.arrived[i] = 0;
+        for (int i = tid; i < p.H >> 4; i += WAVES * 64) p.arrived[i] = 0;
     }
 
     const int units = p.F >> 5, n_active = __builtin_amdgcn_readfirstlane(picks.n);
-    const int KT = FP4 ? (p.H + 127) >> 7 : p.H >> 5, groups = (p.H + 511) >> 9, steps = (KT + WAVES - 1) / WAVES;
+    const int KT = FP4 ? (p.H + 127) >> 7 : p.H >> 5, groups = (p.H + 511) >> 9, G = (KT + TASK - 1) / TASK;
     const int items = (n_active + p.Ns) * units, mine = items > (int)blockIdx.x ? (items - 1 - blockIdx.x) / gridDim.x + 1 : 0;
-    const char* const xa = p.x + (size_t)min(rl, p.T - 1) * p.H * 2 + g * (FP4 ? 64 : 16);
+    const int tasks = mine * G;
     const uint32_t lane_w = (uint32_t)(rl * 64 + ((g ^ block_swizzle(rl)) << 4)), lane_s = (uint32_t)(rl * 16 + g * 4);
-    constexpr int DEPTH = FP4 ? 2 : 4, PARTS = FP4 ? 4 : 1, XSTEP = FP4 ? 256 : 64;
-    u32x4 a[DEPTH][2][2], x[DEPTH][PARTS];
-    uint32_t sc[DEPTH][2][2];
-    // what is asked for next: step `ls` of item blockIdx.x + li * gridDim.x, its expert's matrices and columns
-    int li = 0, ls = 0;
+    constexpr int PARTS = FP4 ? 4 : 1;
+    u32x4 a[TASK][2][2], x[XLDS ? 1 : TASK][PARTS];
+    uint32_t sc[2][2], sc_next[2][2];
+    const uint32_t lane_x = (uint32_t)(x_row * 64 + g * 16);
+    // asked for next: step `ls` of task group lg of the li-th item
+    int lq = wave, li = wave / G, lg = wave - li * G, ls = 0;
     const char *lw[2] = {nullptr, nullptr};
+    int block = 0;
     auto load = [&](const int slot) __attribute__((always_inline)) {
-        if (li >= mine) return;
-        const int item = blockIdx.x + li * gridDim.x, at = item / units, unit = item - at * units;
+        if (lq >= tasks) return;
         if (ls == 0) {
-            const int e = at < n_active ? picks.active[at] : p.E + at - n_active;
+            const int item = blockIdx.x + li * gridDim.x, at = item / units, e = at < n_active ? picks.active[at] : p.E + at - n_active;
+            block = (item - at * units) * 2;
             lw[0] = uniform(matrix[0][e]);
             lw[1] = uniform(matrix[1][e]);
+            if (FP4)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) sc_next[m][c] = load_word(lw[m] + p.up_scales_at + ((size_t)(block + c) * groups + lg) * 256 + lane_s);
         }
-        const int t = wave + ls * WAVES;
+        const int t = lg * TASK + ls;
         if (t < KT) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int block = unit * 2 + c;
-                    a[slot][m][c] = load_piece<NT>(lw[m] + ((size_t)block * KT + t) * 1024 + lane_w);
-                    if (FP4) sc[slot][m][c] = load_word(lw[m] + p.up_scales_at + ((size_t)block * groups + (t >> 2)) * 256 + lane_s);
-                }
+                for (int c = 0; c < 2; ++c) a[slot][m][c] = load_piece<NT>(lw[m] + ((size_t)(block + c) * KT + t) * 1024 + lane_w);
+            if (!XLDS)
 #pragma unroll
-            for (int f = 0; f < PARTS; ++f) {
-                // past H (a multiple of 64) the weights are zero; x there is not read
-                const bool in = !FP4 || t * 128 + g * 32 < p.H;
-                x[slot][f] = in ? load_piece(xa + (size_t)t * XSTEP + f * 16) : u32x4{0u, 0u, 0u, 0u};
-            }
+                for (int f = 0; f < PARTS; ++f) x[slot % (XLDS ? 1 : TASK)][f] = load_piece(p.x_copy + (size_t)(t * PARTS + f) * p.T * 64 + lane_x);
         }
-        if (++ls == steps) { ls = 0; ++li; }
+        if (++ls == TASK) {
+            ls = 0;
+            lq += WAVES;
+            for (lg += WAVES; lg >= G; lg -= G) ++li;
+        }
     };
 #pragma unroll
-    for (int u = 0; u < DEPTH; ++u) load(u);
-    f32x4 acc[2][2] = {};
-    int i = 0, s = 0;   // item and step that are multiplied next
-    while (i < mine) {
+    for (int u = 0; u < TASK; ++u) load(u);
+    float gate = 0.f, up = 0.f;   // of token tid / 32, column tid % 32 of the item that is being added up
+    int item = 0, group = 0, my_group = wave % G;
+    for (int q0 = 0; q0 < tasks; q0 += WAVES) {
+        f32x4 acc[2][2] = {};
+        if (q0 + wave < tasks) {
 #pragma unroll
-        for (int u = 0; u < DEPTH; ++u) {
-            if (i >= mine) break;
-            if (wave + s * WAVES < KT) {
+            for (int u = 0; u < TASK; ++u) {
+                if (u == 0)
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                    for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const float scale = FP4 ? scale_of(sc[u][m][c], wave) : 0.f;
+                        for (int c = 0; c < 2; ++c) sc[m][c] = sc_next[m][c];
+                const int t = my_group * TASK + u;
+                if (t < KT) {
+                    if (XLDS)
 #pragma unroll
-                        for (int f = 0; f < PARTS; ++f) acc[m][c] = mfma(weight_part<FP4>(a[u][m][c], scale, f), __builtin_bit_cast(bf16x8, x[u][f]), acc[m][c]);
+                        for (int f = 0; f < PARTS; ++f) x[0][f] = *reinterpret_cast<const u32x4*>(x_lds + (t * PARTS + f) * p.T * 64 + lane_x);
+#pragma unroll
+                    for (int f = 0; f < PARTS; ++f) {
+                        // past H (a multiple of 64) the weights are zero and x is not there
+                        u32x4 v = x[XLDS ? 0 : u][f];
+                        if (FP4 && t * 128 + g * 32 >= p.H) v = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+#pragma unroll
+                            for (int c = 0; c < 2; ++c)
+                                acc[m][c] = mfma(weight_part<FP4>(a[u][m][c], FP4 ? scale_of(sc[m][c], u) : 0.f, f), __builtin_bit_cast(bf16x8, v), acc[m][c]);
                     }
+                }
+                load(u);
             }
-            load(u);
-            if (++s < steps) continue;
-            // the item's last step: lane (rl, g) has columns 4 g + r of 16 of token rl
-            float(*const sums)[2][2][256] = room[i & 1];
+            for (my_group += WAVES; my_group >= G;) my_group -= G;
+        }
+        // lane (rl, g) has columns 4 g + r of 16 of token rl
+        float(*const sums)[2][2][256] = room[q0 / WAVES & 1];
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    *reinterpret_cast<f32x4*>(&sums[wave][m][c][rl * 16 + 4 * g]) = acc[m][c];
-                    acc[m][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-                }
-            __syncthreads();
-            {
-                const int item = blockIdx.x + i * gridDim.x, at = item / units, unit = item - at * units;
-                const int e = at < n_active ? picks.active[at] : p.E + at - n_active;
-                const int t = tid >> 5, c = tid >> 4 & 1, n = tid & 15;   // token, half and column of the unit
-                int row = -1;
-                float weight = 1.f;
-                if (t < p.T) {
-                    if (at >= n_active) row = p.T * (p.k + at - n_active) + t;
-                    else if (picks.pick[e][t] >= 0) {
-                        row = t * p.k + picks.pick[e][t];
-                        weight = w[row];
-                    }
-                }
-                if (row >= 0) {
-                    float gate = 0.f, up = 0.f;
+            for (int c = 0; c < 2; ++c) *reinterpret_cast<f32x4*>(&sums[wave][m][c][rl * 16 + 4 * g]) = acc[m][c];
+        __syncthreads();
+        const int t = tid >> 5, c = tid >> 4 & 1, n = tid & 15;
 #pragma unroll
-                    for (int q = 0; q < WAVES; ++q) {
-                        gate += sums[q][0][c][t * 16 + n];
-                        up += sums[q][1][c][t * 16 + n];
-                    }
-                    const float v = weight * (gate / (1.0f + __expf(-gate)) * up);
-                    const __bf16 hi = (__bf16)v;
-                    char* const to = p.h + ((size_t)row * (p.F >> 3) + unit * 4 + c * 2 + (n >> 3)) * 32 + (n & 7) * 2;
-                    *reinterpret_cast<__bf16*>(to) = hi;
-                    *reinterpret_cast<__bf16*>(to + 16) = __builtin_isfinite((float)hi) ? (__bf16)(v - (float)hi) : (__bf16)0.0f;
+        for (int q = 0; q < WAVES; ++q) {
+            if (q0 + q >= tasks) break;
+            gate += sums[q][0][c][t * 16 + n];
+            up += sums[q][1][c][t * 16 + n];
+            if (++group < G) continue;
+            const int it = blockIdx.x + item * gridDim.x, at = it / units, f = (it - at * units) * 32 + c * 16 + n;
+            int row = -1;
+            float weight = 1.f;
+            if (t < p.T) {
+                if (at >= n_active) row = p.T * (p.k + at - n_active) + t;
+                else if (const int j = picks.pick[picks.active[at]][t]; j >= 0) {
+                    row = t * p.k + j;
+                    weight = w[row];
                 }
             }
-            s = 0;
-            ++i;
+            if (row >= 0) {
+                const float v = weight * (gate / (1.0f + __expf(-gate)) * up);
+                const __bf16 hi = (__bf16)v;
+                char* const to = p.h + (size_t)row * p.h_row + h_place<FP4>(f);
+                *reinterpret_cast<__bf16*>(to) = hi;
+                *reinterpret_cast<__bf16*>(to + 64) = __builtin_isfinite((float)hi) ? (__bf16)(v - (float)hi) : (__bf16)0.0f;
+            }
+            gate = up = 0.f;
+            group = 0;
+            ++item;
         }
     }
 }
 
-// Down: 64 columns to a workgroup, and a share of all sub-tiles of all picked and shared experts, one after the other; its wavefronts take every eighth of
-// them.  The shares' sums meet in the workgroup that comes last, which adds them in order: no workgroup waits for another.  Sums and
-// counter pass by the L2s, each of which only its own XCD sees.
-template <bool FP4, bool NT>
+// Down: NB * 16 columns to a workgroup, and a share of the tasks of all picked and shared experts, one after the other; its wavefronts take them in turn.
+// The shares' sums meet in the workgroup that comes last, which adds them in order: no workgroup waits for another.  Sums and counter
+// pass by the L2s, each of which only its own XCD sees.
+template <bool FP4, bool NT, int NB>
 __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
-    __shared__ __attribute__((aligned(16))) Picks picks;
-    __shared__ __attribute__((aligned(16))) float sums[WAVES][4][256];
+    __shared__ Picks picks;
+    __shared__ __attribute__((aligned(16))) float sums[WAVES][NB][256];
     __shared__ const char* matrix[256];   // of every expert
     __shared__ int last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rl = lane & 15, g = lane >> 4;
@@ -325,157 +371,187 @@ __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
     __syncthreads();
     const int n_active = __builtin_amdgcn_readfirstlane(picks.n);
     const int share = blockIdx.x % p.shares, columns = blockIdx.x / p.shares;
-    const int KT = FP4 ? (p.F + 127) >> 7 : p.F >> 5, groups = (p.F + 511) >> 9;
-    constexpr int DEPTH = FP4 ? 2 : 4, PARTS = FP4 ? 4 : 1, HSTEP = FP4 ? 512 : 128, NB = DOWN_COLUMNS / 16;
+    const int KT = FP4 ? (p.F + 127) >> 7 : p.F >> 5, groups = (p.F + 511) >> 9, G = (KT + TASK - 1) / TASK;
+    constexpr int DEPTH = FP4 && NB > 1 ? 2 : TASK, PARTS = FP4 ? 4 : 1, HSTEP = FP4 ? 512 : 128;
     const uint32_t lane_w = (uint32_t)(rl * 64 + ((g ^ block_swizzle(rl)) << 4)), lane_s = (uint32_t)(rl * 16 + g * 4);
-    const int total = (n_active + p.Ns) * KT;
+    const int total = (n_active + p.Ns) * G;
     const int from = (int)((int64_t)total * share / p.shares), to = (int)((int64_t)total * (share + 1) / p.shares);
     u32x4 a[DEPTH][NB], hi[DEPTH][PARTS], lo[DEPTH][PARTS];
-    uint32_t sc[DEPTH][NB];
-    int expert[DEPTH];       // which in the list; -1: none
-    bool picked[DEPTH];
-    int lc = from + wave, le = lc / KT, lt = lc - le * KT;   // sub-tile lt of the le-th expert is asked for next
+    uint32_t sc[NB], sc_next[NB];
+    // asked for next: step `ls` of group lg of the le-th expert
+    int lq = from + wave, le = lq / G, lg = lq - le * G, ls = 0, row = -1;
+    const char* w2 = nullptr;
     auto load = [&](const int slot) __attribute__((always_inline)) {
-        expert[slot] = -1;
-        picked[slot] = false;
-        if (lc >= to) return;
-        expert[slot] = le;
-        const int e = __builtin_amdgcn_readfirstlane(le < n_active ? picks.active[le] : p.E + le - n_active);
-        const char* const w2 = uniform(matrix[e]);
+        if (lq >= to) return;
+        if (ls == 0) {
+            const int e = __builtin_amdgcn_readfirstlane(le < n_active ? picks.active[le] : p.E + le - n_active);
+            w2 = uniform(matrix[e]);
+            row = -1;
+            if (rl < p.T) {
+                if (le >= n_active) row = p.T * (p.k + le - n_active) + rl;
+                else if (const int j = picks.pick[e][rl]; j >= 0) row = rl * p.k + j;
+            }
+            if (FP4)
 #pragma unroll
-        for (int c = 0; c < NB; ++c) {
-            const int block = columns * NB + c;
-            a[slot][c] = load_piece<NT>(w2 + ((size_t)block * KT + lt) * 1024 + lane_w);
-            if (FP4) sc[slot][c] = load_word(w2 + p.down_scales_at + ((size_t)block * groups + (lt >> 2)) * 256 + lane_s) >> (8 * (lt & 3));
+                for (int c = 0; c < NB; ++c) sc_next[c] = load_word(w2 + p.down_scales_at + ((size_t)(columns * NB + c) * groups + lg) * 256 + lane_s);
         }
-        int row = -1;
-        if (rl < p.T) {
-            if (le >= n_active) row = p.T * (p.k + le - n_active) + rl;
-            else if (const int j = picks.pick[e][rl]; j >= 0) row = rl * p.k + j;
-        }
-        picked[slot] = row >= 0;
-        const bool in = row >= 0 && (!FP4 || lt * 128 + g * 32 < p.F);
-        const char* const from_h = p.h + (size_t)max(row, 0) * p.F * 4 + (size_t)lt * HSTEP + g * (FP4 ? 128 : 32);
+        const int t = lg * TASK + ls;
+        if (t < KT) {
 #pragma unroll
-        for (int f = 0; f < PARTS; ++f) {
-            hi[slot][f] = in ? load_piece(from_h + f * 32) : u32x4{0u, 0u, 0u, 0u};
-            lo[slot][f] = in ? load_piece(from_h + f * 32 + 16) : u32x4{0u, 0u, 0u, 0u};
+            for (int c = 0; c < NB; ++c) a[slot][c] = load_piece<NT>(w2 + ((size_t)(columns * NB + c) * KT + t) * 1024 + lane_w);
+            const bool in = row >= 0 && (!FP4 || t * 128 + g * 32 < p.F);
+            const char* const from_h = p.h + (size_t)max(row, 0) * p.h_row + (size_t)t * HSTEP + g * 16;
+#pragma unroll
+            for (int f = 0; f < PARTS; ++f) {
+                hi[slot][f] = in ? load_piece(from_h + f * 128) : u32x4{0u, 0u, 0u, 0u};
+                lo[slot][f] = in ? load_piece(from_h + f * 128 + 64) : u32x4{0u, 0u, 0u, 0u};
+            }
         }
-        lc += WAVES;
-        for (lt += WAVES; lt >= KT; lt -= KT) ++le;
+        if (++ls == TASK) {
+            ls = 0;
+            lq += WAVES;
+            for (lg += WAVES; lg >= G; lg -= G) ++le;
+        }
     };
 #pragma unroll
     for (int u = 0; u < DEPTH; ++u) load(u);
-    // each expert's sum by itself: a token that did not pick it takes nothing from it, not even what is not a number
-    f32x4 acc[NB] = {}, sum[NB] = {};
-    int now = expert[0];
-    bool now_picked = picked[0];
-    auto flush = [&]() __attribute__((always_inline)) {
+    f32x4 sum[NB] = {};
+    for (int q = from + wave; q < to; q += WAVES) {
+        const int at = q / G, group = q - at * G;
+        f32x4 acc[NB] = {};
 #pragma unroll
-        for (int c = 0; c < NB; ++c) {
-            if (now_picked) sum[c] += acc[c];
-            acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-    };
-    for (bool more = expert[0] >= 0; more;) {
+        for (int u = 0; u < TASK; ++u) {
+            if (u == 0)
 #pragma unroll
-        for (int u = 0; u < DEPTH; ++u) {
-            if (expert[u] < 0) { more = false; break; }
-            if (expert[u] != now) {
-                flush();
-                now = expert[u];
-                now_picked = picked[u];
-            }
+                for (int c = 0; c < NB; ++c) sc[c] = sc_next[c];
+            if (group * TASK + u < KT) {
 #pragma unroll
-            for (int c = 0; c < NB; ++c) {
-                const float scale = FP4 ? scale_of(sc[u][c], 0) : 0.f;
+                for (int c = 0; c < NB; ++c) {
+                    const float scale = FP4 ? scale_of(sc[c], u) : 0.f;
 #pragma unroll
-                for (int f = 0; f < PARTS; ++f) {
-                    const bf16x8 v = weight_part<FP4>(a[u][c], scale, f);
-                    acc[c] = mfma(v, __builtin_bit_cast(bf16x8, hi[u][f]), acc[c]);
-                    acc[c] = mfma(v, __builtin_bit_cast(bf16x8, lo[u][f]), acc[c]);
+                    for (int f = 0; f < PARTS; ++f) {
+                        const bf16x8 v = weight_part<FP4>(a[u % DEPTH][c], scale, f);
+                        acc[c] = mfma(v, __builtin_bit_cast(bf16x8, hi[u % DEPTH][f]), acc[c]);
+                        acc[c] = mfma(v, __builtin_bit_cast(bf16x8, lo[u % DEPTH][f]), acc[c]);
+                    }
                 }
             }
-            load(u);
+            load(u % DEPTH);
         }
+        // a token that did not pick the expert takes nothing from it, not even what is not a number
+        bool picked = rl < p.T;
+        if (at < n_active && picked) picked = picks.pick[picks.active[at]][rl] >= 0;
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+            if (picked) sum[c] += acc[c];
     }
-    flush();
 #pragma unroll
     for (int c = 0; c < NB; ++c) *reinterpret_cast<f32x4*>(&sums[wave][c][rl * 16 + 4 * g]) = sum[c];
     __syncthreads();
-    // thread: columns n and n + 32 of a token
-    const int t = tid >> 5, n = tid & 31;
-    float v[2] = {0.f, 0.f};
+    // thread: columns n, n + 32 of a token (NB = 4), or one of 16 columns (NB = 1)
+    constexpr int WIDE = NB == 4 ? 32 : 16, EACH = NB == 4 ? 2 : 1, COLUMNS = NB * 16;
+    const int t = tid / WIDE, n = tid % WIDE;
+    float v[EACH];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < EACH; ++j) {
+        v[j] = 0.f;
+        const int col = j * 32 + n;
+        if (t < FEW_TOKENS)
 #pragma unroll
-        for (int q = 0; q < WAVES; ++q) v[j] += sums[q][j * 2 + (n >> 4)][t * 16 + (n & 15)];
+            for (int q = 0; q < WAVES; ++q) v[j] += sums[q][col >> 4][t * 16 + (col & 15)];
+    }
     if (p.shares > 1) {
-        float* const mine = p.partial + ((size_t)columns * p.shares + share) * (FEW_TOKENS * DOWN_COLUMNS);
+        float* const all = p.partial + (size_t)columns * p.shares * (FEW_TOKENS * COLUMNS);
+        if (t < FEW_TOKENS)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) __hip_atomic_store(&mine[t * DOWN_COLUMNS + j * 32 + n], v[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            for (int j = 0; j < EACH; ++j)
+                __hip_atomic_store(&all[(size_t)share * (FEW_TOKENS * COLUMNS) + t * COLUMNS + j * 32 + n], v[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): they have arrived
         __syncthreads();
         if (tid == 0) last = __hip_atomic_fetch_add(&p.arrived[columns], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.shares - 1;
         __syncthreads();
-        if (!last) return;
-        const float* const all = p.partial + (size_t)columns * p.shares * (FEW_TOKENS * DOWN_COLUMNS);
-        v[0] = v[1] = 0.f;
+        if (!last || t >= p.T) return;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) v[j] = 0.f;
         constexpr int AHEAD = 8;   // loads on their way
         for (int q0 = 0; q0 < p.shares; q0 += AHEAD) {
-            float u[AHEAD][2];
+            float u[AHEAD][EACH];
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    u[q][j] = __hip_atomic_load(&all[(size_t)min(q0 + q, p.shares - 1) * (FEW_TOKENS * DOWN_COLUMNS) + t * DOWN_COLUMNS + j * 32 + n],
+                for (int j = 0; j < EACH; ++j)
+                    u[q][j] = __hip_atomic_load(&all[(size_t)min(q0 + q, p.shares - 1) * (FEW_TOKENS * COLUMNS) + t * COLUMNS + j * 32 + n],
                                                 __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) v[j] += q0 + q < p.shares ? u[q][j] : 0.f;
+                for (int j = 0; j < EACH; ++j) v[j] += q0 + q < p.shares ? u[q][j] : 0.f;
         }
     }
     if (t >= p.T) return;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const size_t o = (size_t)t * p.H + columns * DOWN_COLUMNS + j * 32 + n;
+    for (int j = 0; j < EACH; ++j) {
+        const size_t o = (size_t)t * p.H + columns * COLUMNS + j * 32 + n;
         if (p.out_fp32) *reinterpret_cast<float*>(p.out + o * 4) = v[j];
         else *reinterpret_cast<__bf16*>(p.out + o * 2) = (__bf16)v[j];
     }
 }
 
-}  // namespace
-
-int few_shares(const moe_shape& s, bool fp4) {
-    const int64_t active = std::min<int64_t>(s.E, (int64_t)s.T * s.top_k) + s.num_shared, sub_tiles = active * ((s.F + (fp4 ? 127 : 31)) / (fp4 ? 128 : 32));
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 256 / (s.H / DOWN_COLUMNS), (sub_tiles + WAVES - 1) / WAVES}));
+// Tasks of the down launch.
+int64_t down_tasks(const moe_shape& s, const bool fp4) {
+    const int64_t active = std::min<int64_t>(s.E, (int64_t)s.T * s.top_k) + s.num_shared;
+    return active * ((s.F + (fp4 ? 511 : 127)) / (fp4 ? 512 : 128));
 }
 
-size_t few_h_bytes(const moe_shape& s) { return (size_t)s.T * (s.top_k + s.num_shared) * s.F * 4; }
-size_t few_partial_bytes(const moe_shape& s) { return (size_t)(s.H / DOWN_COLUMNS) * FEW_SHARES * FEW_TOKENS * DOWN_COLUMNS * 4; }
+}  // namespace
 
-bool few_routes_inside(const moe_shape& s) { return (int64_t)((s.E + 15) / 16) * s.H * 32 <= 128 << 10; }
+size_t few_x_bytes(const moe_shape& s) { return (size_t)s.T * ((s.H + 127) / 128 * 128) * 2; }
+int few_h_row(const moe_shape& s) { return (s.F + 127) / 128 * 512; }   // bytes
+size_t few_h_bytes(const moe_shape& s) { return (size_t)s.T * (s.top_k + s.num_shared) * few_h_row(s); }
+size_t few_partial_bytes(const moe_shape& s) { return (size_t)s.H * FEW_SHARES * FEW_TOKENS * 4; }
 
-hipError_t launch_few(const FewArgs& a, bool fp4, hipStream_t st) {
+bool few_x_in_lds(const moe_shape& s) { return few_x_bytes(s) <= FEW_X_LDS; }
+bool few_routes_inside(const moe_shape& s) { return few_x_in_lds(s) && (int64_t)((s.E + 15) / 16) * s.H * 32 <= 128 << 10; }
+
+int few_down_columns(const moe_shape& s, bool fp4) { return down_tasks(s, fp4) <= 32 ? 16 : 64; }
+int few_shares(const moe_shape& s, bool fp4) {
+    const int columns = s.H / few_down_columns(s, fp4);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 256 / columns, (down_tasks(s, fp4) + WAVES - 1) / WAVES}));
+}
+
+hipError_t few_init() {
+    const auto to = hipFuncAttributeMaxDynamicSharedMemorySize;
+    for (const void* k : {reinterpret_cast<const void*>(&few_up_kernel<true, true, true>), reinterpret_cast<const void*>(&few_up_kernel<true, false, true>),
+                          reinterpret_cast<const void*>(&few_up_kernel<false, true, true>), reinterpret_cast<const void*>(&few_up_kernel<false, false, true>)})
+        if (const hipError_t e = hipFuncSetAttribute(k, to, FEW_X_LDS)) return e;
+    return hipSuccess;
+}
+
+namespace {
+
+template <bool FP4, bool NT>
+hipError_t launch(const FewArgs& a, hipStream_t st) {
+    const dim3 block(WAVES * 64);
     if (a.logits) {
-        hipLaunchKernelGGL(few_logits_kernel, dim3((unsigned)((a.E + 15) / 16)), dim3(WAVES * 64), 0, st, a);
+        const int blocks = (a.E + 15) / 16, copies = a.x_in_lds ? 0 : (a.T * (a.H / 8) + WAVES * 64 - 1) / (WAVES * 64);
+        hipLaunchKernelGGL(few_logits_kernel<FP4>, dim3((unsigned)(blocks + copies)), block, 0, st, a);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     const int64_t active = std::min<int64_t>(a.E, (int64_t)a.T * a.k) + a.Ns, items = active * (a.F / 32);
-    const dim3 up((unsigned)std::min<int64_t>(512, items)), down((unsigned)(a.H / DOWN_COLUMNS * a.shares)), block(WAVES * 64);
-#define FEW(FP4_, NT_)                                                                      \
-    do {                                                                                    \
-        hipLaunchKernelGGL((few_up_kernel<FP4_, NT_>), up, block, 0, st, a);                \
-        if (const hipError_t e = hipGetLastError()) return e;                               \
-        hipLaunchKernelGGL((few_down_kernel<FP4_, NT_>), down, block, 0, st, a);            \
-    } while (0)
-    if (fp4 && a.nt) FEW(true, true);
-    else if (fp4) FEW(true, false);
-    else if (a.nt) FEW(false, true);
-    else FEW(false, false);
-#undef FEW
+    const dim3 up((unsigned)std::min<int64_t>(256, items)), down((unsigned)(a.H / a.down_columns * a.shares));
+    if (a.x_in_lds) hipLaunchKernelGGL((few_up_kernel<FP4, NT, true>), up, block, (unsigned)a.x_bytes, st, a);
+    else hipLaunchKernelGGL((few_up_kernel<FP4, NT, false>), up, block, 0, st, a);
+    if (const hipError_t e = hipGetLastError()) return e;
+    if (a.down_columns == 16) hipLaunchKernelGGL((few_down_kernel<FP4, NT, 1>), down, block, 0, st, a);
+    else hipLaunchKernelGGL((few_down_kernel<FP4, NT, 4>), down, block, 0, st, a);
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_few(const FewArgs& a, bool fp4, hipStream_t st) {
+    if (fp4) return a.nt ? launch<true, true>(a, st) : launch<true, false>(a, st);
+    return a.nt ? launch<false, true>(a, st) : launch<false, false>(a, st);
 }
 
 }  // namespace moe
