@@ -108,7 +108,8 @@ __device__ __forceinline__ f32x4 logits_of(const FewArgs& p, const int nb, const
     for (int s0 = first; s0 < KS; s0 += step * AHEAD) {
         u32x4 b[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) b[u] = load_piece(wb + (size_t)min(s0 + u * step, KS - 1) * 1024);
+        for (int u = 0; u < AHEAD; ++u)
+            if (s0 + u * step < KS) b[u] = load_piece(wb + (size_t)(s0 + u * step) * 1024);   // wave-uniform
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
             if (s0 + u * step < KS) acc = mfma(__builtin_bit_cast(bf16x8, x_of(s0 + u * step)), __builtin_bit_cast(bf16x8, b[u]), acc);
@@ -169,20 +170,22 @@ __device__ __forceinline__ int h_place(const int f) {   // byte of the high half
 // A contraction is cut into tasks of four steps (MXFP4: 512, one dword of scales to a lane; bf16: 128).
 constexpr int TASK = 4;
 
-// Gate and up, and the router before them.  An item is 32 columns of both matrices of a picked or shared expert; the tasks of a workgroup's items, one
+// Gate and up, and the router before them.  An item is 32 columns (64 where x does not fit LDS: each load of it then
+// meets twice the weights) of both matrices of a picked or shared expert; the tasks of a workgroup's items, one
 // after the other, go to its wavefronts in turn, and after each round the sums of eight tasks meet in LDS, where every thread adds up one
 // column of a token in the order of the tasks.  Loads run a task ahead.  XLDS: x is in LDS.
 template <bool FP4, bool NT, bool XLDS>
 __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
     extern __shared__ __attribute__((aligned(16))) char x_lds[];
-    // the logits and their parts, then the wavefronts' sums (two places in turn: one barrier a round)
-    __shared__ __attribute__((aligned(16))) float room[2][WAVES][2][2][256];
+    // the logits and their parts, then the wavefronts' sums (in two places in turn one barrier a round is enough)
+    constexpr int NB = XLDS ? 2 : 4, PLACES = XLDS ? 2 : 1, DEPTH = FP4 && !XLDS ? 2 : TASK;
+    __shared__ __attribute__((aligned(16))) float room[PLACES][WAVES][2][NB][256];
     __shared__ Picks picks;
     __shared__ int32_t idx[FEW_TOKENS * FEW_TOP_K];
     __shared__ float w[FEW_TOKENS * FEW_TOP_K];
     __shared__ const char* matrix[2][256];   // of every expert
     float* const logits = &room[0][0][0][0][0];
-    float(*const part)[256] = room[1][0][0];
+    float(*const part)[256] = room[0][WAVES / 2][0];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rl = lane & 15, g = lane >> 4;
     const int experts = p.E + p.Ns, x_row = min(rl, p.T - 1);
     if (tid < 256)
@@ -239,14 +242,14 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
         for (int i = tid; i < p.H >> 4; i += WAVES * 64) p.arrived[i] = 0;
     }
 
-    const int units = p.F >> 5, n_active = __builtin_amdgcn_readfirstlane(picks.n);
+    const int units = p.F / (NB * 16), n_active = __builtin_amdgcn_readfirstlane(picks.n);
     const int KT = FP4 ? (p.H + 127) >> 7 : p.H >> 5, groups = (p.H + 511) >> 9, G = (KT + TASK - 1) / TASK;
     const int items = (n_active + p.Ns) * units, mine = items > (int)blockIdx.x ? (items - 1 - blockIdx.x) / gridDim.x + 1 : 0;
     const int tasks = mine * G;
     const uint32_t lane_w = (uint32_t)(rl * 64 + ((g ^ block_swizzle(rl)) << 4)), lane_s = (uint32_t)(rl * 16 + g * 4);
     constexpr int PARTS = FP4 ? 4 : 1;
-    u32x4 a[TASK][2][2], x[XLDS ? 1 : TASK][PARTS];
-    uint32_t sc[2][2], sc_next[2][2];
+    u32x4 a[DEPTH][2][NB], x[XLDS ? 1 : DEPTH][PARTS];
+    uint32_t sc[2][NB], sc_next[2][NB];
     const uint32_t lane_x = (uint32_t)(x_row * 64 + g * 16);
     // asked for next: step `ls` of task group lg of the li-th item
     int lq = wave, li = wave / G, lg = wave - li * G, ls = 0;
@@ -256,24 +259,24 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
         if (lq >= tasks) return;
         if (ls == 0) {
             const int item = blockIdx.x + li * gridDim.x, at = item / units, e = at < n_active ? picks.active[at] : p.E + at - n_active;
-            block = (item - at * units) * 2;
+            block = (item - at * units) * NB;
             lw[0] = uniform(matrix[0][e]);
             lw[1] = uniform(matrix[1][e]);
             if (FP4)
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) sc_next[m][c] = load_word(lw[m] + p.up_scales_at + ((size_t)(block + c) * groups + lg) * 256 + lane_s);
+                    for (int c = 0; c < NB; ++c) sc_next[m][c] = load_word(lw[m] + p.up_scales_at + ((size_t)(block + c) * groups + lg) * 256 + lane_s);
         }
         const int t = lg * TASK + ls;
         if (t < KT) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) a[slot][m][c] = load_piece<NT>(lw[m] + ((size_t)(block + c) * KT + t) * 1024 + lane_w);
+                for (int c = 0; c < NB; ++c) a[slot][m][c] = load_piece<NT>(lw[m] + ((size_t)(block + c) * KT + t) * 1024 + lane_w);
             if (!XLDS)
 #pragma unroll
-                for (int f = 0; f < PARTS; ++f) x[slot % (XLDS ? 1 : TASK)][f] = load_piece(p.x_copy + (size_t)(t * PARTS + f) * p.T * 64 + lane_x);
+                for (int f = 0; f < PARTS; ++f) x[XLDS ? 0 : slot][f] = load_piece(p.x_copy + (size_t)(t * PARTS + f) * p.T * 64 + lane_x);
         }
         if (++ls == TASK) {
             ls = 0;
@@ -282,11 +285,12 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
         }
     };
 #pragma unroll
-    for (int u = 0; u < TASK; ++u) load(u);
-    float gate = 0.f, up = 0.f;   // of token tid / 32, column tid % 32 of the item that is being added up
+    for (int u = 0; u < DEPTH; ++u) load(u);
+    // of token tid / 32, columns tid % 32 (and 32 further) of the item that is being added up
+    float gate[NB / 2] = {}, up[NB / 2] = {};
     int item = 0, group = 0, my_group = wave % G;
     for (int q0 = 0; q0 < tasks; q0 += WAVES) {
-        f32x4 acc[2][2] = {};
+        f32x4 acc[2][NB] = {};
         if (q0 + wave < tasks) {
 #pragma unroll
             for (int u = 0; u < TASK; ++u) {
@@ -294,7 +298,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
 #pragma unroll
                     for (int m = 0; m < 2; ++m)
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) sc[m][c] = sc_next[m][c];
+                        for (int c = 0; c < NB; ++c) sc[m][c] = sc_next[m][c];
                 const int t = my_group * TASK + u;
                 if (t < KT) {
                     if (XLDS)
@@ -303,34 +307,38 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
 #pragma unroll
                     for (int f = 0; f < PARTS; ++f) {
                         // past H (a multiple of 64) the weights are zero and x is not there
-                        u32x4 v = x[XLDS ? 0 : u][f];
+                        u32x4 v = x[XLDS ? 0 : u % DEPTH][f];
                         if (FP4 && t * 128 + g * 32 >= p.H) v = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
                         for (int m = 0; m < 2; ++m)
 #pragma unroll
-                            for (int c = 0; c < 2; ++c)
-                                acc[m][c] = mfma(weight_part<FP4>(a[u][m][c], FP4 ? scale_of(sc[m][c], u) : 0.f, f), __builtin_bit_cast(bf16x8, v), acc[m][c]);
+                            for (int c = 0; c < NB; ++c)
+                                acc[m][c] = mfma(weight_part<FP4>(a[u % DEPTH][m][c], FP4 ? scale_of(sc[m][c], u) : 0.f, f), __builtin_bit_cast(bf16x8, v), acc[m][c]);
                     }
                 }
-                load(u);
+                load(u % DEPTH);
             }
             for (my_group += WAVES; my_group >= G;) my_group -= G;
         }
         // lane (rl, g) has columns 4 g + r of 16 of token rl
-        float(*const sums)[2][2][256] = room[q0 / WAVES & 1];
+        float(*const sums)[2][NB][256] = room[q0 / WAVES % PLACES];
+        if (PLACES == 1 && q0 > 0) __syncthreads();
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) *reinterpret_cast<f32x4*>(&sums[wave][m][c][rl * 16 + 4 * g]) = acc[m][c];
+            for (int c = 0; c < NB; ++c) *reinterpret_cast<f32x4*>(&sums[wave][m][c][rl * 16 + 4 * g]) = acc[m][c];
         __syncthreads();
         const int t = tid >> 5, c = tid >> 4 & 1, n = tid & 15;
 #pragma unroll
         for (int q = 0; q < WAVES; ++q) {
             if (q0 + q >= tasks) break;
-            gate += sums[q][0][c][t * 16 + n];
-            up += sums[q][1][c][t * 16 + n];
+#pragma unroll
+            for (int j = 0; j < NB / 2; ++j) {
+                gate[j] += sums[q][0][j * 2 + c][t * 16 + n];
+                up[j] += sums[q][1][j * 2 + c][t * 16 + n];
+            }
             if (++group < G) continue;
-            const int it = blockIdx.x + item * gridDim.x, at = it / units, f = (it - at * units) * 32 + c * 16 + n;
+            const int it = blockIdx.x + item * gridDim.x, at = it / units, f0 = (it - at * units) * NB * 16 + c * 16 + n;
             int row = -1;
             float weight = 1.f;
             if (t < p.T) {
@@ -340,14 +348,17 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
                     weight = w[row];
                 }
             }
-            if (row >= 0) {
-                const float v = weight * (gate / (1.0f + __expf(-gate)) * up);
-                const __bf16 hi = (__bf16)v;
-                char* const to = p.h + (size_t)row * p.h_row + h_place<FP4>(f);
-                *reinterpret_cast<__bf16*>(to) = hi;
-                *reinterpret_cast<__bf16*>(to + 64) = __builtin_isfinite((float)hi) ? (__bf16)(v - (float)hi) : (__bf16)0.0f;
+#pragma unroll
+            for (int j = 0; j < NB / 2; ++j) {
+                if (row >= 0) {
+                    const float v = weight * (gate[j] / (1.0f + __expf(-gate[j])) * up[j]);
+                    const __bf16 hi = (__bf16)v;
+                    char* const to = p.h + (size_t)row * p.h_row + h_place<FP4>(f0 + j * 32);
+                    *reinterpret_cast<__bf16*>(to) = hi;
+                    *reinterpret_cast<__bf16*>(to + 64) = __builtin_isfinite((float)hi) ? (__bf16)(v - (float)hi) : (__bf16)0.0f;
+                }
+                gate[j] = up[j] = 0.f;
             }
-            gate = up = 0.f;
             group = 0;
             ++item;
         }
@@ -448,8 +459,8 @@ __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
 #pragma unroll
     for (int c = 0; c < NB; ++c) *reinterpret_cast<f32x4*>(&sums[wave][c][rl * 16 + 4 * g]) = sum[c];
     __syncthreads();
-    // thread: columns n, n + 32 of a token (NB = 4), or one of 16 columns (NB = 1)
-    constexpr int WIDE = NB == 4 ? 32 : 16, EACH = NB == 4 ? 2 : 1, COLUMNS = NB * 16;
+    // thread: columns n, n + 32, .. of a token, or one of 16 columns (NB = 1)
+    constexpr int WIDE = NB > 1 ? 32 : 16, EACH = NB > 1 ? NB / 2 : 1, COLUMNS = NB * 16;
     const int t = tid / WIDE, n = tid % WIDE;
     float v[EACH];
 #pragma unroll
@@ -513,7 +524,7 @@ size_t few_partial_bytes(const moe_shape& s) { return (size_t)s.H * FEW_SHARES *
 bool few_x_in_lds(const moe_shape& s) { return few_x_bytes(s) <= FEW_X_LDS; }
 bool few_routes_inside(const moe_shape& s) { return few_x_in_lds(s) && (int64_t)((s.E + 15) / 16) * s.H * 32 <= 128 << 10; }
 
-int few_down_columns(const moe_shape& s, bool fp4) { return down_tasks(s, fp4) <= 32 ? 16 : 64; }
+int few_down_columns(const moe_shape& s, bool fp4) { return down_tasks(s, fp4) <= 32 ? 16 : (s.H % 128 == 0 && down_tasks(s, fp4) * (s.H / 128) >= 4096 ? 128 : 64); }
 int few_shares(const moe_shape& s, bool fp4) {
     const int columns = s.H / few_down_columns(s, fp4);
     return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 256 / columns, (down_tasks(s, fp4) + WAVES - 1) / WAVES}));
@@ -537,13 +548,14 @@ hipError_t launch(const FewArgs& a, hipStream_t st) {
         hipLaunchKernelGGL(few_logits_kernel<FP4>, dim3((unsigned)(blocks + copies)), block, 0, st, a);
         if (const hipError_t e = hipGetLastError()) return e;
     }
-    const int64_t active = std::min<int64_t>(a.E, (int64_t)a.T * a.k) + a.Ns, items = active * (a.F / 32);
-    const dim3 up((unsigned)std::min<int64_t>(256, items)), down((unsigned)(a.H / a.down_columns * a.shares));
+    const int64_t active = std::min<int64_t>(a.E, (int64_t)a.T * a.k) + a.Ns, items = active * (a.F / (a.x_in_lds ? 32 : 64));
+    const dim3 up((unsigned)(items <= 512 ? items : 256)), down((unsigned)(a.H / a.down_columns * a.shares));
     if (a.x_in_lds) hipLaunchKernelGGL((few_up_kernel<FP4, NT, true>), up, block, (unsigned)a.x_bytes, st, a);
     else hipLaunchKernelGGL((few_up_kernel<FP4, NT, false>), up, block, 0, st, a);
     if (const hipError_t e = hipGetLastError()) return e;
     if (a.down_columns == 16) hipLaunchKernelGGL((few_down_kernel<FP4, NT, 1>), down, block, 0, st, a);
-    else hipLaunchKernelGGL((few_down_kernel<FP4, NT, 4>), down, block, 0, st, a);
+    else if (a.down_columns == 64) hipLaunchKernelGGL((few_down_kernel<FP4, NT, 4>), down, block, 0, st, a);
+    else hipLaunchKernelGGL((few_down_kernel<FP4, NT, 8>), down, block, 0, st, a);
     return hipGetLastError();
 }
 
