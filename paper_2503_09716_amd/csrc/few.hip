@@ -228,7 +228,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
     }
     const float* const l = p.logits ? p.logits : logits;
     const int stride = p.logits ? p.ep : LOGIT_STRIDE;
-    if (wave < 4) {
+    if (wave * 4 < p.T) {
         if (p.E <= 16) select<1>(p, l, stride, idx, w);
         else if (p.E <= 64) select<4>(p, l, stride, idx, w);
         else if (p.E <= 160) select<10>(p, l, stride, idx, w);
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
     __shared__ const char* matrix[256];   // of every expert
     __shared__ int last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rl = lane & 15, g = lane >> 4;
-    const int experts = p.E + p.Ns;
+    const int experts = p.E + p.Ns, x_row = min(rl, p.T - 1);
     if (tid < 256) matrix[tid] = (const char*)p.weights[2 * experts + min(tid, experts - 1)];
     const u32x4* const from_up = reinterpret_cast<const u32x4*>(p.picks);
     for (int i = tid; i < (int)sizeof(Picks) / 16; i += WAVES * 64) reinterpret_cast<u32x4*>(&picks)[i] = from_up[i];
@@ -390,18 +390,16 @@ __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
     u32x4 a[DEPTH][NB], hi[DEPTH][PARTS], lo[DEPTH][PARTS];
     uint32_t sc[NB], sc_next[NB];
     // asked for next: step `ls` of group lg of the le-th expert
-    int lq = from + wave, le = lq / G, lg = lq - le * G, ls = 0, row = -1;
-    const char* w2 = nullptr;
+    int lq = from + wave, le = lq / G, lg = lq - le * G, ls = 0;
+    const char *w2 = nullptr, *h_at = nullptr;
     auto load = [&](const int slot) __attribute__((always_inline)) {
         if (lq >= to) return;
         if (ls == 0) {
             const int e = __builtin_amdgcn_readfirstlane(le < n_active ? picks.active[le] : p.E + le - n_active);
             w2 = uniform(matrix[e]);
-            row = -1;
-            if (rl < p.T) {
-                if (le >= n_active) row = p.T * (p.k + le - n_active) + rl;
-                else if (const int j = picks.pick[e][rl]; j >= 0) row = rl * p.k + j;
-            }
+            // a token that did not pick the expert multiplies another row: its column of the product is not used
+            const int j = picks.pick[min(e, p.E - 1)][x_row], row = le >= n_active ? p.T * (p.k + le - n_active) + x_row : (j >= 0 ? x_row * p.k + j : 0);
+            h_at = p.h + (size_t)row * p.h_row + g * 16;
             if (FP4)
 #pragma unroll
                 for (int c = 0; c < NB; ++c) sc_next[c] = load_word(w2 + p.down_scales_at + ((size_t)(columns * NB + c) * groups + lg) * 256 + lane_s);
@@ -410,12 +408,11 @@ __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
         if (t < KT) {
 #pragma unroll
             for (int c = 0; c < NB; ++c) a[slot][c] = load_piece<NT>(w2 + ((size_t)(columns * NB + c) * KT + t) * 1024 + lane_w);
-            const bool in = row >= 0 && (!FP4 || t * 128 + g * 32 < p.F);
-            const char* const from_h = p.h + (size_t)max(row, 0) * p.h_row + (size_t)t * HSTEP + g * 16;
+            const char* const from_h = h_at + (uint32_t)(t * HSTEP);
 #pragma unroll
             for (int f = 0; f < PARTS; ++f) {
-                hi[slot][f] = in ? load_piece(from_h + f * 128) : u32x4{0u, 0u, 0u, 0u};
-                lo[slot][f] = in ? load_piece(from_h + f * 128 + 64) : u32x4{0u, 0u, 0u, 0u};
+                hi[slot][f] = load_piece(from_h + f * 128);
+                lo[slot][f] = load_piece(from_h + f * 128 + 64);
             }
         }
         if (++ls == TASK) {
@@ -435,7 +432,13 @@ __global__ __launch_bounds__(WAVES * 64) void few_down_kernel(const FewArgs p) {
             if (u == 0)
 #pragma unroll
                 for (int c = 0; c < NB; ++c) sc[c] = sc_next[c];
-            if (group * TASK + u < KT) {
+            const int t = group * TASK + u;
+            if (t < KT) {
+                if (FP4 && t * 128 + 128 > p.F) {   // past F (a multiple of 64) the weights are zero and nothing was written
+#pragma unroll
+                    for (int f = 0; f < PARTS; ++f)
+                        if (t * 128 + g * 32 >= p.F) hi[u % DEPTH][f] = lo[u % DEPTH][f] = u32x4{0u, 0u, 0u, 0u};
+                }
 #pragma unroll
                 for (int c = 0; c < NB; ++c) {
                     const float scale = FP4 ? scale_of(sc[c], u) : 0.f;
