@@ -238,6 +238,7 @@ class Moe:
             raise MoeError(st, "moe_create failed on device %d" % device)
         self.h = h
         self.y_dtype, self.out_dtype = torch.float32, torch.bfloat16   # as options "y_fp32" and "out_fp32" have them
+        self.gate_packed = False
 
     def close(self):
         if getattr(self, "h", None):
@@ -260,6 +261,8 @@ class Moe:
             self.y_dtype = torch.float32 if value else torch.bfloat16
         elif key == "out_fp32":
             self.out_dtype = torch.float32 if value else torch.bfloat16
+        elif key == "gate_packed":
+            self.gate_packed = bool(value)
 
     def new_workspace(self, shape: MoeShape) -> torch.Tensor:
         n = workspace_bytes(shape)
@@ -409,10 +412,11 @@ class Moe:
     def weight_list(self, *weights: Sequence[torch.Tensor]) -> WeightList:
         """One to three matrices of each expert (first all experts' first, ...), packed by mx_pack_weight (uint8) or pack_weight (bf16)."""
         weights = [list(ws) for ws in weights]
+        assert weights and weights[0], "matrices required"
         kind = weights[0][0].dtype
         assert kind in (torch.uint8, torch.bfloat16)
         for ws in weights:
-            assert len(ws) == len(weights[0]) and all(w.dtype is kind and w.numel() == ws[0].numel() and w.get_device() == self.device for w in ws)
+            assert len(ws) == len(weights[0]) and all(w.dtype is kind and w.numel() == ws[0].numel() and w.get_device() == self.device and w.is_contiguous() for w in ws)
         experts, matrices = len(weights[0]), len(weights)
         buffer = torch.empty(int(self.lib.moe_weight_list_bytes(experts, matrices)), dtype=torch.uint8, device="cuda:%d" % self.device)
         struct = WeightListStruct()
@@ -448,10 +452,11 @@ class Moe:
         """The whole layer for up to 16 tokens; weights: weight_list of the gate, up and down matrices, bf16 or MXFP4."""
         T, H, F, E, d = shape.T, shape.H, shape.F, shape.E, self.device
         fp4 = weights.struct.fp4
+        gate = (int(self.lib.moe_gate_packed_bytes(C.byref(shape))) // 2,) if self.gate_packed else (H, E)
         want = [int(self.lib.moe_mx_weight_bytes(*s)) if fp4 else 2 * H * F for s in ((H, F), (H, F), (F, H))]
         assert weights.bytes == want, "three matrices of %d x %d, %d x %d and %d x %d required" % (H, F, H, F, F, H)
-        self._check(self.lib.moe_layer_few(self.h, C.byref(shape), _typed(x, torch.bfloat16, (T, H), d), _ptr(wg), _typed(bias, torch.float32, (E,), d),
-                                           C.byref(weights.struct), _typed(out, self.out_dtype, (T, H), d), _ptr(workspace), workspace.numel(),
+        self._check(self.lib.moe_layer_few(self.h, C.byref(shape), _typed(x, torch.bfloat16, (T, H), d), _typed(wg, torch.bfloat16, gate, d),
+                                           _typed(bias, torch.float32, (E,), d), C.byref(weights.struct), _typed(out, self.out_dtype, (T, H), d), _ptr(workspace), workspace.numel(),
                                            _raw_stream(d)))
 
     # ---- fused call --------------------------------------------------------------------

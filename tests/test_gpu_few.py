@@ -246,7 +246,7 @@ def test_no_tokens_and_refusals(moe):
     def refused(status, a, x=None, list_=None, ws=None, shape=None):
         with pytest.raises(MoeError) as e:
             s = shape or a.shape
-            moe.layer_few(s, a.x if x is None else x, a.wg, None, list_ or a.list, torch.empty((s.T, s.H), dtype=torch.bfloat16, device=DEV),
+            moe.layer_few(s, a.x if x is None else x, a.wg[:, :s.E].contiguous(), None, list_ or a.list, torch.empty((s.T, s.H), dtype=torch.bfloat16, device=DEV),
                           a.workspace if ws is None else ws)
         assert e.value.status == status, e.value
     a = Layer(moe, 4, 128, 64, 6, 2)

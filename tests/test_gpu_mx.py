@@ -365,3 +365,77 @@ def test_refusals(moe):
     moe.mx_quantize(x[:0], empty)
     moe.mx_dequantize(empty, x[:0])
     moe.mx_grouped_product(empty, None, offsets, lst, out[:0], moe.new_mx_workspace(0, 2))
+
+
+# ---- the operators together --------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T,k,shared", [(700, 4, 2), (33, 1, 0), (1, 3, 1)])
+def test_a_layer_stage_by_stage(moe, T, k, shared):
+    """route, permute, quantise, gate and up, quantise, down, combine against 64 bits.  Each stage is held to its own inputs as the stage before left
+    them (h is quantised again: where a value sits at a border, one step of h is no error of a product)."""
+    H, F, E = 320, 192, 12
+    gen = torch.Generator().manual_seed(T)
+    x = torch.randn((T, H), generator=gen).bfloat16().to(DEV)
+    wg = (torch.randn((H, E), generator=gen) * 0.1).bfloat16().to(DEV)
+    w = [[(torch.randn(s, generator=gen) * 0.06).bfloat16().to(DEV) for _ in range(E)] for s in ((H, F), (H, F), (F, H))]
+    ws_shared = [(torch.randn(s, generator=gen) * 0.06).bfloat16().to(DEV) for s in ((H, F * shared), (H, F * shared), (F * shared, H))] if shared else None
+    from paper_2503_09716_amd import make_shape
+    s = make_shape(T, H, F, E, k, 0)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    idx, weight = torch.empty((T, k), **i32), torch.empty((T, k), device=DEV)
+    offsets, perm, inv_perm, row_token = (torch.empty(n, **i32) for n in (E + 1, T * k, T * k, T * k))
+    ws = moe.new_workspace(s)
+    moe.route(s, x, wg, None, idx, weight, None, ws)
+    moe.permute(s, x, idx, None, offsets, perm, inv_perm, row_token, ws)
+    q = moe.new_mx_rows(T, H)
+    moe.mx_quantize(x, q)
+    xv = held(x).to(DEV)
+
+    def ffn(row_index, at, matrices, rows, width):
+        """(y, expected y, bound) of the experts' matrices, [3][experts]."""
+        listed = moe.weight_list(*[[moe.mx_pack_weight(m) for m in ms] for ms in matrices])
+        space = moe.new_mx_workspace(rows, len(matrices[0]))
+        h = torch.empty((rows, width), dtype=torch.bfloat16, device=DEV)
+        moe.mx_grouped_product(q, row_index, at, listed, h, space, gated=True)
+        hq = moe.new_mx_rows(rows, width)
+        moe.mx_quantize(h, hq)
+        y = torch.empty((rows, H), device=DEV)
+        moe.mx_grouped_product(hq, None, at, listed, y, space, first=2)
+        hv, want, bound = held(h).to(DEV), torch.empty((rows, H), dtype=torch.float64, device=DEV), torch.empty((rows, H), dtype=torch.float64, device=DEV)
+        cuts = at.tolist()
+        for e, (m1, m3, m2) in enumerate(zip(*matrices)):
+            lo, hi = cuts[e], cuts[e + 1]
+            v1, v3, v2 = (held(m.t()).t().to(DEV) for m in (m1, m3, m2))
+            rows_e = xv[row_index[lo:hi].long()] if row_index is not None else xv[lo:hi]
+            g, u = rows_e @ v1, rows_e @ v3
+            og, ou = (rows_e.abs() @ v1.abs()) * H * 2.0 ** -23, (rows_e.abs() @ v3.abs()) * H * 2.0 ** -23
+            sg = torch.nn.functional.silu(g)
+            off = 1.1 * og * (u.abs() + ou) + sg.abs() * ou + (sg * u).abs() * (2.0 ** -8 + (8 + g.abs()) * 2.0 ** -23)
+            assert ((h[lo:hi].double() - sg * u).abs() <= off * (1 + 2.0 ** -8)).all()
+            want[lo:hi], bound[lo:hi] = hv[lo:hi] @ v2, (hv[lo:hi].abs() @ v2.abs()) * width * 2.0 ** -23
+        assert ((y.double() - want).abs() <= bound).all()
+        return y, want, bound
+
+    y, y_want, y_bound = ffn(row_token, offsets, w, T * k, F)
+    y_shared, want, bound = None, 0.0, 0.0
+    if shared:
+        y_shared, want, bound = ffn(None, torch.tensor([0, T], **i32), [[m] for m in ws_shared], T, F * shared)
+    moe.set_option("out_fp32", 1)
+    out = torch.empty((T, H), device=DEV)
+    moe.combine(s, y, inv_perm, weight, y_shared, out)
+    moe.set_option("out_fp32", 0)
+    terms = weight.double()[:, :, None] * y_want[inv_perm.long()].view(T, k, H)
+    want = want + terms.sum(dim=1)
+    bound = bound + (weight.double()[:, :, None] * y_bound[inv_perm.long()].view(T, k, H)).sum(dim=1) + (terms.abs().sum(dim=1) + want.abs()) * (k + 2) * 2.0 ** -23
+    assert ((out.double() - want).abs() <= bound).all()
+
+
+def test_the_example_runs():
+    """examples/quantized_experts.py.  Its layer for few tokens rounds nothing that the layer on the values does not round, and a bf16 output by 2^-8 at
+    most on either side; h is rounded there to 2^-8 of each term."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import quantized_experts
+    result = quantized_experts.main(["--tokens", "300", "--steps", "2"])
+    assert 0.0 <= result["few"] < 3 * 2.0 ** -8 and result["long"] == result["long"] and result["long_us"] > 0
