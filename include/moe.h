@@ -416,7 +416,9 @@ moe_status moe_clip_gradients(moe_ctx* ctx, const moe_gradient_list* list, doubl
  *  - Packed weights (moe_mx_weight_bytes bytes), from the transposed matrix W[n][k]: codes in blocks of 16 rows x 128 k = 1 KiB, ordered
  *    [cols/16][ceil(rows/128)], inside a block as in moe_pack_weight's (row r at bytes 64r, its 16-byte piece c, k = 32c .. 32c+31, at slot
  *    c ^ ((4 - r/4) & 3)); then from the next multiple of 256 bytes scales [cols/16][ceil(rows/512)][16 rows][16], in a row as above.
- *  - Limits: rows of x of any number, contraction and output dimensions multiples of 32, every buffer below 4 GiB but the output of a product. */
+ *  - Limits: rows of x of any number, contraction and output dimensions multiples of 32, quantised rows and a matrix in bf16 below 4 GiB, a
+ *    matrix below 2^21 columns.  The output of a product may be larger than 4 GiB.
+ *  - Calls that may run at the same time need workspaces of their own; weights, lists and quantised rows can be shared. */
 
 /* Bytes of `rows` quantised rows of `cols` columns, and of a packed weight matrix [rows = contraction, cols]; 0 for invalid sizes. */
 size_t moe_mx_rows_bytes(int32_t rows, int32_t cols);
@@ -461,7 +463,7 @@ size_t moe_mx_workspace_bytes(int32_t rows, int32_t experts);
  * where x_r is row r of xq, or row row_index[r] of xq (moe_permute's row_token: xq are then the tokens' rows).
  *   xq: moe_mx_quantize of x_rows rows of K columns; row_index_or_null [rows] int32, expert_offsets [E+1] int32: device in, not validated
  *   list: MXFP4 matrices of K rows and N columns
- *   out [rows, N] bf16, or fp32 with out_fp32 = 1: device out, 16-byte aligned.  Rows from expert_offsets[E] on are left as they were.
+ *   out [rows, N] bf16, or fp32 with out_fp32 = 1: device out, 16-byte aligned, not xq.  Rows from expert_offsets[E] on are left as they were.
  *   workspace: device, 256-byte aligned, moe_mx_workspace_bytes(rows, list->experts) bytes
  * rows = 0 is valid and enqueues nothing. */
 moe_status moe_mx_grouped_product(moe_ctx* ctx, int32_t rows, int32_t K, int32_t N, const void* xq, int32_t x_rows,
@@ -469,8 +471,8 @@ moe_status moe_mx_grouped_product(moe_ctx* ctx, int32_t rows, int32_t K, int32_t
                                    int32_t first, int32_t gated, void* out, int32_t out_fp32, void* workspace, size_t workspace_bytes,
                                    void* hip_stream);
 
-/* The whole layer for a few tokens (T <= 16, top_k <= 16), in two launches, or three where the gate matrix is above 256 KiB (one more unless
- * it is packed): moe_layer's formula,
+/* The whole layer for a few tokens (T <= 16, top_k <= 16), in two launches; three where the packed gate matrix is above 128 KiB or the tokens are
+ * above 80 KiB; one more unless the gate matrix is packed.  moe_layer's formula,
  *   out[t] = sum over the picks e of w[t,e] * ( silu(x_t W1_e) * (x_t W3_e) ) W2_e + sum over the shared experts of the same without w,
  * on matrices of moe_pack_weight or in MXFP4.  Nothing is rounded to fewer bits than its input has but out, once: logits, weights and sums are fp32,
  * and h enters the second product with 16 of its bits.  Results differ from moe_layer's in the last bits (it rounds h to bf16); the same

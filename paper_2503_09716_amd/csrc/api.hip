@@ -984,7 +984,7 @@ const char* fp4_size_problem(int64_t rows, int64_t K, bool any_rows) {
 }
 const char* fp4_weight_problem(int64_t K, int64_t N) {
     if (const char* why = fp4_size_problem(N, K, false)) return why;
-    return K * N * 2 >= (int64_t)1 << 32 ? "a matrix reaches 4 GiB" : nullptr;
+    return K * N * 2 >= (int64_t)1 << 32 || N >= 1 << 21 ? "a matrix reaches 4 GiB or 2^21 columns" : nullptr;
 }
 moe_status fp4_status(int64_t K, int64_t N) { return K < 32 || K % 32 || N < 32 || N % 32 ? MOE_E_ARG : MOE_E_UNSUPPORTED; }
 
@@ -1636,10 +1636,10 @@ moe_status moe_mx_grouped_product(moe_ctx* c, int32_t rows, int32_t K, int32_t N
     if (moe_status st = check_list(c, "mx_grouped_product", list)) return st;
     if (!list->fp4) return fail(c, MOE_E_ARG, "mx_grouped_product: the list is not of MXFP4 matrices");
     if (first < 0 || first + gated >= list->matrices) return fail(c, MOE_E_ARG, "mx_grouped_product: the list has no matrix %d", (int)(first + gated));
-    if (fp4_tiles(rows, list->experts, N, gated != 0) > 0x7fffffff || (int64_t)256 * N * 4 >= (int64_t)1 << 31)
-        return fail(c, MOE_E_UNSUPPORTED, "mx_grouped_product: too many rows or columns");
+    if (fp4_tiles(rows, list->experts, N, gated != 0) > 0x7fffffff) return fail(c, MOE_E_UNSUPPORTED, "mx_grouped_product: too many rows and columns");
     if (rows == 0) return MOE_OK;
     if (!xq || !offsets || !out) return fail(c, MOE_E_ARG, "mx_grouped_product: NULL pointer");
+    if (out == xq) return fail(c, MOE_E_ARG, "mx_grouped_product: out must not be xq");
     if (row_index ? x_rows == 0 : x_rows < rows) return fail(c, MOE_E_ARG, "mx_grouped_product: xq has fewer rows than the product");
     if (misaligned({xq}, 256) || misaligned({out}, 16) || misaligned({row_index, offsets}, 4))
         return fail(c, MOE_E_ARG, "mx_grouped_product: misaligned pointer");

@@ -27,7 +27,7 @@ struct FewArgs {
     int32_t* arrived;                    // workgroups that have left theirs; cleared by the launch before
     char* out;
     int32_t shares;                      // workgroups to the same columns
-    int32_t down_columns;                // columns of a workgroup of the down launch: 16 or 64
+    int32_t down_columns;                // columns of a workgroup of the down launch: 16, 64 or 128
     int32_t h_row, x_bytes, x_in_lds;
     int32_t nt;                          // 1: weights past the caches
     int32_t T, H, F, E, k, Ns, ep, renorm, out_fp32;

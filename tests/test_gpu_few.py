@@ -263,3 +263,60 @@ def test_no_tokens_and_refusals(moe):
         refused(1, a, list_=moe.weight_list(a.packed[0], a.packed[1]))
     with pytest.raises(AssertionError):
         refused(1, a, x=a.x[:3])
+
+
+@pytest.mark.parametrize("T,H,F,E,k,shared", [
+    (1, 32768, 64, 3, 2, 0),
+    (16, 32768, 64, 2, 1, 1),
+    (16, 64, 65536, 2, 2, 0),
+    (16, 2560, 192, 16, 3, 1),     # the most x that LDS takes
+    (15, 2752, 192, 16, 3, 1),     # and a little more
+    (1, 4096, 64, 16, 2, 0),       # the largest gate matrix of the gate/up launch
+    (1, 4096, 64, 17, 2, 0),
+])
+@pytest.mark.parametrize("fp4", [True, False])
+def test_largest_sizes_and_both_sides_of_the_rules(moe, T, H, F, E, k, shared, fp4):
+    Layer(moe, T, H, F, E, k, shared, True, fp4, seed=H + F).check()
+
+
+def test_calls_at_the_same_time(moe):
+    """One list on two streams, with workspaces of their own, over and over."""
+    a = Layer(moe, 16, 1024, 704, 16, 4, 1, seed=9)
+    want = a.run(True).clone()
+    flipped = a.x.flip(0).contiguous()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.empty_like(want) for _ in range(8)] for _ in streams]
+    spaces = [moe.new_few_workspace(a.shape) for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for s, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                moe.layer_few(a.shape, flipped if s else a.x, a.wg, None, a.list, outs[s][i], spaces[s])
+    torch.cuda.synchronize()
+    for i in range(8):
+        assert torch.equal(outs[0][i], want)
+        assert torch.equal(outs[1][i], outs[1][0])
+    want64, bound = a.expected()
+    assert ((outs[1][0].flip(0).double() - want64).abs() <= bound).all()
+
+
+def test_two_graphs_share_a_workspace(moe):
+    a, b = Layer(moe, 5, 512, 320, 12, 3, seed=3), Layer(moe, 16, 512, 320, 12, 4, 1, seed=4)
+    want = [a.run(True).clone(), b.run(True).clone()]
+    shared = b.workspace if b.workspace.numel() > a.workspace.numel() else a.workspace
+    outs, graphs = [torch.empty_like(w) for w in want], []
+    for layer, out in zip((a, b), outs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            moe.layer_few(layer.shape, layer.x, layer.wg, None, layer.list, out, shared)
+        graphs.append(graph)
+    for _ in range(3):
+        for out in outs:
+            out.zero_()
+        for graph in graphs:
+            graph.replay()
+        shared.fill_(0xFF)
+        torch.cuda.synchronize()
+        for out, w in zip(outs, want):
+            assert torch.equal(out, w)

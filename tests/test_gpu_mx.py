@@ -296,6 +296,42 @@ def test_rows_behind_the_last_group_stay_as_they_were(moe):
     assert (out == 7.0).all()
 
 
+def test_rows_in_front_of_the_first_group_stay_as_they_were(moe):
+    p = Product(moe, [40, 300], 256, 64, False)
+    whole = p.run(torch.float32).clone()
+    p.offsets = torch.tensor([5, 40, 340], dtype=torch.int32, device=DEV)
+    out = torch.full_like(whole, 7.0)
+    p.run(torch.float32, out)
+    assert torch.equal(out[5:], whole[5:]) and (out[:5] == 7.0).all()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_outputs_above_4_gib(moe, gated):
+    """Tiles behind the 32-bit border are those of the same rows alone."""
+    rows, N = 70016, 32768
+    gen = torch.Generator().manual_seed(1)
+    w = [[moe.mx_pack_weight((torch.randn((32, N), generator=gen) * 0.05).bfloat16().to(DEV))] for _ in range(1 + gated)]
+    x = torch.randn((rows, 32), generator=gen).bfloat16().to(DEV)
+    lst, ws = moe.weight_list(*w), moe.new_mx_workspace(rows, 1)
+    q, out = moe.new_mx_rows(rows, 32), torch.empty((rows, N), dtype=torch.bfloat16, device=DEV)
+    moe.mx_quantize(x, q)
+    moe.mx_grouped_product(q, None, torch.tensor([0, rows], dtype=torch.int32, device=DEV), lst, out, ws, gated=gated)
+    for at in (0, 65500, rows - 100):
+        q2, part = moe.new_mx_rows(100, 32), torch.empty((100, N), dtype=torch.bfloat16, device=DEV)
+        moe.mx_quantize(x[at:at + 100], q2)
+        moe.mx_grouped_product(q2, None, torch.tensor([0, 100], dtype=torch.int32, device=DEV), lst, part, ws, gated=gated)
+        assert torch.equal(part, out[at:at + 100])
+
+
+def test_out_must_not_be_the_quantised_rows(moe):
+    q = moe.new_mx_rows(4, 512)
+    moe.mx_quantize(torch.zeros((4, 512), dtype=torch.bfloat16, device=DEV), q)
+    lst = moe.weight_list([moe.mx_pack_weight(torch.zeros((512, 32), dtype=torch.bfloat16, device=DEV))])
+    with pytest.raises(MoeError) as e:
+        moe.mx_grouped_product(q, None, torch.tensor([0, 4], dtype=torch.int32, device=DEV), lst, q.buffer[:256].view(torch.bfloat16).view(4, 32), moe.new_mx_workspace(4, 1))
+    assert e.value.status == 1
+
+
 def test_one_list_for_a_layer(moe):
     """Gate, up and down matrices in one list: `first` picks."""
     gen = torch.Generator().manual_seed(7)

@@ -39,6 +39,11 @@ def test_sizes_that_are_refused(lib):
         assert lib.moe_weight_list_bytes(experts, matrices) == 0
 
 
+def test_matrices_of_very_many_columns_are_refused(lib):
+    assert lib.moe_mx_weight_bytes(32, (1 << 21) - 32) == packed((1 << 21) - 32, 32)
+    assert lib.moe_mx_weight_bytes(32, 1 << 21) == 0 and lib.moe_mx_weight_bytes(32, 1 << 25) == 0
+
+
 def test_workspace_bytes(lib):
     # a list entry of 16 bytes for 128 rows and for every expert, and the list's header
     for rows, experts in [(0, 1), (1, 1), (100000, 160), (1 << 24, 256)]:
