@@ -39,6 +39,7 @@ struct Fp4Product {
     int32_t out_fp32;
     uint32_t scales_at;           // of a weight matrix: its scales, from its start
     int32_t n_tiles, max_mtiles, group_m;
+    int32_t inside, rounds;       // 1: no list of m-tiles in memory, workgroups find theirs, of which each has at most that many (rounded up)
 };
 struct Fp4Layout {
     size_t plan, descs, total;

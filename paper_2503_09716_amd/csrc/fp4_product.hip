@@ -39,7 +39,10 @@ struct Ring {
     static constexpr int BYTES = C::NS * STAGE + C::SCALES * SCALE_STAGE;
     static constexpr int XL = C::ROWS / 16 / C::NW, WL = WROWS / 16 / C::NW, SL = 8 / C::NW;   // loads of a sub-tile per wavefront, of a tile of full height
 };
-static_assert(Ring<Long>::BYTES <= 160 * 1024 && Ring<Short>::BYTES <= 80 * 1024, "LDS");
+constexpr int ROUNDS = 64;   // tiles of a workgroup that it can list itself
+template <class C>
+constexpr int OWN = C::NEXT ? ROUNDS * 16 : 0;
+static_assert(Ring<Long>::BYTES + OWN<Long> <= 160 * 1024 && Ring<Short>::BYTES <= 80 * 1024, "LDS");
 
 typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
@@ -151,12 +154,9 @@ __device__ __forceinline__ int tile_order(const int wg, const int total) {
     return (wg - r) + (r & 7) * 32 + (r >> 3);
 }
 
-// The tile at place `at` of the launch: its descriptor (nrows = 0: there is none) and columns.
+// m-tile and columns of the tile at place `at` of `count` m-tiles, the first n_run of which are in group order.
 template <bool GATED>
-__device__ __forceinline__ TileDesc tile_at(const Fp4Product& p, const int count, const int n_run, const int at, int& n0) {
-    TileDesc d = {0, 0, 0, 0};
-    n0 = 0;
-    if (at >= count * p.n_tiles) return d;
+__device__ __forceinline__ int place_of(const Fp4Product& p, const int count, const int n_run, const int at, int& n0) {
     const int L = tile_order(at, count * p.n_tiles);
     int mt, n_tile;
     if (L < n_run * p.n_tiles) {   // group_m m-tiles side by side along n: they share panels of W, and those along n panels of x
@@ -169,11 +169,101 @@ __device__ __forceinline__ TileDesc tile_at(const Fp4Product& p, const int count
         mt = n_run + rem / p.n_tiles;
         n_tile = rem - (mt - n_run) * p.n_tiles;
     }
-    const i32x4 v = scalar_load((const i32x4*)p.descs + __builtin_amdgcn_readfirstlane(mt));
-    d = TileDesc{v[0], v[1], v[2], v[3]};
-    d.nrows &= TILE_ROWS_MASK;
     n0 = n_tile * (GATED ? 128 : WROWS);
+    return mt;
+}
+
+// The list of m-tiles that plan_list would leave in memory, by one wavefront in its registers: group 64 q + lane is slot q of a lane.
+constexpr int SLOTS = 4;
+struct WaveList {
+    int row0[SLOTS], rows[SLOTS], h[SLOTS], nfull[SLOTS], first[SLOTS], nrun[SLOTS];   // first: of its tiles in group order
+    int blocks[SLOTS];                                                                // of 32 rows of its moved tail, or 0
+    int n_run, count;
+};
+__device__ __forceinline__ int scan_wave(int v) {   // inclusive prefix sums over the lanes
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // lane 15 of a row to the next one
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // lane 31 to the upper half
+    return v;
+}
+template <int TM>
+__device__ __forceinline__ WaveList wave_list(const Fp4Product& p, const int lane) {
+    WaveList l = {};
+    int at[SLOTS] = {}, end[SLOTS] = {};
+#pragma unroll
+    for (int q = 0; q < SLOTS; ++q)
+        if (q * 64 < p.E) {
+            const int e = min(q * 64 + lane, p.E - 1);
+            at[q] = p.offsets[e];
+            end[q] = p.offsets[e + 1];
+        }
+    int moved = 0;
+#pragma unroll
+    for (int q = 0; q < SLOTS; ++q)
+        if (q * 64 < p.E) {
+            l.row0[q] = at[q];
+            l.rows[q] = q * 64 + lane < p.E ? end[q] - at[q] : 0;
+            const GroupCut cut = cut_group(l.rows[q], TM, false, true);
+            const int blocks = (cut.tail + 31) >> 5;
+            const bool last = blocks > 0 && !cut.even && blocks * 64 <= TM;
+            l.h[q] = cut.h;
+            l.nfull[q] = cut.nfull;
+            l.nrun[q] = cut.nfull + (blocks > 0 && !last);
+            l.blocks[q] = last ? blocks : 0;
+            const int upto = scan_wave(l.nrun[q]);
+            l.first[q] = l.n_run + upto - l.nrun[q];
+            l.n_run += __builtin_amdgcn_readlane(upto, 63);
+            moved += __popcll(__ballot(last));
+        }
+    l.count = l.n_run + moved;
+    return l;
+}
+__device__ __forceinline__ TileDesc m_tile_at(const Fp4Product& p, const WaveList& l, const int mt, const int lane) {
+    TileDesc d = {0, 0, 0, 0};
+    if (mt < l.n_run) {
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q)
+            if (q * 64 < p.E) {
+                const int i = mt - l.first[q];
+                const uint64_t hit = __ballot(i >= 0 && i < l.nrun[q]);
+                if (hit == 0) continue;
+                const int from = __ffsll((unsigned long long)hit) - 1, at = min(i, l.nfull[q]) * l.h[q];
+                d = TileDesc{q * 64 + from, __builtin_amdgcn_readlane(l.row0[q] + at, from), __builtin_amdgcn_readlane(min(l.h[q], l.rows[q] - at), from), 0};
+            }
+        return d;
+    }
+    int rank = mt - l.n_run;   // of the tails: higher ones first, then in group order
+    for (int b = 4; b > 0; --b)
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q)
+            if (q * 64 < p.E) {
+                const uint64_t tails = __ballot(l.blocks[q] == b);
+                const int n = __popcll(tails);
+                if (rank >= 0 && rank < n) {
+                    const int from = __ffsll((unsigned long long)__ballot((tails >> lane & 1) && __popcll(tails & ((1ull << lane) - 1)) == rank)) - 1, at = l.nfull[q] * l.h[q];
+                    d = TileDesc{q * 64 + from, __builtin_amdgcn_readlane(l.row0[q] + at, from), __builtin_amdgcn_readlane(l.rows[q] - at, from), 0};
+                }
+                rank -= n;
+            }
     return d;
+}
+// The tile at place `at` of the launch (nrows = 0: there is none).
+template <bool GATED>
+__device__ __forceinline__ TileDesc tile_at(const Fp4Product& p, const WaveList& l, const int at, const int lane, int& n0) {
+    n0 = 0;
+    if (at >= l.count * p.n_tiles) return TileDesc{0, 0, 0, 0};
+    return m_tile_at(p, l, place_of<GATED>(p, l.count, l.n_run, at, n0), lane);
+}
+// From the list in memory.
+template <bool GATED>
+__device__ __forceinline__ TileDesc tile_at(const Fp4Product& p, const int count, const int n_run, const int at, int& n0) {
+    n0 = 0;
+    if (at >= count * p.n_tiles) return TileDesc{0, 0, 0, 0};
+    const i32x4 v = scalar_load((const i32x4*)p.descs + __builtin_amdgcn_readfirstlane(place_of<GATED>(p, count, n_run, at, n0)));
+    return TileDesc{v[0], v[1], v[2] & TILE_ROWS_MASK, v[3]};
 }
 
 // Rows of x for the four pieces that this lane loads of a sub-tile, and for its scales; rows past the end are the last one again.
@@ -484,11 +574,38 @@ template <class C, bool GATED, bool NT>
 __global__ __launch_bounds__(C::NW * 64, 2) void fp4_tile_kernel(const Fp4Product p) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int count = scalar_load(&p.plan->n_gate_up), n_run = scalar_load(&p.plan->n_run_up), KT = p.sub_tiles;
+    const int KT = p.sub_tiles;
     lds_t const ring = (lds_t)lds, scale_ring = ring + C::NS * Ring<C>::STAGE;
     const __amdgpu_buffer_rsrc_t rs_x = rsrc_of(p.codes), rs_xs = rsrc_of(p.scales);
-    int at = blockIdx.x, n0, n0_next = 0, n0_after = 0, n0_last = 0, base = 0, sbase = 0;
-    const TileDesc d = tile_at<GATED>(p, count, n_run, at, n0);
+    typedef __attribute__((address_space(3))) i32x4* lentry_t;
+    lentry_t const own = (lentry_t)(ring + Ring<C>::BYTES);   // this workgroup's tiles
+    int count = 0, n_run = 0, round = 0;
+    TileDesc d = {0, 0, 0, 0};
+    int n0 = 0, n0_next = 0, n0_after = 0, n0_last = 0, base = 0, sbase = 0;
+    if (p.inside) {
+        const WaveList l = wave_list<C::ROWS>(p, lane);
+        if (C::NEXT) {
+            for (int i = wave; i < p.rounds; i += C::NW) {
+                const TileDesc t = tile_at<GATED>(p, l, blockIdx.x + i * gridDim.x, lane, n0);
+                if (lane == 0) own[i] = i32x4{t.group, t.row0, t.nrows, n0};
+            }
+            __syncthreads();
+        } else {
+            d = tile_at<GATED>(p, l, blockIdx.x, lane, n0);
+        }
+    } else {
+        count = scalar_load(&p.plan->n_gate_up);
+        n_run = scalar_load(&p.plan->n_run_up);
+    }
+    auto following = [&](int& n0) __attribute__((always_inline)) {
+        if (C::NEXT && p.inside) {
+            const i32x4 v = own[round++];
+            n0 = __builtin_amdgcn_readfirstlane(v[3]);
+            return TileDesc{__builtin_amdgcn_readfirstlane(v[0]), __builtin_amdgcn_readfirstlane(v[1]), __builtin_amdgcn_readfirstlane(v[2]), 0};
+        }
+        return tile_at<GATED>(p, count, n_run, blockIdx.x + round++ * gridDim.x, n0);
+    };
+    if (C::NEXT || !p.inside) d = following(n0);
     if (d.nrows == 0) return;
     const char *w_at, *u_at;
     tile_weights<GATED>(p, d, w_at, u_at);
@@ -498,23 +615,22 @@ __global__ __launch_bounds__(C::NW * 64, 2) void fp4_tile_kernel(const Fp4Produc
     next.any = false;
     TileDesc after = {0, 0, 0, 0};   // two tiles on
     if (C::NEXT) {
-        const TileDesc d_next = tile_at<GATED>(p, count, n_run, at += gridDim.x, n0_next);
+        const TileDesc d_next = following(n0_next);
         tile_weights<GATED>(p, d_next, w_at, u_at);
         next = tile_loads<C, GATED>(p, d_next, n0_next, tile_rows<C>(p, d_next, lane, wave), w_at, u_at, lane, wave);
-        after = tile_at<GATED>(p, count, n_run, at += gridDim.x, n0_after);
+        after = following(n0_after);
     }
     ring_sync<0>();
     for (;;) {
         TileRows<C> rows;
         TileDesc last;
-        at += gridDim.x;
         auto run = [&](auto ti_tag) __attribute__((always_inline)) {
             constexpr int TI = decltype(ti_tag)::value;
             f32x4 acc[WB][Grid<C, TI>::XB];
             multiply<C, TI, GATED>(p, t, next, rs_x, rs_xs, ring, base, sbase, acc);
             if (C::NEXT) {   // on their way while this tile is stored
                 tile_weights<GATED>(p, after, w_at, u_at);
-                last = tile_at<GATED>(p, count, n_run, at, n0_last);
+                last = following(n0_last);
                 rows = tile_rows<C>(p, after, fresh_lane(), wave);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -546,15 +662,15 @@ __global__ __launch_bounds__(C::NW * 64, 2) void fp4_tile_kernel(const Fp4Produc
 
 template <class C, bool NT>
 void launch_tiles(const Fp4Product& p, const bool gated, const dim3 grid, hipStream_t st) {
-    if (gated) hipLaunchKernelGGL((fp4_tile_kernel<C, true, NT>), grid, dim3(C::NW * 64), Ring<C>::BYTES, st, p);
-    else hipLaunchKernelGGL((fp4_tile_kernel<C, false, NT>), grid, dim3(C::NW * 64), Ring<C>::BYTES, st, p);
+    if (gated) hipLaunchKernelGGL((fp4_tile_kernel<C, true, NT>), grid, dim3(C::NW * 64), Ring<C>::BYTES + OWN<C>, st, p);
+    else hipLaunchKernelGGL((fp4_tile_kernel<C, false, NT>), grid, dim3(C::NW * 64), Ring<C>::BYTES + OWN<C>, st, p);
 }
 
 template <class C, bool NT>
 hipError_t set_lds() {
     const auto to = hipFuncAttributeMaxDynamicSharedMemorySize;
-    if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&fp4_tile_kernel<C, true, NT>), to, Ring<C>::BYTES)) return e;
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&fp4_tile_kernel<C, false, NT>), to, Ring<C>::BYTES);
+    if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&fp4_tile_kernel<C, true, NT>), to, Ring<C>::BYTES + OWN<C>)) return e;
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&fp4_tile_kernel<C, false, NT>), to, Ring<C>::BYTES + OWN<C>);
 }
 
 }  // namespace
@@ -590,21 +706,28 @@ hipError_t launch_fp4_product(const Fp4Product& args, bool gated, hipStream_t st
     // 287, 249; K = 1536, 160 experts, 16000 593, 538; gate/up of K = 2048 339, 326, of K = 5120, 160 experts, 3000 tokens 306, 288), but for gated ones of a
     // long contraction and tall groups, which are few bytes for their time, in half lines (K = 4096, 8 experts, 16000 tokens 1828, 1852).
     const bool nt = !gated || p.sub_tiles <= 16 || per <= 128;
-    PlanArgs a = {};
-    a.offsets = p.offsets;
-    a.E = p.E;
-    a.tm_up = is_long ? Long::ROWS : Short::ROWS;
-    a.nt_up = p.n_tiles;
-    a.tails_last_up = 1;
-    a.small_tiles = 1;
-    a.e_hi = p.E;
-    a.plan = p.plan;
-    a.descs_up = p.descs;
     p.group_m = 8;
-    p.max_mtiles = p.rows / a.tm_up + p.E;
-    hipLaunchKernelGGL(fp4_plan_kernel, dim3(1), dim3(256), 0, st, a);
-    if (const hipError_t e = hipGetLastError()) return e;
+    p.max_mtiles = p.rows / (is_long ? Long::ROWS : Short::ROWS) + p.E;
     const dim3 all((unsigned)(p.max_mtiles * p.n_tiles)), cus(std::min(all.x, 256u));
+    // The list of m-tiles: a launch of its own is 3 to 5 us and a gap, finding tiles costs each workgroup a little under 1 us.  us, with the launch and without:
+    // gate/up 8 experts, K = 512, 64 to 256 rows 10.7, 8.3; 64 experts, K = 2048, 94 rows (1400 workgroups) 56.4, 55.2; down K = 1408, 94 rows (1000) 28.5, 26.2,
+    // 1500 rows (long) 204, 200; but 160 experts, K = 5120, 2 to 75 rows (2000 to 3800) 230, 233; K = 1536 (3300 to 6400) 133, 139.
+    p.rounds = (int32_t)std::min<int64_t>((all.x + cus.x - 1) / cus.x + 3, ROUNDS + 1);
+    p.inside = is_long ? p.rounds <= ROUNDS : all.x <= 3 * 512;
+    if (!p.inside) {
+        PlanArgs a = {};
+        a.offsets = p.offsets;
+        a.E = p.E;
+        a.tm_up = is_long ? Long::ROWS : Short::ROWS;
+        a.nt_up = p.n_tiles;
+        a.tails_last_up = 1;
+        a.small_tiles = 1;
+        a.e_hi = p.E;
+        a.plan = p.plan;
+        a.descs_up = p.descs;
+        hipLaunchKernelGGL(fp4_plan_kernel, dim3(1), dim3(256), 0, st, a);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
     if (is_long && nt) launch_tiles<Long, true>(p, gated, cus, st);
     else if (is_long) launch_tiles<Long, false>(p, gated, cus, st);
     else if (nt) launch_tiles<Short, true>(p, gated, all, st);

@@ -269,6 +269,20 @@ def test_products_of_many_groups_with_few_rows(moe):
     Product(moe, counts, 256, 64, True).check(torch.float32)
 
 
+@pytest.mark.parametrize("E,high,K,N,gated", [
+    (256, 60, 64, 1088, True),     # short tiles, too many for workgroups to find theirs
+    (200, 300, 96, 544, True),     # long ones that workgroups find, groups in every slot
+    (130, 700, 64, 288, False),
+    (65, 40, 160, 320, False),     # short ones that workgroups find
+])
+def test_products_of_many_groups(moe, E, high, K, N, gated):
+    gen = torch.Generator().manual_seed(E)
+    counts = torch.randint(0, high, (E,), generator=gen)
+    counts[torch.randint(0, E, (E // 5,), generator=gen)] = 0
+    counts[[0, E - 1]] = torch.tensor([0, high])
+    Product(moe, counts.tolist(), K, N, gated, tokens=500 if gated else 0, seed=E).check(torch.float32)
+
+
 @pytest.mark.parametrize("gated", [False, True])
 def test_blocks_that_are_not_a_number_spoil_their_rows_and_columns_alone(moe, gated):
     def spoil(x, w):
