@@ -63,14 +63,14 @@ __device__ __forceinline__ u32x4 values_of(const uint32_t c, const uint32_t byte
 constexpr int QUANTIZE_WAVES = 4;
 
 template <bool FP32>
-__global__ __launch_bounds__(QUANTIZE_WAVES * 64) void fp4_quantize_kernel(const char* __restrict__ x, const int64_t units, const int groups,
+__global__ __launch_bounds__(QUANTIZE_WAVES * 64) void fp4_quantize_kernel(const char* __restrict__ x, const uint32_t units, const int groups,
                                                                           const int K, const int sub_tiles, char* __restrict__ codes,
                                                                           char* __restrict__ scales) {
     const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * QUANTIZE_WAVES + (threadIdx.x >> 6);
+    const uint32_t unit = blockIdx.x * QUANTIZE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= units) return;
-    const int64_t row = unit / groups;
-    const int q = (int)(unit - row * groups), k = q * FP4_GROUP + lane * 8;
+    const size_t row = unit / (uint32_t)groups;   // below 2^26 units: each takes 80 bytes of 4 GiB or more
+    const int q = (int)(unit - (uint32_t)row * (uint32_t)groups), k = q * FP4_GROUP + lane * 8;
     uint32_t code = 0, byte = 127;
     if (k < K) {   // K is a multiple of 32: the four lanes of a block agree
         if (FP32) {
@@ -98,13 +98,13 @@ __global__ __launch_bounds__(QUANTIZE_WAVES * 64) void fp4_quantize_kernel(const
 
 template <bool FP32>
 __global__ __launch_bounds__(QUANTIZE_WAVES * 64) void fp4_dequantize_kernel(const char* __restrict__ codes, const char* __restrict__ scales,
-                                                                            const int64_t units, const int groups, const int K,
+                                                                            const uint32_t units, const int groups, const int K,
                                                                             const int sub_tiles, char* __restrict__ out) {
     const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * QUANTIZE_WAVES + (threadIdx.x >> 6);
+    const uint32_t unit = blockIdx.x * QUANTIZE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= units) return;
-    const int64_t row = unit / groups;
-    const int q = (int)(unit - row * groups), k = q * FP4_GROUP + lane * 8;
+    const size_t row = unit / (uint32_t)groups;   // below 2^26 units: each takes 80 bytes of 4 GiB or more
+    const int q = (int)(unit - (uint32_t)row * (uint32_t)groups), k = q * FP4_GROUP + lane * 8;
     if (k >= K) return;
     const int b = lane >> 2;
     const uint32_t code = *reinterpret_cast<const uint32_t*>(codes + row * sub_tiles * 64 + (k >> 1));
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(PACK_WAVES * 64) void fp4_unpack_kernel(const char*
 
 hipError_t launch_fp4_quantize(const void* x, bool fp32, int64_t rows, int K, void* q, hipStream_t st) {
     const int sub_tiles = (int)fp4_sub_tiles(K), groups = (int)fp4_groups(K);
-    const int64_t units = rows * groups;
+    const uint32_t units = (uint32_t)(rows * groups);
     const dim3 grid((unsigned)((units + QUANTIZE_WAVES - 1) / QUANTIZE_WAVES)), block(QUANTIZE_WAVES * 64);
     char* const codes = (char*)q;
     char* const scales = codes + fp4_scales_at(rows, K);
@@ -206,7 +206,7 @@ hipError_t launch_fp4_quantize(const void* x, bool fp32, int64_t rows, int K, vo
 
 hipError_t launch_fp4_dequantize(const void* q, int64_t rows, int K, void* out, bool fp32, hipStream_t st) {
     const int sub_tiles = (int)fp4_sub_tiles(K), groups = (int)fp4_groups(K);
-    const int64_t units = rows * groups;
+    const uint32_t units = (uint32_t)(rows * groups);
     const dim3 grid((unsigned)((units + QUANTIZE_WAVES - 1) / QUANTIZE_WAVES)), block(QUANTIZE_WAVES * 64);
     const char* const codes = (const char*)q;
     const char* const scales = codes + fp4_scales_at(rows, K);
