@@ -527,7 +527,14 @@ size_t few_partial_bytes(const moe_shape& s) { return (size_t)s.H * FEW_SHARES *
 bool few_x_in_lds(const moe_shape& s) { return few_x_bytes(s) <= FEW_X_LDS; }
 bool few_routes_inside(const moe_shape& s) { return few_x_in_lds(s) && (int64_t)((s.E + 15) / 16) * s.H * 32 <= 128 << 10; }
 
-int few_down_columns(const moe_shape& s, bool fp4) { return down_tasks(s, fp4) <= 32 ? 16 : (s.H % 128 == 0 && down_tasks(s, fp4) * (s.H / 128) >= 4096 ? 128 : 64); }
+// Columns of a down workgroup.  Few tasks: 16, so that there are workgroups enough and each has little to do one after the other; else 64, where a load of h
+// meets four of weights, and 128 in the longest launches (whole layers, us, 16 and 64 columns; tasks x columns / 64): 8 experts, H = 512, one
+// token 12.6, 14.3 (128), 16 tokens bf16 16.2, 17.6 (512); 64 + 2 experts, H = 2048, one token 24.7, 26.3 (768), bf16 43.8, 39.2 (2816); H = 2048, 16 tokens 33.4, 31.1
+// (2048); 8 experts, H = 4096, one token 59.7, 51.1 (3584).
+int few_down_columns(const moe_shape& s, bool fp4) {
+    const int64_t work = down_tasks(s, fp4) * (s.H / 64);
+    return work <= 1024 ? 16 : (work >= 8192 && s.H % 128 == 0 ? 128 : 64);
+}
 int few_shares(const moe_shape& s, bool fp4) {
     const int columns = s.H / few_down_columns(s, fp4);
     return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 256 / columns, (down_tasks(s, fp4) + WAVES - 1) / WAVES}));
