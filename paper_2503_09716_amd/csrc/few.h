@@ -6,7 +6,8 @@ namespace moe {
 
 constexpr int FEW_TOKENS = 16, FEW_TOP_K = 16;
 constexpr int FEW_SHARES = 32;        // workgroups to the same columns of the down launch at most
-constexpr size_t FEW_X_LDS = 80 << 10;
+constexpr size_t FEW_X_LDS = 80 << 10;     // beside the gate/up launch's own 75 KiB
+constexpr int FEW_X_TWO = 5 << 10;         // and with that much a CU holds two of its workgroups
 
 // Where the picks of the tokens sit: pick[e][t] = j of token t's pick e, or -1; the experts that have any, ascending.
 struct alignas(16) Picks {

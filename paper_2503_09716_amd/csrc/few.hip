@@ -524,17 +524,23 @@ int few_h_row(const moe_shape& s) { return (s.F + 127) / 128 * 512; }   // bytes
 size_t few_h_bytes(const moe_shape& s) { return (size_t)s.T * (s.top_k + s.num_shared) * few_h_row(s); }
 size_t few_partial_bytes(const moe_shape& s) { return (size_t)s.H * FEW_SHARES * FEW_TOKENS * 4; }
 
+// x in LDS (whole layers, us, with and without: 8 experts, H = 512, one token 12.9, 15.6; 8 experts, H = 4096, 7 tokens 132, 143; 64 + 2 experts, H = 2048, 16 tokens
+// 68.4, 69.9), and then a gate matrix of up to 128 KiB with it, which every workgroup reads (inside and in a launch of its own: 64 KiB 51.3, 54.6; 256 KiB,
+// 64 experts, one token 29.6, 25.0; 1.6 MiB 107, 48).
 bool few_x_in_lds(const moe_shape& s) { return few_x_bytes(s) <= FEW_X_LDS; }
 bool few_routes_inside(const moe_shape& s) { return few_x_in_lds(s) && (int64_t)((s.E + 15) / 16) * s.H * 32 <= 128 << 10; }
 
 // Columns of a down workgroup.  Few tasks: 16, so that there are workgroups enough and each has little to do one after the other; else 64, where a load of h
-// meets four of weights, and 128 in the longest launches (whole layers, us, 16 and 64 columns; tasks x columns / 64): 8 experts, H = 512, one
-// token 12.6, 14.3 (128), 16 tokens bf16 16.2, 17.6 (512); 64 + 2 experts, H = 2048, one token 24.7, 26.3 (768), bf16 43.8, 39.2 (2816); H = 2048, 16 tokens 33.4, 31.1
-// (2048); 8 experts, H = 4096, one token 59.7, 51.1 (3584).
+// meets four of weights, and 128 in the longest launches on MXFP4.  Whole layers, us; tasks x columns / 64:
+//   16 and 64: 8 experts, H = 512, one token 12.6, 14.3 (128), 16 tokens bf16 16.2, 17.6 (512); 64 + 2 experts, H = 2048, one token 24.7, 26.3 (768), bf16 43.8, 39.2
+//     (2816); H = 2048, 16 tokens 33.4, 31.1 (2048); 8 experts, H = 4096, one token 59.7, 51.1 (3584)
+//   64 and 128: 160 + 2 experts, H = 5120, 7 tokens 115, 113 (10560), 16 tokens 207, 201 (23520); 8 experts, H = 4096, 16 tokens 159, 154 (14336), but bf16 432, 437;
+//     64 + 2 experts, 16 tokens, bf16 154, 159
 int few_down_columns(const moe_shape& s, bool fp4) {
     const int64_t work = down_tasks(s, fp4) * (s.H / 64);
-    return work <= 1024 ? 16 : (work >= 8192 && s.H % 128 == 0 ? 128 : 64);
+    return work <= 1024 ? 16 : (fp4 && work >= 8192 && s.H % 128 == 0 ? 128 : 64);
 }
+// Workgroups that share columns: as many as fill the chip, but eight tasks each (64 + 2 experts, 16 tokens, bf16, at most 8 and 32: 171, 159 us).
 int few_shares(const moe_shape& s, bool fp4) {
     const int columns = s.H / few_down_columns(s, fp4);
     return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 256 / columns, (down_tasks(s, fp4) + WAVES - 1) / WAVES}));
@@ -558,8 +564,12 @@ hipError_t launch(const FewArgs& a, hipStream_t st) {
         hipLaunchKernelGGL(few_logits_kernel<FP4>, dim3((unsigned)(blocks + copies)), block, 0, st, a);
         if (const hipError_t e = hipGetLastError()) return e;
     }
+    // Gate/up: a workgroup to an item where all are on the chip at once, two to a CU (64 + 2 experts, one token, 352 items, whole layer 25.0 us; 256 workgroups
+    // 25.5), else 256 that take several, whose loads then run on into the next one (160 + 2 experts, one token, 384 items, of which a CU holds one at a
+    // time, 48.0 and 42.3 us; 64 + 2 experts, 7 tokens, 1936 items 77, 48).
     const int64_t active = std::min<int64_t>(a.E, (int64_t)a.T * a.k) + a.Ns, items = active * (a.F / (a.x_in_lds ? 32 : 64));
-    const dim3 up((unsigned)(items <= 512 ? items : 256)), down((unsigned)(a.H / a.down_columns * a.shares));
+    const bool two = !a.x_in_lds || a.x_bytes <= FEW_X_TWO;
+    const dim3 up((unsigned)(two && items <= 512 ? items : std::min<int64_t>(items, 256))), down((unsigned)(a.H / a.down_columns * a.shares));
     if (a.x_in_lds) hipLaunchKernelGGL((few_up_kernel<FP4, NT, true>), up, block, (unsigned)a.x_bytes, st, a);
     else hipLaunchKernelGGL((few_up_kernel<FP4, NT, false>), up, block, 0, st, a);
     if (const hipError_t e = hipGetLastError()) return e;
@@ -571,6 +581,8 @@ hipError_t launch(const FewArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// nt: lists above 256 MB, which no cache holds from one call to the next (us, without and with: 64 + 2 experts, one token, bf16 43.3, 39.3; 8 experts, H = 4096, 7
+// tokens 143, 131; a list of 7 MB 12.9, 13.9).
 hipError_t launch_few(const FewArgs& a, bool fp4, hipStream_t st) {
     if (fp4) return a.nt ? launch<true, true>(a, st) : launch<true, false>(a, st);
     return a.nt ? launch<false, true>(a, st) : launch<false, false>(a, st);
