@@ -5,7 +5,8 @@
 // byte is max(e - 2, 0).  A value is rounded to the nearest code, ties to the even one, by the conversion instructions, which
 // saturate.  A block that holds an infinity or NaN has the scale 255 and reads back as 32 NaN.
 //
-// All four kernels are bound by memory: one pass, each element in one lane's registers.
+// All four kernels are bound by memory: one pass, each element in one lane's registers.  Rows to MXFP4: 5.4 to 5.8 TB/s from 18006 x 1408 bf16 (12 us) on; what is
+// read goes through the caches (past them 14), where the kernel before has left it.
 #include "fp4.h"
 
 namespace moe {
@@ -96,6 +97,9 @@ __global__ __launch_bounds__(QUANTIZE_WAVES * 64) void fp4_quantize_kernel(const
     if ((lane & 3) == 0) scales[(row * groups + q) * 16 + (b & 3) * 4 + (b >> 2)] = (char)byte;
 }
 
+// The way back: bf16 as above; fp32 in two halves of the group of four neighbours to a lane, so that each store is 1 KiB in one piece.  Stores past the caches
+// (98304 x 1408 to bf16 75 -> 50 us, 7.0 TB/s, and with a kernel that reads it 172 -> 162; 18006 x 1408 11.5 -> 10.7, 26.5 -> 27.5; 5003 x 2048 to fp32 10.5 -> 7.7, which
+// past the caches without the halves are 13.4).
 template <bool FP32>
 __global__ __launch_bounds__(QUANTIZE_WAVES * 64) void fp4_dequantize_kernel(const char* __restrict__ codes, const char* __restrict__ scales,
                                                                             const uint32_t units, const int groups, const int K,
@@ -103,29 +107,38 @@ __global__ __launch_bounds__(QUANTIZE_WAVES * 64) void fp4_dequantize_kernel(con
     const int lane = threadIdx.x & 63;
     const uint32_t unit = blockIdx.x * QUANTIZE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= units) return;
-    const size_t row = unit / (uint32_t)groups;   // below 2^26 units: each takes 80 bytes of 4 GiB or more
-    const int q = (int)(unit - (uint32_t)row * (uint32_t)groups), k = q * FP4_GROUP + lane * 8;
-    if (k >= K) return;
-    const int b = lane >> 2;
-    const uint32_t code = *reinterpret_cast<const uint32_t*>(codes + row * sub_tiles * 64 + (k >> 1));
-    const uint32_t byte = (uint8_t)scales[(row * groups + q) * 16 + (b & 3) * 4 + (b >> 2)];
-    const u32x4 v = values_of(code, byte);
-    if (FP32) {
-        u32x4* const at = reinterpret_cast<u32x4*>(out + (row * K + k) * 4);
-        at[0] = u32x4{v[0] << 16, v[0] & 0xffff0000u, v[1] << 16, v[1] & 0xffff0000u};
-        at[1] = u32x4{v[2] << 16, v[2] & 0xffff0000u, v[3] << 16, v[3] & 0xffff0000u};
+    const size_t row = unit / (uint32_t)groups;
+    const int q = (int)(unit - (uint32_t)row * (uint32_t)groups);
+    const char* const row_codes = codes + row * sub_tiles * 64;
+    const char* const row_scales = scales + (row * groups + q) * 16;
+    auto byte_of = [&](const int b) __attribute__((always_inline)) { return (uint32_t)(uint8_t)row_scales[(b & 3) * 4 + (b >> 2)]; };   // block b of the group
+    if constexpr (FP32) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int at = j * 256 + lane * 4, k = q * FP4_GROUP + at;
+            if (k >= K) continue;
+            const u32x4 v = values_of(*reinterpret_cast<const uint16_t*>(row_codes + (k >> 1)), byte_of(at >> 5));
+            __builtin_nontemporal_store(u32x4{v[0] << 16, v[0] & 0xffff0000u, v[1] << 16, v[1] & 0xffff0000u}, reinterpret_cast<u32x4*>(out + (row * K + k) * 4));
+        }
     } else {
-        *reinterpret_cast<u32x4*>(out + (row * K + k) * 2) = v;
+        const int k = q * FP4_GROUP + lane * 8;
+        if (k >= K) return;
+        const u32x4 v = values_of(*reinterpret_cast<const uint32_t*>(row_codes + (k >> 1)), byte_of(lane >> 2));
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(out + (row * K + k) * 2));
     }
 }
 
 // Weights [K, N] row-major to blocks of their transpose: a lane holds 32 k of two neighbouring columns, so a block's largest
-// magnitude needs no other lane, and each of a wavefront's loads is 256 consecutive bytes of a row.
-constexpr int PACK_WAVES = 4;   // as many neighbouring blocks along K
+// magnitude needs no other lane, and each of a wavefront's loads is 256 consecutive bytes of a row.  A workgroup has a sub-tile of 128 columns, whose
+// 1 KiB blocks pass through LDS and are stored whole (K = 4096, N = 14336: 33.3 us; 16 bytes a lane straight to memory 39.8).  The way back loads them
+// piece by piece (30.5 us, through LDS 32.8).  The matrix itself passes the caches by, where it would displace what is used again: 33.3 -> 29.4 us (5.0 TB/s), 30.5 -> 24
+// (6.1).
+constexpr int PACK_WAVES = 4;   // as many neighbouring blocks along K: a sub-tile
+constexpr int PACK_COLUMNS = 128, PACK_BLOCKS = PACK_COLUMNS / 16;
 
-__device__ __forceinline__ size_t weight_piece(const int n, const int kb, const int sub_tiles) {   // of column n, block kb of 32 k
+__device__ __forceinline__ int tile_piece(const int n, const int kb) {   // of a sub-tile's blocks: column n, block kb of 32 k
     const int r = n & 15;
-    return ((size_t)(n >> 4) * sub_tiles + (kb >> 2)) * 1024 + r * 64 + (((kb & 3) ^ block_swizzle(r)) << 4);
+    return (n >> 4) * 64 + r * 4 + ((kb & 3) ^ block_swizzle(r));
 }
 __device__ __forceinline__ size_t weight_scale(const int n, const int kb, const int groups) {
     return ((size_t)(n >> 4) * groups + (kb >> 4)) * 256 + (n & 15) * 16 + (kb & 3) * 4 + (kb >> 2 & 3);
@@ -133,15 +146,16 @@ __device__ __forceinline__ size_t weight_scale(const int n, const int kb, const 
 
 __global__ __launch_bounds__(PACK_WAVES * 64) void fp4_pack_kernel(const uint32_t* __restrict__ w, const int K, const int N, const int sub_tiles,
                                                                   const int groups, char* __restrict__ codes, char* __restrict__ scales) {
-    const int n = blockIdx.y * 128 + (threadIdx.x & 63) * 2;
-    const int kb = blockIdx.x * PACK_WAVES + (threadIdx.x >> 6);   // up to groups * 16: past K come zeros
-    if (n >= N) return;
+    __shared__ u32x4 tile[PACK_BLOCKS * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n0 = blockIdx.y * PACK_COLUMNS, n = n0 + lane * 2;
+    const int kb = blockIdx.x * PACK_WAVES + wave;   // up to groups * 16: past K come zeros
     u32x4 code[2] = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
     uint32_t byte[2] = {127u, 127u};
-    if (kb * 32 < K) {
+    if (n < N && kb * 32 < K) {
         uint32_t v[32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = w[((size_t)(kb * 32 + i) * N + n) >> 1];
+        for (int i = 0; i < 32; ++i) v[i] = __builtin_nontemporal_load(&w[((size_t)(kb * 32 + i) * N + n) >> 1]);
         uint32_t m0 = 0, m1 = 0;
 #pragma unroll
         for (int i = 0; i < 32; ++i) { m0 = max(m0, v[i] & 0x7fffu); m1 = max(m1, v[i] >> 16 & 0x7fffu); }
@@ -160,23 +174,27 @@ __global__ __launch_bounds__(PACK_WAVES * 64) void fp4_pack_kernel(const uint32_
             code[1][p] = byte[1] == 255u ? 0u : codes_of_bf16(b, byte[1]);
         }
     }
+    if (n < N)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        if (kb < sub_tiles * 4) *reinterpret_cast<u32x4*>(codes + weight_piece(n + j, kb, sub_tiles)) = code[j];
-        scales[weight_scale(n + j, kb, groups)] = (char)byte[j];
-    }
+        for (int j = 0; j < 2; ++j) scales[weight_scale(n + j, kb, groups)] = (char)byte[j];
+    if ((int)blockIdx.x >= sub_tiles) return;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) tile[tile_piece(lane * 2 + j, wave)] = code[j];
+    __syncthreads();
+    for (int b = wave; b < PACK_BLOCKS && n0 + b * 16 < N; b += PACK_WAVES)
+        *reinterpret_cast<u32x4*>(codes + ((size_t)((n0 >> 4) + b) * sub_tiles + blockIdx.x) * 1024 + lane * 16) = tile[b * 64 + lane];
 }
 
 __global__ __launch_bounds__(PACK_WAVES * 64) void fp4_unpack_kernel(const char* __restrict__ codes, const char* __restrict__ scales, const int K,
                                                                     const int N, const int sub_tiles, const int groups, uint32_t* __restrict__ w) {
-    const int n = blockIdx.y * 128 + (threadIdx.x & 63) * 2;
+    const int n = blockIdx.y * PACK_COLUMNS + (threadIdx.x & 63) * 2;
     const int kb = blockIdx.x * PACK_WAVES + (threadIdx.x >> 6);
     if (n >= N || kb * 32 >= K) return;
     u32x4 code[2];
     uint32_t byte[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        code[j] = *reinterpret_cast<const u32x4*>(codes + weight_piece(n + j, kb, sub_tiles));
+        code[j] = *reinterpret_cast<const u32x4*>(codes + ((size_t)((n + j) >> 4) * sub_tiles + (kb >> 2)) * 1024 + tile_piece((n + j) & 15, kb) * 16);
         byte[j] = (uint8_t)scales[weight_scale(n + j, kb, groups)];
     }
 #pragma unroll
@@ -185,8 +203,8 @@ __global__ __launch_bounds__(PACK_WAVES * 64) void fp4_unpack_kernel(const char*
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const size_t at = ((size_t)(kb * 32 + p * 8 + 2 * i) * N + n) >> 1;
-            w[at] = (a[i] & 0xffffu) | b[i] << 16;
-            w[at + (N >> 1)] = a[i] >> 16 | (b[i] & 0xffff0000u);
+            __builtin_nontemporal_store((a[i] & 0xffffu) | b[i] << 16, &w[at]);
+            __builtin_nontemporal_store(a[i] >> 16 | (b[i] & 0xffff0000u), &w[at + (N >> 1)]);
         }
     }
 }
@@ -217,7 +235,7 @@ hipError_t launch_fp4_dequantize(const void* q, int64_t rows, int K, void* out, 
 
 hipError_t launch_fp4_pack(const void* w, int K, int N, void* q, hipStream_t st) {
     const int sub_tiles = (int)fp4_sub_tiles(K), groups = (int)fp4_groups(K);
-    const dim3 grid((unsigned)(groups * 16 / PACK_WAVES), (unsigned)((N + 127) / 128));
+    const dim3 grid((unsigned)(groups * 16 / PACK_WAVES), (unsigned)((N + PACK_COLUMNS - 1) / PACK_COLUMNS));
     hipLaunchKernelGGL(fp4_pack_kernel, grid, dim3(PACK_WAVES * 64), 0, st, (const uint32_t*)w, K, N, sub_tiles, groups, (char*)q,
                        (char*)q + fp4_scales_at(N, K));
     return hipGetLastError();
@@ -225,7 +243,7 @@ hipError_t launch_fp4_pack(const void* w, int K, int N, void* q, hipStream_t st)
 
 hipError_t launch_fp4_unpack(const void* q, int K, int N, void* w, hipStream_t st) {
     const int sub_tiles = (int)fp4_sub_tiles(K), groups = (int)fp4_groups(K);
-    const dim3 grid((unsigned)((K / 32 + PACK_WAVES - 1) / PACK_WAVES), (unsigned)((N + 127) / 128));
+    const dim3 grid((unsigned)((K / 32 + PACK_WAVES - 1) / PACK_WAVES), (unsigned)((N + PACK_COLUMNS - 1) / PACK_COLUMNS));
     hipLaunchKernelGGL(fp4_unpack_kernel, grid, dim3(PACK_WAVES * 64), 0, st, (const char*)q, (const char*)q + fp4_scales_at(N, K), K, N, sub_tiles,
                        groups, (uint32_t*)w);
     return hipGetLastError();
