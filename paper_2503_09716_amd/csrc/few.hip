@@ -1,4 +1,4 @@
-// The whole MoE layer for up to 16 tokens in two launches (three where the gate matrix is large), on bf16 or MXFP4 weights.
+// The whole MoE layer for up to 16 tokens in two launches (three where the gate matrix or x is large), on bf16 or MXFP4 weights.
 //
 //   few_up_kernel    routes, and leaves h[t, j] = w_tj * silu(x_t W1_e) * (x_t W3_e) for each pick e of token t, and of each shared expert
 //   few_down_kernel  out[t] = sum over the picks and the shared experts of h W2_e
@@ -8,7 +8,11 @@
 // holds their values exactly, in registers.
 //
 // A wavefront takes 16 columns: W is the row operand straight from memory, the tokens are the 16 columns of the other one, whether they picked
-// the expert or not; what they did not pick is not stored (gate and up) or zero (down).
+// the expert or not; what they did not pick is not stored (gate and up) or left out of the sum (down).
+//
+// Bound by reading the weights where they are large (8 experts, H = 4096, F = 14336, MXFP4, 16 tokens 154 us, 5.0 TB/s; 160 + 2 experts, H = 5120, F = 1536 182 us, 5.2), and
+// by the chain of launches, routing and first loads where they are small (64 + 2 experts, H = 2048, one token 23.5 us: logits 3.5, gate/up 12, down 8.5; 8 experts,
+// H = 512, F = 1024, bf16, 16 tokens 15.8 us, where the layer for any batch takes 24).
 #include <algorithm>
 
 #include "few.h"
