@@ -123,18 +123,19 @@ __device__ __forceinline__ f32x4 logits_of(const FewArgs& p, const int nb, const
 
 // A large gate matrix, or more x than LDS holds: one workgroup to 16 experts, K cut over its wavefronts, sums in wave order; those behind them
 // copy x.
+constexpr int LOGIT_WAVES = 16;   // (whole layer, us, with 8: 160 + 2 experts, H = 5120, 16 tokens 180.9, 178.8; 64 + 2 experts, one token 24.5, 24.2)
 template <bool FP4>
-__global__ __launch_bounds__(WAVES * 64) void few_logits_kernel(const FewArgs p) {
-    __shared__ float part[WAVES][256];
+__global__ __launch_bounds__(LOGIT_WAVES * 64) void few_logits_kernel(const FewArgs p) {
+    __shared__ float part[LOGIT_WAVES][256];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int blocks = (p.E + 15) >> 4;
     if ((int)blockIdx.x >= blocks) {
-        const int pieces = p.H >> 3, i = (blockIdx.x - blocks) * WAVES * 64 + tid, row = i / pieces, piece = i - row * pieces;
+        const int pieces = p.H >> 3, i = (blockIdx.x - blocks) * LOGIT_WAVES * 64 + tid, row = i / pieces, piece = i - row * pieces;
         if (row < p.T) *reinterpret_cast<u32x4*>(p.x_copy + x_place<FP4>(piece, row, p.T)) = load_piece(p.x + (size_t)i * 16);
         return;
     }
     const char* const xa = p.x + (size_t)min(lane & 15, p.T - 1) * p.H * 2 + (lane >> 4) * 16;
-    const f32x4 acc = logits_of(p, blockIdx.x, wave, WAVES, [&](const int s) __attribute__((always_inline)) { return load_piece(xa + (size_t)s * 64); });
+    const f32x4 acc = logits_of(p, blockIdx.x, wave, LOGIT_WAVES, [&](const int s) __attribute__((always_inline)) { return load_piece(xa + (size_t)s * 64); });
 #pragma unroll
     for (int r = 0; r < 4; ++r) part[wave][(4 * (lane >> 4) + r) * 16 + (lane & 15)] = acc[r];
     __syncthreads();
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_logits_kernel(const FewArgs p)
     if (t >= p.T) return;
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) v += part[w][tid];
+    for (int w = 0; w < LOGIT_WAVES; ++w) v += part[w][tid];
     p.logits_out[t * p.ep + blockIdx.x * 16 + (tid & 15)] = v;
 }
 
@@ -564,8 +565,8 @@ template <bool FP4, bool NT>
 hipError_t launch(const FewArgs& a, hipStream_t st) {
     const dim3 block(WAVES * 64);
     if (a.logits) {
-        const int blocks = (a.E + 15) / 16, copies = a.x_in_lds ? 0 : (a.T * (a.H / 8) + WAVES * 64 - 1) / (WAVES * 64);
-        hipLaunchKernelGGL(few_logits_kernel<FP4>, dim3((unsigned)(blocks + copies)), block, 0, st, a);
+        const int blocks = (a.E + 15) / 16, copies = a.x_in_lds ? 0 : (a.T * (a.H / 8) + LOGIT_WAVES * 64 - 1) / (LOGIT_WAVES * 64);
+        hipLaunchKernelGGL(few_logits_kernel<FP4>, dim3((unsigned)(blocks + copies)), dim3(LOGIT_WAVES * 64), 0, st, a);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     // Gate/up: a workgroup to an item where all are on the chip at once, two to a CU (64 + 2 experts, one token, 352 items, whole layer 25.0 us; 256 workgroups
