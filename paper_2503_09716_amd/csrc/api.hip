@@ -966,7 +966,7 @@ FewLayout few_layout(const moe_shape& s) {
     const size_t ep = (size_t)route_gemm_config(s).ep;
     L.picks = take(sizeof(Picks));
     L.arrived = take((size_t)(s.H / 16) * 4);
-    L.logits = take((size_t)s.T * ep * 4);
+    L.logits = take((size_t)few_logit_shares(s) * s.T * ep * 4);
     L.gate = take(ep * s.H * 2);
     L.x_copy = take(few_x_in_lds(s) ? 0 : few_x_bytes(s));
     L.h = take(few_h_bytes(s));
@@ -1719,6 +1719,7 @@ moe_status moe_layer_few(moe_ctx* c, const moe_shape* s, const void* x, const vo
     a.h_row = few_h_row(*s);
     a.down_columns = few_down_columns(*s, list->fp4 != 0);
     a.shares = few_shares(*s, list->fp4 != 0);
+    a.logit_shares = few_logit_shares(*s);
     a.nt = (double)list->experts * 3 * s->H * s->F * (list->fp4 ? 0.53125 : 2.0) > (double)(256 << 20);
     a.out = (char*)out;
     a.T = s->T;

@@ -18,7 +18,7 @@ struct alignas(16) Picks {
 
 struct FewArgs {
     const char *x, *wg;                  // tokens; packed gate matrix
-    const float *bias, *logits;          // bias: or nullptr; logits [T][ep]: computed by a launch before, or nullptr
+    const float *bias, *logits;          // bias: or nullptr; logits [logit_shares][T][ep]: computed by a launch before, or nullptr
     float* logits_out;                   // that launch's
     const void* const* weights;          // device table of packed matrices [3][E + Ns]
     Picks* picks;                        // from the first launch to the second
@@ -28,6 +28,7 @@ struct FewArgs {
     int32_t* arrived;                    // workgroups that have left theirs; cleared by the launch before
     char* out;
     int32_t shares;                      // workgroups to the same columns
+    int32_t logit_shares;                // of the logits
     int32_t down_columns;                // columns of a workgroup of the down launch: 16, 64 or 128
     int32_t h_row, x_bytes, x_in_lds;
     int32_t nt;                          // 1: weights past the caches
@@ -41,6 +42,7 @@ size_t few_h_bytes(const moe_shape& s);
 size_t few_partial_bytes(const moe_shape& s);
 bool few_x_in_lds(const moe_shape& s);
 bool few_routes_inside(const moe_shape& s);   // no launch for the logits
+int few_logit_shares(const moe_shape& s);
 int few_down_columns(const moe_shape& s, bool fp4);
 int few_shares(const moe_shape& s, bool fp4);
 hipError_t few_init();

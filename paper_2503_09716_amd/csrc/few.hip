@@ -121,21 +121,21 @@ __device__ __forceinline__ f32x4 logits_of(const FewArgs& p, const int nb, const
     return acc;
 }
 
-// A large gate matrix, or more x than LDS holds: one workgroup to 16 experts, K cut over its wavefronts, sums in wave order; those behind them
-// copy x.
+// A large gate matrix, or more x than LDS holds: K cut over the wavefronts of few_logit_shares workgroups to 16 experts, sums in wave order, and over the workgroups
+// where the logits are read; the workgroups behind them copy x.
 constexpr int LOGIT_WAVES = 16;   // (whole layer, us, with 8: 160 + 2 experts, H = 5120, 16 tokens 180.9, 178.8; 64 + 2 experts, one token 24.5, 24.2)
 template <bool FP4>
 __global__ __launch_bounds__(LOGIT_WAVES * 64) void few_logits_kernel(const FewArgs p) {
     __shared__ float part[LOGIT_WAVES][256];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int blocks = (p.E + 15) >> 4;
-    if ((int)blockIdx.x >= blocks) {
-        const int pieces = p.H >> 3, i = (blockIdx.x - blocks) * LOGIT_WAVES * 64 + tid, row = i / pieces, piece = i - row * pieces;
+    const int blocks = (p.E + 15) >> 4, share = blockIdx.x / blocks, nb = blockIdx.x - share * blocks;
+    if (share >= p.logit_shares) {
+        const int pieces = p.H >> 3, i = (blockIdx.x - blocks * p.logit_shares) * LOGIT_WAVES * 64 + tid, row = i / pieces, piece = i - row * pieces;
         if (row < p.T) *reinterpret_cast<u32x4*>(p.x_copy + x_place<FP4>(piece, row, p.T)) = load_piece(p.x + (size_t)i * 16);
         return;
     }
     const char* const xa = p.x + (size_t)min(lane & 15, p.T - 1) * p.H * 2 + (lane >> 4) * 16;
-    const f32x4 acc = logits_of(p, blockIdx.x, wave, LOGIT_WAVES, [&](const int s) __attribute__((always_inline)) { return load_piece(xa + (size_t)s * 64); });
+    const f32x4 acc = logits_of(p, nb, share * LOGIT_WAVES + wave, p.logit_shares * LOGIT_WAVES, [&](const int s) __attribute__((always_inline)) { return load_piece(xa + (size_t)s * 64); });
 #pragma unroll
     for (int r = 0; r < 4; ++r) part[wave][(4 * (lane >> 4) + r) * 16 + (lane & 15)] = acc[r];
     __syncthreads();
@@ -144,18 +144,29 @@ __global__ __launch_bounds__(LOGIT_WAVES * 64) void few_logits_kernel(const FewA
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < LOGIT_WAVES; ++w) v += part[w][tid];
-    p.logits_out[t * p.ep + blockIdx.x * 16 + (tid & 15)] = v;
+    p.logits_out[(share * p.T + t) * p.ep + nb * 16 + (tid & 15)] = v;
 }
 
-// Softmax and top-k of all tokens, by four wavefronts, into idx and w [16][16] in LDS.
+// Softmax and top-k of all tokens, by four wavefronts, into idx and w [16][16] in LDS.  logits: `shares` matrices that are added in order.
 template <int NV>
-__device__ __forceinline__ void select(const FewArgs& p, const float* logits, const int stride, int32_t* idx, float* w) {
+__device__ __forceinline__ void select(const FewArgs& p, const float* logits, const int stride, const int shares, int32_t* idx, float* w) {
     const int lane = threadIdx.x & 63, row = lane & 15, t = (threadIdx.x >> 6) * 4 + (lane >> 4);
     float v[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int e = row + 16 * i;
-        v[i] = e < p.E ? logits[min(t, p.T - 1) * stride + e] + (p.bias ? p.bias[e] : 0.f) : -INFINITY;
+        v[i] = e < p.E ? logits[min(t, p.T - 1) * stride + e] : 0.f;
+    }
+    for (int q = 1; q < shares; ++q)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = row + 16 * i;
+            if (e < p.E) v[i] += logits[(q * p.T + min(t, p.T - 1)) * stride + e];
+        }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = row + 16 * i;
+        v[i] = e < p.E ? v[i] + (p.bias ? p.bias[e] : 0.f) : -INFINITY;
     }
     int e;
     float we;
@@ -232,12 +243,12 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
         }
     }
     const float* const l = p.logits ? p.logits : logits;
-    const int stride = p.logits ? p.ep : LOGIT_STRIDE;
+    const int stride = p.logits ? p.ep : LOGIT_STRIDE, shares = p.logits ? p.logit_shares : 1;
     if (wave * 4 < p.T) {
-        if (p.E <= 16) select<1>(p, l, stride, idx, w);
-        else if (p.E <= 64) select<4>(p, l, stride, idx, w);
-        else if (p.E <= 160) select<10>(p, l, stride, idx, w);
-        else select<16>(p, l, stride, idx, w);
+        if (p.E <= 16) select<1>(p, l, stride, shares, idx, w);
+        else if (p.E <= 64) select<4>(p, l, stride, shares, idx, w);
+        else if (p.E <= 160) select<10>(p, l, stride, shares, idx, w);
+        else select<16>(p, l, stride, shares, idx, w);
     }
     __syncthreads();
     gather_picks(picks, idx, p.T, p.k, p.E);
@@ -535,6 +546,10 @@ size_t few_partial_bytes(const moe_shape& s) { return (size_t)s.H * FEW_SHARES *
 bool few_x_in_lds(const moe_shape& s) { return few_x_bytes(s) <= FEW_X_LDS; }
 bool few_routes_inside(const moe_shape& s) { return few_x_in_lds(s) && (int64_t)((s.E + 15) / 16) * s.H * 32 <= 128 << 10; }
 
+// Workgroups to the logits of 16 experts: one to 1024 of H where there is more x than LDS holds (whole layers, us, one and H / 1024: 160 + 2 experts, H = 5120, 16 tokens
+// 206, 202.5; 8 experts, H = 4096, 16 tokens 153.4, 151.1; with less x the sums cost more: 64 + 2 experts, one token 24.4, 25.0).
+int few_logit_shares(const moe_shape& s) { return few_x_in_lds(s) ? 1 : std::max(1, std::min(s.H / 1024, 8)); }
+
 // Columns of a down workgroup.  Few tasks: 16, so that there are workgroups enough and each has little to do one after the other; else 64, where a load of h
 // meets four of weights, and 128 in the longest launches on MXFP4.  Whole layers, us; tasks x columns / 64:
 //   16 and 64: 8 experts, H = 512, one token 12.6, 14.3 (128), 16 tokens bf16 16.2, 17.6 (512); 64 + 2 experts, H = 2048, one token 24.7, 26.3 (768), bf16 43.8, 39.2
@@ -566,7 +581,7 @@ hipError_t launch(const FewArgs& a, hipStream_t st) {
     const dim3 block(WAVES * 64);
     if (a.logits) {
         const int blocks = (a.E + 15) / 16, copies = a.x_in_lds ? 0 : (a.T * (a.H / 8) + LOGIT_WAVES * 64 - 1) / (LOGIT_WAVES * 64);
-        hipLaunchKernelGGL(few_logits_kernel<FP4>, dim3((unsigned)(blocks + copies)), dim3(LOGIT_WAVES * 64), 0, st, a);
+        hipLaunchKernelGGL(few_logits_kernel<FP4>, dim3((unsigned)(blocks * a.logit_shares + copies)), dim3(LOGIT_WAVES * 64), 0, st, a);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     // Gate/up: a workgroup to an item where all are on the chip at once, two to a CU (64 + 2 experts, one token, 352 items, whole layer 25.0 us; 256 workgroups
