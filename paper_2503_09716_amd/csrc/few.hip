@@ -560,10 +560,13 @@ int few_down_columns(const moe_shape& s, bool fp4) {
     const int64_t work = down_tasks(s, fp4) * (s.H / 64);
     return work <= 1024 ? 16 : (fp4 && work >= 8192 && s.H % 128 == 0 ? 128 : 64);
 }
-// Workgroups that share columns: as many as fill the chip, but eight tasks each (64 + 2 experts, 16 tokens, bf16, at most 8 and 32: 171, 159 us).
+// Workgroups that share columns: as many as fill the chip (a CU holds one), but one to up to eight tasks, and more to four of MXFP4, which are four times as long, or
+// eight of bf16 (64 + 2 experts, 16 tokens, bf16, at most 8 and 32 shares: 171, 159 us; 8 experts, H = 512, 16 tokens, 16 tasks of MXFP4 by eight and by four 17.2, 15.5; 8
+// tasks, bf16, in one and two shares 16.4, 17.4; 64 + 2 experts, one token, in 256 and 384 workgroups 24.8, 29.1).
 int few_shares(const moe_shape& s, bool fp4) {
-    const int columns = s.H / few_down_columns(s, fp4);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 256 / columns, (down_tasks(s, fp4) + WAVES - 1) / WAVES}));
+    const int64_t tasks = down_tasks(s, fp4), each = fp4 ? WAVES / 2 : WAVES;
+    if (tasks <= WAVES) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)FEW_SHARES, 256 / (s.H / few_down_columns(s, fp4)), (tasks + each - 1) / each}));
 }
 
 hipError_t few_init() {
