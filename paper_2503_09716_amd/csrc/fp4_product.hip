@@ -47,7 +47,7 @@ struct Ring {
 };
 constexpr int ROUNDS = 64;   // tiles of a workgroup that it can list itself
 template <class C>
-constexpr int OWN = C::NEXT ? ROUNDS * 16 : 0;
+constexpr int OWN = C::NEXT ? (ROUNDS + 1) * 16 : 0;
 static_assert(Ring<Long>::BYTES + OWN<Long> <= 160 * 1024 && Ring<Short>::BYTES <= 80 * 1024, "LDS");
 
 typedef const __attribute__((address_space(1))) void* gptr_t;
@@ -591,9 +591,9 @@ __global__ __launch_bounds__(C::NW * 64, 2) void fp4_tile_kernel(const Fp4Produc
     if (p.inside) {
         const WaveList l = wave_list<C::ROWS>(p, lane);
         if (C::NEXT) {
-            for (int i = wave; i < p.rounds; i += C::NW) {
+            for (int i = wave; i <= p.rounds; i += C::NW) {   // the list ends with none
                 const TileDesc t = tile_at<GATED>(p, l, blockIdx.x + i * gridDim.x, lane, n0);
-                if (lane == 0) own[i] = i32x4{t.group, t.row0, t.nrows, n0};
+                if (lane == 0) own[i] = i32x4{t.group, t.row0, i < p.rounds ? t.nrows : 0, n0};
             }
             __syncthreads();
         } else {

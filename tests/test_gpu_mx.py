@@ -310,6 +310,22 @@ def test_rows_behind_the_last_group_stay_as_they_were(moe):
     assert (out == 7.0).all()
 
 
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("ends", [[0, 0, 0, 0], [0, 0, 300, 300], [7, 7, 2000, 2001], [0, 5000, 5000, 9000], [8000, 8500, 8500, 9000]])
+def test_long_launches_with_fewer_rows_than_they_have_room_for(moe, ends, gated):
+    p = Product(moe, [3000, 3000, 3000], 96, 8224, gated, seed=3)
+    whole = p.run(torch.float32).clone()
+    p.offsets = torch.tensor(ends, dtype=torch.int32, device=DEV)
+    out = torch.full_like(whole, 7.0)
+    p.run(torch.float32, out)
+    assert (out[:ends[0]] == 7.0).all() and (out[ends[3]:] == 7.0).all()
+    for e in range(3):   # rows that are in the same group as before have the same bits
+        a, b = max(ends[e], 3000 * e), min(ends[e + 1], 3000 * (e + 1))
+        if a < b:
+            assert torch.equal(out[a:b], whole[a:b])
+    assert torch.isfinite(out).all()
+
+
 def test_rows_in_front_of_the_first_group_stay_as_they_were(moe):
     p = Product(moe, [40, 300], 256, 64, False)
     whole = p.run(torch.float32).clone()
@@ -381,6 +397,40 @@ def test_products_in_a_replayed_graph_and_on_another_stream(moe):
         torch.cuda.synchronize()
         assert torch.equal(out, want)
         p.run(torch.bfloat16)
+
+
+def test_two_graphs_share_a_workspace_and_two_streams_do_not(moe):
+    gen = torch.Generator().manual_seed(11)
+    cases = [Product(moe, torch.randint(0, 40, (256,), generator=gen).tolist(), 64, 1088, True, seed=s) for s in (1, 2)]   # with a list of tiles in the workspace
+    want = [p.run(torch.bfloat16).clone() for p in cases]
+    outs = [torch.zeros_like(w) for w in want]
+    own = [p.workspace for p in cases]
+    shared = max(own, key=lambda w: w.numel())
+    graphs = []
+    for p, out in zip(cases, outs):
+        p.workspace = shared
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            p.run(torch.bfloat16, out)
+        graphs.append(graph)
+    for _ in range(3):
+        for out in outs:
+            out.zero_()
+        for graph in graphs:
+            graph.replay()
+        shared.fill_(0xFF)
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, w) for out, w in zip(outs, want))
+    streams = [torch.cuda.Stream() for _ in cases]
+    many = [[torch.zeros_like(w) for _ in range(6)] for w in want]
+    torch.cuda.synchronize()
+    for i in range(6):
+        for p, stream, out, ws in zip(cases, streams, many, own):
+            p.workspace = ws
+            with torch.cuda.stream(stream):
+                p.run(torch.bfloat16, out[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for out, w in zip(many, want) for o in out)
 
 
 def test_refusals(moe):
