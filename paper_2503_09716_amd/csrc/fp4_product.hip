@@ -460,6 +460,10 @@ __device__ __forceinline__ void multiply(const Fp4Product& p, const TileLoads<C>
         for (int jj = i * PER; jj < (i + 1) * PER && jj < WBH; ++jj) read_w(stage_of(0), 0, jj);
         __builtin_amdgcn_sched_barrier(0);
     }
+    // One of the two wavefronts of a SIMD goes first, so that the other's matrix instructions fill its gaps instead of both meeting at each hand-over (us,
+    // without and with: 8 experts, K = 4096, 250 rows gate/up 172, 162, 1024 rows 531, 525; down, K = 14336 108, 100 and 253, 248; 160 experts, K = 5120, 300 rows
+    // 523, 510); not in the epilogue, which should not hold up the next tile's start (64 experts, K = 1408, 1500 rows to fp32 247.7, 245.5).
+    if (C::NEXT && wave >= C::NW / 2) __builtin_amdgcn_s_setprio(1);
     int s = 0;
     // Scales may be among the loads that are younger than sub-tile s + 1, which then waits for a few more than it has to.
     auto steady = [] __attribute__((always_inline)) { ring_sync<(NS - 3) * NL + NL0>(); };
@@ -509,6 +513,7 @@ __device__ __forceinline__ void store_tile(const Fp4Product& p, const TileLoads<
     constexpr int XB = Grid<C, TI>::XB;
     const int lane = fresh_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rl = lane & 15, g = lane >> 4;
     const int N = p.N, x_row = Grid<C, TI>::x_row(wave), wn_row = Grid<C, TI>::w_row(wave, GATED);
+    if (C::NEXT) __builtin_amdgcn_s_setprio(0);
     mfma_drain();
     __builtin_amdgcn_sched_barrier(0);
     // W is the row operand: a lane has the four columns 4g .. 4g+3 of row rl of a block.  Rows past the end get an offset that the descriptor drops.
