@@ -7,7 +7,7 @@
 // What bounds it: at low heights reading the matrices once; above some hundred rows a group the matrix cores, which on real data the power limit holds at 6.2 to
 // 6.7 PFLOP/s in a loop of registers alone (8.0 to 8.4 on zeros; 23 of 16 cycles an instruction), and what such a loop leaves out: a sub-tile of 256 x 256
 // takes 1470 cycles without its loads and 1770 with them, a gated epilogue 9800 cycles, of exponentials and reciprocals.  Measured: gate/up of 8 experts, K = 4096, N =
-// 14336, 8192 rows 529 us (3.6 PFLOP/s); of 64 experts, K = 2048, N = 1408, 18006 rows 96 us; down, K = 1408, N = 2048, 98304 rows to fp32 255 us (3.8 TB/s); K = 1536, N =
+// 14336, 8192 rows 523 us (3.7 PFLOP/s); of 64 experts, K = 2048, N = 1408, 18006 rows 98 us; down, K = 1408, N = 2048, 98304 rows to fp32 255 us (3.8 TB/s); K = 1536, N =
 // 5120, 160 experts, 12000 rows 142 us (5.7 TB/s).
 #include <algorithm>
 #include <initializer_list>
