@@ -710,7 +710,9 @@ hipError_t launch_fp4_product(const Fp4Product& args, bool gated, hipStream_t st
     // 187; K = 1408 94 26, 30, 281 60, 54; 160 experts, K = 1536 37 154, 152, 112 202, 189, 600 740, 626; 8 experts, K = 4096, gated 100 104, 114, 250 176,
     // 186, 750 438, 407.  Few tiles: a CU has one workgroup in either form, and a long contraction is better off with the deeper ring (8 experts, K = 14336, 25 rows
     // 86, 47), a short one with lower tiles (K = 512, 750 rows 14.2, 14.5).
-    const int64_t per = (p.rows + p.E - 1) / p.E, groups = std::min(p.E, p.rows);
+    // (64 bits: rows + E may pass 2^31.  A grid of the short form has fewer than 2^24 workgroups, above which its threads would pass 2^32: up to 100 rows
+    // a group it is at most 456 m-tiles of 16384 columns' tiles.)
+    const int64_t per = ((int64_t)p.rows + p.E - 1) / p.E, groups = std::min(p.E, p.rows);
     const int64_t long_tiles = groups * ((per + Long::ROWS - 1) / Long::ROWS) * p.n_tiles, short_tiles = groups * ((per + Short::ROWS - 1) / Short::ROWS) * p.n_tiles;
     const bool is_long = (per > 100 && long_tiles >= 256) || (short_tiles <= 256 && p.sub_tiles >= 32);
     // Outputs go past the L2s, where they would displace what tiles share (us, without and with: down of K = 1408, 64 experts, 16000 tokens, bf16 230, 195, fp32

@@ -1,0 +1,40 @@
+"""Grouped products of MXFP4 at the ends of their ranges."""
+import pytest
+import torch
+
+from paper_2503_09716_amd import Moe
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def moe():
+    m = Moe(0)
+    yield m
+    m.close()
+
+
+def test_room_for_nearly_2_31_rows(moe):
+    """rows + experts passes 2^31.  The last 40000 of the rows, over 300 tiles of 128, are those of a small call, to the bit."""
+    rows, E, n = 2 ** 31 - 32, 64, 40000
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("needs 160 GiB of free memory")
+    gen = torch.Generator().manual_seed(2)
+    x = torch.randn((n, 32), generator=gen).bfloat16().to(DEV)
+    q = moe.new_mx_rows(n, 32)
+    moe.mx_quantize(x, q)
+    lst = moe.weight_list([moe.mx_pack_weight((torch.randn((32, 32), generator=gen) * 0.05).bfloat16().to(DEV)) for _ in range(E)])
+    cuts = [0] * (E - 2) + [17130, 17131, n]
+    want = torch.empty((n, 32), dtype=torch.bfloat16, device=DEV)
+    moe.mx_grouped_product(q, None, torch.tensor(cuts, dtype=torch.int32, device=DEV), lst, want, moe.new_mx_workspace(n, E))
+    index = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    index[rows - n:] = torch.arange(n, dtype=torch.int32, device=DEV)
+    out = torch.empty((rows, 32), dtype=torch.bfloat16, device=DEV)
+    out[rows - n - 64:] = 7.0
+    offsets = (torch.tensor(cuts, dtype=torch.int64) + (rows - n)).int().to(DEV)
+    moe.mx_grouped_product(q, index, offsets, lst, out, moe.new_mx_workspace(rows, E))
+    assert torch.equal(out[rows - n:], want) and (out[rows - n - 64:rows - n] == 7.0).all()
+    del index, out
+    torch.cuda.empty_cache()
