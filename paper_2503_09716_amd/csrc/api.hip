@@ -1635,7 +1635,7 @@ moe_status moe_mx_grouped_product(moe_ctx* c, int32_t rows, int32_t K, int32_t N
     if ((gated != 0 && gated != 1) || (out_fp32 != 0 && out_fp32 != 1)) return fail(c, MOE_E_ARG, "mx_grouped_product: gated and out_fp32 must be 0 or 1");
     if (moe_status st = check_list(c, "mx_grouped_product", list)) return st;
     if (!list->fp4) return fail(c, MOE_E_ARG, "mx_grouped_product: the list is not of MXFP4 matrices");
-    if (first < 0 || first + gated >= list->matrices) return fail(c, MOE_E_ARG, "mx_grouped_product: the list has no matrix %d", (int)(first + gated));
+    if (first < 0 || first >= list->matrices - gated) return fail(c, MOE_E_ARG, "mx_grouped_product: the list has no matrix %lld", (long long)first + gated);
     if (fp4_tiles(rows, list->experts, N, gated != 0) > 0x7fffffff) return fail(c, MOE_E_UNSUPPORTED, "mx_grouped_product: too many rows and columns");
     if (rows == 0) return MOE_OK;
     if (!xq || !offsets || !out) return fail(c, MOE_E_ARG, "mx_grouped_product: NULL pointer");

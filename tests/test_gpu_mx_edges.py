@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2503_09716_amd import Moe
+from paper_2503_09716_amd import Moe, MoeError
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -38,3 +38,20 @@ def test_room_for_nearly_2_31_rows(moe):
     assert torch.equal(out[rows - n:], want) and (out[rows - n - 64:rows - n] == 7.0).all()
     del index, out
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("first", [-2 ** 31, -1, 1, 2, 2 ** 31 - 2, 2 ** 31 - 1])
+def test_numbers_of_matrices_that_the_list_has_not(moe, first, gated):
+    """first + 1 passes 2^31, too; refused with rows and without."""
+    matrices = 1 + gated
+    q = moe.new_mx_rows(4, 64)
+    moe.mx_quantize(torch.zeros((4, 64), dtype=torch.bfloat16, device=DEV), q)
+    lst = moe.weight_list(*[[moe.mx_pack_weight(torch.zeros((64, 32), dtype=torch.bfloat16, device=DEV))] for _ in range(matrices)])
+    offsets, ws, out = torch.tensor([0, 4], dtype=torch.int32, device=DEV), moe.new_mx_workspace(4, 1), torch.full((4, 32), 7.0, device=DEV)
+    for rows in (0, 4):
+        with pytest.raises(MoeError) as e:
+            moe.mx_grouped_product(q, None, offsets, lst, out[:rows], ws, gated=gated, first=first)
+        assert e.value.status == 1 and str(first + gated) in str(e.value)
+    moe.mx_grouped_product(q, None, offsets, lst, out, ws, gated=gated)
+    assert (out == 0.0).all()
