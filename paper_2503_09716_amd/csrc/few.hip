@@ -368,10 +368,11 @@ __global__ __launch_bounds__(WAVES * 64) void few_up_kernel(const FewArgs p) {
             for (int j = 0; j < NB / 2; ++j) {
                 if (row >= 0) {
                     const float v = weight * (gate[j] / (1.0f + __expf(-gate[j])) * up[j]);
-                    const __bf16 hi = (__bf16)v;
+                    // what is finite in fp32 stays finite: above the largest bf16 that one is the high half; an infinity or NaN has no low half
+                    const __bf16 hi = __builtin_isfinite(v) ? (__bf16)fminf(fmaxf(v, -0x1.fep127f), 0x1.fep127f) : (__bf16)v;
                     char* const to = p.h + (size_t)row * p.h_row + h_place<FP4>(f0 + j * 32);
                     *reinterpret_cast<__bf16*>(to) = hi;
-                    *reinterpret_cast<__bf16*>(to + 64) = __builtin_isfinite((float)hi) ? (__bf16)(v - (float)hi) : (__bf16)0.0f;
+                    *reinterpret_cast<__bf16*>(to + 64) = __builtin_isfinite(v) ? (__bf16)(v - (float)hi) : (__bf16)0.0f;
                 }
                 gate[j] = up[j] = 0.f;
             }

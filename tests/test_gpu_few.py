@@ -320,3 +320,21 @@ def test_two_graphs_share_a_workspace(moe):
         torch.cuda.synchronize()
         for out, w in zip(outs, want):
             assert torch.equal(out, w)
+
+
+@pytest.mark.parametrize("shared", [0, 1])
+@pytest.mark.parametrize("fp4", [True, False])
+def test_h_between_the_largest_bf16_and_the_largest_fp32(moe, fp4, shared):
+    """h = 2^64 (2^64 - 2^54) rounds to no finite bf16, and is finite in fp32.  Exact throughout: one value of h meets ones, the others zeros."""
+    def spoil(a, w):
+        a.x.zero_()
+        a.x[:, 0], a.x[:, 1], a.x[:, 2] = 1.0, 1.0, -2.0 ** -8
+        for e in range(1 + shared):
+            for ms in w:
+                ms[e].zero_()
+            w[0][e][0], w[1][e][1], w[1][e][2] = 2.0 ** 64, 2.0 ** 64, 2.0 ** 62
+        w[2][shared][3] = 1.0
+    a = Layer(moe, 3, 64, 64, 1, 1, shared, fp4=fp4, spoil=spoil)
+    want, _ = a.expected()
+    assert (want == 2.0 ** 128 * (1 - 2.0 ** -10)).all()
+    assert torch.equal(a.run(True).double(), want)
