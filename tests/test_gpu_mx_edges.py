@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2503_09716_amd import Moe, MoeError
+from test_gpu_mx import Product, held
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -55,3 +56,92 @@ def test_numbers_of_matrices_that_the_list_has_not(moe, first, gated):
         assert e.value.status == 1 and str(first + gated) in str(e.value)
     moe.mx_grouped_product(q, None, offsets, lst, out, ws, gated=gated)
     assert (out == 0.0).all()
+
+
+class Columns:
+    """Experts of very many columns, packed whole and in pieces of columns: the pieces' launches are short enough for workgroups to find their tiles
+    themselves, the whole matrices' launch has the list of tiles in the workspace."""
+
+    def __init__(self, moe, E, K, N, pieces, gated, x_rows, seed):
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.moe, self.K, self.N, self.pieces, self.gated = moe, K, N, pieces, gated
+        self.sample = torch.randperm(N, generator=gen, device=DEV)[:24].sort().values
+        self.some, whole, parts = [], [], [[] for _ in range(pieces)]
+        for _ in range(2 if gated else 1):
+            whole.append([])
+            self.some.append([])
+            for p in parts:
+                p.append([])
+            for _ in range(E):
+                w = torch.empty((K, N), dtype=torch.bfloat16, device=DEV).normal_(0.0, 0.05, generator=gen)
+                whole[-1].append(moe.mx_pack_weight(w))
+                for i, p in enumerate(parts):
+                    p[-1].append(moe.mx_pack_weight(w[:, i * N // pieces:(i + 1) * N // pieces].contiguous()))
+                self.some[-1].append(held(w[:, self.sample].t()).t().to(DEV))
+        self.whole, self.parts = moe.weight_list(*whole), [moe.weight_list(*p) for p in parts]
+        x = torch.empty((x_rows, K), dtype=torch.bfloat16, device=DEV).normal_(0.0, 1.0, generator=gen)
+        self.q = moe.new_mx_rows(x_rows, K)
+        moe.mx_quantize(x, self.q)
+        self.x = held(x).to(DEV)
+
+    def run(self, lst, N, cuts, rows, index, dtype):
+        out = torch.full((rows, N), 7.0, dtype=dtype, device=DEV)
+        ws = self.moe.new_mx_workspace(rows, len(cuts) - 1)
+        ws.fill_(0xFF)
+        self.moe.mx_grouped_product(self.q, index, torch.tensor(cuts, dtype=torch.int32, device=DEV), lst, out, ws, gated=self.gated)
+        return out
+
+
+@pytest.mark.parametrize("K,N,pieces,gated,dtype", [
+    (544, 65536, 4, True, torch.bfloat16),      # five sub-tiles, the last one short
+    (2080, 65536, 4, True, torch.bfloat16),     # a long contraction of tall groups: outputs through the caches
+    (544, 131072, 8, False, torch.float32),
+])
+def test_long_launches_with_a_list_of_tiles_in_memory(moe, K, N, pieces, gated, dtype):
+    """Empty groups, short tails that go last, even cuts, groups of whole tiles, and less in the groups than there is room for.  Every value
+    is that of a shorter launch, to the bit; some columns are held to 64 bits, with the bound of a sum of K products and of the output's rounding."""
+    counts = [0, 1500, 300, 33, 2560, 0, 1029, 700, 97, 257]
+    room, E = sum(counts) + 700, len(counts)
+    tiles = (room // 256 + E) * (N // (128 if gated else 256))
+    assert tiles > 61 * 256 >= (room // 256 + E) * (N // pieces // (128 if gated else 256))
+    c = Columns(moe, E, K, N, pieces, gated, 900, seed=K)
+    index = torch.randint(0, 900, (room,), generator=torch.Generator().manual_seed(K)).int().to(DEV)
+    cuts = [5]
+    for n in counts:
+        cuts.append(cuts[-1] + n)
+    out = c.run(c.whole, N, cuts, room, index, dtype)
+    assert (out[:5] == 7.0).all() and (out[cuts[-1]:] == 7.0).all()
+    for i, lst in enumerate(c.parts):
+        a, b = i * N // pieces, (i + 1) * N // pieces
+        assert torch.equal(c.run(lst, b - a, cuts, room, index, dtype), out[:, a:b]), i
+    for e in range(E):
+        rows = slice(cuts[e], cuts[e + 1])
+        x = c.x[index[rows].long()]
+        y = [x @ some[e] for some in c.some]
+        off = [(x.abs() @ some[e].abs()) * (K * 2.0 ** -23) for some in c.some]
+        if gated:
+            s = torch.nn.functional.silu(y[0])
+            want = s * y[1]
+            off = 1.1 * off[0] * (y[1].abs() + off[1]) + s.abs() * off[1] + want.abs() * (8 + y[0].abs()) * 2.0 ** -23
+        else:
+            want, off = y[0], off[0]
+        if dtype is torch.bfloat16:
+            off = off * (1 + 2.0 ** -8) + want.abs() * 2.0 ** -8
+        assert ((out[rows][:, c.sample].double() - want).abs() <= off).all(), e
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("counts,K,N,gated,nt", [
+    ([900, 0, 700], 2080, 544, True, False),       # above 16 sub-tiles and 128 rows a group: the only outputs that go through the caches
+    ([120, 136, 130], 2080, 544, True, False),     # 129 rows a group
+    ([118, 136, 130], 2080, 544, True, True),      # 128
+    ([900, 0, 700], 2048, 544, True, True),        # 16 sub-tiles
+    ([900, 0, 700], 2080, 544, False, True),
+])
+def test_outputs_through_and_past_the_caches(moe, counts, K, N, gated, nt):
+    """Which way the outputs go depends on the contraction and the rows a group, not on their size."""
+    per = -(-sum(counts) // len(counts))
+    assert nt == (not gated or K <= 16 * 128 or per <= 128)
+    p = Product(moe, counts, K, N, gated, seed=K + gated)
+    p.check(torch.float32)
+    p.check(torch.bfloat16)
