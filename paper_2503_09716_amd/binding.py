@@ -195,6 +195,13 @@ def _same_rows(t, shape) -> bool:
     return t.numel() == math.prod(shape) and (len(shape) == 1 or t.dim() < 2 or t.shape[-1] == shape[-1])
 
 
+def _buffer(t: torch.Tensor, device: int):
+    """Address of a buffer that the library alone knows the inside of, on the call's device."""
+    if t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    raise AssertionError("contiguous buffer on cuda:%d required" % device)
+
+
 def _float_type(t: torch.Tensor):
     return torch.float32 if t.dtype is torch.float32 else torch.bfloat16
 
@@ -212,9 +219,11 @@ class GradientList:
 
 
 class MxRows:
-    """Rows in MXFP4 (Moe.mx_quantize): `rows` of `cols` values in one opaque buffer."""
+    """Rows in MXFP4 (Moe.mx_quantize): `rows` of `cols` values in one opaque buffer of moe_mx_rows_bytes bytes."""
 
     def __init__(self, rows: int, cols: int, buffer: torch.Tensor):
+        n = int(load_library().moe_mx_rows_bytes(rows, cols))
+        assert buffer.dtype is torch.uint8 and buffer.is_cuda and buffer.is_contiguous() and buffer.numel() >= n, "uint8 buffer of %d bytes on a GPU required" % n
         self.rows, self.cols, self.buffer = rows, cols, buffer
 
 
@@ -384,11 +393,11 @@ class Moe:
     def mx_quantize(self, x, q: MxRows):
         """x: bf16 or fp32 [rows, cols]."""
         self._check(self.lib.moe_mx_quantize(self.h, _typed(x, _float_type(x), (q.rows, q.cols), self.device), int(x.dtype is torch.float32), q.rows, q.cols,
-                                              q.buffer.data_ptr(), _raw_stream(self.device)))
+                                              _buffer(q.buffer, self.device), _raw_stream(self.device)))
 
     def mx_dequantize(self, q: MxRows, out):
         """out: bf16 or fp32 [rows, cols]."""
-        self._check(self.lib.moe_mx_dequantize(self.h, q.buffer.data_ptr(), q.rows, q.cols, _typed(out, _float_type(out), (q.rows, q.cols), self.device),
+        self._check(self.lib.moe_mx_dequantize(self.h, _buffer(q.buffer, self.device), q.rows, q.cols, _typed(out, _float_type(out), (q.rows, q.cols), self.device),
                                                 int(out.dtype is torch.float32), _raw_stream(self.device)))
 
     def mx_pack_weight(self, w: torch.Tensor, packed: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -434,12 +443,13 @@ class Moe:
     def mx_grouped_product(self, q: MxRows, row_index, expert_offsets, weights: WeightList, out, workspace, gated: bool = False, first: int = 0):
         """out: bf16 or fp32 [rows, N]; row_index: int32 [rows] or None; weights: matrices number `first` and, gated, the next of each expert."""
         d, (rows, N) = self.device, out.shape
+        _buffer(weights.buffer, d)
         n = int(self.lib.moe_mx_weight_bytes(q.cols, N))
         assert all(b == n for b in weights.bytes[first:first + 1 + bool(gated)]), "matrices of %d x %d in MXFP4 required" % (q.cols, N)
-        self._check(self.lib.moe_mx_grouped_product(self.h, rows, q.cols, N, q.buffer.data_ptr(), q.rows, _typed(row_index, torch.int32, (rows,), d),
+        self._check(self.lib.moe_mx_grouped_product(self.h, rows, q.cols, N, _buffer(q.buffer, d), q.rows, _typed(row_index, torch.int32, (rows,), d),
                                                      _typed(expert_offsets, torch.int32, (weights.struct.experts + 1,), d), C.byref(weights.struct),
                                                      first, int(gated), _typed(out, _float_type(out), (rows, N), d), int(out.dtype is torch.float32),
-                                                     _ptr(workspace), workspace.numel(), _raw_stream(d)))
+                                                     _buffer(workspace, d), workspace.numel(), _raw_stream(d)))
 
     def new_few_workspace(self, shape: MoeShape) -> torch.Tensor:
         """Workspace of layer_few."""
@@ -452,11 +462,12 @@ class Moe:
         """The whole layer for up to 16 tokens; weights: weight_list of the gate, up and down matrices, bf16 or MXFP4."""
         T, H, F, E, d = shape.T, shape.H, shape.F, shape.E, self.device
         fp4 = weights.struct.fp4
+        _buffer(weights.buffer, d)
         gate = (int(self.lib.moe_gate_packed_bytes(C.byref(shape))) // 2,) if self.gate_packed else (H, E)
         want = [int(self.lib.moe_mx_weight_bytes(*s)) if fp4 else 2 * H * F for s in ((H, F), (H, F), (F, H))]
         assert weights.bytes == want, "three matrices of %d x %d, %d x %d and %d x %d required" % (H, F, H, F, F, H)
         self._check(self.lib.moe_layer_few(self.h, C.byref(shape), _typed(x, torch.bfloat16, (T, H), d), _typed(wg, torch.bfloat16, gate, d),
-                                           _typed(bias, torch.float32, (E,), d), C.byref(weights.struct), _typed(out, self.out_dtype, (T, H), d), _ptr(workspace), workspace.numel(),
+                                           _typed(bias, torch.float32, (E,), d), C.byref(weights.struct), _typed(out, self.out_dtype, (T, H), d), _buffer(workspace, d), workspace.numel(),
                                            _raw_stream(d)))
 
     # ---- fused call --------------------------------------------------------------------
