@@ -224,14 +224,20 @@ class MxRows:
     def __init__(self, rows: int, cols: int, buffer: torch.Tensor):
         n = int(load_library().moe_mx_rows_bytes(rows, cols))
         assert buffer.dtype is torch.uint8 and buffer.is_cuda and buffer.is_contiguous() and buffer.numel() >= n, "uint8 buffer of %d bytes on a GPU required" % n
-        self.rows, self.cols, self.buffer = rows, cols, buffer
+        self.rows, self.cols, self.buffer, self.device = rows, cols, buffer, buffer.get_device()
+
+    def address(self, device: int) -> int:
+        """Of the buffer, for a call on `device`."""
+        if device != self.device:
+            raise AssertionError("rows on cuda:%d required" % device)
+        return self.buffer.data_ptr()
 
 
 class WeightList:
     """Expert matrices that calls find through a device table made once (Moe.weight_list): keeps them and the table alive."""
 
     def __init__(self, struct: WeightListStruct, buffer: torch.Tensor, weights):
-        self.struct, self.buffer, self.weights = struct, buffer, weights
+        self.struct, self.buffer, self.weights, self.device = struct, buffer, weights, buffer.get_device()
         self.bytes = [ws[0].numel() * ws[0].element_size() for ws in weights]   # of a matrix, by its number
 
 
@@ -393,11 +399,11 @@ class Moe:
     def mx_quantize(self, x, q: MxRows):
         """x: bf16 or fp32 [rows, cols]."""
         self._check(self.lib.moe_mx_quantize(self.h, _typed(x, _float_type(x), (q.rows, q.cols), self.device), int(x.dtype is torch.float32), q.rows, q.cols,
-                                              _buffer(q.buffer, self.device), _raw_stream(self.device)))
+                                              q.address(self.device), _raw_stream(self.device)))
 
     def mx_dequantize(self, q: MxRows, out):
         """out: bf16 or fp32 [rows, cols]."""
-        self._check(self.lib.moe_mx_dequantize(self.h, _buffer(q.buffer, self.device), q.rows, q.cols, _typed(out, _float_type(out), (q.rows, q.cols), self.device),
+        self._check(self.lib.moe_mx_dequantize(self.h, q.address(self.device), q.rows, q.cols, _typed(out, _float_type(out), (q.rows, q.cols), self.device),
                                                 int(out.dtype is torch.float32), _raw_stream(self.device)))
 
     def mx_pack_weight(self, w: torch.Tensor, packed: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -443,10 +449,10 @@ class Moe:
     def mx_grouped_product(self, q: MxRows, row_index, expert_offsets, weights: WeightList, out, workspace, gated: bool = False, first: int = 0):
         """out: bf16 or fp32 [rows, N]; row_index: int32 [rows] or None; weights: matrices number `first` and, gated, the next of each expert."""
         d, (rows, N) = self.device, out.shape
-        _buffer(weights.buffer, d)
+        assert weights.device == d, "a list on cuda:%d required" % d
         n = int(self.lib.moe_mx_weight_bytes(q.cols, N))
         assert all(b == n for b in weights.bytes[first:first + 1 + bool(gated)]), "matrices of %d x %d in MXFP4 required" % (q.cols, N)
-        self._check(self.lib.moe_mx_grouped_product(self.h, rows, q.cols, N, _buffer(q.buffer, d), q.rows, _typed(row_index, torch.int32, (rows,), d),
+        self._check(self.lib.moe_mx_grouped_product(self.h, rows, q.cols, N, q.address(d), q.rows, _typed(row_index, torch.int32, (rows,), d),
                                                      _typed(expert_offsets, torch.int32, (weights.struct.experts + 1,), d), C.byref(weights.struct),
                                                      first, int(gated), _typed(out, _float_type(out), (rows, N), d), int(out.dtype is torch.float32),
                                                      _buffer(workspace, d), workspace.numel(), _raw_stream(d)))
@@ -462,7 +468,7 @@ class Moe:
         """The whole layer for up to 16 tokens; weights: weight_list of the gate, up and down matrices, bf16 or MXFP4."""
         T, H, F, E, d = shape.T, shape.H, shape.F, shape.E, self.device
         fp4 = weights.struct.fp4
-        _buffer(weights.buffer, d)
+        assert weights.device == d, "a list on cuda:%d required" % d
         gate = (int(self.lib.moe_gate_packed_bytes(C.byref(shape))) // 2,) if self.gate_packed else (H, E)
         want = [int(self.lib.moe_mx_weight_bytes(*s)) if fp4 else 2 * H * F for s in ((H, F), (H, F), (F, H))]
         assert weights.bytes == want, "three matrices of %d x %d, %d x %d and %d x %d required" % (H, F, H, F, F, H)
