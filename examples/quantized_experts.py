@@ -23,7 +23,8 @@ from paper_2503_09716_amd import Moe, make_shape, workspace_bytes  # noqa: E402
 
 
 class QuantizedLayer:
-    """The weights of a layer in MXFP4; shared experts are summed, so they are one of their width together."""
+    """The weights of a layer in MXFP4.  Shared experts are summed, so in a long batch they are one expert of their width together, packed a second time; the layer for few
+    tokens takes them one by one."""
 
     def __init__(self, moe: Moe, wg, w1, w3, w2, k, num_shared):
         self.moe, self.wg, self.k, self.num_shared = moe, wg, k, num_shared

@@ -10,9 +10,11 @@
 // A wavefront takes 16 columns: W is the row operand straight from memory, the tokens are the 16 columns of the other one, whether they picked
 // the expert or not; what they did not pick is not stored (gate and up) or left out of the sum (down).
 //
-// Bound by reading the weights where they are large (8 experts, H = 4096, F = 14336, MXFP4, 16 tokens 154 us, 5.0 TB/s; 160 + 2 experts, H = 5120, F = 1536 182 us, 5.2), and
-// by the chain of launches, routing and first loads where they are small (64 + 2 experts, H = 2048, one token 23.5 us: logits 3.5, gate/up 12, down 8.5; 8 experts,
-// H = 512, F = 1024, bf16, 16 tokens 15.8 us, where the layer for any batch takes 24).
+// Bound by reading the weights where they are large and bf16 (8 experts, H = 4096, F = 14336, 16 tokens 418 us, 6.7 TB/s).  The same layer in MXFP4 takes 148 (5.1 TB/s) and 160 + 2
+// experts, H = 5120, F = 1536 178 to 188 (5.2): there a piece of 1 KiB is 16 conversions and four to eight matrix instructions, which share the time with its load.  Gate/up and
+// down launch of the former: 103 and 54 us, without conversions 87 and 48, without loads of weights 59 and 31.  By the chain of launches, routing and first loads where
+// they are small (64 + 2 experts, H = 2048, one token 23.5 us: logits 3.5, gate/up 12, down 8.5; 8 experts, H = 512, F = 1024, bf16, 16 tokens 15.8 us, where the
+// layer for any batch takes 17.7).
 #include <algorithm>
 
 #include "few.h"

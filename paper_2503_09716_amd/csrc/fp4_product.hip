@@ -4,11 +4,13 @@
 // for the rows r of group e.  v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 x 128 by 128 x 16 values in 16 cycles, four times what
 // the bf16 form does, and takes one scale for 32 values of a row.
 //
-// What bounds it: at low heights reading the matrices once; above some hundred rows a group the matrix cores, which on real data the power limit holds at 6.2 to
-// 6.7 PFLOP/s in a loop of registers alone (8.0 to 8.4 on zeros; 23 of 16 cycles an instruction), and what such a loop leaves out: a sub-tile of 256 x 256
-// takes 1470 cycles without its loads and 1770 with them, a gated epilogue 9800 cycles, of exponentials and reciprocals.  Measured: gate/up of 8 experts, K = 4096, N =
-// 14336, 8192 rows 523 us (3.7 PFLOP/s); of 64 experts, K = 2048, N = 1408, 18006 rows 98 us; down, K = 1408, N = 2048, 98304 rows to fp32 255 us (3.8 TB/s); K = 1536, N =
-// 5120, 160 experts, 12000 rows 142 us (5.7 TB/s).
+// What bounds it: at low heights reading the matrices once.  Above some hundred rows a group no single thing.  A sub-tile of 256 x 256 takes 0.90 us, 0.74 without its loads and
+// 0.79 without its matrix instructions, which the power limit holds at 23 for 16 cycles on real data (6.2 to 6.7 PFLOP/s in a loop of registers alone, 8.0 to 8.4 on
+// zeros).  A tile's epilogue comes behind its K loop, not beside one: the next tile's first hand-overs wait for the stores, which are older than the loads that
+// they may leave on their way.  Measured, and in a copy without the epilogues: gate/up of 8 experts, K = 4096, N = 14336, 8192 rows 503 us (3.8 PFLOP/s; 14 tiles
+// to a workgroup of 29 us of K loop, 3 of waits at its ends, 4 of epilogue), 443; of 64 experts, K = 2048, N = 1408, 18006 rows 98, 80; down, K = 1408, N = 2048,
+// 98304 rows to fp32 254 (12 tiles of 10 us of K loop, 1.6 of waits, 10 of stores at 6.9 TB/s), 138, to bf16 203, 138; K = 1536, N = 5120, 160 experts, 12000 rows
+// 143 (5.6 TB/s), 116.
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>
@@ -706,10 +708,11 @@ hipError_t launch_fp4_product(const Fp4Product& args, bool gated, hipStream_t st
     Fp4Product p = args;
     const int bn = gated ? 128 : WROWS;
     p.n_tiles = (p.N + bn - 1) / bn;
-    // Which form, by the tiles that even groups would have (us, short and long; rows per group): 64 experts, K = 2048, gated 94 rows 45, 46, 281 89, 91, 750 196,
-    // 187; K = 1408 94 26, 30, 281 60, 54; 160 experts, K = 1536 37 154, 152, 112 202, 189, 600 740, 626; 8 experts, K = 4096, gated 100 104, 114, 250 176,
-    // 186, 750 438, 407.  Few tiles: a CU has one workgroup in either form, and a long contraction is better off with the deeper ring (8 experts, K = 14336, 25 rows
-    // 86, 47), a short one with lower tiles (K = 512, 750 rows 14.2, 14.5).
+    // Which form, by the tiles that even groups would have (us, short and long; rows per group): 64 experts, K = 2048, gated 94 rows 54.8, 53.0, 141 64.8, 60.3, 281
+    // 99.5, 97.9, 750 198, 176; K = 1408 94 26.0, 28.7, 112 36.0, 30.4, 281 57.9, 55.5, 750 125, 104; 160 experts, K = 1536 37 141.3, 141.6, 112 175.8, 175.5, 600
+    // 616, 533; 8 experts, K = 4096, gated 25 86.6, 90.5, 100 105, 108, 250 183, 165, 750 406, 368.  Few tiles: a CU has one workgroup in either form, and a long
+    // contraction is better off with the deeper ring (8 experts, K = 14336, 25 rows 92, 61, 100 98, 78), a short one with lower tiles (K = 512, gated 250 rows 8.8, 11.4, 750
+    // 11.4, 13.5).
     // (64 bits: rows + E may pass 2^31.  A grid of the short form has fewer than 2^24 workgroups, above which its threads would pass 2^32: up to 100 rows
     // a group it is at most 456 m-tiles of 16384 columns' tiles.)
     const int64_t per = ((int64_t)p.rows + p.E - 1) / p.E, groups = std::min(p.E, p.rows);
